@@ -543,6 +543,112 @@ int mdet_flodance_eval(const double* coef, int32_t q, const double* n_values, in
                        double* out, void* stream);
 
 /* ------------------------------------------------------------------------
+ * Training a network and forming the Gram matrix of its Jacobian
+ *
+ * The matrices whose log-determinants this library takes are Gram matrices J J^T of a network's
+ * Jacobian (the NTK, Sec. 2.1).  These operators are the step in front: dense layers and their
+ * gradients, an optimiser step, and the Gram matrix itself, on the GPU.  All pointers are DEVICE
+ * pointers unless said otherwise; matrices are row-major with any leading dimension and only need
+ * the alignment of their elements; the caller owns every buffer.  Each call only queues kernels on
+ * `stream` (a hipStream_t or NULL), allocates nothing and returns MDET_EINVAL for inconsistent
+ * arguments, MDET_ENOMEM_DEVICE for a workspace that is too small and MDET_EHIP if a launch failed.
+ * A workspace starts on 256 bytes.  Sizes of zero are allowed: an empty sum is zero, a call
+ * without results does nothing.
+ * ---------------------------------------------------------------------- */
+
+typedef enum {
+  MDET_ACT_NONE = 0,
+  MDET_ACT_RELU = 1,
+  MDET_ACT_GELU = 2,       /* z Phi(z)                                                       */
+  MDET_ACT_GELU_TANH = 3,  /* z (1 + tanh(sqrt(2/pi) (z + 0.044715 z^3))) / 2                */
+  MDET_ACT_SILU = 4        /* z / (1 + exp(-z))                                              */
+} mdet_activation;
+
+/* Device bytes of workspace for a linear layer of these sizes (pure host code): the forward call, or
+ * with backward != 0 the gradient. */
+int mdet_linear_workspace_query(int32_t dtype, int32_t backward, int64_t m, int64_t n, int64_t k,
+                                uint64_t* bytes);
+
+/* y = act(z) + residual,  z = x w^T + bias:  x is m x k, w n x k, y, z and residual m x n, bias n
+ * elements, all of dtype (MDET_F32, MDET_F16 or MDET_BF16).  bias, residual and z (where the sums
+ * before the activation are kept for the gradient) may be NULL.  Sums are fp32; y is formed from the
+ * unrounded z.  y may be the same matrix as residual (same leading dimension); no output may
+ * overlap any other operand. */
+int mdet_linear_forward(int32_t dtype, int32_t activation, int64_t m, int64_t n, int64_t k,
+                        const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias,
+                        const void* residual, int64_t ldr, void* y, int64_t ldy, void* z,
+                        int64_t ldz, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Gradient of the same layer: with dz = dy act'(z),  dx = dz w,  dw = dz^T x,  db = column sums of
+ * dz; any of dx, dw, db may be NULL (not wanted; so may then what only they read).  The gradient of
+ * the residual is dy itself.  z is not read for MDET_ACT_NONE.  dw and db are of grad_dtype: dtype or
+ * MDET_F32.  dz is rounded to dtype in front of the two products; db sums the unrounded one.  Where dz
+ * is not NULL it receives the rounded one (m x n; what mdet_ntk_gram takes as g). */
+int mdet_linear_backward(int32_t dtype, int32_t grad_dtype, int32_t activation, int64_t m, int64_t n,
+                         int64_t k, const void* dy, int64_t lddy, const void* z, int64_t ldz,
+                         const void* x, int64_t ldx, const void* w, int64_t ldw, void* dx,
+                         int64_t lddx, void* dw, int64_t lddw, void* db, void* dz, int64_t lddz,
+                         void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* One tensor of an optimiser step, n consecutive elements. */
+typedef struct mdet_adamw_tensor {
+  void* p;          /* parameters, updated in place                                          */
+  const void* g;    /* gradient                                                              */
+  void* m;          /* running mean of the gradient: float, or int8_t codes                  */
+  void* v;          /* running mean of its square: float; or uint8_t codes of the ROOT of it */
+  float* scales;    /* 8-bit states: 2 * ceil(n / 256) floats, for each 256 elements the
+                       scale of m, then that of the root of v (value = code * scale); zeros
+                       with any codes are the state before the first step                    */
+  void* copy;       /* 16-bit copy of the updated parameters, or unused                      */
+  int64_t n;
+} mdet_adamw_tensor;
+
+/* Parameters of a step, the same for all tensors.  Zero-initialise, then set fields. */
+typedef struct mdet_adamw_params {
+  uint32_t struct_size;   /* = sizeof(mdet_adamw_params)                                     */
+  int32_t dtype;          /* of p: MDET_F32, MDET_F16 or MDET_BF16                           */
+  int32_t grad_dtype;     /* of g: likewise                                                  */
+  int32_t state_bits;     /* 32 or 8                                                         */
+  int32_t copy_dtype;     /* MDET_F16 or MDET_BF16; -1: no copies                            */
+  uint32_t seed;          /* of the random rounding of 8-bit states; another one each step   */
+  int64_t step;           /* number of this step, from 1 (bias correction)                   */
+  double lr, beta1, beta2, eps, weight_decay;
+  const float* grad_scale; /* DEVICE pointer to a factor on all gradients, NULL for 1        */
+} mdet_adamw_params;
+
+/* m <- beta1 m + (1 - beta1) g, v <- beta2 v + (1 - beta2) g^2,
+ * p <- p (1 - lr weight_decay) - lr mhat / (sqrt(vhat) + eps) with mhat = m / (1 - beta1^step) and
+ * vhat = v / (1 - beta2^step), on `count` tensors (a HOST array), in fp32.  8-bit states are rounded up
+ * or down at random, with a mean that is what is rounded; a gradient that is not finite makes the
+ * 256 elements of its scale NaN at the next step.  Up to 48 tensors share a launch. */
+int mdet_adamw_step(const mdet_adamw_params* params, const mdet_adamw_tensor* tensors, int64_t count,
+                    void* stream);
+
+/* What a dense layer z = W a + b of a network with `outputs` outputs contributes to the Jacobian on
+ * n samples: its inputs a (n x p, leading dimension lda) and the derivatives g of the network's
+ * outputs by z (n * outputs x q, leading dimension ldg; row i * outputs + r: output r at sample i). */
+typedef struct mdet_ntk_layer {
+  const void* a;
+  int64_t lda, p;
+  const void* g;
+  int64_t ldg, q;
+} mdet_ntk_layer;
+
+/* K[(i,r),(j,s)] = scale sum_layers (a_i . a_j + bias) (g_ir . g_js)   (+ K with accumulate != 0),
+ * the LOWER triangle of order n * outputs (what the log-determinant calls read; nothing above the diagonal is
+ * written), leading dimension ldk.  bias: 1 for layers with a bias vector, 0 without.  Operands
+ * are of dtype, K of out_dtype: MDET_F32 or MDET_F64 (MDET_F64 where dtype is), which is also the type
+ * of the arithmetic; narrower operands are widened exactly.  `layers` is a HOST array. */
+int mdet_ntk_gram(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs,
+                  const mdet_ntk_layer* layers, int32_t count, double bias, double scale,
+                  int32_t accumulate, void* K, int64_t ldk, void* workspace,
+                  uint64_t workspace_bytes, void* stream);
+
+/* Device bytes of workspace for such a call (pure host code; the pointers in `layers` are not looked at). */
+int mdet_ntk_workspace_query(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs,
+                             const mdet_ntk_layer* layers, int32_t count, uint64_t* bytes);
+
+/* ------------------------------------------------------------------------
  * Measuring sticks for the benchmark (asynchronous, enqueue only; DEVICE pointers).
  * ---------------------------------------------------------------------- */
 

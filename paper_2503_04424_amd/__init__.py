@@ -13,7 +13,9 @@ from .binding import (  # noqa: F401
     mdet_paper_fma_count, mdet_step_schur_update, mdet_step_panel_factor, mdet_step_panel_factor_pivoted, mdet_step_panel_factor_general,
     mdet_step_logdet_reduce, mdet_strerror, mdet_version,
     mdet_sequence_workspace_query, mdet_principal_logdets, mdet_flodance_fit, mdet_flodance_eval,
+    ACTIVATIONS, mdet_linear_workspace_query, mdet_linear_forward, mdet_linear_backward, mdet_adamw_step,
+    mdet_ntk_gram, mdet_ntk_workspace_query,
     mdet_step_copy, mdet_step_mfma_peak, mdet_logdet_device_noalloc,
     pack_lower_block_columns, pack_general_block_columns,
 )
-from .api import memdet, parse_bytes, FitLogdet  # noqa: E402,F401
+from .api import memdet, parse_bytes, FitLogdet, linear, AdamW  # noqa: E402,F401

@@ -140,3 +140,95 @@ class FitLogdet:
     def parameters(self):
         """c_0, nu_0 .. nu_q, L_{n0}, residual norm, as the library returns them."""
         return None if self.coef is None else self.coef.cpu().numpy()
+
+
+def _linear_function():
+    """The autograd node of ``linear``, made at its first use (importing the package does not import torch)."""
+    import torch
+
+    class LinearFunction(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, bias, residual, activation):
+            rows = x.reshape(-1, x.shape[-1])
+            keep = activation != "none" and any(ctx.needs_input_grad[:3])
+            z = rows.new_empty((rows.shape[0], w.shape[0])) if keep else None
+            r = None if residual is None else residual.reshape(-1, residual.shape[-1])
+            y = B.mdet_linear_forward(_rows(rows), _rows(w), bias, None if r is None else _rows(r), activation, preact=z)
+            ctx.save_for_backward(rows, w, z)
+            ctx.activation, ctx.shape = activation, x.shape
+            return y.view(*x.shape[:-1], w.shape[0])
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dy):
+            x, w, z = ctx.saved_tensors
+            need_x, need_w, need_b, need_r, _ = ctx.needs_input_grad
+            dx = dw = db = None
+            if need_x or need_w or need_b:
+                dx, dw, db = B.mdet_linear_backward(_rows(dy.reshape(-1, dy.shape[-1])), _rows(x), _rows(w), z, ctx.activation,
+                                                    dx=need_x, dw=need_w, db=need_b)
+            return None if dx is None else dx.view(ctx.shape), dw, db, dy if need_r else None, None
+
+    return LinearFunction
+
+
+def _rows(t):
+    """Rows of consecutive elements: the tensor itself where it has them (views and slices do), or a copy."""
+    return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
+
+
+_linear = None
+
+
+def linear(x, w, bias=None, residual=None, activation="none"):
+    """``act(x w^T + bias) + residual`` with its gradient (autograd): x (..., k), w (n, k), residual (..., n).
+    activation: 'none', 'relu', 'gelu', 'gelu_tanh' or 'silu'.  One launch or two for the whole layer."""
+    global _linear
+    if residual is not None and tuple(residual.shape) != (*x.shape[:-1], w.shape[0]):
+        raise ValueError(f"residual: shape {(*x.shape[:-1], w.shape[0])} expected, not {tuple(residual.shape)}")
+    if _linear is None:
+        _linear = _linear_function()
+    return _linear.apply(x, w, bias, residual, activation)
+
+
+class AdamW:
+    """AdamW over a list of CUDA tensors, updated in place by ``step()`` (``mdet_adamw_step``; asynchronous).
+
+    state_bits: 32, or 8 for a mean and a root mean square in 8 bits each with two scales per 256 elements.
+    copy_dtype: torch.bfloat16 or torch.float16 keeps a 16-bit copy of every tensor in ``copies``, written by the step."""
+
+    def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, copy_dtype=None, seed=0):
+        import torch
+        self.params = list(params)
+        if state_bits not in (32, 8):
+            raise ValueError("state_bits must be 32 or 8")
+        self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
+        self.state_bits, self.seed, self.steps = state_bits, int(seed), 0
+        types = (torch.float32, torch.float32) if state_bits == 32 else (torch.int8, torch.uint8)
+        self.exp_avg = [torch.zeros(p.shape, dtype=types[0], device=p.device) for p in self.params]
+        self.exp_avg_sq = [torch.zeros(p.shape, dtype=types[1], device=p.device) for p in self.params]
+        self.scales = None if state_bits == 32 else [torch.zeros((p.numel() + 255) // 256, 2, device=p.device) for p in self.params]
+        self.copies = None if copy_dtype is None else [p.detach().to(copy_dtype) for p in self.params]
+
+    def step(self, grads=None, grad_scale=None, stream=None):
+        """One step with ``grads``, or with the tensors' own ``.grad``."""
+        if grads is None:
+            grads = [p.grad for p in self.params]
+        if any(g is None for g in grads):
+            raise ValueError("a gradient for every tensor expected")
+        self.steps += 1
+        B.mdet_adamw_step([p.detach() for p in self.params], grads, self.exp_avg, self.exp_avg_sq, lr=self.lr, step=self.steps,
+                          beta1=self.betas[0], beta2=self.betas[1], eps=self.eps, weight_decay=self.weight_decay,
+                          scales=self.scales, copies=self.copies, grad_scale=grad_scale, seed=self.seed + self.steps, stream=stream)
+
+    def state_dict(self):
+        return {"steps": self.steps, "seed": self.seed, "state_bits": self.state_bits, "exp_avg": list(self.exp_avg),
+                "exp_avg_sq": list(self.exp_avg_sq), "scales": None if self.scales is None else list(self.scales)}
+
+    def load_state_dict(self, state):
+        if state["state_bits"] != self.state_bits or len(state["exp_avg"]) != len(self.params):
+            raise ValueError("a state of the same width and number of tensors expected")
+        self.steps, self.seed = int(state["steps"]), int(state["seed"])
+        for mine, other in ((self.exp_avg, state["exp_avg"]), (self.exp_avg_sq, state["exp_avg_sq"]), (self.scales or [], state["scales"] or [])):
+            for a, b in zip(mine, other):
+                a.copy_(b)

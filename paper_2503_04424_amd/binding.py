@@ -24,6 +24,7 @@ FLAG_SCALED_COPY = 32
 FLAG_PIVOT = 64
 FLAG_GENERAL = 128
 FLAG_PIVOT_BLOCK = 256
+ACTIVATIONS = {"none": 0, "relu": 1, "gelu": 2, "gelu_tanh": 3, "silu": 4}
 
 
 class Status:
@@ -68,6 +69,22 @@ class _PlanInfo(C.Structure):
     ]
 
 
+class _AdamwParams(C.Structure):
+    _fields_ = [
+        ("struct_size", C.c_uint32), ("dtype", C.c_int32), ("grad_dtype", C.c_int32),
+        ("state_bits", C.c_int32), ("copy_dtype", C.c_int32), ("seed", C.c_uint32),
+        ("step", C.c_int64), ("lr", C.c_double), ("beta1", C.c_double), ("beta2", C.c_double),
+        ("eps", C.c_double), ("weight_decay", C.c_double), ("grad_scale", C.c_void_p),
+    ]
+
+
+class _NtkLayer(C.Structure):
+    _fields_ = [
+        ("a", C.c_void_p), ("lda", C.c_int64), ("p", C.c_int64),
+        ("g", C.c_void_p), ("ldg", C.c_int64), ("q", C.c_int64),
+    ]
+
+
 PROVIDER_CB = C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64,
                           C.c_void_p, C.c_int64)
 PROVIDER_DEVICE_CB = C.CFUNCTYPE(C.c_int, C.c_void_p, C.c_int64, C.c_int64, C.c_int64, C.c_int64,
@@ -83,6 +100,8 @@ EXPORTS = [
     "mdet_sequence_workspace_query", "mdet_principal_logdets", "mdet_flodance_fit",
     "mdet_flodance_eval", "mdet_step_copy", "mdet_step_mfma_peak",
     "mdet_logdet_device_noalloc",
+    "mdet_linear_workspace_query", "mdet_linear_forward", "mdet_linear_backward",
+    "mdet_adamw_step", "mdet_ntk_gram", "mdet_ntk_workspace_query",
 ]
 
 _lib = None
@@ -126,6 +145,13 @@ def load():
     L.mdet_logdet_device_noalloc.argtypes = [C.POINTER(_Params), vp, i64, vp, vp]
     L.mdet_step_copy.argtypes = [vp, vp, u64, vp]
     L.mdet_step_mfma_peak.argtypes = [i32, i32, i32, i32, vp, C.POINTER(C.c_double), vp]
+    L.mdet_linear_workspace_query.argtypes = [i32, i32, i64, i64, i64, C.POINTER(u64)]
+    L.mdet_linear_forward.argtypes = [i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, i64, vp, i64, vp, u64, vp]
+    L.mdet_linear_backward.argtypes = [i32, i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64, vp, i64,
+                                       vp, vp, i64, vp, u64, vp]
+    L.mdet_adamw_step.argtypes = [C.POINTER(_AdamwParams), vp, i64, vp]
+    L.mdet_ntk_gram.argtypes = [i32, i32, i64, i64, vp, i32, C.c_double, C.c_double, i32, vp, i64, vp, u64, vp]
+    L.mdet_ntk_workspace_query.argtypes = [i32, i32, i64, i64, vp, i32, C.POINTER(u64)]
     L.mdet_strerror.argtypes = [C.c_int]
     L.mdet_strerror.restype = C.c_char_p
     L.mdet_version.restype = C.c_char_p
@@ -563,6 +589,249 @@ def mdet_flodance_eval(coef, q, n_values, out=None, stream=None):
                                    out.data_ptr(), _stream_handle(stream))
     if st != Status.OK:
         raise MemdetError(st)
+    return out
+
+
+_TYPE_CODES = {}
+
+
+def _type_code(dtype) -> int:
+    """_dtype_code, remembered by the torch type."""
+    code = _TYPE_CODES.get(dtype)
+    if code is None:
+        code = _TYPE_CODES[dtype] = _dtype_code(dtype)
+    return code
+
+
+def _activation(name) -> int:
+    try:
+        return ACTIVATIONS[name]
+    except KeyError:
+        raise ValueError(f"activation must be one of {sorted(ACTIVATIONS)}, not {name!r}") from None
+
+
+def _operand_type(t):
+    code = _type_code(t)
+    if code == MDET_F64:
+        raise ValueError("float32, float16 or bfloat16 expected, not float64")
+    return t
+
+
+def _matrix(t, name, rows, cols, dtype):
+    """(address, leading dimension) of a row-major CUDA matrix of this shape and type."""
+    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype != dtype or not t.is_cuda:
+        raise ValueError(f"{name}: a CUDA tensor of {rows} x {cols} {dtype} expected, not {tuple(t.shape)} {t.dtype}")
+    ld, inner = t.stride()
+    if inner != 1 and cols > 1:
+        raise ValueError(f"{name}: rows of consecutive elements expected")
+    return t.data_ptr(), (ld if rows > 1 else max(ld, cols))
+
+
+def _vector(t, name, n, dtype):
+    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous CUDA tensor of {n} {dtype} expected, not {tuple(t.shape)} {t.dtype}")
+    return t.data_ptr()
+
+
+def _check_status(st):
+    if st != Status.OK:
+        raise MemdetError(st)
+
+
+def _new(stream, make):
+    """make() with the stream that the tensor will be used on as the current one: its memory goes back to that stream's
+    order when the tensor is dropped, and a fill runs on it."""
+    if stream is None:
+        return make()
+    import torch
+    s = stream if isinstance(stream, torch.cuda.Stream) else torch.cuda.ExternalStream(_stream_handle(stream).value or 0)
+    with torch.cuda.stream(s):
+        return make()
+
+
+def _operator_workspace(workspace, need, like, stream):
+    """(address, bytes, tensor): the caller's, or a new one of the bytes that are needed."""
+    if workspace is not None:
+        return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
+    if need == 0:
+        return None, 0, None
+    import torch
+    ws = _new(stream, lambda: torch.empty(need, dtype=torch.uint8, device=like.device))
+    return ws.data_ptr(), need, ws
+
+
+def mdet_linear_workspace_query(dtype, m, n, k, backward=False) -> int:
+    """Device bytes of workspace for ``mdet_linear_forward`` or, with ``backward``, the gradient."""
+    b = C.c_uint64(0)
+    _check_status(load().mdet_linear_workspace_query(_type_code(dtype), int(backward), int(m), int(n), int(k), C.byref(b)))
+    return b.value
+
+
+def mdet_linear_forward(x, w, bias=None, residual=None, activation="none", out=None, preact=None, workspace=None,
+                        stream=None):
+    """``act(x w^T + bias) + residual`` on the GPU (asynchronous): x (m, k), w (n, k), bias (n,), residual (m, n), all
+    of one type (float32, float16 or bfloat16), rows of consecutive elements at any distance.  ``preact`` (m, n)
+    receives x w^T + bias for the gradient; ``out`` may be ``residual``.  Returns out."""
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w: matrices expected")
+    t = _operand_type(x.dtype)
+    m, k = x.shape
+    n = w.shape[0]
+    act = _activation(activation)
+    xp, ldx = _matrix(x, "x", m, k, t)
+    wp, ldw = _matrix(w, "w", n, k, t)
+    bp = None if bias is None else _vector(bias, "bias", n, t)
+    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", m, n, t)
+    if out is None:
+        out = _new(stream, lambda: x.new_empty((m, n)))
+    yp, ldy = _matrix(out, "out", m, n, t)
+    zp, ldz = (None, 0) if preact is None else _matrix(preact, "preact", m, n, t)
+    need = 0 if workspace is not None else mdet_linear_workspace_query(t, m, n, k)
+    wsp, wsb, _ws = _operator_workspace(workspace, need, x, stream)
+    _check_status(load().mdet_linear_forward(_type_code(t), act, m, n, k, xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, zp, ldz,
+                                             wsp, wsb, _stream_handle(stream)))
+    return out
+
+
+def mdet_linear_backward(dy, x, w, preact=None, activation="none", dx=True, dw=True, db=True, grad_dtype=None,
+                         dz=None, workspace=None, stream=None):
+    """Gradient of ``mdet_linear_forward`` (asynchronous): (dx, dw, db) from dy (m, n), its x and w, and the ``preact``
+    that it kept (not needed for activation "none").  dx, dw, db: True for a new tensor, False or None for a gradient that
+    is not wanted (None is returned), or the tensor to write; dw and db are of ``grad_dtype``: x's type or float32.
+    ``dz`` (m, n) receives the gradient by x w^T + bias.  The gradient of the residual is dy."""
+    import torch
+    if x.dim() != 2 or w.dim() != 2:
+        raise ValueError("x and w: matrices expected")
+    t = _operand_type(x.dtype)
+    m, k = x.shape
+    n = w.shape[0]
+    act = _activation(activation)
+    gt = t if grad_dtype is None else grad_dtype
+    dyp, lddy = _matrix(dy, "dy", m, n, t)
+    xp, ldx = _matrix(x, "x", m, k, t)
+    wp, ldw = _matrix(w, "w", n, k, t)
+    if act and preact is None:
+        raise ValueError("the gradient through an activation needs preact")
+    zp, ldz = _matrix(preact, "preact", m, n, t) if act else (None, 0)
+
+    def result(what, shape, dtype):
+        if what is True:
+            return _new(stream, lambda: torch.empty(shape, dtype=dtype, device=x.device))
+        return None if what is False else what
+    dx, dw, db = result(dx, (m, k), t), result(dw, (n, k), gt), result(db, (n,), gt)
+    dxp, lddx = (None, 0) if dx is None else _matrix(dx, "dx", m, k, t)
+    dwp, lddw = (None, 0) if dw is None else _matrix(dw, "dw", n, k, gt)
+    dbp = None if db is None else _vector(db, "db", n, gt)
+    dzp, lddz = (None, 0) if dz is None else _matrix(dz, "dz", m, n, t)
+    need = 0 if workspace is not None else mdet_linear_workspace_query(t, m, n, k, backward=True)
+    wsp, wsb, _ws = _operator_workspace(workspace, need, x, stream)
+    _check_status(load().mdet_linear_backward(_type_code(t), _type_code(gt), act, m, n, k, dyp, lddy, zp, ldz, xp, ldx, wp, ldw,
+                                              dxp, lddx, dwp, lddw, dbp, dzp, lddz, wsp, wsb, _stream_handle(stream)))
+    return dx, dw, db
+
+
+def _adamw_pointers(tensors, name, count, dtype, sizes=None):
+    """Addresses of `count` contiguous CUDA tensors of one type (and these sizes)."""
+    if len(tensors) != count:
+        raise ValueError(f"{name}: {count} tensors expected, not {len(tensors)}")
+    for i, t in enumerate(tensors):
+        if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or (sizes is not None and t.numel() != sizes[i]):
+            raise ValueError(f"{name}[{i}]: a contiguous CUDA tensor of {'the same number of ' if sizes else ''}{dtype} expected, "
+                             f"not {tuple(t.shape)} {t.dtype}")
+    return [t.data_ptr() for t in tensors]
+
+
+def mdet_adamw_step(params, grads, exp_avg, exp_avg_sq, *, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
+                    scales=None, copies=None, grad_scale=None, seed=0, stream=None) -> None:
+    """One AdamW step over lists of tensors, in place (asynchronous).  States: float32, or int8 codes of the mean and
+    uint8 codes of the root of the mean square with ``scales[i]``, float32 of ceil(n / 256) x 2.  ``copies``: 16-bit
+    tensors that receive the updated parameters as well.  ``grad_scale``: a float32 CUDA tensor of one element, a
+    factor on all gradients.  ``seed``: of the random rounding of 8-bit states, another one each step."""
+    import torch
+    count = len(params)
+    if count == 0:
+        if any(len(v) for v in (grads, exp_avg, exp_avg_sq)):
+            raise ValueError("no params, but other tensors")
+        return
+    sizes = [t.numel() for t in params]
+    wide = scales is None
+    a = _AdamwParams()
+    a.struct_size = C.sizeof(_AdamwParams)
+    a.dtype, a.grad_dtype = _type_code(params[0].dtype), _type_code(grads[0].dtype if grads else params[0].dtype)
+    a.state_bits = 32 if wide else 8
+    a.copy_dtype = -1 if copies is None else _type_code(copies[0].dtype if copies else torch.bfloat16)
+    a.seed, a.step = int(seed) & 0xFFFFFFFF, int(step)
+    a.lr, a.beta1, a.beta2, a.eps, a.weight_decay = float(lr), float(beta1), float(beta2), float(eps), float(weight_decay)
+    if grad_scale is not None:
+        if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or not grad_scale.is_cuda:
+            raise ValueError("grad_scale: a CUDA tensor of one float32 expected")
+        a.grad_scale = grad_scale.data_ptr()
+    none = [0] * count
+    fields = (
+        _adamw_pointers(params, "params", count, params[0].dtype),
+        _adamw_pointers(grads, "grads", count, grads[0].dtype if grads else None, sizes),
+        _adamw_pointers(exp_avg, "exp_avg", count, torch.float32 if wide else torch.int8, sizes),
+        _adamw_pointers(exp_avg_sq, "exp_avg_sq", count, torch.float32 if wide else torch.uint8, sizes),
+        none if wide else _adamw_pointers(scales, "scales", count, torch.float32, [(n + 255) // 256 * 2 for n in sizes]),
+        none if copies is None else _adamw_pointers(copies, "copies", count, copies[0].dtype if copies else None, sizes),
+        sizes)
+    table = (C.c_uint64 * (7 * count))(*[v for row in zip(*fields) for v in row])
+    _check_status(load().mdet_adamw_step(C.byref(a), C.cast(table, C.c_void_p), count, _stream_handle(stream)))
+
+
+def _ntk_layers(inputs, signals, outputs):
+    if len(inputs) != len(signals):
+        raise ValueError("inputs and signals: one of each for every layer expected")
+    if not inputs:
+        raise ValueError("at least one layer expected")
+    n, dtype = inputs[0].shape[0], inputs[0].dtype
+    table = (_NtkLayer * len(inputs))()
+    for layer, a, g in zip(table, inputs, signals):
+        if a.dim() != 2 or g.dim() != 2:
+            raise ValueError("inputs and signals: matrices expected")
+        layer.p, layer.q = a.shape[1], g.shape[1]
+        layer.a, layer.lda = _matrix(a, "inputs", n, layer.p, dtype)
+        layer.g, layer.ldg = _matrix(g, "signals", n * outputs, layer.q, dtype)
+    return n, dtype, table
+
+
+def mdet_ntk_workspace_query(inputs, signals, out_dtype, outputs=1) -> int:
+    """Device bytes of workspace for ``mdet_ntk_gram`` on these layers."""
+    n, dtype, table = _ntk_layers(inputs, signals, int(outputs))
+    b = C.c_uint64(0)
+    _check_status(load().mdet_ntk_workspace_query(_type_code(dtype), _type_code(out_dtype), n, int(outputs),
+                                                  C.cast(table, C.c_void_p), len(table), C.byref(b)))
+    return b.value
+
+
+def mdet_ntk_gram(inputs, signals, out=None, outputs=1, bias=1.0, scale=1.0, accumulate=False, workspace=None, stream=None):
+    """Lower triangle of the Gram matrix of a network's Jacobian on the GPU (asynchronous):
+    ``scale * sum_layers (a a^T + bias) * (g g^T)`` from each layer's inputs a (n, p) and the derivatives g
+    (n * outputs, q) of the network's outputs by the layer's results, row i * outputs + r for output r at sample i.
+    ``out`` (float32 or float64, also the type of the arithmetic; nothing above its diagonal is written) is
+    added to with ``accumulate``; a new one is zero above the diagonal.  Returns out."""
+    import torch
+    outputs = int(outputs)
+    if outputs < 1:
+        raise ValueError("outputs must be 1 or more")
+    n, dtype, table = _ntk_layers(inputs, signals, outputs)
+    order = n * outputs
+    if out is None:
+        if accumulate:
+            raise ValueError("accumulate needs out")
+        wide = torch.float64 if dtype == torch.float64 else torch.float32
+        out = _new(stream, lambda: torch.zeros((order, order), dtype=wide, device=inputs[0].device))
+    if out.dtype not in (torch.float32, torch.float64):
+        raise ValueError("out: float32 or float64 expected")
+    kp, ldk = _matrix(out, "out", order, order, out.dtype)
+    lib_, layers = load(), C.cast(table, C.c_void_p)
+    need = C.c_uint64(0)
+    codes = _type_code(dtype), _type_code(out.dtype)
+    if workspace is None:
+        _check_status(lib_.mdet_ntk_workspace_query(*codes, n, outputs, layers, len(table), C.byref(need)))
+    wsp, wsb, _ws = _operator_workspace(workspace, need.value, out, stream)
+    _check_status(lib_.mdet_ntk_gram(*codes, n, outputs, layers, len(table), float(bias), float(scale), int(bool(accumulate)),
+                                     kp, ldk, wsp, wsb, _stream_handle(stream)))
     return out
 
 

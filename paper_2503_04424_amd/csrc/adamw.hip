@@ -1,0 +1,93 @@
+// C ABI of the AdamW step over many tensors: argument checks and kernel launches.  A call only queues work on the
+// caller's stream; nothing is allocated and nothing is waited for.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "kernels_adamw.h"
+
+namespace {
+
+using namespace mdet;
+
+template <typename P, typename G, typename CP>
+void launch(const int bits, const AdamwFactors& f, const AdamwTensors& list, hipStream_t st) {
+  const dim3 grid(list.first[list.count]), block(ADAMW_THREADS);
+  if (bits == 32) hipLaunchKernelGGL((adamw_kernel<P, G, CP, 32>), grid, block, 0, st, f, list);
+  else hipLaunchKernelGGL((adamw_kernel<P, G, CP, 8>), grid, block, 0, st, f, list);
+}
+
+template <typename P, typename G>
+void launch_copy(const mdet_adamw_params& a, const AdamwFactors& f, const AdamwTensors& list, hipStream_t st) {
+  if (a.copy_dtype == MDET_BF16) launch<P, G, __bf16>(a.state_bits, f, list, st);
+  else if (a.copy_dtype == MDET_F16) launch<P, G, _Float16>(a.state_bits, f, list, st);
+  else launch<P, G, void>(a.state_bits, f, list, st);
+}
+
+template <typename P>
+void launch_grad(const mdet_adamw_params& a, const AdamwFactors& f, const AdamwTensors& list, hipStream_t st) {
+  if (a.grad_dtype == MDET_F32) launch_copy<P, float>(a, f, list, st);
+  else if (a.grad_dtype == MDET_BF16) launch_copy<P, __bf16>(a, f, list, st);
+  else launch_copy<P, _Float16>(a, f, list, st);
+}
+
+bool is_param_type(int t) { return t == MDET_F32 || t == MDET_F16 || t == MDET_BF16; }
+bool is_part(double x) { return x >= 0.0 && x < 1.0; }
+
+}  // namespace
+
+extern "C" int mdet_adamw_step(const mdet_adamw_params* a, const mdet_adamw_tensor* tensors, int64_t count, void* stream) {
+  if (!a || a->struct_size != sizeof(mdet_adamw_params) || count < 0 || (count > 0 && !tensors)) return MDET_EINVAL;
+  if (!is_param_type(a->dtype) || !is_param_type(a->grad_dtype)) return MDET_EINVAL;
+  if (a->copy_dtype != -1 && a->copy_dtype != MDET_F16 && a->copy_dtype != MDET_BF16) return MDET_EINVAL;
+  if ((a->state_bits != 32 && a->state_bits != 8) || a->step < 1 || count > INT32_MAX) return MDET_EINVAL;
+  if (!is_part(a->beta1) || !is_part(a->beta2) || !(a->eps >= 0.0) || !std::isfinite(a->lr) || !std::isfinite(a->weight_decay) ||
+      !std::isfinite(a->eps))
+    return MDET_EINVAL;
+  for (int64_t i = 0; i < count; ++i) {
+    const mdet_adamw_tensor& t = tensors[i];
+    if (t.n < 0) return MDET_EINVAL;
+    if (t.n == 0) continue;
+    if (!t.p || !t.g || !t.m || !t.v || (a->state_bits == 8 && !t.scales) || (a->copy_dtype != -1 && !t.copy)) return MDET_EINVAL;
+    const uintptr_t ps = a->dtype == MDET_F32 ? 4 : 2, gs = a->grad_dtype == MDET_F32 ? 4 : 2;
+    if ((uintptr_t)t.p % ps || (uintptr_t)t.g % gs) return MDET_EINVAL;
+    if (a->state_bits == 32 && (((uintptr_t)t.m | (uintptr_t)t.v) % 4)) return MDET_EINVAL;
+    if ((a->state_bits == 8 && (uintptr_t)t.scales % 4) || (a->copy_dtype != -1 && (uintptr_t)t.copy % 2)) return MDET_EINVAL;
+    if (t.n > (int64_t)INT32_MAX * ADAMW_CHUNK) return MDET_EINVAL;
+  }
+  AdamwFactors f;
+  f.b1 = (float)a->beta1;
+  f.a1 = (float)(1.0 - a->beta1);
+  f.b2 = (float)a->beta2;
+  f.a2 = (float)(1.0 - a->beta2);
+  f.keep = (float)(1.0 - a->lr * a->weight_decay);
+  f.rate = (float)(a->lr / (1.0 - std::pow(a->beta1, (double)a->step)));
+  f.root = (float)(1.0 / std::sqrt(1.0 - std::pow(a->beta2, (double)a->step)));
+  f.eps = (float)a->eps;
+  f.grad_scale = a->grad_scale;
+  f.seed = a->seed;
+  hipStream_t st = (hipStream_t)stream;
+  AdamwTensors list;
+  list.count = 0;
+  list.first[0] = 0;
+  f.first_tensor = 0;
+  // Tensors without elements keep their number (the hash goes by it) and take no chunk.
+  for (int64_t i = 0; i <= count; ++i) {
+    const int64_t chunks = i < count ? (tensors[i].n + ADAMW_CHUNK - 1) / ADAMW_CHUNK : 0;
+    if (i == count || list.count == ADAMW_TENSORS || list.first[list.count] + chunks > INT32_MAX) {
+      if (list.first[list.count] > 0) {
+        if (a->dtype == MDET_F32) launch_grad<float>(*a, f, list, st);
+        else if (a->dtype == MDET_BF16) launch_grad<__bf16>(*a, f, list, st);
+        else launch_grad<_Float16>(*a, f, list, st);
+        if (hipGetLastError() != hipSuccess) return MDET_EHIP;
+      }
+      f.first_tensor = (int)i;
+      list.count = 0;
+    }
+    if (i == count) break;
+    list.t[list.count] = tensors[i];
+    list.first[list.count + 1] = list.first[list.count] + (uint32_t)chunks;
+    ++list.count;
+  }
+  return MDET_OK;
+}

@@ -1,0 +1,139 @@
+// C ABI of the Gram matrix of a network's Jacobian: argument checks, workspace layout and kernel launches.  A call only
+// queues work on the caller's stream; nothing is allocated and nothing is waited for.
+#include <hip/hip_runtime.h>
+
+#include <cmath>
+
+#include "kernels_ntk.h"
+#include "../../include/memdet.h"
+
+namespace {
+
+using namespace mdet;
+
+inline uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
+inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
+inline int64_t size_of(int32_t t) { return t == MDET_F64 ? 8 : t == MDET_F32 ? 4 : 2; }
+inline int launch_status() { return hipGetLastError() == hipSuccess ? MDET_OK : MDET_EHIP; }
+
+constexpr int64_t MOST = int64_t(1) << 31;
+
+// Types, sizes and strides; pointers only where `pointers` is set.
+int check(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs, const mdet_ntk_layer* layers, int32_t count, bool pointers) {
+  if (dtype < MDET_F32 || dtype > MDET_BF16 || (out_dtype != MDET_F32 && out_dtype != MDET_F64)) return MDET_EINVAL;
+  if (dtype == MDET_F64 && out_dtype == MDET_F32) return MDET_EINVAL;      // arithmetic narrower than the operands
+  if (n < 0 || outputs < 1 || count < 0 || (count > 0 && !layers)) return MDET_EINVAL;
+  if (n > MOST || outputs > MOST || (n > 0 && outputs > MOST / n)) return MDET_EINVAL;
+  for (int l = 0; l < count; ++l) {
+    const mdet_ntk_layer& x = layers[l];
+    if (x.p < 0 || x.q < 0 || x.p > MOST || x.q > MOST) return MDET_EINVAL;
+    if (!pointers || n == 0) continue;
+    const int64_t s = size_of(dtype);
+    if (x.p > 0 && (!x.a || (uintptr_t)x.a % s || x.lda > MOST || x.lda < 0 || (n > 1 && x.lda < x.p))) return MDET_EINVAL;
+    if (x.q > 0 && (!x.g || (uintptr_t)x.g % s || x.ldg > MOST || x.ldg < 0 || (n * outputs > 1 && x.ldg < x.q))) return MDET_EINVAL;
+  }
+  return MDET_OK;
+}
+
+// A widened operand's bytes, rows of whole pieces.
+inline uint64_t wide_bytes(int64_t rows, int64_t cols) { return up256((uint64_t)rows * (ceil_div(cols, 2) * 2) * 8); }
+
+template <typename S>
+void widen(const void* from, int64_t ld, int64_t rows, int64_t cols, double* to, hipStream_t st) {
+  const int64_t ldto = ceil_div(cols, 2) * 2, blocks = ceil_div(rows * ldto, 256);
+  if (blocks > 0) hipLaunchKernelGGL(ntk_widen_kernel<S>, dim3((unsigned)blocks), dim3(256), 0, st, (const S*)from, ld, to, rows, cols, ldto);
+}
+
+struct Call {
+  int64_t n, d;
+  double bias, scale;
+  int accumulate;
+  void* K;
+  int64_t ldk;
+  hipStream_t st;
+};
+
+template <typename T>
+int gram(const mdet_ntk_layer* layers, int32_t count, const Call& c) {
+  typedef typename Core<T>::acc1_t A;
+  const int64_t rows = ceil_div(c.n * c.d, PLAIN_TILE), blocks = rows * (rows + 1) / 2;
+  if (blocks > INT32_MAX) return MDET_EINVAL;
+  int accumulate = c.accumulate;
+  for (int32_t l0 = 0; l0 == 0 || l0 < count; l0 += NTK_LAYERS) {
+    NtkLayers<T> list;
+    list.count = count - l0 < NTK_LAYERS ? count - l0 : NTK_LAYERS;
+    for (int l = 0; l < list.count; ++l) {
+      const mdet_ntk_layer& x = layers[l0 + l];
+      list.a[l] = (const T*)x.a, list.lda[l] = x.lda, list.p[l] = x.p;
+      list.g[l] = (const T*)x.g, list.ldg[l] = x.ldg, list.q[l] = x.q;
+    }
+    hipLaunchKernelGGL(ntk_plain_kernel<T>, dim3((unsigned)blocks), dim3(PLAIN_THREADS), 0, c.st, list, c.n, c.d, (A)c.bias, (A)c.scale,
+                       accumulate, (A*)c.K, c.ldk);
+    accumulate = 1;
+  }
+  return launch_status();
+}
+
+}  // namespace
+
+extern "C" {
+
+int mdet_ntk_workspace_query(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs, const mdet_ntk_layer* layers, int32_t count,
+                             uint64_t* bytes) {
+  if (!bytes) return MDET_EINVAL;
+  const int status = check(dtype, out_dtype, n, outputs, layers, count, false);
+  if (status != MDET_OK) return status;
+  uint64_t sum = 0;
+  if (out_dtype == MDET_F64 && dtype != MDET_F64)
+    for (int l = 0; l < count; ++l) sum += wide_bytes(n, layers[l].p) + wide_bytes(n * outputs, layers[l].q);
+  *bytes = sum;
+  return MDET_OK;
+}
+
+int mdet_ntk_gram(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs, const mdet_ntk_layer* layers, int32_t count, double bias,
+                  double scale, int32_t accumulate, void* K, int64_t ldk, void* workspace, uint64_t workspace_bytes, void* stream) {
+  int status = check(dtype, out_dtype, n, outputs, layers, count, true);
+  if (status != MDET_OK) return status;
+  if (!std::isfinite(bias) || !std::isfinite(scale)) return MDET_EINVAL;
+  const int64_t N = n * outputs;
+  if (N == 0) return MDET_OK;
+  if (!K || (uintptr_t)K % size_of(out_dtype) || (N > 1 && ldk < N) || ldk > MOST) return MDET_EINVAL;
+  uint64_t need = 0;
+  mdet_ntk_workspace_query(dtype, out_dtype, n, outputs, layers, count, &need);
+  if (need && (!workspace || (uintptr_t)workspace % 256)) return MDET_EINVAL;
+  if (workspace_bytes < need) return MDET_ENOMEM_DEVICE;
+  hipStream_t st = (hipStream_t)stream;
+  const Call c{n, outputs, bias, scale, accumulate, K, ldk, st};
+  if (out_dtype == MDET_F32)
+    return dtype == MDET_F32 ? gram<float>(layers, count, c) : dtype == MDET_BF16 ? gram<__bf16>(layers, count, c) : gram<_Float16>(layers, count, c);
+  if (dtype == MDET_F64) return gram<double>(layers, count, c);
+  // narrower operands: exact copies in fp64, one launch's layers after the other in the workspace
+  char* at = (char*)workspace;
+  int acc = accumulate;
+  for (int32_t l0 = 0; l0 == 0 || l0 < count; l0 += NTK_LAYERS) {
+    mdet_ntk_layer wide[NTK_LAYERS];
+    const int some = count - l0 < NTK_LAYERS ? count - l0 : NTK_LAYERS;
+    for (int l = 0; l < some; ++l) {
+      wide[l] = layers[l0 + l];
+      auto one = [&](const void*& p, int64_t& ld, int64_t rows, int64_t cols) {
+        double* const to = (double*)at;
+        at += wide_bytes(rows, cols);
+        if (dtype == MDET_F32) widen<float>(p, ld, rows, cols, to, st);
+        else if (dtype == MDET_BF16) widen<__bf16>(p, ld, rows, cols, to, st);
+        else widen<_Float16>(p, ld, rows, cols, to, st);
+        p = to;
+        ld = ceil_div(cols, 2) * 2;
+      };
+      one(wide[l].a, wide[l].lda, n, wide[l].p);
+      one(wide[l].g, wide[l].ldg, N, wide[l].q);
+    }
+    Call part = c;
+    part.accumulate = acc;
+    status = gram<double>(wide, some, part);
+    if (status != MDET_OK) return status;
+    acc = 1;
+  }
+  return MDET_OK;
+}
+
+}  // extern "C"
