@@ -81,6 +81,7 @@ struct LinearOut {
   int64_t ldz;
   int act;
   int64_t rows, cols;
+  bool vec;                            // rows of y, bias, residual and z start where four elements can be moved at once
 };
 
 template <typename T, typename O, int ACT>
@@ -105,6 +106,138 @@ __global__ __launch_bounds__(PLAIN_THREADS) void linear_plain_kernel(const Opera
       if (row0 + i < out.rows && col0 + j < out.cols) linear_put<T, O, decltype(act)::value>(out, row0 + i, col0 + j, acc[a][b][e]);
     });
   });
+}
+
+// Four neighbours of a row, from column j on.
+template <typename T, typename O, int ACT>
+__device__ __forceinline__ void linear_put4(const LinearOut<T, O>& o, const int64_t i, const int64_t j, const float (&in)[4]) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  typedef O o4 __attribute__((ext_vector_type(4)));
+  if (!o.vec || j + 4 > o.cols) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e)
+      if (j + e < o.cols) linear_put<T, O, ACT>(o, i, j + e, in[e]);
+    return;
+  }
+  float v[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = in[e];
+  if (o.bias) {
+    const t4 b = *reinterpret_cast<const t4*>(o.bias + j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += (float)b[e];
+  }
+  if (o.z) {
+    t4 z;
+#pragma unroll
+    for (int e = 0; e < 4; ++e) z[e] = (T)v[e];
+    *reinterpret_cast<t4*>(o.z + i * o.ldz + j) = z;
+  }
+#pragma unroll
+  for (int e = 0; e < 4; ++e) v[e] = act_value<ACT>(v[e]);
+  if (o.residual) {
+    const t4 r = *reinterpret_cast<const t4*>(o.residual + i * o.ldr + j);
+#pragma unroll
+    for (int e = 0; e < 4; ++e) v[e] += (float)r[e];
+  }
+  o4 y;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) y[e] = (O)v[e];
+  *reinterpret_cast<o4*>(o.y + i * o.ldy + j) = y;
+}
+
+// Rows of a wavefront's part that go through its share of LDS at once on their way out: what lies 16 lanes apart in the
+// accumulators is put side by side, whole lines leave, and the code of the activations stands once in a loop.
+template <typename S>
+struct LinearLds {
+  static constexpr int ROWS = S::TM * 16 < 64 ? S::TM * 16 : 64, COLS = S::TN * 16, PITCH = COLS + 4;
+  static constexpr int WAVE_BYTES = ROWS * PITCH * 4;
+  static constexpr int BYTES = S::WAVES * WAVE_BYTES > 2 * S::SLAB ? S::WAVES * WAVE_BYTES : 2 * S::SLAB;
+};
+
+// A tile of the layer.  SPLIT: part blockIdx / tiles of the sum over k, kept in fp32 for linear_join_kernel.
+template <typename T, typename O, typename S, bool ROUTER, bool COUTER, bool DIRECT, bool SPLIT>
+__global__ __launch_bounds__(S::THREADS) void linear_tile_kernel(const Operand<T> r, const Operand<T> c, const int64_t k, const LinearOut<T, O> out,
+                                                                 float* const parts, const int splits, const int64_t kpart) {
+  typedef LinearLds<S> L;
+  __shared__ __attribute__((aligned(16))) char lds[L::BYTES];
+  const int64_t down = (out.rows + S::BM - 1) / S::BM, across = (out.cols + S::BN - 1) / S::BN, tiles = down * across;
+  const int64_t t = gemm_tile_number(blockIdx.x, tiles * splits);
+  if (t < 0) return;
+  int64_t bi, bj;
+  gemm_tile_place(t % tiles, down, across, bi, bj);
+  const int64_t part = t / tiles, k0 = part * kpart, kend = k0 + kpart < k ? k0 + kpart : k;
+  const int64_t row0 = bi * S::BM, col0 = bj * S::BN;
+  typename Core<T>::acc_t acc[S::TN][S::TM] = {};
+  tile_accumulate<T, S, ROUTER, COUTER, DIRECT>(acc, lds, r, c, row0, col0, k0, kend);
+
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  float* const mine = reinterpret_cast<float*>(lds + wave * L::WAVE_BYTES);
+  const int64_t wrow = row0 + wave / S::WN * S::TM * 16, wcol = col0 + wave % S::WN * S::TN * 16;
+  constexpr int LANES = L::COLS / 4, STEP = 64 / LANES;        // lanes of a row, rows of a step
+  __syncthreads();                                             // the operands are not read any more
+#pragma unroll
+  for (int b0 = 0; b0 < S::TM; b0 += L::ROWS / 16) {
+#pragma unroll
+    for (int b = 0; b < L::ROWS / 16; ++b)
+#pragma unroll
+      for (int a = 0; a < S::TN; ++a)
+        *reinterpret_cast<typename Core<T>::acc_t*>(mine + (16 * b + (lane & 15)) * L::PITCH + 16 * a + 4 * (lane >> 4)) = acc[a][b0 + b];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    auto rows = [&](auto&& f) {
+#pragma unroll 1
+      for (int s = 0; s < L::ROWS; s += STEP) {
+        const int row = s + lane / LANES, col = lane % LANES * 4;
+        const int64_t i = wrow + b0 * 16 + row, j = wcol + col;
+        const typename Core<T>::acc_t v = *reinterpret_cast<const typename Core<T>::acc_t*>(mine + row * L::PITCH + col);
+        const float in[4] = {v[0], v[1], v[2], v[3]};
+        if (i < out.rows && j < out.cols) f(i, j, in);
+      }
+    };
+    if constexpr (SPLIT) {
+      float* const to = parts + part * out.rows * out.cols;
+      const bool vec = out.cols % 4 == 0;
+      rows([&](const int64_t i, const int64_t j, const float (&in)[4]) {
+        if (vec) *reinterpret_cast<typename Core<T>::acc_t*>(to + i * out.cols + j) = typename Core<T>::acc_t{in[0], in[1], in[2], in[3]};
+        else
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (j + e < out.cols) to[i * out.cols + j + e] = in[e];
+      });
+    } else {
+      act_switch(out.act, [&](auto act) {
+        rows([&](const int64_t i, const int64_t j, const float (&in)[4]) { linear_put4<T, O, decltype(act)::value>(out, i, j, in); });
+      });
+    }
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
+}
+
+// The parts of the sum over k, added in their order, on their way out.
+template <typename T, typename O>
+__global__ __launch_bounds__(256) void linear_join_kernel(const float* __restrict__ parts, const int splits, const LinearOut<T, O> out) {
+  const int64_t across = (out.cols + 3) / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+  const int64_t i = id / across, j = id % across * 4;
+  if (i >= out.rows) return;
+  const int64_t size = out.rows * out.cols;
+  const float* from = parts + i * out.cols + j;
+  float v[4] = {};
+  if (out.cols % 4 == 0) {
+    typedef float f4 __attribute__((ext_vector_type(4)));
+    for (int s = 0; s < splits; ++s, from += size) {
+      const f4 x = *reinterpret_cast<const f4*>(from);
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] += x[e];
+    }
+  } else {
+    for (int s = 0; s < splits; ++s, from += size)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        if (j + e < out.cols) v[e] += from[e];
+  }
+  act_switch(out.act, [&](auto act) { linear_put4<T, O, decltype(act)::value>(out, i, j, v); });
 }
 
 // dz = dy act'(z) and the column sums of DZ_ROWS rows of it: a workgroup takes 64 columns, thread (t, c) every fourth row of

@@ -30,25 +30,101 @@ inline bool matrix_ok(const void* p, int64_t r, int64_t c, int64_t ld, int64_t s
   return p && (uintptr_t)p % size == 0 && (r == 1 || ld >= c) && ld >= 0 && ld <= MOST;
 }
 
+// Whether four elements at a time can be moved at this place.
+template <typename T>
+bool four(const void* p, int64_t ld, int64_t rows) {
+  return !p || ((uintptr_t)p % (4 * sizeof(T)) == 0 && (rows == 1 || ld % 4 == 0));
+}
+
+// Whether an operand's pieces can go straight to LDS: rows on 16 bytes (with k outer their number a whole number of
+// pieces), offsets within a slab in 32 bits.
+template <typename T, bool OUTER, int B>
+bool straight(const Operand<T>& o, int64_t k) {
+  const int64_t bytes = o.stride * (int64_t)sizeof(T), lines = OUTER ? k : o.rows;
+  return (uintptr_t)o.p % 16 == 0 && (lines == 1 || bytes % 16 == 0) && (!OUTER || o.rows % Core<T>::VEC == 0) &&
+         bytes < (int64_t(1) << 31) / (B > 64 ? B : 64);
+}
+
+typedef Tile<256, 256, 2, 4> Big;
+typedef Tile<128, 128, 2, 2> Mid;
+typedef Tile<64, 64, 2, 2> Small;
+
+// How a product is cut: tile shape and parts of the sum over k.
+struct Cut {
+  int shape;                           // 0 small, 1 mid, 2 big
+  int splits;
+  int64_t kpart;
+};
+Cut cut_of(int64_t rows, int64_t cols, int64_t k, int64_t size) {
+  Cut c;
+  const int64_t bk = 128 / size;
+  auto tiles = [&](int64_t b) { return ceil_div(rows, b) * ceil_div(cols, b); };
+  c.shape = size == 2 && tiles(256) >= 192 ? 2 : tiles(128) >= 192 ? 1 : 0;
+  c.splits = 1;
+  c.kpart = k;
+  const int64_t t = tiles(c.shape == 2 ? 256 : c.shape == 1 ? 128 : 64);
+  if (c.shape == 0 && t < 256 && k >= 8 * bk) {
+    int64_t most = k / (4 * bk), want = ceil_div(512, t);
+    int64_t s = want < most ? want : most;
+    if (s > 16) s = 16;
+    if (s > 1) {
+      c.kpart = ceil_div(ceil_div(k, s), bk) * bk;
+      c.splits = (int)ceil_div(k, c.kpart);
+    }
+  }
+  return c;
+}
+uint64_t parts_bytes(const Cut& c, int64_t rows, int64_t cols) { return c.splits > 1 ? up256((uint64_t)c.splits * rows * cols * 4) : 0; }
+
+template <typename T, typename O, typename S, bool ROUTER, bool COUTER>
+void tiles(const Operand<T>& r, const Operand<T>& c, int64_t k, const LinearOut<T, O>& out, const Cut& cut, float* parts, hipStream_t st) {
+  const int64_t n = ceil_div(out.rows, S::BM) * ceil_div(out.cols, S::BN) * cut.splits;
+  const dim3 grid((unsigned)(ceil_div(n, 8) * 8)), block(S::THREADS);
+  const bool direct = straight<T, ROUTER, S::BM>(r, k) && straight<T, COUTER, S::BN>(c, k);
+  auto go = [&](auto d, auto split) {
+    hipLaunchKernelGGL((linear_tile_kernel<T, O, S, ROUTER, COUTER, decltype(d)::value, decltype(split)::value>), grid, block, 0, st, r, c, k, out,
+                       parts, cut.splits, cut.kpart);
+  };
+  using std::false_type;
+  using std::true_type;
+  if (cut.splits > 1) {
+    if constexpr (S::BM == 64) {
+      if (direct) go(true_type{}, true_type{});
+      else go(false_type{}, true_type{});
+      const int64_t groups = ceil_div(out.rows * ceil_div(out.cols, 4), 256);
+      hipLaunchKernelGGL((linear_join_kernel<T, O>), dim3((unsigned)groups), dim3(256), 0, st, (const float*)parts, cut.splits, out);
+    }
+  } else if (direct) go(true_type{}, false_type{});
+  else go(false_type{}, false_type{});
+}
+
 template <typename T, typename O, bool ROUTER, bool COUTER>
-int product(const Operand<T>& r, const Operand<T>& c, int64_t k, const LinearOut<T, O>& out, hipStream_t st) {
-  const int64_t tiles = ceil_div(out.rows, PLAIN_TILE) * ceil_div(out.cols, PLAIN_TILE);
-  if (tiles > INT32_MAX) return MDET_EINVAL;
-  hipLaunchKernelGGL((linear_plain_kernel<T, O, ROUTER, COUTER>), dim3((unsigned)tiles), dim3(PLAIN_THREADS), 0, st, r, c, k, out);
+int product(const Operand<T>& r, const Operand<T>& c, int64_t k, LinearOut<T, O> out, float* parts, hipStream_t st) {
+  const Cut cut = cut_of(out.rows, out.cols, k, sizeof(T));
+  if (ceil_div(out.rows, 64) * ceil_div(out.cols, 64) > INT32_MAX / 32) return MDET_EINVAL;
+  out.vec = four<O>(out.y, out.ldy, out.rows) && four<T>(out.bias, 0, 1) && four<T>(out.residual, out.ldr, out.rows) &&
+            four<T>(out.z, out.ldz, out.rows);
+  if (cut.shape == 2) {
+    if constexpr (sizeof(T) == 2) tiles<T, O, Big, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
+  } else if (cut.shape == 1) tiles<T, O, Mid, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
+  else tiles<T, O, Small, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
   return launch_status();
 }
 
-// Workspace of the gradient: dz, then the strips' column sums.
+// Workspace of the gradient: dz, then the strips' column sums, then the parts of a product that is split.
 struct GradLayout {
   int64_t strips, lddz;
-  uint64_t sums, bytes;
+  uint64_t sums, parts, bytes;
 };
-GradLayout grad_layout(int32_t dtype, int64_t m, int64_t n) {
+GradLayout grad_layout(int32_t dtype, int64_t m, int64_t n, int64_t k) {
   GradLayout g;
   g.strips = ceil_div(m, DZ_ROWS);
   g.lddz = ceil_div(n, 8) * 8;
   g.sums = up256((uint64_t)m * g.lddz * size_of(dtype));
-  g.bytes = g.sums + up256((uint64_t)g.strips * n * 4);
+  g.parts = g.sums + up256((uint64_t)g.strips * n * 4);
+  const int64_t s = size_of(dtype);
+  const uint64_t dx = parts_bytes(cut_of(m, k, n, s), m, k), dw = parts_bytes(cut_of(n, k, m, s), n, k);
+  g.bytes = g.parts + (dx > dw ? dx : dw);
   return g;
 }
 
@@ -65,7 +141,8 @@ struct Grad {
 
 template <typename T, typename O>
 int backward(const Grad& g) {
-  const GradLayout lay = grad_layout(std::is_same<T, float>::value ? MDET_F32 : MDET_F16, g.m, g.n);
+  const GradLayout lay = grad_layout(std::is_same<T, float>::value ? MDET_F32 : MDET_F16, g.m, g.n, g.k);
+  float* const parts = (float*)(g.workspace + lay.parts);
   const bool own_dz = g.dz || (g.act != MDET_ACT_NONE && (g.dx || g.dw));
   T* const dz = g.dz ? (T*)g.dz : own_dz ? (T*)g.workspace : nullptr;
   const int64_t lddz = g.dz ? g.lddz : lay.lddz;
@@ -83,12 +160,12 @@ int backward(const Grad& g) {
   const T* const d = own_dz ? dz : (const T*)g.dy;
   const int64_t ldd = own_dz ? lddz : g.lddy;
   if (status == MDET_OK && g.dx && g.m > 0 && g.k > 0) {
-    const LinearOut<T, T> out{(T*)g.dx, g.lddx, nullptr, nullptr, 0, nullptr, 0, MDET_ACT_NONE, g.m, g.k};
-    status = product<T, T, false, true>(Operand<T>{d, ldd, g.m}, Operand<T>{(const T*)g.w, g.ldw, g.k}, g.n, out, g.st);
+    const LinearOut<T, T> out{(T*)g.dx, g.lddx, nullptr, nullptr, 0, nullptr, 0, MDET_ACT_NONE, g.m, g.k, false};
+    status = product<T, T, false, true>(Operand<T>{d, ldd, g.m}, Operand<T>{(const T*)g.w, g.ldw, g.k}, g.n, out, parts, g.st);
   }
   if (status == MDET_OK && g.dw && g.n > 0 && g.k > 0) {
-    const LinearOut<T, O> out{(O*)g.dw, g.lddw, nullptr, nullptr, 0, nullptr, 0, MDET_ACT_NONE, g.n, g.k};
-    status = product<T, O, true, true>(Operand<T>{d, ldd, g.n}, Operand<T>{(const T*)g.x, g.ldx, g.k}, g.m, out, g.st);
+    const LinearOut<T, O> out{(O*)g.dw, g.lddw, nullptr, nullptr, 0, nullptr, 0, MDET_ACT_NONE, g.n, g.k, false};
+    status = product<T, O, true, true>(Operand<T>{d, ldd, g.n}, Operand<T>{(const T*)g.x, g.ldx, g.k}, g.m, out, parts, g.st);
   }
   return status;
 }
@@ -99,7 +176,7 @@ extern "C" {
 
 int mdet_linear_workspace_query(int32_t dtype, int32_t backward, int64_t m, int64_t n, int64_t k, uint64_t* bytes) {
   if (!bytes || !is_type(dtype) || !sizes_fit(m, n, k)) return MDET_EINVAL;
-  *bytes = backward ? grad_layout(dtype, m, n).bytes : 0;
+  *bytes = backward ? grad_layout(dtype, m, n, k).bytes : parts_bytes(cut_of(m, n, k, size_of(dtype)), m, n);
   return MDET_OK;
 }
 
@@ -112,13 +189,13 @@ int mdet_linear_forward(int32_t dtype, int32_t activation, int64_t m, int64_t n,
   if ((residual && !matrix_ok(residual, m, n, ldr, s)) || (z && !matrix_ok(z, m, n, ldz, s)) || (uintptr_t)bias % s) return MDET_EINVAL;
   uint64_t need = 0;
   mdet_linear_workspace_query(dtype, 0, m, n, k, &need);
-  if (need && !workspace) return MDET_EINVAL;
+  if (need && (!workspace || (uintptr_t)workspace % 256)) return MDET_EINVAL;
   if (workspace_bytes < need) return MDET_ENOMEM_DEVICE;
   if (m == 0 || n == 0) return MDET_OK;
   auto call = [&](auto zero) {
     typedef decltype(zero) T;
-    const LinearOut<T, T> out{(T*)y, ldy, (const T*)bias, (const T*)residual, ldr, (T*)z, ldz, activation, m, n};
-    return product<T, T, false, false>(Operand<T>{(const T*)x, ldx, m}, Operand<T>{(const T*)w, ldw, n}, k, out, (hipStream_t)stream);
+    const LinearOut<T, T> out{(T*)y, ldy, (const T*)bias, (const T*)residual, ldr, (T*)z, ldz, activation, m, n, false};
+    return product<T, T, false, false>(Operand<T>{(const T*)x, ldx, m}, Operand<T>{(const T*)w, ldw, n}, k, out, (float*)workspace, (hipStream_t)stream);
   };
   return dtype == MDET_F32 ? call(0.0f) : dtype == MDET_BF16 ? call((__bf16)0.0f) : call((_Float16)0.0f);
 }
