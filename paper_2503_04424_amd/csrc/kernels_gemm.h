@@ -74,75 +74,6 @@ struct Operand {
 };
 
 // ---------------------------------------------------------------------------
-// The plain tile: 64 x 64 of D by four wavefronts (32 x 32 each), any strides and alignment, every element guarded.
-// ---------------------------------------------------------------------------
-constexpr int PLAIN_TILE = 64;
-constexpr int PLAIN_THREADS = 256;
-
-template <typename T>
-struct PlainLds {
-  typename Core<T>::piece_t r[PLAIN_TILE][GEMM_PIECES + 1], c[PLAIN_TILE][GEMM_PIECES + 1];
-};
-
-// One slab of one operand, rows i0 .. i0 + 63, into LDS; what lies outside of the operand is zero.
-template <typename T, bool OUTER>
-__device__ __forceinline__ void plain_stage(typename Core<T>::piece_t (&to)[PLAIN_TILE][GEMM_PIECES + 1], const Operand<T>& o,
-                                            const int64_t i0, const int64_t k0, const int64_t kend) {
-  constexpr int VEC = Core<T>::VEC;
-#pragma unroll
-  for (int s = 0; s < PLAIN_TILE * GEMM_PIECES / PLAIN_THREADS; ++s) {
-    const int id = s * PLAIN_THREADS + (int)threadIdx.x;
-    // neighbouring threads read neighbouring memory
-    const int row = OUTER ? id % PLAIN_TILE : id / GEMM_PIECES, piece = OUTER ? id / PLAIN_TILE : id % GEMM_PIECES;
-    const int64_t i = i0 + row, k = k0 + piece * VEC;
-    typename Core<T>::piece_t v;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) {
-      T x = T(0);
-      if (i < o.rows && k + e < kend) x = OUTER ? o.p[(k + e) * o.stride + i] : o.p[i * o.stride + k + e];
-      v[e] = x;
-    }
-    to[row][piece] = v;
-  }
-}
-
-// acc[a][b] += columns 16 a .. + 15 times rows 16 b .. + 15 of this wavefront's part of the tile, over k0 .. kend - 1.
-template <typename T, bool ROUTER, bool COUTER>
-__device__ __forceinline__ void plain_accumulate(typename Core<T>::acc_t (&acc)[2][2], PlainLds<T>& lds, const Operand<T>& r,
-                                                 const Operand<T>& c, const int64_t row0, const int64_t col0, const int64_t k0,
-                                                 const int64_t kend) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int rw = (wave >> 1) * 32 + (lane & 15), cw = (wave & 1) * 32 + (lane & 15);
-  for (int64_t k = k0; k < kend; k += GEMM_PIECES * Core<T>::VEC) {
-    __syncthreads();
-    plain_stage<T, ROUTER>(lds.r, r, row0, k, kend);
-    plain_stage<T, COUTER>(lds.c, c, col0, k, kend);
-    __syncthreads();
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int piece = 4 * h + (lane >> 4);
-#pragma unroll
-      for (int a = 0; a < 2; ++a)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) Core<T>::mma(lds.c[cw + 16 * a][piece], lds.r[rw + 16 * b][piece], acc[a][b]);
-    }
-  }
-}
-
-// What a lane holds of a 16 x 16 part: element e of acc[a][b] belongs to row `lane & 15` and column Core::col(lane, e).
-template <typename T, typename F>
-__device__ __forceinline__ void plain_each(F&& f) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-#pragma unroll
-  for (int a = 0; a < 2; ++a)
-#pragma unroll
-    for (int b = 0; b < 2; ++b)
-#pragma unroll
-      for (int e = 0; e < 4; ++e)
-        f(a, b, e, (wave >> 1) * 32 + 16 * b + (lane & 15), (wave & 1) * 32 + 16 * a + Core<T>::col(lane, e));
-}
-
-// ---------------------------------------------------------------------------
 // The staged tile: BM x BN of D by WM x WN wavefronts, slabs of both operands double buffered in LDS.
 //
 // A slab of B rows takes 128 B bytes of LDS.  With k inner, row i's eight pieces stand in the order piece ^ (i & 7): the
@@ -340,6 +271,28 @@ __device__ __forceinline__ void tile_accumulate(typename Core<T>::acc_t (&acc)[S
     }
     if (held) put(s + 1);
   }
+}
+
+// f(a, b, e, row, column of the tile) for each element e of acc[a][b] that this lane holds.
+template <typename T, typename S, typename F>
+__device__ __forceinline__ void tile_each(F&& f) {
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+#pragma unroll
+  for (int b = 0; b < S::TM; ++b)
+#pragma unroll
+    for (int a = 0; a < S::TN; ++a)
+#pragma unroll
+      for (int e = 0; e < 4; ++e)
+        f(a, b, e, (wave / S::WN * S::TM + b) * 16 + (lane & 15), (wave % S::WN * S::TN + a) * 16 + Core<T>::col(lane, e));
+}
+
+// Whether an operand's pieces can go straight to LDS: rows on 16 bytes (with k outer their number a whole number of
+// pieces), offsets within a slab in 32 bits.
+template <typename T, bool OUTER, int B>
+bool gemm_straight(const Operand<T>& o, const int64_t k) {
+  const int64_t bytes = o.stride * (int64_t)sizeof(T), lines = OUTER ? k : o.rows;
+  return (uintptr_t)o.p % 16 == 0 && (lines == 1 || bytes % 16 == 0) && (!OUTER || o.rows % Core<T>::VEC == 0) &&
+         bytes < (int64_t(1) << 31) / (B > 64 ? B : 64);
 }
 
 // Tile number of workgroup `id` of a launch of 8 ceil(total / 8): workgroups go round the eight chiplets, each of which gets

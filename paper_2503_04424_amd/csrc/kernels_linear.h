@@ -93,21 +93,6 @@ __device__ __forceinline__ void linear_put(const LinearOut<T, O>& o, const int64
   o.y[i * o.ldy + j] = (O)v;
 }
 
-template <typename T, typename O, bool ROUTER, bool COUTER>
-__global__ __launch_bounds__(PLAIN_THREADS) void linear_plain_kernel(const Operand<T> r, const Operand<T> c, const int64_t k,
-                                                                     const LinearOut<T, O> out) {
-  __shared__ PlainLds<T> lds;
-  const int64_t across = (out.cols + PLAIN_TILE - 1) / PLAIN_TILE;
-  const int64_t row0 = blockIdx.x / across * PLAIN_TILE, col0 = blockIdx.x % across * PLAIN_TILE;
-  typename Core<T>::acc_t acc[2][2] = {};
-  plain_accumulate<T, ROUTER, COUTER>(acc, lds, r, c, row0, col0, 0, k);
-  act_switch(out.act, [&](auto act) {
-    plain_each<T>([&](int a, int b, int e, int i, int j) {
-      if (row0 + i < out.rows && col0 + j < out.cols) linear_put<T, O, decltype(act)::value>(out, row0 + i, col0 + j, acc[a][b][e]);
-    });
-  });
-}
-
 // Four neighbours of a row, from column j on.
 template <typename T, typename O, int ACT>
 __device__ __forceinline__ void linear_put4(const LinearOut<T, O>& o, const int64_t i, const int64_t j, const float (&in)[4]) {

@@ -34,78 +34,81 @@ __global__ __launch_bounds__(256) void ntk_widen_kernel(const S* __restrict__ fr
   if (i < rows) to[i * ldto + k] = k < cols ? (double)from[i * ld + k] : 0.0;
 }
 
-// Block number t of the lower triangle, row by row.
-__device__ __forceinline__ void ntk_block(const int64_t t, int64_t& bi, int64_t& bj) {
-  bi = (int64_t)((sqrt(8.0 * (double)t + 1.0) - 1.0) * 0.5);
-  while (bi * (bi + 1) / 2 > t) --bi;
-  while ((bi + 1) * (bi + 2) / 2 <= t) ++bi;
-  bj = t - bi * (bi + 1) / 2;
+// Block number t of the lower triangle of `rows` blocks: bands of eight rows of blocks, each column by column, so that
+// neighbours read the same operands; band r has 64 (r + 1) numbers.  False: above the diagonal or behind the end.
+__host__ __device__ __forceinline__ int64_t ntk_numbers(const int64_t rows) {
+  const int64_t bands = (rows + 7) / 8;
+  return 32 * bands * (bands + 1);
+}
+__device__ __forceinline__ bool ntk_block(const int64_t t, const int64_t rows, int64_t& bi, int64_t& bj) {
+  int64_t r = (int64_t)((sqrt(1.0 + 0.125 * (double)t) - 1.0) * 0.5);
+  while (32 * r * (r + 1) > t) --r;
+  while (32 * (r + 1) * (r + 2) <= t) ++r;
+  const int64_t u = t - 32 * r * (r + 1);
+  bi = 8 * r + (u & 7);
+  bj = u >> 3;
+  return bi < rows && bj <= bi;
 }
 
-// One 64 x 64 block: total += (a a^T + bias) * (g g^T), layer after layer, written once.  Rows of a: that of sample i
-// stands for rows i d .. i d + d - 1 of K.
-template <typename T>
-struct NtkRows {                       // rows i / d of a, as an operand whose rows repeat
-  const T* p;
-  int64_t stride, rows, d;
-};
-
-template <typename T>
-__device__ __forceinline__ void ntk_stage(typename Core<T>::piece_t (&to)[PLAIN_TILE][GEMM_PIECES + 1], const NtkRows<T>& o, const int64_t i0,
-                                          const int64_t k0, const int64_t kend) {
-  constexpr int VEC = Core<T>::VEC;
-#pragma unroll
-  for (int s = 0; s < PLAIN_TILE * GEMM_PIECES / PLAIN_THREADS; ++s) {
-    const int id = s * PLAIN_THREADS + (int)threadIdx.x, row = id / GEMM_PIECES, piece = id % GEMM_PIECES;
-    const int64_t i = i0 + row, k = k0 + piece * VEC;
-    typename Core<T>::piece_t v;
-#pragma unroll
-    for (int e = 0; e < VEC; ++e) v[e] = i < o.rows && k + e < kend ? o.p[i / o.d * o.stride + k + e] : T(0);
-    to[row][piece] = v;
-  }
+// first[l] = a_l a_l^T + bias, lower triangle of n x n, for networks of several outputs: every pair of samples' product
+// serves outputs^2 elements of K.
+template <typename T, typename S, bool DIRECT>
+__global__ __launch_bounds__(S::THREADS) void ntk_first_kernel(const NtkLayers<T> layers, const int64_t n, const typename Core<T>::acc1_t bias,
+                                                               typename Core<T>::acc1_t* __restrict__ first) {
+  __shared__ __attribute__((aligned(16))) char lds[2 * S::SLAB];
+  const int64_t rows = (n + S::BM - 1) / S::BM, numbers = ntk_numbers(rows);
+  const int64_t t = gemm_tile_number(blockIdx.x, numbers * layers.count);
+  int64_t bi, bj;
+  if (t < 0 || !ntk_block(t % numbers, rows, bi, bj)) return;
+  const int l = (int)(t / numbers);
+  const Operand<T> a{layers.a[l], layers.lda[l], n};
+  typename Core<T>::acc_t acc[S::TN][S::TM] = {};
+  tile_accumulate<T, S, false, false, DIRECT>(acc, lds, a, a, bi * S::BM, bj * S::BN, 0, layers.p[l]);
+  typename Core<T>::acc1_t* const to = first + l * n * n;
+  tile_each<T, S>([&](int a0, int b0, int e, int i, int j) {
+    const int64_t I = bi * S::BM + i, J = bj * S::BN + j;
+    if (I < n && J <= I) to[I * n + J] = acc[a0][b0][e] + bias;
+  });
 }
 
-template <typename T>
-__device__ __forceinline__ void ntk_accumulate(typename Core<T>::acc_t (&acc)[2][2], PlainLds<T>& lds, const NtkRows<T>& o, const int64_t row0,
-                                               const int64_t col0, const int64_t kend) {
-  const int lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-  const int rw = (wave >> 1) * 32 + (lane & 15), cw = (wave & 1) * 32 + (lane & 15);
-  for (int64_t k = 0; k < kend; k += GEMM_PIECES * Core<T>::VEC) {
-    __syncthreads();
-    ntk_stage<T>(lds.r, o, row0, k, kend);
-    ntk_stage<T>(lds.c, o, col0, k, kend);
-    __syncthreads();
+// A block of K.  FIRST: the first factors stand in `first`; otherwise (one output) both products are formed here, one
+// after the other, and multiplied in registers.  The sum over layers stays in registers, K is written once.
+template <typename T, typename S, bool DIRECT, bool FIRST>
+__global__ __launch_bounds__(S::THREADS) void ntk_gram_kernel(const NtkLayers<T> layers, const int64_t n, const int d,
+                                                              const typename Core<T>::acc1_t bias, const typename Core<T>::acc1_t scale,
+                                                              const int accumulate, const typename Core<T>::acc1_t* __restrict__ first,
+                                                              typename Core<T>::acc1_t* __restrict__ K, const int64_t ldk) {
+  typedef typename Core<T>::acc_t acc_t;
+  __shared__ __attribute__((aligned(16))) char lds[2 * S::SLAB];
+  const int64_t N = n * d, rows = (N + S::BM - 1) / S::BM;
+  const int64_t t = gemm_tile_number(blockIdx.x, ntk_numbers(rows));
+  int64_t bi, bj;
+  if (t < 0 || !ntk_block(t, rows, bi, bj)) return;
+  const int64_t row0 = bi * S::BM, col0 = bj * S::BN;
+  acc_t total[S::TN][S::TM] = {};
+  for (int l = 0; l < layers.count; ++l) {
+    acc_t second[S::TN][S::TM] = {};
+    const Operand<T> g{layers.g[l], layers.ldg[l], N};
+    __syncthreads();                               // the product before reads its last slab
+    tile_accumulate<T, S, false, false, DIRECT>(second, lds, g, g, row0, col0, 0, layers.q[l]);
+    if constexpr (FIRST) {
+      const typename Core<T>::acc1_t* const from = first + l * n * n;
+      tile_each<T, S>([&](int a, int b, int e, int i, int j) {
+        int64_t I = row0 + i, J = col0 + j;
+        if (I < N && J <= I) total[a][b][e] += from[I / d * n + J / d] * second[a][b][e];
+      });
+    } else {
+      const Operand<T> x{layers.a[l], layers.lda[l], N};
+      acc_t one[S::TN][S::TM] = {};
+      __syncthreads();
+      tile_accumulate<T, S, false, false, DIRECT>(one, lds, x, x, row0, col0, 0, layers.p[l]);
 #pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      const int piece = 4 * h + (lane >> 4);
+      for (int a = 0; a < S::TN; ++a)
 #pragma unroll
-      for (int a = 0; a < 2; ++a)
-#pragma unroll
-        for (int b = 0; b < 2; ++b) Core<T>::mma(lds.c[cw + 16 * a][piece], lds.r[rw + 16 * b][piece], acc[a][b]);
+        for (int b = 0; b < S::TM; ++b) total[a][b] += (one[a][b] + bias) * second[a][b];
     }
   }
-}
-
-template <typename T>
-__global__ __launch_bounds__(PLAIN_THREADS) void ntk_plain_kernel(const NtkLayers<T> layers, const int64_t n, const int64_t d,
-                                                                  const typename Core<T>::acc1_t bias, const typename Core<T>::acc1_t scale,
-                                                                  const int accumulate, typename Core<T>::acc1_t* __restrict__ K, const int64_t ldk) {
-  typedef typename Core<T>::acc_t acc_t;
-  __shared__ PlainLds<T> lds;
-  int64_t bi, bj;
-  ntk_block(blockIdx.x, bi, bj);
-  const int64_t row0 = bi * PLAIN_TILE, col0 = bj * PLAIN_TILE, N = n * d;
-  acc_t total[2][2] = {};
-  for (int l = 0; l < layers.count; ++l) {
-    acc_t first[2][2] = {}, second[2][2] = {};
-    ntk_accumulate<T>(first, lds, NtkRows<T>{layers.a[l], layers.lda[l], N, d}, row0, col0, layers.p[l]);
-    ntk_accumulate<T>(second, lds, NtkRows<T>{layers.g[l], layers.ldg[l], N, 1}, row0, col0, layers.q[l]);
-#pragma unroll
-    for (int a = 0; a < 2; ++a)
-#pragma unroll
-      for (int b = 0; b < 2; ++b) total[a][b] += (first[a][b] + bias) * second[a][b];
-  }
-  plain_each<T>([&](int a, int b, int e, int i, int j) {
+  tile_each<T, S>([&](int a, int b, int e, int i, int j) {
     const int64_t I = row0 + i, J = col0 + j;
     if (I >= N || J > I) return;
     auto v = total[a][b][e] * scale;

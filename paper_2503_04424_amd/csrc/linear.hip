@@ -36,15 +36,6 @@ bool four(const void* p, int64_t ld, int64_t rows) {
   return !p || ((uintptr_t)p % (4 * sizeof(T)) == 0 && (rows == 1 || ld % 4 == 0));
 }
 
-// Whether an operand's pieces can go straight to LDS: rows on 16 bytes (with k outer their number a whole number of
-// pieces), offsets within a slab in 32 bits.
-template <typename T, bool OUTER, int B>
-bool straight(const Operand<T>& o, int64_t k) {
-  const int64_t bytes = o.stride * (int64_t)sizeof(T), lines = OUTER ? k : o.rows;
-  return (uintptr_t)o.p % 16 == 0 && (lines == 1 || bytes % 16 == 0) && (!OUTER || o.rows % Core<T>::VEC == 0) &&
-         bytes < (int64_t(1) << 31) / (B > 64 ? B : 64);
-}
-
 typedef Tile<256, 256, 2, 4> Big;
 typedef Tile<128, 128, 2, 2> Mid;
 typedef Tile<64, 64, 2, 2> Small;
@@ -80,7 +71,7 @@ template <typename T, typename O, typename S, bool ROUTER, bool COUTER>
 void tiles(const Operand<T>& r, const Operand<T>& c, int64_t k, const LinearOut<T, O>& out, const Cut& cut, float* parts, hipStream_t st) {
   const int64_t n = ceil_div(out.rows, S::BM) * ceil_div(out.cols, S::BN) * cut.splits;
   const dim3 grid((unsigned)(ceil_div(n, 8) * 8)), block(S::THREADS);
-  const bool direct = straight<T, ROUTER, S::BM>(r, k) && straight<T, COUTER, S::BN>(c, k);
+  const bool direct = gemm_straight<T, ROUTER, S::BM>(r, k) && gemm_straight<T, COUTER, S::BN>(c, k);
   auto go = [&](auto d, auto split) {
     hipLaunchKernelGGL((linear_tile_kernel<T, O, S, ROUTER, COUTER, decltype(d)::value, decltype(split)::value>), grid, block, 0, st, r, c, k, out,
                        parts, cut.splits, cut.kpart);

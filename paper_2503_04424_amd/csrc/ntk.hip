@@ -3,6 +3,7 @@
 #include <hip/hip_runtime.h>
 
 #include <cmath>
+#include <type_traits>
 
 #include "kernels_ntk.h"
 #include "../../include/memdet.h"
@@ -53,12 +54,45 @@ struct Call {
   hipStream_t st;
 };
 
-template <typename T>
-int gram(const mdet_ntk_layer* layers, int32_t count, const Call& c) {
+typedef Tile<128, 128, 2, 4> Large;
+typedef Tile<64, 64, 2, 2> Small;
+
+// First factors of one launch's layers, for several outputs.
+inline uint64_t first_bytes(int64_t n, int64_t d, int32_t layers, int64_t size) {
+  return d > 1 ? up256((uint64_t)(layers < NTK_LAYERS ? layers : NTK_LAYERS) * n * n * size) : 0;
+}
+
+template <typename T, typename S>
+int gram_tiles(const NtkLayers<T>& list, const Call& c, int accumulate, void* first) {
   typedef typename Core<T>::acc1_t A;
-  const int64_t rows = ceil_div(c.n * c.d, PLAIN_TILE), blocks = rows * (rows + 1) / 2;
-  if (blocks > INT32_MAX) return MDET_EINVAL;
+  bool direct = true;
+  for (int l = 0; l < list.count; ++l)
+    direct = direct && (list.p[l] == 0 || gemm_straight<T, false, S::BM>(Operand<T>{list.a[l], list.lda[l], c.n}, list.p[l])) &&
+             (list.q[l] == 0 || gemm_straight<T, false, S::BM>(Operand<T>{list.g[l], list.ldg[l], c.n * c.d}, list.q[l]));
+  auto grid = [](int64_t rows, int64_t times) { return ceil_div(ntk_numbers(ceil_div(rows, S::BM)) * times, 8) * 8; };
+  const int64_t all = grid(c.n * c.d, 1), firsts = c.d > 1 ? grid(c.n, list.count) : 0;
+  if (all > INT32_MAX || firsts > INT32_MAX) return MDET_EINVAL;
+  auto go = [&](auto d) {
+    constexpr bool D = decltype(d)::value;
+    if (c.d > 1) {
+      if (list.count > 0)
+        hipLaunchKernelGGL((ntk_first_kernel<T, S, D>), dim3((unsigned)firsts), dim3(S::THREADS), 0, c.st, list, c.n, (A)c.bias, (A*)first);
+      hipLaunchKernelGGL((ntk_gram_kernel<T, S, D, true>), dim3((unsigned)all), dim3(S::THREADS), 0, c.st, list, c.n, (int)c.d, (A)c.bias,
+                         (A)c.scale, accumulate, (const A*)first, (A*)c.K, c.ldk);
+    } else {
+      hipLaunchKernelGGL((ntk_gram_kernel<T, S, D, false>), dim3((unsigned)all), dim3(S::THREADS), 0, c.st, list, c.n, 1, (A)c.bias,
+                         (A)c.scale, accumulate, (const A*)nullptr, (A*)c.K, c.ldk);
+    }
+  };
+  if (direct) go(std::true_type{});
+  else go(std::false_type{});
+  return launch_status();
+}
+
+template <typename T>
+int gram(const mdet_ntk_layer* layers, int32_t count, const Call& c, void* first) {
   int accumulate = c.accumulate;
+  const int64_t large = ceil_div(c.n * c.d, 128);
   for (int32_t l0 = 0; l0 == 0 || l0 < count; l0 += NTK_LAYERS) {
     NtkLayers<T> list;
     list.count = count - l0 < NTK_LAYERS ? count - l0 : NTK_LAYERS;
@@ -67,11 +101,12 @@ int gram(const mdet_ntk_layer* layers, int32_t count, const Call& c) {
       list.a[l] = (const T*)x.a, list.lda[l] = x.lda, list.p[l] = x.p;
       list.g[l] = (const T*)x.g, list.ldg[l] = x.ldg, list.q[l] = x.q;
     }
-    hipLaunchKernelGGL(ntk_plain_kernel<T>, dim3((unsigned)blocks), dim3(PLAIN_THREADS), 0, c.st, list, c.n, c.d, (A)c.bias, (A)c.scale,
-                       accumulate, (A*)c.K, c.ldk);
+    const int status = large * (large + 1) / 2 >= 256 ? gram_tiles<T, Large>(list, c, accumulate, first)
+                                                      : gram_tiles<T, Small>(list, c, accumulate, first);
+    if (status != MDET_OK) return status;
     accumulate = 1;
   }
-  return launch_status();
+  return MDET_OK;
 }
 
 }  // namespace
@@ -83,7 +118,7 @@ int mdet_ntk_workspace_query(int32_t dtype, int32_t out_dtype, int64_t n, int64_
   if (!bytes) return MDET_EINVAL;
   const int status = check(dtype, out_dtype, n, outputs, layers, count, false);
   if (status != MDET_OK) return status;
-  uint64_t sum = 0;
+  uint64_t sum = first_bytes(n, outputs, count, size_of(out_dtype));
   if (out_dtype == MDET_F64 && dtype != MDET_F64)
     for (int l = 0; l < count; ++l) sum += wide_bytes(n, layers[l].p) + wide_bytes(n * outputs, layers[l].q);
   *bytes = sum;
@@ -105,10 +140,10 @@ int mdet_ntk_gram(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs, 
   hipStream_t st = (hipStream_t)stream;
   const Call c{n, outputs, bias, scale, accumulate, K, ldk, st};
   if (out_dtype == MDET_F32)
-    return dtype == MDET_F32 ? gram<float>(layers, count, c) : dtype == MDET_BF16 ? gram<__bf16>(layers, count, c) : gram<_Float16>(layers, count, c);
-  if (dtype == MDET_F64) return gram<double>(layers, count, c);
+    return dtype == MDET_F32 ? gram<float>(layers, count, c, workspace) : dtype == MDET_BF16 ? gram<__bf16>(layers, count, c, workspace) : gram<_Float16>(layers, count, c, workspace);
+  if (dtype == MDET_F64) return gram<double>(layers, count, c, workspace);
   // narrower operands: exact copies in fp64, one launch's layers after the other in the workspace
-  char* at = (char*)workspace;
+  char* at = (char*)workspace + first_bytes(n, outputs, count, 8);
   int acc = accumulate;
   for (int32_t l0 = 0; l0 == 0 || l0 < count; l0 += NTK_LAYERS) {
     mdet_ntk_layer wide[NTK_LAYERS];
@@ -129,7 +164,7 @@ int mdet_ntk_gram(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs, 
     }
     Call part = c;
     part.accumulate = acc;
-    status = gram<double>(wide, some, part);
+    status = gram<double>(wide, some, part, workspace);
     if (status != MDET_OK) return status;
     acc = 1;
   }
