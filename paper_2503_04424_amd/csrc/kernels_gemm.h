@@ -2,8 +2,8 @@
 // Gram matrix of a network's Jacobian.  R is the row operand (its index runs along the rows of D), C the column operand.
 //
 // Pieces.  Every operand is handled in pieces of 16 bytes along k: 8 elements in 16 bits, 4 in fp32, 2 in fp64.  A slab
-// is eight pieces (128 bytes) of k.  Lane l of a wavefront supplies piece l / 16 of row l % 16 to a product, which takes
-// the four pieces of one half slab at once: one instruction of 16 x 16 x 32 in 16 bits, four of 16 x 16 x 4 in fp32, two
+// is four or eight pieces of k.  Lane l of a wavefront supplies piece l / 16 of row l % 16 to a product, which takes
+// four pieces at once: one instruction of 16 x 16 x 32 in 16 bits, four of 16 x 16 x 4 in fp32, two
 // in fp64 (the e-th elements of the four pieces form the e-th of them; any assignment of k's is valid as long as R and C
 // use the same one).  Sums are fp32 for operands in 16 and 32 bits, fp64 for fp64.
 //
@@ -13,9 +13,9 @@
 #include <hip/hip_runtime.h>
 #include <stdint.h>
 
-namespace mdet {
+#include <type_traits>
 
-constexpr int GEMM_PIECES = 8;        // pieces of a slab
+namespace mdet {
 
 template <typename T> struct Core;
 
@@ -71,20 +71,23 @@ struct Operand {
   const T* p;
   int64_t stride;
   int64_t rows;                        // i < rows
+  bool near;                           // offsets within a slab fit 32 bits
+  bool straight;                       // and its whole slabs can go straight to LDS
 };
 
 // ---------------------------------------------------------------------------
-// The staged tile: BM x BN of D by WM x WN wavefronts, slabs of both operands double buffered in LDS.
+// The staged tile: BM x BN of D by WM x WN wavefronts, slabs of both operands in NB buffers in LDS.
 //
-// A slab of B rows takes 128 B bytes of LDS.  With k inner, row i's eight pieces stand in the order piece ^ (i & 7): the
-// eight lanes that one LDS cycle serves read one piece of eight rows, from eight different places.  With k outer, the slab
+// With k inner, lines of 128 bytes hold eight pieces, of one row or of two, line i's in the order piece ^ (i & 7): lanes
+// that read one piece of consecutive rows read from different places.  With k outer, the slab
 // lies as it does in memory, row k's elements side by side: in 16 bits the transposing read hands lane l the four k's of
 // column l % 16 out of four rows of 32 bytes, in fp32 the instructions take single elements.  There the blocks of 16
 // columns of row k stand in the order block ^ f(k), so that the rows read together lie in different banks.
 //
 // DIRECT: memory goes straight into LDS (every lane names the 16 bytes that land at its place), for operands whose rows
-// start on 16 bytes.  Otherwise, and for the ragged last slab, pieces pass through registers, whole ones in one load of
-// any alignment, those that hang over an edge element by element.
+// start on 16 bytes.  Otherwise pieces pass through registers, whole ones in one load of any alignment, those that hang
+// over an edge element by element, beside the products of the slab before; in a DIRECT product that is done without such an
+// overlap, for the ragged last slab and for an operand beside the others that is not straight.
 // ---------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) char* gemm_lds_ptr;
 
@@ -98,39 +101,42 @@ __device__ __forceinline__ void gemm_to_lds(const char* base, const unsigned off
   asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(at), "v"(off), "s"(from));
 }
 
-// All of a wavefront's loads and LDS accesses are done, and behind the barrier those of all.
+// All of a wavefront's loads but the last `LATER` and all of its LDS accesses are done, and behind the barrier those of all.
+template <int LATER>
 __device__ __forceinline__ void gemm_landed() {
-  asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)" ::: "memory");
+  asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)" ::"i"(LATER) : "memory");
   __builtin_amdgcn_s_barrier();
   asm volatile("" ::: "memory");
 }
 
-template <int BM_, int BN_, int WM_, int WN_>
+// P: pieces of k that a slab holds; NB: slabs in LDS.
+template <int BM_, int BN_, int WM_, int WN_, int P_, int NB_>
 struct Tile {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, P = P_, NB = NB_;
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;   // 16 x 16 parts of a wavefront, down and across
-  static constexpr int SLAB = 128 * (BM + BN);                 // bytes of one slab of both operands
+  static constexpr int SLAB = 16 * P * (BM + BN);              // bytes of one slab of both operands
 };
 
 // Staging of an operand: B rows of it from i0 on.
-template <typename T, int B, int WAVES, bool OUTER, bool DIRECT>
+template <typename T, int B, int WAVES, int P, bool OUTER, bool DIRECT>
 struct Stage {
   typedef typename Core<T>::piece_t piece_t;
-  static constexpr int VEC = Core<T>::VEC, BK = GEMM_PIECES * VEC;
-  static constexpr int NP = B * GEMM_PIECES / (64 * WAVES);    // pieces a lane brings of a slab
+  static constexpr int VEC = Core<T>::VEC, BK = P * VEC;
+  static constexpr int NP = B * P / (64 * WAVES);              // pieces a lane brings of a slab
   static constexpr int PR = B / VEC;                           // k outer: pieces of a row k
-  static_assert(NP * 64 * WAVES == B * GEMM_PIECES, "whole pieces");
+  static_assert(NP * 64 * WAVES == B * P && (P == 4 || P == 8), "whole pieces");
 
   const T* p;
   int64_t stride, rows, i0;
-  unsigned off[DIRECT ? NP : 1];
+  unsigned off[NP];                    // bytes from the slab's first element to the pieces
+  bool hangs[NP];                      // k outer, not DIRECT: the piece is not all of the operand's
   piece_t held[NP];
 
   // Order of the blocks of 16 columns of row k.
   static __device__ __forceinline__ int swizzle(const int k) {
     if constexpr (sizeof(T) == 2) return ((k & 3) | ((k >> 1) & 4)) & (B / 16 - 1);
-    else return (k >> 2) & 3;
+    else return (k >> 2) & 3 & (B / 16 - 1);
   }
   // Row and k of the piece that stands at place `id` of the slab.
   static __device__ __forceinline__ void piece_at(const int id, int& row, int& k) {
@@ -140,36 +146,55 @@ struct Stage {
       const int at = id % PR;
       row = (((at / PB) ^ swizzle(k)) * PB + at % PB) * VEC;
     } else {
-      row = id / GEMM_PIECES;
-      k = ((id % GEMM_PIECES) ^ (row & 7)) * VEC;
+      // eight pieces a line of 128 bytes, of one row or of two
+      const int line = id / 8, at = (id % 8) ^ (line & 7);
+      row = line * (8 / P) + at / P;
+      k = at % P * VEC;
     }
   }
   static __device__ __forceinline__ int place(const int v) {
     return (v * WAVES + __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6)) * 64 + ((int)threadIdx.x & 63);
   }
 
-  __device__ __forceinline__ Stage(const Operand<T>& o, const int64_t first) : p(o.p), stride(o.stride), rows(o.rows), i0(first) {
-    if constexpr (DIRECT) {
+  // Rows from `first` on, which is one of the operand's: a lane's place is held against the last row from there.
+  __device__ __forceinline__ void set(const Operand<T>& o, const int64_t first) {
+    p = o.p;
+    stride = o.stride;
+    rows = o.rows;
+    i0 = first;
 #pragma unroll
-      for (int v = 0; v < NP; ++v) {
-        int row, k;
-        piece_at(place(v), row, k);
-        // rows behind the last are not stored: any memory of the operand will do for them
-        if (OUTER) {
-          const int64_t i = i0 + row > rows - VEC ? rows - VEC : i0 + row;
-          off[v] = (unsigned)((k * stride + (i - i0)) * (int64_t)sizeof(T));
-        } else {
-          const int64_t i = i0 + row > rows - 1 ? rows - 1 : i0 + row;
-          off[v] = (unsigned)(((i - i0) * stride + k) * (int64_t)sizeof(T));
-        }
-      }
+    for (int v = 0; v < NP; ++v) {
+      int row, k;
+      piece_at(place(v), row, k);
+      // rows behind the last are not stored: any memory of the operand will do for them
+      const int64_t last = OUTER ? rows - VEC : rows - 1;
+      hangs[v] = OUTER && !DIRECT && i0 + row > last;
+      const int64_t i = i0 + row > last && !hangs[v] ? last - i0 : row;
+      off[v] = (unsigned)((OUTER ? k * stride + i : i * stride + k) * (int64_t)sizeof(T));
     }
   }
-  // The slab from k on straight to LDS at byte `at`.
-  __device__ __forceinline__ void direct(const int64_t k, const unsigned at) const {
-    const char* const base = reinterpret_cast<const char*>(OUTER ? p + k * stride + i0 : p + i0 * stride + k);
+  __device__ __forceinline__ const char* base(const int64_t k) const {
+    return reinterpret_cast<const char*>(OUTER ? p + k * stride + i0 : p + i0 * stride + k);
+  }
+  // Piece v of the slab at `from` = base(k) straight to LDS, the slab at byte `at`.
+  __device__ __forceinline__ void direct(const char* const from, const int v, const unsigned at) const {
+    gemm_to_lds(from, off[v], at + 16u * (unsigned)(place(v) & ~63));
+  }
+  // A whole slab into registers, `from` = base(k).
+  __device__ __forceinline__ void load(const char* const from) {
 #pragma unroll
-    for (int v = 0; v < NP; ++v) gemm_to_lds(base, off[v], at + 16u * (unsigned)(place(v) & ~63));
+    for (int v = 0; v < NP; ++v) {
+      if (OUTER && hangs[v]) {
+        int row, k;
+        piece_at(place(v), row, k);
+        const T* const x = reinterpret_cast<const T*>(from + off[v]);
+        piece_t y = {};
+#pragma unroll
+        for (int e = 0; e < VEC; ++e)
+          if (i0 + row + e < rows) y[e] = x[e];
+        held[v] = y;
+      } else __builtin_memcpy(&held[v], from + off[v], 16);
+    }
   }
   // The slab from k on into registers; what lies outside of the operand is zero.
   __device__ __forceinline__ void load(const int64_t k0, const int64_t kend) {
@@ -198,7 +223,8 @@ struct Stage {
   static __device__ __forceinline__ piece_t fragment(const char* const lds, const int t, const int h) {
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
     if constexpr (!OUTER) {
-      return *reinterpret_cast<const piece_t*>(lds + (16 * t + j) * 128 + (((4 * h + g) ^ (j & 7)) << 4));
+      const int line = (P == 8 ? 16 : 8) * t + (P == 8 ? j : j >> 1), at = P == 8 ? 4 * h + g : 4 * (j & 1) + g;
+      return *reinterpret_cast<const piece_t*>(lds + line * 128 + ((at ^ (line & 7)) << 4));
     } else if constexpr (sizeof(T) == 2) {
       typedef short half_t __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) half_t* lds_half_ptr;
@@ -221,57 +247,168 @@ struct Stage {
   }
 };
 
-// acc[a][b] += columns 16 a .. times rows 16 b .. of this wavefront's part of the tile at (row0, col0), over k0 .. kend - 1.
-// `lds`: 2 * Tile::SLAB bytes, which are not read any more when the last wavefront returns.
+// A workgroup's way through one product after another: slabs are brought in their order, NB - 1 ahead of the one that is
+// multiplied and past the end of its product.  `lds`: NB * SLAB bytes.
 template <typename T, typename S, bool ROUTER, bool COUTER, bool DIRECT>
-__device__ __forceinline__ void tile_accumulate(typename Core<T>::acc_t (&acc)[S::TN][S::TM], char* const lds, const Operand<T>& r,
-                                                const Operand<T>& c, const int64_t row0, const int64_t col0, const int64_t k0,
-                                                const int64_t kend) {
-  typedef Stage<T, S::BM, S::WAVES, ROUTER, DIRECT> RS;
-  typedef Stage<T, S::BN, S::WAVES, COUTER, DIRECT> CS;
-  constexpr int BK = RS::BK;
-  RS rs(r, row0);
-  CS cs(c, col0);
-  const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int wr = wave / S::WN * S::TM, wc = wave % S::WN * S::TN;      // first 16 x 16 part of this wavefront
-  const unsigned lds0 = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(gemm_lds_ptr)lds);
-  const int slabs = (int)((kend - k0 + BK - 1) / BK);
-  // brings slab s: straight to LDS where it is whole, otherwise into registers
-  auto bring = [&](const int s) {
-    const int64_t k = k0 + (int64_t)s * BK;
-    if (DIRECT && k + BK <= kend) {
-      rs.direct(k, lds0 + (s & 1) * S::SLAB);
-      cs.direct(k, lds0 + (s & 1) * S::SLAB + 128 * S::BM);
-      return false;
-    }
-    rs.load(k, kend);
-    cs.load(k, kend);
-    return true;
-  };
-  auto put = [&](const int s) {
-    rs.put(lds + (s & 1) * S::SLAB);
-    cs.put(lds + (s & 1) * S::SLAB + 128 * S::BM);
-  };
-  if (slabs > 0 && bring(0)) put(0);
-  for (int s = 0; s < slabs; ++s) {
-    gemm_landed();
-    const bool held = s + 1 < slabs && bring(s + 1);
-    const char* const at = lds + (s & 1) * S::SLAB;
-#pragma unroll
-    for (int h = 0; h < 2; ++h) {
-      typename Core<T>::piece_t cf[S::TN], rf[S::TM];
-#pragma unroll
-      for (int a = 0; a < S::TN; ++a) cf[a] = CS::fragment(at + 128 * S::BM, wc + a, h);
-#pragma unroll
-      for (int b = 0; b < S::TM; ++b) rf[b] = RS::fragment(at, wr + b, h);
-#pragma unroll
-      for (int b = 0; b < S::TM; ++b)
-#pragma unroll
-        for (int a = 0; a < S::TN; ++a) Core<T>::mma(cf[a], rf[b], acc[a][b]);
-    }
-    if (held) put(s + 1);
+struct TileStream {
+  typedef Stage<T, S::BM, S::WAVES, S::P, ROUTER, DIRECT> RS;
+  typedef Stage<T, S::BN, S::WAVES, S::P, COUTER, DIRECT> CS;
+  typedef typename Core<T>::piece_t piece_t;
+  static constexpr int BK = RS::BK, LOADS = RS::NP + CS::NP;   // loads of a wavefront for a slab
+  RS rs;
+  CS cs;
+  bool rquick, cquick, held;           // whole slabs need no look at their edges
+  int64_t k, kend;                     // what is left to be brought of the product that slabs are brought of
+  int to, at, ahead;                   // buffers to fill and to multiply next, slabs in between
+  char* const lds;
+  const unsigned lds0;
+
+  __device__ __forceinline__ explicit TileStream(char* where)
+      : held(false), k(0), kend(0), to(0), at(0), ahead(0), lds(where),
+        lds0(__builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)(gemm_lds_ptr)where)) {}
+
+  // Slabs come from this product from here on: the tile at (row0, col0), k from `from` to `end` - 1.
+  __device__ __forceinline__ void set(const Operand<T>& r, const Operand<T>& c, const int64_t row0, const int64_t col0, const int64_t from,
+                                      const int64_t end) {
+    k = from;
+    kend = end;
+    rquick = DIRECT ? r.straight : r.near;
+    cquick = DIRECT ? c.straight : c.near;
+    rs.set(r, row0);
+    cs.set(c, col0);
   }
-}
+  static __device__ __forceinline__ int slabs(const int64_t from, const int64_t end) { return end > from ? (int)((end - from + BK - 1) / BK) : 0; }
+
+  // The next slab, whatever it needs: straight to LDS where that goes and the slab is whole, otherwise through registers.
+  template <typename F>
+  __device__ __forceinline__ void bring(F&& next) {
+    while (k >= kend)
+      if (!next()) return;
+    char* const slab = lds + to * S::SLAB;
+    if constexpr (DIRECT) {
+      const bool whole = k + BK <= kend, rcomes = whole && rquick, ccomes = whole && cquick;
+      const unsigned place = lds0 + to * S::SLAB;
+      if (rcomes) {
+#pragma unroll
+        for (int v = 0; v < RS::NP; ++v) rs.direct(rs.base(k), v, place);
+      } else {
+        rs.load(k, kend);
+        rs.put(slab);
+      }
+      if (ccomes) {
+#pragma unroll
+        for (int v = 0; v < CS::NP; ++v) cs.direct(cs.base(k), v, place + 16 * S::P * S::BM);
+      } else {
+        cs.load(k, kend);
+        cs.put(slab + 16 * S::P * S::BM);
+      }
+      // run() counts loads straight to LDS: where some are missing, none is left to be counted
+      if (!(rcomes && ccomes)) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    } else {
+      rs.load(k, kend);
+      cs.load(k, kend);
+      held = true;
+    }
+    k += BK;
+    ++ahead;
+    to = to + 1 == S::NB ? 0 : to + 1;
+  }
+  // What bring() left in registers.
+  __device__ __forceinline__ void put() {
+    if (!DIRECT && held) {
+      char* const slab = lds + (to == 0 ? S::NB - 1 : to - 1) * S::SLAB;
+      rs.put(slab);
+      cs.put(slab + 16 * S::P * S::BM);
+      held = false;
+    }
+  }
+  // next(): sets the product after the one that has been brought whole; false behind the last.
+  template <typename F>
+  __device__ __forceinline__ void begin(F&& next) {
+#pragma unroll
+    for (int i = 0; i < (DIRECT ? S::NB - 1 : 1); ++i) bring(next);
+    put();
+  }
+  // acc[a][b] += columns 16 a .. times rows 16 b .. of this wavefront's part of the tile, over the next `count` slabs.
+  template <typename F>
+  __device__ __forceinline__ void run(typename Core<T>::acc_t (&acc)[S::TN][S::TM], const int count, F&& next) {
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wr = wave / S::WN * S::TM, wc = wave % S::WN * S::TN;    // first 16 x 16 part of this wavefront
+    auto multiply = [&](const char* const slab, auto&& between) {
+#pragma unroll
+      for (int h = 0; h < S::P / 4; ++h) {
+        piece_t cf[S::TN], rf[S::TM];
+#pragma unroll
+        for (int a = 0; a < S::TN; ++a) cf[a] = CS::fragment(slab + 16 * S::P * S::BM, wc + a, h);
+#pragma unroll
+        for (int b = 0; b < S::TM; ++b) rf[b] = RS::fragment(slab, wr + b, h);
+#pragma unroll
+        for (int b = 0; b < S::TM; ++b) {
+          between(h * S::TM + b);
+#pragma unroll
+          for (int a = 0; a < S::TN; ++a) Core<T>::mma(cf[a], rf[b], acc[a][b]);
+        }
+      }
+    };
+    int left = count;
+    {
+      // The long stretch, without a branch: every slab brought meanwhile is a whole one of this product.
+      const int64_t whole = rquick && cquick && k < kend ? (kend - k) / BK : 0;
+      int steady = __builtin_amdgcn_readfirstlane(whole < left - ahead ? (int)whole : left - ahead);
+      if (ahead == (DIRECT ? S::NB - 1 : 1) && steady > 0) {
+        left -= steady;
+        const char *rfrom = rs.base(k), *cfrom = cs.base(k);
+        const int64_t rstep = rs.base(k + BK) - rfrom, cstep = cs.base(k + BK) - cfrom;
+        k += (int64_t)steady * BK;
+        for (; steady > 0; --steady) {
+          gemm_landed<DIRECT ? (S::NB - 2) * LOADS : 0>();
+          const unsigned place = lds0 + to * S::SLAB;
+          // The loads of a later slab: all in front of this one's products where both operands are read in 128-byte pieces
+          // of rows in 16 bits (8192 x 16384 x 4096 1257 TFLOP/s, spread 1176), which wait longest; one behind each strip of
+          // products otherwise (k outer 4096 x 4096 x 8192 1384, in front 1324; fp32 4096^3 142, 139).
+          constexpr bool FIRST = sizeof(T) == 2 && !ROUTER && !COUTER;
+          constexpr int Q = S::TM * S::P / 4, EACH = (LOADS + Q - 1) / Q;
+          auto pieces = [&](const int from, const int end) {
+#pragma unroll
+            for (int v = from; v < end; ++v) {
+              if (v >= LOADS) break;
+              if (v < RS::NP) rs.direct(rfrom, v, place);
+              else cs.direct(cfrom, v - RS::NP, place + 16 * S::P * S::BM);
+            }
+          };
+          if constexpr (!DIRECT) {
+            rs.load(rfrom);
+            cs.load(cfrom);
+          } else if constexpr (FIRST) pieces(0, LOADS);
+          multiply(lds + at * S::SLAB, [&](const int q) {
+            if constexpr (DIRECT && !FIRST) {
+              pieces(q * EACH, (q + 1) * EACH);
+              __builtin_amdgcn_sched_barrier(0x107);
+            }
+          });
+          if constexpr (!DIRECT) {
+            rs.put(lds + to * S::SLAB);
+            cs.put(lds + to * S::SLAB + 16 * S::P * S::BM);
+          }
+          rfrom += rstep;
+          cfrom += cstep;
+          to = to + 1 == S::NB ? 0 : to + 1;
+          at = at + 1 == S::NB ? 0 : at + 1;
+        }
+      }
+    }
+    for (; left > 0; --left) {
+      --ahead;
+      if (DIRECT && S::NB > 3 && ahead >= 2) gemm_landed<2 * LOADS>();
+      else if (DIRECT && S::NB > 2 && ahead >= 1) gemm_landed<LOADS>();
+      else gemm_landed<0>();
+      bring(next);
+      multiply(lds + at * S::SLAB, [](int) {});
+      put();
+      at = at + 1 == S::NB ? 0 : at + 1;
+    }
+  }
+};
 
 // f(a, b, e, row, column of the tile) for each element e of acc[a][b] that this lane holds.
 template <typename T, typename S, typename F>
@@ -286,13 +423,14 @@ __device__ __forceinline__ void tile_each(F&& f) {
         f(a, b, e, (wave / S::WN * S::TM + b) * 16 + (lane & 15), (wave % S::WN * S::TN + a) * 16 + Core<T>::col(lane, e));
 }
 
-// Whether an operand's pieces can go straight to LDS: rows on 16 bytes (with k outer their number a whole number of
-// pieces), offsets within a slab in 32 bits.
+// An operand with what is to be known of its place: offsets within a slab of B rows in 32 bits; pieces that can go straight to
+// LDS, with rows on 16 bytes (with k outer their number a whole number of pieces).
 template <typename T, bool OUTER, int B>
-bool gemm_straight(const Operand<T>& o, const int64_t k) {
-  const int64_t bytes = o.stride * (int64_t)sizeof(T), lines = OUTER ? k : o.rows;
-  return (uintptr_t)o.p % 16 == 0 && (lines == 1 || bytes % 16 == 0) && (!OUTER || o.rows % Core<T>::VEC == 0) &&
-         bytes < (int64_t(1) << 31) / (B > 64 ? B : 64);
+Operand<T> gemm_operand(const void* p, const int64_t stride, const int64_t rows, const int64_t k) {
+  const int64_t bytes = stride * (int64_t)sizeof(T), lines = OUTER ? k : rows;
+  const bool near = bytes < (int64_t(1) << 31) / (B > 64 ? B : 64);
+  const bool straight = near && (uintptr_t)p % 16 == 0 && (lines == 1 || bytes % 16 == 0) && (!OUTER || rows % Core<T>::VEC == 0);
+  return Operand<T>{(const T*)p, stride, rows, near, straight};
 }
 
 // Tile number of workgroup `id` of a launch of 8 ceil(total / 8): workgroups go round the eight chiplets, each of which gets

@@ -137,7 +137,7 @@ template <typename S>
 struct LinearLds {
   static constexpr int ROWS = S::TM * 16 < 64 ? S::TM * 16 : 64, COLS = S::TN * 16, PITCH = COLS + 4;
   static constexpr int WAVE_BYTES = ROWS * PITCH * 4;
-  static constexpr int BYTES = S::WAVES * WAVE_BYTES > 2 * S::SLAB ? S::WAVES * WAVE_BYTES : 2 * S::SLAB;
+  static constexpr int BYTES = S::WAVES * WAVE_BYTES > S::NB * S::SLAB ? S::WAVES * WAVE_BYTES : S::NB * S::SLAB;
 };
 
 // A tile of the layer.  SPLIT: part blockIdx / tiles of the sum over k, kept in fp32 for linear_join_kernel.
@@ -154,7 +154,11 @@ __global__ __launch_bounds__(S::THREADS) void linear_tile_kernel(const Operand<T
   const int64_t part = t / tiles, k0 = part * kpart, kend = k0 + kpart < k ? k0 + kpart : k;
   const int64_t row0 = bi * S::BM, col0 = bj * S::BN;
   typename Core<T>::acc_t acc[S::TN][S::TM] = {};
-  tile_accumulate<T, S, ROUTER, COUTER, DIRECT>(acc, lds, r, c, row0, col0, k0, kend);
+  TileStream<T, S, ROUTER, COUTER, DIRECT> stream(lds);
+  auto none = [] { return false; };
+  stream.set(r, c, row0, col0, k0, kend);
+  stream.begin(none);
+  stream.run(acc, stream.slabs(k0, kend), none);
 
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   float* const mine = reinterpret_cast<float*>(lds + wave * L::WAVE_BYTES);

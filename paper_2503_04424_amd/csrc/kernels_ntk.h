@@ -23,7 +23,9 @@ struct NtkLayers {
   const T* a[NTK_LAYERS];
   const T* g[NTK_LAYERS];
   int64_t lda[NTK_LAYERS], ldg[NTK_LAYERS];
+  uint32_t near_a, near_g, straight_a, straight_g;   // bit l: see Operand
 };
+static_assert(NTK_LAYERS <= 32, "a bit for each");
 
 // Element i of a matrix in type S, as a double; the conversions to fp64 are exact.
 template <typename S>
@@ -34,20 +36,30 @@ __global__ __launch_bounds__(256) void ntk_widen_kernel(const S* __restrict__ fr
   if (i < rows) to[i * ldto + k] = k < cols ? (double)from[i * ld + k] : 0.0;
 }
 
-// Block number t of the lower triangle of `rows` blocks: bands of eight rows of blocks, each column by column, so that
-// neighbours read the same operands; band r has 64 (r + 1) numbers.  False: above the diagonal or behind the end.
-__host__ __device__ __forceinline__ int64_t ntk_numbers(const int64_t rows) {
-  const int64_t bands = (rows + 7) / 8;
-  return 32 * bands * (bands + 1);
+// Blocks of the lower triangle: BM rows each, C = BM / BN blocks for every BM columns.  Bands of eight rows of blocks, each
+// column by column and the triangle at its end row by row, so that neighbours read the same operands.
+template <int C>
+__host__ __device__ __forceinline__ int64_t ntk_blocks(const int64_t rows) {
+  return C * (rows * (rows + 1) / 2);
 }
-__device__ __forceinline__ bool ntk_block(const int64_t t, const int64_t rows, int64_t& bi, int64_t& bj) {
-  int64_t r = (int64_t)((sqrt(1.0 + 0.125 * (double)t) - 1.0) * 0.5);
-  while (32 * r * (r + 1) > t) --r;
-  while (32 * (r + 1) * (r + 2) <= t) ++r;
-  const int64_t u = t - 32 * r * (r + 1);
-  bi = 8 * r + (u & 7);
-  bj = u >> 3;
-  return bi < rows && bj <= bi;
+template <int C>
+__device__ __forceinline__ void ntk_block(const int64_t t, const int64_t rows, int64_t& bi, int64_t& bj) {
+  // C (32 r^2 + 4 r) blocks stand before band r
+  int64_t r = (int64_t)((sqrt(16.0 + (128.0 / C) * (double)t) - 4.0) * (1.0 / 64.0));
+  while (C * (32 * r * r + 4 * r) > t) --r;
+  while (C * (32 * (r + 1) * (r + 1) + 4 * (r + 1)) <= t) ++r;
+  const int64_t u = t - C * (32 * r * r + 4 * r);
+  const int height = rows - 8 * r < 8 ? (int)(rows - 8 * r) : 8;
+  if (u < height * 8 * C * r) {
+    bi = 8 * r + u % height;
+    bj = u / height;
+  } else {
+    const int v = (int)(u - height * 8 * C * r);
+    int i = 0;
+    while (C * ((i + 1) * (i + 2) / 2) <= v) ++i;
+    bi = 8 * r + i;
+    bj = 8 * C * r + v - C * (i * (i + 1) / 2);
+  }
 }
 
 // first[l] = a_l a_l^T + bias, lower triangle of n x n, for networks of several outputs: every pair of samples' product
@@ -55,15 +67,21 @@ __device__ __forceinline__ bool ntk_block(const int64_t t, const int64_t rows, i
 template <typename T, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS) void ntk_first_kernel(const NtkLayers<T> layers, const int64_t n, const typename Core<T>::acc1_t bias,
                                                                typename Core<T>::acc1_t* __restrict__ first) {
-  __shared__ __attribute__((aligned(16))) char lds[2 * S::SLAB];
-  const int64_t rows = (n + S::BM - 1) / S::BM, numbers = ntk_numbers(rows);
-  const int64_t t = gemm_tile_number(blockIdx.x, numbers * layers.count);
+  __shared__ __attribute__((aligned(16))) char lds[S::NB * S::SLAB];
+  const int64_t rows = (n + S::BM - 1) / S::BM, blocks = ntk_blocks<S::BM / S::BN>(rows);
+  const int64_t t = gemm_tile_number(blockIdx.x, blocks * layers.count);
+  if (t < 0) return;
   int64_t bi, bj;
-  if (t < 0 || !ntk_block(t % numbers, rows, bi, bj)) return;
-  const int l = (int)(t / numbers);
-  const Operand<T> a{layers.a[l], layers.lda[l], n};
+  ntk_block<S::BM / S::BN>(t % blocks, rows, bi, bj);
+  if (bj * S::BN >= n) return;                     // the last rows' block may reach less far than its columns
+  const int l = (int)(t / blocks);
+  const Operand<T> a{layers.a[l], layers.lda[l], n, (layers.near_a >> l & 1) != 0, (layers.straight_a >> l & 1) != 0};
   typename Core<T>::acc_t acc[S::TN][S::TM] = {};
-  tile_accumulate<T, S, false, false, DIRECT>(acc, lds, a, a, bi * S::BM, bj * S::BN, 0, layers.p[l]);
+  TileStream<T, S, false, false, DIRECT> stream(lds);
+  auto none = [] { return false; };
+  stream.set(a, a, bi * S::BM, bj * S::BN, 0, layers.p[l]);
+  stream.begin(none);
+  stream.run(acc, stream.slabs(0, layers.p[l]), none);
   typename Core<T>::acc1_t* const to = first + l * n * n;
   tile_each<T, S>([&](int a0, int b0, int e, int i, int j) {
     const int64_t I = bi * S::BM + i, J = bj * S::BN + j;
@@ -79,29 +97,52 @@ __global__ __launch_bounds__(S::THREADS) void ntk_gram_kernel(const NtkLayers<T>
                                                               const int accumulate, const typename Core<T>::acc1_t* __restrict__ first,
                                                               typename Core<T>::acc1_t* __restrict__ K, const int64_t ldk) {
   typedef typename Core<T>::acc_t acc_t;
-  __shared__ __attribute__((aligned(16))) char lds[2 * S::SLAB];
+  __shared__ __attribute__((aligned(16))) char lds[S::NB * S::SLAB];
   const int64_t N = n * d, rows = (N + S::BM - 1) / S::BM;
-  const int64_t t = gemm_tile_number(blockIdx.x, ntk_numbers(rows));
+  const int64_t t = gemm_tile_number(blockIdx.x, ntk_blocks<S::BM / S::BN>(rows));
+  if (t < 0) return;
   int64_t bi, bj;
-  if (t < 0 || !ntk_block(t, rows, bi, bj)) return;
+  ntk_block<S::BM / S::BN>(t, rows, bi, bj);
   const int64_t row0 = bi * S::BM, col0 = bj * S::BN;
+  if (col0 >= N) return;                           // the last rows' block may reach less far than its columns
   acc_t total[S::TN][S::TM] = {};
+  // the samples of this lane's rows and columns; where nothing is stored, any pair will do
+  int sample_row[S::TM], sample_col[S::TN][4];
+  if constexpr (FIRST)
+    tile_each<T, S>([&](int a, int b, int e, int i, int j) {
+      const uint32_t I = (uint32_t)(row0 + i), J = (uint32_t)(col0 + j);
+      if (a == 0 && e == 0) sample_row[b] = row0 + i < N ? (int)(I / (uint32_t)d) : (int)n - 1;
+      if (b == 0) sample_col[a][e] = col0 + j < N ? (int)(J / (uint32_t)d) : 0;
+    });
+  auto of_a = [&](const int l) { return Operand<T>{layers.a[l], layers.lda[l], N, (layers.near_a >> l & 1) != 0, (layers.straight_a >> l & 1) != 0}; };
+  auto of_g = [&](const int l) { return Operand<T>{layers.g[l], layers.ldg[l], N, (layers.near_g >> l & 1) != 0, (layers.straight_g >> l & 1) != 0}; };
+  TileStream<T, S, false, false, DIRECT> stream(lds);
+  // the products in their order: g_l g_l^T, then (one output) a_l a_l^T
+  int product = 0;
+  auto next = [&] {
+    const int l = FIRST ? product : product >> 1;
+    if (l >= layers.count) return false;
+    const bool second = FIRST || !(product & 1);
+    const Operand<T> o = second ? of_g(l) : of_a(l);
+    stream.set(o, o, row0, col0, 0, second ? layers.q[l] : layers.p[l]);
+    ++product;
+    return true;
+  };
+  stream.begin(next);
   for (int l = 0; l < layers.count; ++l) {
     acc_t second[S::TN][S::TM] = {};
-    const Operand<T> g{layers.g[l], layers.ldg[l], N};
-    __syncthreads();                               // the product before reads its last slab
-    tile_accumulate<T, S, false, false, DIRECT>(second, lds, g, g, row0, col0, 0, layers.q[l]);
+    stream.run(second, stream.slabs(0, layers.q[l]), next);
     if constexpr (FIRST) {
       const typename Core<T>::acc1_t* const from = first + l * n * n;
-      tile_each<T, S>([&](int a, int b, int e, int i, int j) {
-        int64_t I = row0 + i, J = col0 + j;
-        if (I < N && J <= I) total[a][b][e] += from[I / d * n + J / d] * second[a][b][e];
-      });
+#pragma unroll
+      for (int b = 0; b < S::TM; ++b)
+#pragma unroll
+        for (int a = 0; a < S::TN; ++a)
+#pragma unroll
+          for (int e = 0; e < 4; ++e) total[a][b][e] += from[(int64_t)sample_row[b] * n + sample_col[a][e]] * second[a][b][e];
     } else {
-      const Operand<T> x{layers.a[l], layers.lda[l], N};
       acc_t one[S::TN][S::TM] = {};
-      __syncthreads();
-      tile_accumulate<T, S, false, false, DIRECT>(one, lds, x, x, row0, col0, 0, layers.p[l]);
+      stream.run(one, stream.slabs(0, layers.p[l]), next);
 #pragma unroll
       for (int a = 0; a < S::TN; ++a)
 #pragma unroll

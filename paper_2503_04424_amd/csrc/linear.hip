@@ -36,13 +36,15 @@ bool four(const void* p, int64_t ld, int64_t rows) {
   return !p || ((uintptr_t)p % (4 * sizeof(T)) == 0 && (rows == 1 || ld % 4 == 0));
 }
 
-typedef Tile<256, 256, 2, 4> Big;
-typedef Tile<128, 128, 2, 2> Mid;
-typedef Tile<64, 64, 2, 2> Small;
+typedef Tile<256, 256, 2, 4, 8, 2> Big;
+typedef Tile<128, 128, 2, 2, 8, 2> Mid;
+template <typename T>
+using Small = Tile<64, 64, 2, 2, 8, sizeof(T) == 2 ? 4 : 2>;
+typedef Tile<32, 32, 2, 2, 8, 4> Tiny;
 
 // How a product is cut: tile shape and parts of the sum over k.
 struct Cut {
-  int shape;                           // 0 small, 1 mid, 2 big
+  int tile;                            // rows and columns of a tile: 32, 64, 128 or 256
   int splits;
   int64_t kpart;
 };
@@ -50,11 +52,11 @@ Cut cut_of(int64_t rows, int64_t cols, int64_t k, int64_t size) {
   Cut c;
   const int64_t bk = 128 / size;
   auto tiles = [&](int64_t b) { return ceil_div(rows, b) * ceil_div(cols, b); };
-  c.shape = size == 2 && tiles(256) >= 192 ? 2 : tiles(128) >= 192 ? 1 : 0;
+  c.tile = size == 2 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : tiles(64) >= 256 ? 64 : 32;
   c.splits = 1;
   c.kpart = k;
-  const int64_t t = tiles(c.shape == 2 ? 256 : c.shape == 1 ? 128 : 64);
-  if (c.shape == 0 && t < 256 && k >= 8 * bk) {
+  const int64_t t = tiles(c.tile);
+  if (c.tile <= 64 && t < 256 && k >= 8 * bk) {
     int64_t most = k / (4 * bk), want = ceil_div(512, t);
     int64_t s = want < most ? want : most;
     if (s > 16) s = 16;
@@ -68,18 +70,20 @@ Cut cut_of(int64_t rows, int64_t cols, int64_t k, int64_t size) {
 uint64_t parts_bytes(const Cut& c, int64_t rows, int64_t cols) { return c.splits > 1 ? up256((uint64_t)c.splits * rows * cols * 4) : 0; }
 
 template <typename T, typename O, typename S, bool ROUTER, bool COUTER>
-void tiles(const Operand<T>& r, const Operand<T>& c, int64_t k, const LinearOut<T, O>& out, const Cut& cut, float* parts, hipStream_t st) {
+void tiles(Operand<T> r, Operand<T> c, int64_t k, const LinearOut<T, O>& out, const Cut& cut, float* parts, hipStream_t st) {
   const int64_t n = ceil_div(out.rows, S::BM) * ceil_div(out.cols, S::BN) * cut.splits;
-  const dim3 grid((unsigned)(ceil_div(n, 8) * 8)), block(S::THREADS);
-  const bool direct = gemm_straight<T, ROUTER, S::BM>(r, k) && gemm_straight<T, COUTER, S::BN>(c, k);
+  const dim3 grid((unsigned)(ceil_div(n, 8) * 8));
+  r = gemm_operand<T, ROUTER, S::BM>(r.p, r.stride, r.rows, k);
+  c = gemm_operand<T, COUTER, S::BN>(c.p, c.stride, c.rows, k);
+  const bool direct = r.straight && c.straight;
   auto go = [&](auto d, auto split) {
-    hipLaunchKernelGGL((linear_tile_kernel<T, O, S, ROUTER, COUTER, decltype(d)::value, decltype(split)::value>), grid, block, 0, st, r, c, k, out,
+    hipLaunchKernelGGL((linear_tile_kernel<T, O, S, ROUTER, COUTER, decltype(d)::value, decltype(split)::value>), grid, dim3(S::THREADS), 0, st, r, c, k, out,
                        parts, cut.splits, cut.kpart);
   };
   using std::false_type;
   using std::true_type;
   if (cut.splits > 1) {
-    if constexpr (S::BM == 64) {
+    if constexpr (S::BM <= 64) {
       if (direct) go(true_type{}, true_type{});
       else go(false_type{}, true_type{});
       const int64_t groups = ceil_div(out.rows * ceil_div(out.cols, 4), 256);
@@ -90,15 +94,16 @@ void tiles(const Operand<T>& r, const Operand<T>& c, int64_t k, const LinearOut<
 }
 
 template <typename T, typename O, bool ROUTER, bool COUTER>
-int product(const Operand<T>& r, const Operand<T>& c, int64_t k, LinearOut<T, O> out, float* parts, hipStream_t st) {
+int product(Operand<T> r, Operand<T> c, int64_t k, LinearOut<T, O> out, float* parts, hipStream_t st) {
   const Cut cut = cut_of(out.rows, out.cols, k, sizeof(T));
-  if (ceil_div(out.rows, 64) * ceil_div(out.cols, 64) > INT32_MAX / 32) return MDET_EINVAL;
+  if (ceil_div(out.rows, 32) * ceil_div(out.cols, 32) > INT32_MAX / 32) return MDET_EINVAL;
   out.vec = four<O>(out.y, out.ldy, out.rows) && four<T>(out.bias, 0, 1) && four<T>(out.residual, out.ldr, out.rows) &&
             four<T>(out.z, out.ldz, out.rows);
-  if (cut.shape == 2) {
+  if (cut.tile == 256) {
     if constexpr (sizeof(T) == 2) tiles<T, O, Big, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
-  } else if (cut.shape == 1) tiles<T, O, Mid, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
-  else tiles<T, O, Small, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
+  } else if (cut.tile == 128) tiles<T, O, Mid, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
+  else if (cut.tile == 64) tiles<T, O, Small<T>, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
+  else tiles<T, O, Tiny, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
   return launch_status();
 }
 
@@ -152,11 +157,11 @@ int backward(const Grad& g) {
   const int64_t ldd = own_dz ? lddz : g.lddy;
   if (status == MDET_OK && g.dx && g.m > 0 && g.k > 0) {
     const LinearOut<T, T> out{(T*)g.dx, g.lddx, nullptr, nullptr, 0, nullptr, 0, MDET_ACT_NONE, g.m, g.k, false};
-    status = product<T, T, false, true>(Operand<T>{d, ldd, g.m}, Operand<T>{(const T*)g.w, g.ldw, g.k}, g.n, out, parts, g.st);
+    status = product<T, T, false, true>(Operand<T>{d, ldd, g.m, false, false}, Operand<T>{(const T*)g.w, g.ldw, g.k, false, false}, g.n, out, parts, g.st);
   }
   if (status == MDET_OK && g.dw && g.n > 0 && g.k > 0) {
     const LinearOut<T, O> out{(O*)g.dw, g.lddw, nullptr, nullptr, 0, nullptr, 0, MDET_ACT_NONE, g.n, g.k, false};
-    status = product<T, O, true, true>(Operand<T>{d, ldd, g.n}, Operand<T>{(const T*)g.x, g.ldx, g.k}, g.m, out, parts, g.st);
+    status = product<T, O, true, true>(Operand<T>{d, ldd, g.n, false, false}, Operand<T>{(const T*)g.x, g.ldx, g.k, false, false}, g.m, out, parts, g.st);
   }
   return status;
 }
@@ -186,7 +191,7 @@ int mdet_linear_forward(int32_t dtype, int32_t activation, int64_t m, int64_t n,
   auto call = [&](auto zero) {
     typedef decltype(zero) T;
     const LinearOut<T, T> out{(T*)y, ldy, (const T*)bias, (const T*)residual, ldr, (T*)z, ldz, activation, m, n, false};
-    return product<T, T, false, false>(Operand<T>{(const T*)x, ldx, m}, Operand<T>{(const T*)w, ldw, n}, k, out, (float*)workspace, (hipStream_t)stream);
+    return product<T, T, false, false>(Operand<T>{(const T*)x, ldx, m, false, false}, Operand<T>{(const T*)w, ldw, n, false, false}, k, out, (float*)workspace, (hipStream_t)stream);
   };
   return dtype == MDET_F32 ? call(0.0f) : dtype == MDET_BF16 ? call((__bf16)0.0f) : call((_Float16)0.0f);
 }

@@ -17,7 +17,7 @@ inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t size_of(int32_t t) { return t == MDET_F64 ? 8 : t == MDET_F32 ? 4 : 2; }
 inline int launch_status() { return hipGetLastError() == hipSuccess ? MDET_OK : MDET_EHIP; }
 
-constexpr int64_t MOST = int64_t(1) << 31;
+constexpr int64_t MOST = INT32_MAX;
 
 // Types, sizes and strides; pointers only where `pointers` is set.
 int check(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs, const mdet_ntk_layer* layers, int32_t count, bool pointers) {
@@ -54,8 +54,9 @@ struct Call {
   hipStream_t st;
 };
 
-typedef Tile<128, 128, 2, 4> Large;
-typedef Tile<64, 64, 2, 2> Small;
+typedef Tile<128, 128, 2, 4, 8, 2> Large;
+typedef Tile<64, 64, 2, 2, 8, 2> Small;
+typedef Tile<32, 32, 2, 2, 8, 4> Tiny;
 
 // First factors of one launch's layers, for several outputs.
 inline uint64_t first_bytes(int64_t n, int64_t d, int32_t layers, int64_t size) {
@@ -63,36 +64,56 @@ inline uint64_t first_bytes(int64_t n, int64_t d, int32_t layers, int64_t size) 
 }
 
 template <typename T, typename S>
-int gram_tiles(const NtkLayers<T>& list, const Call& c, int accumulate, void* first) {
+int gram_tiles(NtkLayers<T>& list, const Call& c, int accumulate, void* first) {
   typedef typename Core<T>::acc1_t A;
-  bool direct = true;
-  for (int l = 0; l < list.count; ++l)
-    direct = direct && (list.p[l] == 0 || gemm_straight<T, false, S::BM>(Operand<T>{list.a[l], list.lda[l], c.n}, list.p[l])) &&
-             (list.q[l] == 0 || gemm_straight<T, false, S::BM>(Operand<T>{list.g[l], list.ldg[l], c.n * c.d}, list.q[l]));
-  auto grid = [](int64_t rows, int64_t times) { return ceil_div(ntk_numbers(ceil_div(rows, S::BM)) * times, 8) * 8; };
+  // A launch goes straight to LDS where most of what it reads can go there: a last layer of one output, whose rows are
+  // single elements, does not hold up the others.
+  int64_t yes_a = 0, no_a = 0, yes_g = 0, no_g = 0;
+  list.near_a = list.near_g = list.straight_a = list.straight_g = 0;
+  for (int l = 0; l < list.count; ++l) {
+    const Operand<T> a = gemm_operand<T, false, S::BM>(list.a[l], list.lda[l], c.n, list.p[l]);
+    const Operand<T> g = gemm_operand<T, false, S::BM>(list.g[l], list.ldg[l], c.n * c.d, list.q[l]);
+    list.near_a |= (uint32_t)a.near << l;
+    list.near_g |= (uint32_t)g.near << l;
+    list.straight_a |= (uint32_t)a.straight << l;
+    list.straight_g |= (uint32_t)g.straight << l;
+    (a.straight ? yes_a : no_a) += list.p[l];
+    (g.straight ? yes_g : no_g) += list.q[l];
+  }
+  // in fp64 the large tile has no registers left for operands that pass through them
+  constexpr bool REGISTERS = !(std::is_same<T, double>::value && S::BM == 128);
+  if constexpr (!REGISTERS) {
+    if (no_g > yes_g / 8 || (c.d > 1 && no_a > yes_a / 8) || (c.d == 1 && no_a + no_g > (yes_a + yes_g) / 8))
+      return gram_tiles<T, Small>(list, c, accumulate, first);
+  }
+  auto grid = [](int64_t rows, int64_t times) { return ceil_div(ntk_blocks<S::BM / S::BN>(ceil_div(rows, S::BM)) * times, 8) * 8; };
   const int64_t all = grid(c.n * c.d, 1), firsts = c.d > 1 ? grid(c.n, list.count) : 0;
   if (all > INT32_MAX || firsts > INT32_MAX) return MDET_EINVAL;
-  auto go = [&](auto d) {
-    constexpr bool D = decltype(d)::value;
-    if (c.d > 1) {
-      if (list.count > 0)
-        hipLaunchKernelGGL((ntk_first_kernel<T, S, D>), dim3((unsigned)firsts), dim3(S::THREADS), 0, c.st, list, c.n, (A)c.bias, (A*)first);
-      hipLaunchKernelGGL((ntk_gram_kernel<T, S, D, true>), dim3((unsigned)all), dim3(S::THREADS), 0, c.st, list, c.n, (int)c.d, (A)c.bias,
-                         (A)c.scale, accumulate, (const A*)first, (A*)c.K, c.ldk);
-    } else {
-      hipLaunchKernelGGL((ntk_gram_kernel<T, S, D, false>), dim3((unsigned)all), dim3(S::THREADS), 0, c.st, list, c.n, 1, (A)c.bias,
-                         (A)c.scale, accumulate, (const A*)nullptr, (A*)c.K, c.ldk);
-    }
+  using std::false_type;
+  using std::true_type;
+  auto gram = [&](auto direct, auto several) {
+    hipLaunchKernelGGL((ntk_gram_kernel<T, S, decltype(direct)::value, decltype(several)::value>), dim3((unsigned)all), dim3(S::THREADS), 0, c.st,
+                       list, c.n, (int)c.d, (A)c.bias, (A)c.scale, accumulate, (const A*)first, (A*)c.K, c.ldk);
   };
-  if (direct) go(std::true_type{});
-  else go(std::false_type{});
+  if (c.d > 1) {
+    auto firsts_of = [&](auto direct) {
+      hipLaunchKernelGGL((ntk_first_kernel<T, S, decltype(direct)::value>), dim3((unsigned)firsts), dim3(S::THREADS), 0, c.st, list, c.n, (A)c.bias,
+                         (A*)first);
+    };
+    if (list.count > 0) {
+      if (no_a <= yes_a / 8) firsts_of(true_type{});
+      else if constexpr (REGISTERS) firsts_of(false_type{});
+    }
+    if (no_g <= yes_g / 8) gram(true_type{}, true_type{});
+    else if constexpr (REGISTERS) gram(false_type{}, true_type{});
+  } else if (no_a + no_g <= (yes_a + yes_g) / 8) gram(true_type{}, false_type{});
+  else if constexpr (REGISTERS) gram(false_type{}, false_type{});
   return launch_status();
 }
 
 template <typename T>
 int gram(const mdet_ntk_layer* layers, int32_t count, const Call& c, void* first) {
   int accumulate = c.accumulate;
-  const int64_t large = ceil_div(c.n * c.d, 128);
   for (int32_t l0 = 0; l0 == 0 || l0 < count; l0 += NTK_LAYERS) {
     NtkLayers<T> list;
     list.count = count - l0 < NTK_LAYERS ? count - l0 : NTK_LAYERS;
@@ -101,8 +122,17 @@ int gram(const mdet_ntk_layer* layers, int32_t count, const Call& c, void* first
       list.a[l] = (const T*)x.a, list.lda[l] = x.lda, list.p[l] = x.p;
       list.g[l] = (const T*)x.g, list.ldg[l] = x.ldg, list.q[l] = x.q;
     }
-    const int status = large * (large + 1) / 2 >= 256 ? gram_tiles<T, Large>(list, c, accumulate, first)
-                                                      : gram_tiles<T, Small>(list, c, accumulate, first);
+    // Several workgroups a compute unit, and so the 64 x 64 tile, are better than one large one (fp32 n = 8192, three layers:
+    // 1.48 ms, 1.65 with 128 x 128; fp64 n = 4096 54 and 47 TFLOP/s) except at the largest orders in fp64 (n = 8192 62.0 TFLOP/s,
+    // 59.6 with the small tile) and in 16 bits with several outputs (order 10000 433 us, 461).  A few small blocks would leave most
+    // compute units without one: n = 512 in fp32 21 us with the 32 x 32 tile, 35 with 64 x 64, in fp64 29 and 63.
+    const int64_t order = c.n * c.d;
+    int status;
+    if (order >= 8000 && (sizeof(T) == 8 || (sizeof(T) == 2 && c.d > 1))) {
+      if constexpr (sizeof(T) != 4) status = gram_tiles<T, Large>(list, c, accumulate, first);
+    } else if (sizeof(T) != 2 && order < 1500) {
+      if constexpr (sizeof(T) != 2) status = gram_tiles<T, Tiny>(list, c, accumulate, first);
+    } else status = gram_tiles<T, Small>(list, c, accumulate, first);
     if (status != MDET_OK) return status;
     accumulate = 1;
   }
