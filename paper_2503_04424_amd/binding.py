@@ -7,7 +7,10 @@ fallback of any kind.
 from __future__ import annotations
 
 import ctypes as C
+import functools
+import itertools
 import math
+import operator
 import os
 from dataclasses import dataclass
 from typing import Callable, Optional
@@ -593,6 +596,7 @@ def mdet_flodance_eval(coef, q, n_values, out=None, stream=None):
 
 
 _TYPE_CODES = {}
+_IS_CUDA = operator.attrgetter("is_cuda")
 
 
 def _type_code(dtype) -> int:
@@ -619,7 +623,7 @@ def _operand_type(t):
 
 def _matrix(t, name, rows, cols, dtype):
     """(address, leading dimension) of a row-major CUDA matrix of this shape and type."""
-    if t.dim() != 2 or t.shape[0] != rows or t.shape[1] != cols or t.dtype != dtype or not t.is_cuda:
+    if t.shape != (rows, cols) or t.dtype != dtype or not t.is_cuda:
         raise ValueError(f"{name}: a CUDA tensor of {rows} x {cols} {dtype} expected, not {tuple(t.shape)} {t.dtype}")
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
@@ -628,9 +632,24 @@ def _matrix(t, name, rows, cols, dtype):
 
 
 def _vector(t, name, n, dtype):
-    if t.dim() != 1 or t.shape[0] != n or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
+    if t.shape != (n,) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous CUDA tensor of {n} {dtype} expected, not {tuple(t.shape)} {t.dtype}")
     return t.data_ptr()
+
+
+_raw_stream = None
+
+
+def _operator_stream(stream, like):
+    """Handle of the caller's stream, or of the current one on the tensor's device."""
+    if stream is not None:
+        return _stream_handle(stream)
+    global _raw_stream
+    if _raw_stream is None:
+        import torch
+        # the handle alone where torch offers it: a tenth of the time of making a Stream object
+        _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
+    return _raw_stream(like.device.index)
 
 
 def _check_status(st):
@@ -660,6 +679,7 @@ def _operator_workspace(workspace, need, like, stream):
     return ws.data_ptr(), need, ws
 
 
+@functools.lru_cache(maxsize=1024)
 def mdet_linear_workspace_query(dtype, m, n, k, backward=False) -> int:
     """Device bytes of workspace for ``mdet_linear_forward`` or, with ``backward``, the gradient."""
     b = C.c_uint64(0)
@@ -689,7 +709,7 @@ def mdet_linear_forward(x, w, bias=None, residual=None, activation="none", out=N
     need = 0 if workspace is not None else mdet_linear_workspace_query(t, m, n, k)
     wsp, wsb, _ws = _operator_workspace(workspace, need, x, stream)
     _check_status(load().mdet_linear_forward(_type_code(t), act, m, n, k, xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, zp, ldz,
-                                             wsp, wsb, _stream_handle(stream)))
+                                             wsp, wsb, _operator_stream(stream, x)))
     return out
 
 
@@ -726,19 +746,18 @@ def mdet_linear_backward(dy, x, w, preact=None, activation="none", dx=True, dw=T
     need = 0 if workspace is not None else mdet_linear_workspace_query(t, m, n, k, backward=True)
     wsp, wsb, _ws = _operator_workspace(workspace, need, x, stream)
     _check_status(load().mdet_linear_backward(_type_code(t), _type_code(gt), act, m, n, k, dyp, lddy, zp, ldz, xp, ldx, wp, ldw,
-                                              dxp, lddx, dwp, lddw, dbp, dzp, lddz, wsp, wsb, _stream_handle(stream)))
+                                              dxp, lddx, dwp, lddw, dbp, dzp, lddz, wsp, wsb, _operator_stream(stream, x)))
     return dx, dw, db
 
 
-def _adamw_pointers(tensors, name, count, dtype, sizes=None):
-    """Addresses of `count` contiguous CUDA tensors of one type (and these sizes)."""
-    if len(tensors) != count:
-        raise ValueError(f"{name}: {count} tensors expected, not {len(tensors)}")
-    for i, t in enumerate(tensors):
-        if t.dtype != dtype or not t.is_cuda or not t.is_contiguous() or (sizes is not None and t.numel() != sizes[i]):
-            raise ValueError(f"{name}[{i}]: a contiguous CUDA tensor of {'the same number of ' if sizes else ''}{dtype} expected, "
-                             f"not {tuple(t.shape)} {t.dtype}")
-    return [t.data_ptr() for t in tensors]
+def _adamw_pointers(tensors, name, dtype, sizes):
+    """Addresses of contiguous CUDA tensors of one type and these sizes."""
+    from torch import Tensor
+    if list(map(Tensor.numel, tensors)) != sizes or not all(map(Tensor.is_contiguous, tensors)) or \
+            not all(map(_IS_CUDA, tensors)) or any(t.dtype != dtype for t in tensors):
+        raise ValueError(f"{name}: contiguous CUDA tensors of {dtype} with {sizes} elements expected, not "
+                         f"{[(tuple(t.shape), t.dtype) for t in tensors]}")
+    return map(Tensor.data_ptr, tensors)
 
 
 def mdet_adamw_step(params, grads, exp_avg, exp_avg_sq, *, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
@@ -768,15 +787,15 @@ def mdet_adamw_step(params, grads, exp_avg, exp_avg_sq, *, lr, step, beta1=0.9, 
         a.grad_scale = grad_scale.data_ptr()
     none = [0] * count
     fields = (
-        _adamw_pointers(params, "params", count, params[0].dtype),
-        _adamw_pointers(grads, "grads", count, grads[0].dtype if grads else None, sizes),
-        _adamw_pointers(exp_avg, "exp_avg", count, torch.float32 if wide else torch.int8, sizes),
-        _adamw_pointers(exp_avg_sq, "exp_avg_sq", count, torch.float32 if wide else torch.uint8, sizes),
-        none if wide else _adamw_pointers(scales, "scales", count, torch.float32, [(n + 255) // 256 * 2 for n in sizes]),
-        none if copies is None else _adamw_pointers(copies, "copies", count, copies[0].dtype if copies else None, sizes),
+        _adamw_pointers(params, "params", params[0].dtype, sizes),
+        _adamw_pointers(grads, "grads", grads[0].dtype if grads else None, sizes),
+        _adamw_pointers(exp_avg, "exp_avg", torch.float32 if wide else torch.int8, sizes),
+        _adamw_pointers(exp_avg_sq, "exp_avg_sq", torch.float32 if wide else torch.uint8, sizes),
+        none if wide else _adamw_pointers(scales, "scales", torch.float32, [(n + 255) // 256 * 2 for n in sizes]),
+        none if copies is None else _adamw_pointers(copies, "copies", copies[0].dtype if copies else None, sizes),
         sizes)
-    table = (C.c_uint64 * (7 * count))(*[v for row in zip(*fields) for v in row])
-    _check_status(load().mdet_adamw_step(C.byref(a), C.cast(table, C.c_void_p), count, _stream_handle(stream)))
+    table = (C.c_uint64 * (7 * count))(*itertools.chain.from_iterable(zip(*fields)))
+    _check_status(load().mdet_adamw_step(C.byref(a), C.cast(table, C.c_void_p), count, _operator_stream(stream, params[0])))
 
 
 def _ntk_layers(inputs, signals, outputs):
@@ -831,7 +850,7 @@ def mdet_ntk_gram(inputs, signals, out=None, outputs=1, bias=1.0, scale=1.0, acc
         _check_status(lib_.mdet_ntk_workspace_query(*codes, n, outputs, layers, len(table), C.byref(need)))
     wsp, wsb, _ws = _operator_workspace(workspace, need.value, out, stream)
     _check_status(lib_.mdet_ntk_gram(*codes, n, outputs, layers, len(table), float(bias), float(scale), int(bool(accumulate)),
-                                     kp, ldk, wsp, wsb, _stream_handle(stream)))
+                                     kp, ldk, wsp, wsb, _operator_stream(stream, out)))
     return out
 
 

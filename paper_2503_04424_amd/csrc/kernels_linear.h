@@ -229,6 +229,59 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const float* __restric
   act_switch(out.act, [&](auto act) { linear_put4<T, O, decltype(act)::value>(out, i, j, v); });
 }
 
+// Up to 16 rows of x (single tokens): W is read once, 16 rows of it by a workgroup whose wavefronts share k, each piece
+// straight into the registers of its product.  Bytes of W bound it, and how many are on their way: sixteen wavefronts a
+// workgroup (4096 x 4096 bf16, one row: 8.7 us, 3.9 TB/s; with four 9.4, as split 32-row tiles and a join 11.4).
+template <typename T, typename O, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void linear_rows_kernel(const Operand<T> x, const Operand<T> w, const int64_t k, const LinearOut<T, O> out) {
+  typedef typename Core<T>::piece_t piece_t;
+  typedef typename Core<T>::acc_t acc_t;
+  constexpr int VEC = Core<T>::VEC, STEP = 4 * VEC, UNROLL = 8;
+  __shared__ acc_t sums[WAVES][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), j = lane & 15, g = lane >> 4;
+  const int64_t col0 = (int64_t)blockIdx.x * 16;
+  // rows behind the last are not stored
+  const T* const wp = w.p + (col0 + j < w.rows ? col0 + j : w.rows - 1) * w.stride + g * VEC;
+  const T* const xp = x.p + (j < x.rows ? j : x.rows - 1) * x.stride + g * VEC;
+  acc_t acc = {};
+  const int64_t steps = k / STEP, each = (steps + WAVES - 1) / WAVES;
+  int64_t s = wave * each;
+  const int64_t end = s + each < steps ? s + each : steps;
+  auto some = [&](auto count) {
+    constexpr int U = decltype(count)::value;
+    piece_t wf[U], xf[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) __builtin_memcpy(&wf[u], wp + (s + u) * STEP, 16);
+#pragma unroll
+    for (int u = 0; u < U; ++u) __builtin_memcpy(&xf[u], xp + (s + u) * STEP, 16);
+#pragma unroll
+    for (int u = 0; u < U; ++u) Core<T>::mma(wf[u], xf[u], acc);
+  };
+  for (; s + UNROLL <= end; s += UNROLL) some(std::integral_constant<int, UNROLL>{});
+  for (; s < end; ++s) some(std::integral_constant<int, 1>{});
+  if (wave == WAVES - 1 && steps * STEP < k) {                 // what is left over, element by element
+    const int64_t at = steps * STEP;
+    piece_t wf = {}, xf = {};
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (at + g * VEC + e < k) {
+        wf[e] = wp[at + e];
+        xf[e] = xp[at + e];
+      }
+    Core<T>::mma(wf, xf, acc);
+  }
+  sums[wave][lane] = acc;
+  __syncthreads();
+  if (wave == 0) {
+    acc_t v = sums[0][lane];
+#pragma unroll
+    for (int p = 1; p < WAVES; ++p) v += sums[p][lane];
+    const int64_t c = col0 + 4 * g;
+    const float in[4] = {v[0], v[1], v[2], v[3]};
+    if (j < out.rows && c < out.cols) act_switch(out.act, [&](auto act) { linear_put4<T, O, decltype(act)::value>(out, j, c, in); });
+  }
+}
+
 // dz = dy act'(z) and the column sums of DZ_ROWS rows of it: a workgroup takes 64 columns, thread (t, c) every fourth row of
 // column c.
 constexpr int DZ_COLS = 64, DZ_ROWS = 64;

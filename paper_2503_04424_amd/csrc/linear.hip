@@ -42,14 +42,26 @@ template <typename T>
 using Small = Tile<64, 64, 2, 2, 8, sizeof(T) == 2 ? 4 : 2>;
 typedef Tile<32, 32, 2, 2, 8, 4> Tiny;
 
+// Few rows: W is read once.  Beyond 8192 rows of W a split sum over tiles is as fast for one row (16384 x 4096 bf16 22.3 us,
+// 23.7 this way) and faster for sixteen (23.4, 32.2), as it is for more rows at any size (17 rows of 4096 x 4096 11.5 us).
+inline bool few_rows(int64_t rows, int64_t cols) { return rows <= 16 && cols <= 8192; }
+
+template <typename T, typename O>
+void rows_product(const Operand<T>& r, const Operand<T>& c, int64_t k, const LinearOut<T, O>& out, hipStream_t st) {
+  const dim3 grid((unsigned)ceil_div(out.cols, 16));
+  if (k * (int64_t)sizeof(T) >= 4096) hipLaunchKernelGGL((linear_rows_kernel<T, O, 16>), grid, dim3(1024), 0, st, r, c, k, out);
+  else hipLaunchKernelGGL((linear_rows_kernel<T, O, 4>), grid, dim3(256), 0, st, r, c, k, out);
+}
+
 // How a product is cut: tile shape and parts of the sum over k.
 struct Cut {
-  int tile;                            // rows and columns of a tile: 32, 64, 128 or 256
+  int tile;                            // rows and columns of a tile: 32, 64, 128 or 256; 0: few rows
   int splits;
   int64_t kpart;
 };
-Cut cut_of(int64_t rows, int64_t cols, int64_t k, int64_t size) {
+Cut cut_of(int64_t rows, int64_t cols, int64_t k, int64_t size, bool inner) {
   Cut c;
+  if (inner && few_rows(rows, cols)) return Cut{0, 1, k};
   const int64_t bk = 128 / size;
   auto tiles = [&](int64_t b) { return ceil_div(rows, b) * ceil_div(cols, b); };
   c.tile = size == 2 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : tiles(64) >= 256 ? 64 : 32;
@@ -95,11 +107,13 @@ void tiles(Operand<T> r, Operand<T> c, int64_t k, const LinearOut<T, O>& out, co
 
 template <typename T, typename O, bool ROUTER, bool COUTER>
 int product(Operand<T> r, Operand<T> c, int64_t k, LinearOut<T, O> out, float* parts, hipStream_t st) {
-  const Cut cut = cut_of(out.rows, out.cols, k, sizeof(T));
+  const Cut cut = cut_of(out.rows, out.cols, k, sizeof(T), !ROUTER && !COUTER);
   if (ceil_div(out.rows, 32) * ceil_div(out.cols, 32) > INT32_MAX / 32) return MDET_EINVAL;
   out.vec = four<O>(out.y, out.ldy, out.rows) && four<T>(out.bias, 0, 1) && four<T>(out.residual, out.ldr, out.rows) &&
             four<T>(out.z, out.ldz, out.rows);
-  if (cut.tile == 256) {
+  if (cut.tile == 0) {
+    if constexpr (!ROUTER && !COUTER) rows_product<T, O>(r, c, k, out, st);
+  } else if (cut.tile == 256) {
     if constexpr (sizeof(T) == 2) tiles<T, O, Big, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
   } else if (cut.tile == 128) tiles<T, O, Mid, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
   else if (cut.tile == 64) tiles<T, O, Small<T>, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
@@ -119,7 +133,7 @@ GradLayout grad_layout(int32_t dtype, int64_t m, int64_t n, int64_t k) {
   g.sums = up256((uint64_t)m * g.lddz * size_of(dtype));
   g.parts = g.sums + up256((uint64_t)g.strips * n * 4);
   const int64_t s = size_of(dtype);
-  const uint64_t dx = parts_bytes(cut_of(m, k, n, s), m, k), dw = parts_bytes(cut_of(n, k, m, s), n, k);
+  const uint64_t dx = parts_bytes(cut_of(m, k, n, s, false), m, k), dw = parts_bytes(cut_of(n, k, m, s, false), n, k);
   g.bytes = g.parts + (dx > dw ? dx : dw);
   return g;
 }
@@ -172,7 +186,7 @@ extern "C" {
 
 int mdet_linear_workspace_query(int32_t dtype, int32_t backward, int64_t m, int64_t n, int64_t k, uint64_t* bytes) {
   if (!bytes || !is_type(dtype) || !sizes_fit(m, n, k)) return MDET_EINVAL;
-  *bytes = backward ? grad_layout(dtype, m, n, k).bytes : parts_bytes(cut_of(m, n, k, size_of(dtype)), m, n);
+  *bytes = backward ? grad_layout(dtype, m, n, k).bytes : parts_bytes(cut_of(m, n, k, size_of(dtype), true), m, n);
   return MDET_OK;
 }
 
