@@ -44,6 +44,7 @@ extern "C" int mdet_adamw_step(const mdet_adamw_params* a, const mdet_adamw_tens
   if (!is_part(a->beta1) || !is_part(a->beta2) || !(a->eps >= 0.0) || !std::isfinite(a->lr) || !std::isfinite(a->weight_decay) ||
       !std::isfinite(a->eps))
     return MDET_EINVAL;
+  int64_t total = 0;
   for (int64_t i = 0; i < count; ++i) {
     const mdet_adamw_tensor& t = tensors[i];
     if (t.n < 0) return MDET_EINVAL;
@@ -53,7 +54,8 @@ extern "C" int mdet_adamw_step(const mdet_adamw_params* a, const mdet_adamw_tens
     if ((uintptr_t)t.p % ps || (uintptr_t)t.g % gs) return MDET_EINVAL;
     if (a->state_bits == 32 && (((uintptr_t)t.m | (uintptr_t)t.v) % 4)) return MDET_EINVAL;
     if ((a->state_bits == 8 && (uintptr_t)t.scales % 4) || (a->copy_dtype != -1 && (uintptr_t)t.copy % 2)) return MDET_EINVAL;
-    if (t.n > (int64_t)INT32_MAX * ADAMW_CHUNK) return MDET_EINVAL;
+    if (t.n > (int64_t)INT32_MAX * ADAMW_STEP) return MDET_EINVAL;
+    total += t.n;
   }
   AdamwFactors f;
   f.b1 = (float)a->beta1;
@@ -70,10 +72,13 @@ extern "C" int mdet_adamw_step(const mdet_adamw_params* a, const mdet_adamw_tens
   AdamwTensors list;
   list.count = 0;
   list.first[0] = 0;
+  // A few steps a workgroup while there are enough of them to fill the device; 1.2 million elements in 8 bits take 14.4 us
+  // with four, 10.5 with one.
+  list.chunk = (total < (int64_t)4 << 20 ? 1 : 4) * ADAMW_STEP;
   f.first_tensor = 0;
   // Tensors without elements keep their number (the hash goes by it) and take no chunk.
   for (int64_t i = 0; i <= count; ++i) {
-    const int64_t chunks = i < count ? (tensors[i].n + ADAMW_CHUNK - 1) / ADAMW_CHUNK : 0;
+    const int64_t chunks = i < count ? (tensors[i].n + list.chunk - 1) / list.chunk : 0;
     if (i == count || list.count == ADAMW_TENSORS || list.first[list.count] + chunks > INT32_MAX) {
       if (list.first[list.count] > 0) {
         if (a->dtype == MDET_F32) launch_grad<float>(*a, f, list, st);

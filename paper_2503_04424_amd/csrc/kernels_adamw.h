@@ -26,7 +26,7 @@ namespace mdet {
 
 constexpr int ADAMW_BLOCK = 256;       // elements that share a scale: one wavefront's, four a lane
 constexpr int ADAMW_THREADS = 256;
-constexpr int ADAMW_CHUNK = 4096;      // elements a workgroup takes
+constexpr int ADAMW_STEP = 1024;       // elements a workgroup takes at a time
 constexpr int ADAMW_TENSORS = 48;      // a launch's, so that they fit the kernel's arguments
 
 struct AdamwFactors {
@@ -38,6 +38,7 @@ struct AdamwFactors {
 
 struct AdamwTensors {
   int count;
+  int chunk;                           // elements a workgroup takes, whole steps
   uint32_t first[ADAMW_TENSORS + 1];   // number of each tensor's first chunk in the launch
   mdet_adamw_tensor t[ADAMW_TENSORS];
 };
@@ -51,14 +52,36 @@ __device__ __forceinline__ uint32_t adamw_bits(const uint32_t key, const int64_t
   return h ^ (h >> 16);
 }
 
-__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
-#pragma unroll
-  for (int d = 32; d > 0; d >>= 1) {
-    const uint32_t o = (uint32_t)__shfl_xor((int)x, d);
-    x = x > o ? x : o;
-  }
-  return x;
+// The largest of the wavefront's, in all lanes: rows of 16 by shifts, then across rows.
+template <int CTRL>
+__device__ __forceinline__ uint32_t dpp_max(const uint32_t x) {
+  const uint32_t o = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)x, CTRL, 0xF, 0xF, false);
+  return x > o ? x : o;
 }
+__device__ __forceinline__ uint32_t wave_max(uint32_t x) {
+  x = dpp_max<0x111>(x);               // row_shr 1, 2, 4, 8
+  x = dpp_max<0x112>(x);
+  x = dpp_max<0x114>(x);
+  x = dpp_max<0x118>(x);
+  x = dpp_max<0x142>(x);               // row_bcast 15, 31
+  x = dpp_max<0x143>(x);
+  return (uint32_t)__builtin_amdgcn_readlane((int)x, 63);
+}
+
+// x / d for a d that a whole block shares, correctly rounded: with y the correctly rounded reciprocal of d and q = x y, the
+// remainder x - q d is exact and q + (x - q d) y rounds to the quotient (Markstein).  Three instructions in place of some
+// ten.  Where d is so small or large that a step could leave the range, it is an ordinary division; a quotient too small
+// for the remainder to be exact is lost beside the random number that is added to it.
+struct BlockDivisor {
+  float d, y;
+  bool quick;
+  __device__ __forceinline__ explicit BlockDivisor(const float by) : d(by), y(1.0f / by), quick(by > 0x1p-60f && by < 0x1p60f) {}
+  __device__ __forceinline__ float operator()(const float x) const {
+    if (!quick) return x / d;
+    const float q = x * y;
+    return __builtin_fmaf(__builtin_fmaf(-q, d, x), y, q);
+  }
+};
 
 // Four elements from `i` on; those at n and beyond are zero.
 template <typename T>
@@ -109,17 +132,16 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwFactors
     else hi = mid;
   }
   const mdet_adamw_tensor t = list.t[lo];
-  const int64_t n = t.n, base = (int64_t)(blockIdx.x - list.first[lo]) * ADAMW_CHUNK;
+  const int64_t n = t.n, base = (int64_t)(blockIdx.x - list.first[lo]) * list.chunk;
   P* const p = (P*)t.p;
   const G* const g = (const G*)t.g;
   const float gs = f.grad_scale ? *f.grad_scale : 1.0f;
   const bool pv = (uintptr_t)p % (4 * sizeof(P)) == 0, gv = (uintptr_t)g % (4 * sizeof(G)) == 0;
-  constexpr int STEP = 4 * ADAMW_THREADS;
-#pragma unroll 2
-  for (int c = 0; c < ADAMW_CHUNK / STEP; ++c) {
-    const int64_t i = base + c * STEP + 4 * (int)threadIdx.x;
+  static_assert(ADAMW_STEP == 4 * ADAMW_THREADS, "four elements a lane");
+  for (int c = 0; c < list.chunk; c += ADAMW_STEP) {
+    const int64_t i = base + c + 4 * (int)threadIdx.x;
     // in whole wavefronts: the lanes of a block find its scale together
-    if (base + c * STEP + 4 * (int)(threadIdx.x & ~63u) >= n) return;
+    if (base + c + 4 * (int)(threadIdx.x & ~63u) >= n) return;
     float pe[4], ge[4], me[4], ve[4];
     adamw_load(pe, p, i, n, pv);
     adamw_load(ge, g, i, n, gv);
@@ -156,14 +178,15 @@ __global__ __launch_bounds__(ADAMW_THREADS) void adamw_kernel(const AdamwFactors
         top2 = top2 > b ? top2 : b;
       }
       const float n1 = __uint_as_float(wave_max(top1)) * (1.0f / 127.0f), n2 = __uint_as_float(wave_max(top2)) * (1.0f / 255.0f);
+      // comparisons that a NaN fails: a block whose scale is zero or not finite has codes of zero
+      const bool ok1 = n1 > 0.0f && n1 < INFINITY, ok2 = n2 > 0.0f && n2 < INFINITY;
+      const BlockDivisor by1(n1), by2(n2);
       const uint32_t key = (uint32_t)(f.first_tensor + lo) * 0xA54FF53Bu + f.seed;
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
         const uint32_t bits = adamw_bits(key, i + e);
-        const float x1 = floorf(me[e] / n1 + (float)(bits & 0xFFFFu) * (1.0f / 65536.0f));
-        const float x2 = floorf(ve[e] / n2 + (float)(bits >> 16) * (1.0f / 65536.0f));
-        // comparisons that a NaN fails: a block whose scale is zero or not finite has codes of zero
-        const bool ok1 = n1 > 0.0f && n1 < INFINITY, ok2 = n2 > 0.0f && n2 < INFINITY;
+        const float x1 = floorf(by1(me[e]) + (float)(bits & 0xFFFFu) * (1.0f / 65536.0f));
+        const float x2 = floorf(by2(ve[e]) + (float)(bits >> 16) * (1.0f / 65536.0f));
         const float least = ve[e] > 0.0f ? 1.0f : 0.0f;
         me[e] = ok1 ? fminf(fmaxf(x1, -127.0f), 127.0f) : 0.0f;
         ve[e] = ok2 ? fminf(fmaxf(x2, least), 255.0f) : 0.0f;
