@@ -109,6 +109,13 @@ __device__ __forceinline__ void gemm_landed() {
   asm volatile("" ::: "memory");
 }
 
+// All of a wavefront's LDS accesses are done, and behind the barrier those of all; loads into registers go on.
+__device__ __forceinline__ void gemm_put_down() {
+  asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+  __builtin_amdgcn_s_barrier();
+  asm volatile("" ::: "memory");
+}
+
 // P: pieces of k that a slab holds; NB: slabs in LDS.
 template <int BM_, int BN_, int WM_, int WN_, int P_, int NB_>
 struct Tile {
@@ -119,7 +126,7 @@ struct Tile {
 };
 
 // Staging of an operand: B rows of it from i0 on.
-template <typename T, int B, int WAVES, int P, bool OUTER, bool DIRECT>
+template <typename T, int B, int WAVES, int P, bool OUTER, bool DIRECT, int HOLD>
 struct Stage {
   typedef typename Core<T>::piece_t piece_t;
   static constexpr int VEC = Core<T>::VEC, BK = P * VEC;
@@ -131,7 +138,7 @@ struct Stage {
   int64_t stride, rows, i0;
   unsigned off[NP];                    // bytes from the slab's first element to the pieces
   bool hangs[NP];                      // k outer, not DIRECT: the piece is not all of the operand's
-  piece_t held[NP];
+  piece_t held[HOLD][NP];
 
   // Order of the blocks of 16 columns of row k.
   static __device__ __forceinline__ int swizzle(const int k) {
@@ -180,8 +187,8 @@ struct Stage {
   __device__ __forceinline__ void direct(const char* const from, const int v, const unsigned at) const {
     gemm_to_lds(from, off[v], at + 16u * (unsigned)(place(v) & ~63));
   }
-  // A whole slab into registers, `from` = base(k).
-  __device__ __forceinline__ void load(const char* const from) {
+  // A whole slab into registers, set `h` of them; `from` = base(k).
+  __device__ __forceinline__ void load(const char* const from, const int h) {
 #pragma unroll
     for (int v = 0; v < NP; ++v) {
       if (OUTER && hangs[v]) {
@@ -192,8 +199,8 @@ struct Stage {
 #pragma unroll
         for (int e = 0; e < VEC; ++e)
           if (i0 + row + e < rows) y[e] = x[e];
-        held[v] = y;
-      } else __builtin_memcpy(&held[v], from + off[v], 16);
+        held[h][v] = y;
+      } else __builtin_memcpy(&held[h][v], from + off[v], 16);
     }
   }
   // The slab from k on into registers; what lies outside of the operand is zero.
@@ -212,12 +219,12 @@ struct Stage {
         for (int e = 0; e < VEC - 1; ++e)
           if (e < left) x[e] = from[e];
       }
-      held[v] = x;
+      held[0][v] = x;
     }
   }
-  __device__ __forceinline__ void put(char* const lds) const {
+  __device__ __forceinline__ void put(char* const lds, const int h) const {
 #pragma unroll
-    for (int v = 0; v < NP; ++v) *reinterpret_cast<piece_t*>(lds + 16 * place(v)) = held[v];
+    for (int v = 0; v < NP; ++v) *reinterpret_cast<piece_t*>(lds + 16 * place(v)) = held[h][v];
   }
   // Rows 16 t + lane % 16, piece 4 h + lane / 16: what the lane supplies to a product.
   static __device__ __forceinline__ piece_t fragment(const char* const lds, const int t, const int h) {
@@ -251,8 +258,10 @@ struct Stage {
 // multiplied and past the end of its product.  `lds`: NB * SLAB bytes.
 template <typename T, typename S, bool ROUTER, bool COUTER, bool DIRECT>
 struct TileStream {
-  typedef Stage<T, S::BM, S::WAVES, S::P, ROUTER, DIRECT> RS;
-  typedef Stage<T, S::BN, S::WAVES, S::P, COUTER, DIRECT> CS;
+  // slabs in registers: as many as small tiles, which wait for memory, have room for
+  static constexpr int HOLD = DIRECT ? 1 : S::BM <= 32 ? 4 : S::BM <= 64 && sizeof(T) < 8 ? 3 : 1;
+  typedef Stage<T, S::BM, S::WAVES, S::P, ROUTER, DIRECT, HOLD> RS;
+  typedef Stage<T, S::BN, S::WAVES, S::P, COUTER, DIRECT, HOLD> CS;
   typedef typename Core<T>::piece_t piece_t;
   static constexpr int BK = RS::BK, LOADS = RS::NP + CS::NP;   // loads of a wavefront for a slab
   RS rs;
@@ -293,14 +302,14 @@ struct TileStream {
         for (int v = 0; v < RS::NP; ++v) rs.direct(rs.base(k), v, place);
       } else {
         rs.load(k, kend);
-        rs.put(slab);
+        rs.put(slab, 0);
       }
       if (ccomes) {
 #pragma unroll
         for (int v = 0; v < CS::NP; ++v) cs.direct(cs.base(k), v, place + 16 * S::P * S::BM);
       } else {
         cs.load(k, kend);
-        cs.put(slab + 16 * S::P * S::BM);
+        cs.put(slab + 16 * S::P * S::BM, 0);
       }
       // run() counts loads straight to LDS: where some are missing, none is left to be counted
       if (!(rcomes && ccomes)) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -317,8 +326,8 @@ struct TileStream {
   __device__ __forceinline__ void put() {
     if (!DIRECT && held) {
       char* const slab = lds + (to == 0 ? S::NB - 1 : to - 1) * S::SLAB;
-      rs.put(slab);
-      cs.put(slab + 16 * S::P * S::BM);
+      rs.put(slab, 0);
+      cs.put(slab + 16 * S::P * S::BM, 0);
       held = false;
     }
   }
@@ -360,40 +369,61 @@ struct TileStream {
         const char *rfrom = rs.base(k), *cfrom = cs.base(k);
         const int64_t rstep = rs.base(k + BK) - rfrom, cstep = cs.base(k + BK) - cfrom;
         k += (int64_t)steady * BK;
-        for (; steady > 0; --steady) {
-          gemm_landed<DIRECT ? (S::NB - 2) * LOADS : 0>();
-          const unsigned place = lds0 + to * S::SLAB;
-          // The loads of a later slab: all in front of this one's products where both operands are read in 128-byte pieces
-          // of rows in 16 bits (8192 x 16384 x 4096 1257 TFLOP/s, spread 1176), which wait longest; one behind each strip of
-          // products otherwise (k outer 4096 x 4096 x 8192 1384, in front 1324; fp32 4096^3 142, 139).
-          constexpr bool FIRST = sizeof(T) == 2 && !ROUTER && !COUTER;
-          constexpr int Q = S::TM * S::P / 4, EACH = (LOADS + Q - 1) / Q;
-          auto pieces = [&](const int from, const int end) {
-#pragma unroll
-            for (int v = from; v < end; ++v) {
-              if (v >= LOADS) break;
-              if (v < RS::NP) rs.direct(rfrom, v, place);
-              else cs.direct(cfrom, v - RS::NP, place + 16 * S::P * S::BM);
-            }
-          };
-          if constexpr (!DIRECT) {
-            rs.load(rfrom);
-            cs.load(cfrom);
-          } else if constexpr (FIRST) pieces(0, LOADS);
-          multiply(lds + at * S::SLAB, [&](const int q) {
-            if constexpr (DIRECT && !FIRST) {
-              pieces(q * EACH, (q + 1) * EACH);
-              __builtin_amdgcn_sched_barrier(0x107);
-            }
-          });
-          if constexpr (!DIRECT) {
-            rs.put(lds + to * S::SLAB);
-            cs.put(lds + to * S::SLAB + 16 * S::P * S::BM);
-          }
-          rfrom += rstep;
-          cfrom += cstep;
+        auto onward = [&] {
           to = to + 1 == S::NB ? 0 : to + 1;
           at = at + 1 == S::NB ? 0 : at + 1;
+        };
+        if constexpr (DIRECT) {
+          for (; steady > 0; --steady) {
+            gemm_landed<(S::NB - 2) * LOADS>();
+            const unsigned place = lds0 + to * S::SLAB;
+            // The loads of a later slab: all in front of this one's products where both operands are read in 128-byte pieces
+            // of rows in 16 bits (8192 x 16384 x 4096 1257 TFLOP/s, spread 1176), which wait longest; one behind each strip of
+            // products otherwise (k outer 4096 x 4096 x 8192 1384, in front 1324; fp32 4096^3 142, 139).
+            constexpr bool FIRST = sizeof(T) == 2 && !ROUTER && !COUTER;
+            constexpr int Q = S::TM * S::P / 4, EACH = (LOADS + Q - 1) / Q;
+            auto pieces = [&](const int from, const int end) {
+#pragma unroll
+              for (int v = from; v < end; ++v) {
+                if (v >= LOADS) break;
+                if (v < RS::NP) rs.direct(rfrom, v, place);
+                else cs.direct(cfrom, v - RS::NP, place + 16 * S::P * S::BM);
+              }
+            };
+            if constexpr (FIRST) pieces(0, LOADS);
+            multiply(lds + at * S::SLAB, [&](const int q) {
+              if constexpr (!FIRST) {
+                pieces(q * EACH, (q + 1) * EACH);
+                __builtin_amdgcn_sched_barrier(0x107);
+              }
+            });
+            rfrom += rstep;
+            cfrom += cstep;
+            onward();
+          }
+        } else {
+          // HOLD slabs are in registers or on their way there: one is put into LDS behind each slab that is multiplied.
+          auto load = [&](const int h) {
+            rs.load(rfrom, h);
+            cs.load(cfrom, h);
+            rfrom += rstep;
+            cfrom += cstep;
+          };
+#pragma unroll
+          for (int h = 0; h < HOLD - 1; ++h)
+            if (h < steady) load(h);
+          for (int s = 0; s < steady; s += HOLD) {
+#pragma unroll
+            for (int h = 0; h < HOLD; ++h) {
+              if (s + h >= steady) break;
+              gemm_put_down();
+              if (s + h + HOLD - 1 < steady) load((h + HOLD - 1) % HOLD);
+              multiply(lds + at * S::SLAB, [](int) {});
+              rs.put(lds + to * S::SLAB, h);
+              cs.put(lds + to * S::SLAB + 16 * S::P * S::BM, h);
+              onward();
+            }
+          }
         }
       }
     }

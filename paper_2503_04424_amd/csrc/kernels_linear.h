@@ -282,33 +282,70 @@ __global__ __launch_bounds__(64 * WAVES) void linear_rows_kernel(const Operand<T
   }
 }
 
-// dz = dy act'(z) and the column sums of DZ_ROWS rows of it: a workgroup takes 64 columns, thread (t, c) every fourth row of
-// column c.
-constexpr int DZ_COLS = 64, DZ_ROWS = 64;
+// dz = dy act'(z) and the column sums of DZ_ROWS rows of it.  A workgroup takes 16 pieces of 16 bytes across; thread (t, c)
+// every sixteenth row of piece c, all of its loads at once.  Bytes bound it.
+constexpr int DZ_ROWS = 64, DZ_PIECES = 16;
 
 template <typename T>
 __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dy, const int64_t lddy, const T* __restrict__ z,
                                                         const int64_t ldz, T* __restrict__ dz, const int64_t lddz,
                                                         float* __restrict__ sums, const int64_t rows, const int64_t cols, const int act) {
-  __shared__ float part[4][DZ_COLS];
-  const int64_t across = (cols + DZ_COLS - 1) / DZ_COLS;
-  const int64_t strip = blockIdx.x / across, col = blockIdx.x % across * DZ_COLS + (threadIdx.x & 63);
-  const int t = threadIdx.x >> 6;
-  float sum = 0.0f;
-  if (col < cols) {
-    act_switch(act, [&](auto a) {
-      for (int64_t i = strip * DZ_ROWS + t; i < rows && i < (strip + 1) * DZ_ROWS; i += 4) {
-        float v = (float)dy[i * lddy + col];
-        if constexpr (decltype(a)::value != MDET_ACT_NONE) v *= act_slope<decltype(a)::value>((float)z[i * ldz + col]);
-        if (dz) dz[i * lddz + col] = (T)v;
-        sum += v;
+  typedef typename Core<T>::piece_t piece_t;
+  constexpr int VEC = Core<T>::VEC, EACH = DZ_ROWS / 16;
+  __shared__ float part[16][DZ_PIECES * VEC];
+  const int64_t across = (cols + DZ_PIECES * VEC - 1) / (DZ_PIECES * VEC);
+  const int t = threadIdx.x / DZ_PIECES, c = threadIdx.x % DZ_PIECES * VEC;
+  const int64_t strip = blockIdx.x / across, col0 = blockIdx.x % across * (DZ_PIECES * VEC), col = col0 + c, row = strip * DZ_ROWS + t;
+  const bool whole = col + VEC <= cols;
+  auto get = [&](const T* const p, const int64_t ld, const int64_t i) {
+    piece_t x = {};
+    if (i >= rows) return x;
+    if (whole) __builtin_memcpy(&x, p + i * ld + col, 16);
+    else
+#pragma unroll
+      for (int e = 0; e < VEC; ++e)
+        if (col + e < cols) x[e] = p[i * ld + col + e];
+    return x;
+  };
+  piece_t y[EACH], a[EACH];
+#pragma unroll
+  for (int r = 0; r < EACH; ++r) y[r] = get(dy, lddy, row + 16 * r);
+  if (act != MDET_ACT_NONE)
+#pragma unroll
+    for (int r = 0; r < EACH; ++r) a[r] = get(z, ldz, row + 16 * r);
+  float sum[VEC] = {};
+  act_switch(act, [&](auto which) {
+    constexpr int ACT = decltype(which)::value;
+#pragma unroll
+    for (int r = 0; r < EACH; ++r) {
+      piece_t d;
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        float v = (float)y[r][e];
+        if constexpr (ACT != MDET_ACT_NONE) v *= act_slope<ACT>((float)a[r][e]);
+        if (row + 16 * r < rows) sum[e] += v;
+        d[e] = (T)v;
       }
-    });
-  }
-  part[t][threadIdx.x & 63] = sum;
+      T* const to = dz + (row + 16 * r) * lddz + col;
+      if (dz && row + 16 * r < rows) {
+        if (whole) __builtin_memcpy(to, &d, 16);
+        else
+#pragma unroll
+          for (int e = 0; e < VEC; ++e)
+            if (col + e < cols) to[e] = d[e];
+      }
+    }
+  });
+  if (!sums) return;
+#pragma unroll
+  for (int e = 0; e < VEC; ++e) part[t][c + e] = sum[e];
   __syncthreads();
-  if (sums && t == 0 && col < cols)
-    sums[strip * cols + col] = (part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]);
+  if (threadIdx.x < DZ_PIECES * VEC && col0 + threadIdx.x < cols) {
+    float v = part[0][threadIdx.x];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) v += part[r][threadIdx.x];
+    sums[strip * cols + col0 + threadIdx.x] = v;
+  }
 }
 
 // db = sum of the strips' sums, four threads a column, in one order.

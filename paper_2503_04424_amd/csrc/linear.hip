@@ -158,7 +158,7 @@ int backward(const Grad& g) {
   const int64_t lddz = g.dz ? g.lddz : lay.lddz;
   float* const sums = g.db ? (float*)(g.workspace + lay.sums) : nullptr;
   if ((dz || sums) && g.m > 0 && g.n > 0) {
-    const int64_t blocks = lay.strips * ceil_div(g.n, DZ_COLS);
+    const int64_t blocks = lay.strips * ceil_div(g.n, DZ_PIECES * Core<T>::VEC);
     if (blocks > INT32_MAX) return MDET_EINVAL;
     hipLaunchKernelGGL((linear_dz_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, g.st, (const T*)g.dy, g.lddy, (const T*)g.z, g.ldz,
                        dz, lddz, sums, g.m, g.n, g.act);
