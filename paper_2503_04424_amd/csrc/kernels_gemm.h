@@ -137,7 +137,6 @@ struct Stage {
   const T* p;
   int64_t stride, rows, i0;
   unsigned off[NP];                    // bytes from the slab's first element to the pieces
-  bool hangs[NP];                      // k outer, not DIRECT: the piece is not all of the operand's
   piece_t held[HOLD][NP];
 
   // Order of the blocks of 16 columns of row k.
@@ -174,12 +173,14 @@ struct Stage {
       int row, k;
       piece_at(place(v), row, k);
       // rows behind the last are not stored: any memory of the operand will do for them
-      const int64_t last = OUTER ? rows - VEC : rows - 1;
-      hangs[v] = OUTER && !DIRECT && i0 + row > last;
-      const int64_t i = i0 + row > last && !hangs[v] ? last - i0 : row;
+      const int64_t last = OUTER ? (rows - 1) / VEC * VEC : rows - 1;
+      const int64_t i = i0 + row > last ? last - i0 : row;
       off[v] = (unsigned)((OUTER ? k * stride + i : i * stride + k) * (int64_t)sizeof(T));
     }
   }
+  // Pieces of rows k < end - spare() are whole in memory: with k outer the last piece of a row k may reach into the rows
+  // behind it, and those behind the last one are not the operand's.
+  __device__ __forceinline__ int spare() const { return OUTER && rows % VEC ? VEC : 0; }
   __device__ __forceinline__ const char* base(const int64_t k) const {
     return reinterpret_cast<const char*>(OUTER ? p + k * stride + i0 : p + i0 * stride + k);
   }
@@ -190,18 +191,7 @@ struct Stage {
   // A whole slab into registers, set `h` of them; `from` = base(k).
   __device__ __forceinline__ void load(const char* const from, const int h) {
 #pragma unroll
-    for (int v = 0; v < NP; ++v) {
-      if (OUTER && hangs[v]) {
-        int row, k;
-        piece_at(place(v), row, k);
-        const T* const x = reinterpret_cast<const T*>(from + off[v]);
-        piece_t y = {};
-#pragma unroll
-        for (int e = 0; e < VEC; ++e)
-          if (i0 + row + e < rows) y[e] = x[e];
-        held[h][v] = y;
-      } else __builtin_memcpy(&held[h][v], from + off[v], 16);
-    }
+    for (int v = 0; v < NP; ++v) __builtin_memcpy(&held[h][v], from + off[v], 16);
   }
   // The slab from k on into registers; what lies outside of the operand is zero.
   __device__ __forceinline__ void load(const int64_t k0, const int64_t kend) {
@@ -295,7 +285,7 @@ struct TileStream {
       if (!next()) return;
     char* const slab = lds + to * S::SLAB;
     if constexpr (DIRECT) {
-      const bool whole = k + BK <= kend, rcomes = whole && rquick, ccomes = whole && cquick;
+      const bool rcomes = rquick && k + BK + rs.spare() <= kend, ccomes = cquick && k + BK + cs.spare() <= kend;
       const unsigned place = lds0 + to * S::SLAB;
       if (rcomes) {
 #pragma unroll
@@ -362,7 +352,8 @@ struct TileStream {
     int left = count;
     {
       // The long stretch, without a branch: every slab brought meanwhile is a whole one of this product.
-      const int64_t whole = rquick && cquick && k < kend ? (kend - k) / BK : 0;
+      const int64_t last = kend - (rs.spare() > cs.spare() ? rs.spare() : cs.spare());
+      const int64_t whole = rquick && cquick && k < last ? (last - k) / BK : 0;
       int steady = __builtin_amdgcn_readfirstlane(whole < left - ahead ? (int)whole : left - ahead);
       if (ahead == (DIRECT ? S::NB - 1 : 1) && steady > 0) {
         left -= steady;
@@ -454,12 +445,12 @@ __device__ __forceinline__ void tile_each(F&& f) {
 }
 
 // An operand with what is to be known of its place: offsets within a slab of B rows in 32 bits; pieces that can go straight to
-// LDS, with rows on 16 bytes (with k outer their number a whole number of pieces).
+// LDS, with rows on 16 bytes.
 template <typename T, bool OUTER, int B>
 Operand<T> gemm_operand(const void* p, const int64_t stride, const int64_t rows, const int64_t k) {
   const int64_t bytes = stride * (int64_t)sizeof(T), lines = OUTER ? k : rows;
   const bool near = bytes < (int64_t(1) << 31) / (B > 64 ? B : 64);
-  const bool straight = near && (uintptr_t)p % 16 == 0 && (lines == 1 || bytes % 16 == 0) && (!OUTER || rows % Core<T>::VEC == 0);
+  const bool straight = near && (uintptr_t)p % 16 == 0 && (lines == 1 || bytes % 16 == 0);
   return Operand<T>{(const T*)p, stride, rows, near, straight};
 }
 

@@ -38,8 +38,8 @@ bool four(const void* p, int64_t ld, int64_t rows) {
 
 typedef Tile<256, 256, 2, 4, 8, 2> Big;
 typedef Tile<128, 128, 2, 2, 8, 2> Mid;
-template <typename T>
-using Small = Tile<64, 64, 2, 2, 8, sizeof(T) == 2 ? 4 : 2>;
+typedef Tile<64, 64, 2, 2, 8, 2> Small;
+typedef Tile<64, 64, 2, 2, 8, 4> Ahead;
 typedef Tile<32, 32, 2, 2, 8, 4> Tiny;
 
 // Few rows: W is read once.  Beyond 8192 rows of W a split sum over tiles is as fast for one row (16384 x 4096 bf16 22.3 us,
@@ -64,7 +64,10 @@ Cut cut_of(int64_t rows, int64_t cols, int64_t k, int64_t size, bool inner) {
   if (inner && few_rows(rows, cols)) return Cut{0, 1, k};
   const int64_t bk = 128 / size;
   auto tiles = [&](int64_t b) { return ceil_div(rows, b) * ceil_div(cols, b); };
-  c.tile = size == 2 && tiles(256) >= 192 ? 256 : tiles(128) >= 192 ? 128 : tiles(64) >= 256 ? 64 : 32;
+  // The largest tile with which the device is full.  In 16 bits larger tiles also need less of LDS and cache for a product
+  // (2500^3, 400 tiles of 128: 59 us, 80 with 64; 2048^3, 256 of them: 28 and 27, k outer 34 and 29); in fp32 the matrix
+  // cores are slow enough for the small tile, whose workgroups even out (2500^3 303 and 266 us, 4096^3 962 us with 128).
+  c.tile = size == 2 && tiles(256) >= 192 ? 256 : tiles(128) > (size == 2 ? 256 : 800) ? 128 : tiles(64) >= 256 ? 64 : 32;
   c.splits = 1;
   c.kpart = k;
   const int64_t t = tiles(c.tile);
@@ -97,12 +100,12 @@ void tiles(Operand<T> r, Operand<T> c, int64_t k, const LinearOut<T, O>& out, co
   if (cut.splits > 1) {
     if constexpr (S::BM <= 64) {
       if (direct) go(true_type{}, true_type{});
-      else go(false_type{}, true_type{});
+      else if constexpr (!std::is_same<S, Ahead>::value) go(false_type{}, true_type{});
       const int64_t groups = ceil_div(out.rows * ceil_div(out.cols, 4), 256);
       hipLaunchKernelGGL((linear_join_kernel<T, O>), dim3((unsigned)groups), dim3(256), 0, st, (const float*)parts, cut.splits, out);
     }
   } else if (direct) go(true_type{}, false_type{});
-  else go(false_type{}, false_type{});
+  else if constexpr (!std::is_same<S, Ahead>::value) go(false_type{}, false_type{});
 }
 
 template <typename T, typename O, bool ROUTER, bool COUTER>
@@ -116,7 +119,15 @@ int product(Operand<T> r, Operand<T> c, int64_t k, LinearOut<T, O> out, float* p
   } else if (cut.tile == 256) {
     if constexpr (sizeof(T) == 2) tiles<T, O, Big, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
   } else if (cut.tile == 128) tiles<T, O, Mid, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
-  else if (cut.tile == 64) tiles<T, O, Small<T>, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
+  else if (cut.tile == 64) {
+    // three slabs on their way in 16 bits, where they last shortest, as long as all of the workgroups have room for them
+    // at once (512 x 4096 x 4096 33 us with one, 28.5 with three)
+    const int64_t n = ceil_div(out.rows, 64) * ceil_div(out.cols, 64) * cut.splits;
+    const bool straight = gemm_operand<T, ROUTER, 64>(r.p, r.stride, r.rows, k).straight && gemm_operand<T, COUTER, 64>(c.p, c.stride, c.rows, k).straight;
+    if (sizeof(T) == 2 && n <= 512 && straight) {
+      if constexpr (sizeof(T) == 2) tiles<T, O, Ahead, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
+    } else tiles<T, O, Small, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
+  }
   else tiles<T, O, Tiny, ROUTER, COUTER>(r, c, k, out, cut, parts, st);
   return launch_status();
 }
