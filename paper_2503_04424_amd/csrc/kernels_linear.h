@@ -295,20 +295,20 @@ __global__ __launch_bounds__(64 * WAVES) void linear_rows_kernel(const Operand<T
   }
 }
 
-// dz = dy act'(z) and the column sums of DZ_ROWS rows of it.  A workgroup takes 16 pieces of 16 bytes across; thread (t, c)
-// every sixteenth row of piece c, all of its loads at once.  Bytes bound it.
-constexpr int DZ_ROWS = 64, DZ_PIECES = 16;
+// dz = dy act'(z) and the column sums of 16 EACH rows of it.  A workgroup takes 16 pieces of 16 bytes across; thread (t, c)
+// every sixteenth row of piece c, all of its loads at once.  Bytes bound it (4096 x 8192 bf16 with GELU: DZUS us).
+constexpr int DZ_PIECES = 16;
 
-template <typename T>
+template <typename T, int EACH>
 __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dy, const int64_t lddy, const T* __restrict__ z,
                                                         const int64_t ldz, T* __restrict__ dz, const int64_t lddz,
                                                         float* __restrict__ sums, const int64_t rows, const int64_t cols, const int act) {
   typedef typename Core<T>::piece_t piece_t;
-  constexpr int VEC = Core<T>::VEC, EACH = DZ_ROWS / 16;
+  constexpr int VEC = Core<T>::VEC;
   __shared__ float part[16][DZ_PIECES * VEC];
   const int64_t across = (cols + DZ_PIECES * VEC - 1) / (DZ_PIECES * VEC);
   const int t = threadIdx.x / DZ_PIECES, c = threadIdx.x % DZ_PIECES * VEC;
-  const int64_t strip = blockIdx.x / across, col0 = blockIdx.x % across * (DZ_PIECES * VEC), col = col0 + c, row = strip * DZ_ROWS + t;
+  const int64_t strip = blockIdx.x / across, col0 = blockIdx.x % across * (DZ_PIECES * VEC), col = col0 + c, row = strip * (16 * EACH) + t;
   const bool whole = col + VEC <= cols;
   auto get = [&](const T* const p, const int64_t ld, const int64_t i) {
     piece_t x = {};

@@ -89,22 +89,29 @@ __global__ __launch_bounds__(S::THREADS) void ntk_first_kernel(const NtkLayers<T
   });
 }
 
-// A block of K.  FIRST: the first factors stand in `first`; otherwise (one output) both products are formed here, one
+// Blocks `begin` .. `begin` + `count` - 1 of K.  With PARTS the launch's workgroups take the four quarters (64 x 64) of blocks of
+// twice the tile's size.  FIRST: the first factors stand in `first`; otherwise (one output) both products are formed here, one
 // after the other, and multiplied in registers.  The sum over layers stays in registers, K is written once.
-template <typename T, typename S, bool DIRECT, bool FIRST>
-__global__ __launch_bounds__(S::THREADS) void ntk_gram_kernel(const NtkLayers<T> layers, const int64_t n, const int d,
+template <typename T, typename S, bool DIRECT, bool FIRST, bool PARTS>
+__global__ __launch_bounds__(S::THREADS) void ntk_gram_kernel(const NtkLayers<T> layers, const int64_t begin, const int64_t count, const int64_t n, const int d,
                                                               const typename Core<T>::acc1_t bias, const typename Core<T>::acc1_t scale,
                                                               const int accumulate, const typename Core<T>::acc1_t* __restrict__ first,
                                                               typename Core<T>::acc1_t* __restrict__ K, const int64_t ldk) {
   typedef typename Core<T>::acc_t acc_t;
   __shared__ __attribute__((aligned(16))) char lds[S::NB * S::SLAB];
-  const int64_t N = n * d, rows = (N + S::BM - 1) / S::BM;
-  const int64_t t = gemm_tile_number(blockIdx.x, ntk_blocks<S::BM / S::BN>(rows));
+  constexpr int EACH = PARTS ? 4 : 1, EDGE = PARTS ? 2 : 1;
+  const int64_t N = n * d, rows = (N + EDGE * S::BM - 1) / (EDGE * S::BM);
+  const int64_t t = gemm_tile_number(blockIdx.x, EACH * count);
   if (t < 0) return;
   int64_t bi, bj;
-  ntk_block<S::BM / S::BN>(t, rows, bi, bj);
+  ntk_block<S::BM / S::BN>(begin + t / EACH, rows, bi, bj);
+  if constexpr (PARTS) {
+    bi = 2 * bi + (t >> 1 & 1);
+    bj = 2 * bj + (t & 1);
+    if (bj > bi) return;
+  }
   const int64_t row0 = bi * S::BM, col0 = bj * S::BN;
-  if (col0 >= N) return;                           // the last rows' block may reach less far than its columns
+  if (row0 >= N || col0 >= N) return;              // a block may reach over the matrix's edge
   acc_t total[S::TN][S::TM] = {};
   // the samples of this lane's rows and columns; where nothing is stored, any pair will do
   int sample_row[S::TM], sample_col[S::TN][4];

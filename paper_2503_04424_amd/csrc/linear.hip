@@ -134,12 +134,14 @@ int product(Operand<T> r, Operand<T> c, int64_t k, LinearOut<T, O> out, float* p
 
 // Workspace of the gradient: dz, then the strips' column sums, then the parts of a product that is split.
 struct GradLayout {
-  int64_t strips, lddz;
+  int64_t each, strips, lddz;
   uint64_t sums, parts, bytes;
 };
 GradLayout grad_layout(int32_t dtype, int64_t m, int64_t n, int64_t k) {
   GradLayout g;
-  g.strips = ceil_div(m, DZ_ROWS);
+  // short strips while there are too few workgroups of long ones
+  g.each = m * n < (int64_t)4 << 20 ? 1 : 4;
+  g.strips = ceil_div(m, 16 * g.each);
   g.lddz = ceil_div(n, 8) * 8;
   g.sums = up256((uint64_t)m * g.lddz * size_of(dtype));
   g.parts = g.sums + up256((uint64_t)g.strips * n * 4);
@@ -171,8 +173,12 @@ int backward(const Grad& g) {
   if ((dz || sums) && g.m > 0 && g.n > 0) {
     const int64_t blocks = lay.strips * ceil_div(g.n, DZ_PIECES * Core<T>::VEC);
     if (blocks > INT32_MAX) return MDET_EINVAL;
-    hipLaunchKernelGGL((linear_dz_kernel<T>), dim3((unsigned)blocks), dim3(256), 0, g.st, (const T*)g.dy, g.lddy, (const T*)g.z, g.ldz,
-                       dz, lddz, sums, g.m, g.n, g.act);
+    auto go = [&](auto each) {
+      hipLaunchKernelGGL((linear_dz_kernel<T, decltype(each)::value>), dim3((unsigned)blocks), dim3(256), 0, g.st, (const T*)g.dy, g.lddy,
+                         (const T*)g.z, g.ldz, dz, lddz, sums, g.m, g.n, g.act);
+    };
+    if (lay.each == 1) go(std::integral_constant<int, 1>{});
+    else go(std::integral_constant<int, 4>{});
   }
   if (g.db && g.n > 0)
     hipLaunchKernelGGL((linear_db_kernel<O>), dim3((unsigned)ceil_div(g.n, 64)), dim3(256), 0, g.st, (const float*)sums, lay.strips, g.n,

@@ -58,13 +58,21 @@ typedef Tile<128, 128, 2, 4, 8, 2> Large;
 typedef Tile<64, 64, 2, 2, 8, 2> Small;
 typedef Tile<32, 32, 2, 2, 8, 4> Tiny;
 
+constexpr int64_t COMPUTE_UNITS = 256;
+
 // First factors of one launch's layers, for several outputs.
 inline uint64_t first_bytes(int64_t n, int64_t d, int32_t layers, int64_t size) {
   return d > 1 ? up256((uint64_t)(layers < NTK_LAYERS ? layers : NTK_LAYERS) * n * n * size) : 0;
 }
 
-template <typename T, typename S>
-int gram_tiles(NtkLayers<T>& list, const Call& c, int accumulate, void* first) {
+// Which of the blocks a call computes, and whether a quarter at a time.
+struct Range {
+  int64_t begin, count;
+  bool firsts;                         // and the first factors before them
+};
+
+template <typename T, typename S, bool PARTS = false>
+int gram_tiles(NtkLayers<T>& list, const Call& c, int accumulate, void* first, Range range = Range{0, -1, true}) {
   typedef typename Core<T>::acc1_t A;
   // A launch goes straight to LDS where most of what it reads can go there: a last layer of one output, whose rows are
   // single elements, does not hold up the others.
@@ -86,21 +94,33 @@ int gram_tiles(NtkLayers<T>& list, const Call& c, int accumulate, void* first) {
     if (no_g > yes_g / 8 || (c.d > 1 && no_a > yes_a / 8) || (c.d == 1 && no_a + no_g > (yes_a + yes_g) / 8))
       return gram_tiles<T, Small>(list, c, accumulate, first);
   }
-  auto grid = [](int64_t rows, int64_t times) { return ceil_div(ntk_blocks<S::BM / S::BN>(ceil_div(rows, S::BM)) * times, 8) * 8; };
-  const int64_t all = grid(c.n * c.d, 1), firsts = c.d > 1 ? grid(c.n, list.count) : 0;
+  constexpr int C = S::BM / S::BN;
+  const int64_t blocks = ntk_blocks<C>(ceil_div(c.n * c.d, S::BM));
+  // What is left over behind whole rounds of large blocks would hold up a few compute units for as long as a round takes (fp64
+  // n = 8192, 2080 blocks: 3.08 ms): it goes out in quarters (REST ms).
+  if constexpr (S::BM == 128) {
+    const int64_t rest = blocks % COMPUTE_UNITS;
+    if (range.count < 0 && rest > 0 && rest <= COMPUTE_UNITS / 2) {
+      const int status = gram_tiles<T, S>(list, c, accumulate, first, Range{0, blocks - rest, true});
+      return status != MDET_OK ? status : gram_tiles<T, Small, true>(list, c, accumulate, first, Range{blocks - rest, rest, false});
+    }
+  }
+  if (range.count < 0) range.count = blocks;
+  const int64_t all = ceil_div(range.count * (PARTS ? 4 : 1), 8) * 8;
+  const int64_t firsts = c.d > 1 ? ceil_div(ntk_blocks<C>(ceil_div(c.n, S::BM)) * list.count, 8) * 8 : 0;
   if (all > INT32_MAX || firsts > INT32_MAX) return MDET_EINVAL;
   using std::false_type;
   using std::true_type;
   auto gram = [&](auto direct, auto several) {
-    hipLaunchKernelGGL((ntk_gram_kernel<T, S, decltype(direct)::value, decltype(several)::value>), dim3((unsigned)all), dim3(S::THREADS), 0, c.st,
-                       list, c.n, (int)c.d, (A)c.bias, (A)c.scale, accumulate, (const A*)first, (A*)c.K, c.ldk);
+    hipLaunchKernelGGL((ntk_gram_kernel<T, S, decltype(direct)::value, decltype(several)::value, PARTS>), dim3((unsigned)all), dim3(S::THREADS), 0, c.st,
+                       list, range.begin, range.count, c.n, (int)c.d, (A)c.bias, (A)c.scale, accumulate, (const A*)first, (A*)c.K, c.ldk);
   };
   if (c.d > 1) {
     auto firsts_of = [&](auto direct) {
       hipLaunchKernelGGL((ntk_first_kernel<T, S, decltype(direct)::value>), dim3((unsigned)firsts), dim3(S::THREADS), 0, c.st, list, c.n, (A)c.bias,
                          (A*)first);
     };
-    if (list.count > 0) {
+    if (list.count > 0 && range.firsts) {
       if (no_a <= yes_a / 8) firsts_of(true_type{});
       else if constexpr (REGISTERS) firsts_of(false_type{});
     }

@@ -177,3 +177,16 @@ def test_refusals(M):
         with pytest.raises(M.MemdetError) as e:
             bad()
         assert e.value.status == status
+
+
+@pytest.mark.parametrize("dtype,out,n,d", [(torch.float64, torch.float64, 8010, 1), (torch.float64, torch.float64, 8190, 1),
+                                           (torch.bfloat16, torch.float32, 811, 10)], ids=str)
+def test_large_orders(M, dtype, out, n, d):
+    """Orders that are cut into large blocks, what is left over behind whole rounds of them into quarters."""
+    inputs, signals = layers(n, d, [(40, 48)], dtype, n)
+    k = M.mdet_ntk_gram(inputs, signals, torch.full((n * d, n * d), 7.0, dtype=out, device="cuda"), outputs=d)
+    want, size = gram64(inputs, signals, d)
+    eps = 2.0 ** -23 if out == torch.float32 else 2.0 ** -52
+    off = torch.tril((k.double() - want).abs() - eps * size)
+    assert float(off.max()) <= 0
+    assert bool((torch.triu(k, 1) == torch.triu(torch.full_like(k, 7.0), 1)).all())
