@@ -153,15 +153,12 @@ struct LinearLds {
   static constexpr int BYTES = S::WAVES * WAVE_BYTES > S::NB * S::SLAB ? S::WAVES * WAVE_BYTES : S::NB * S::SLAB;
 };
 
-// A tile of the layer.  SPLIT: part blockIdx / tiles of the sum over k, kept in fp32 for linear_join_kernel.
+// Tile number t of the layer.  SPLIT: part t / tiles of the sum over k, kept in fp32 for linear_join_kernel.
 template <typename T, typename O, typename S, bool ROUTER, bool COUTER, bool DIRECT, bool SPLIT>
-__global__ __launch_bounds__(S::THREADS) void linear_tile_kernel(const Operand<T> r, const Operand<T> c, const int64_t k, const LinearOut<T, O> out,
-                                                                 float* const parts, const int splits, const int64_t kpart) {
+__device__ __forceinline__ void linear_tile(const int64_t t, char* const lds, const Operand<T>& r, const Operand<T>& c, const int64_t k,
+                                            const LinearOut<T, O>& out, float* const parts, const int64_t kpart) {
   typedef LinearLds<S> L;
-  __shared__ __attribute__((aligned(16))) char lds[L::BYTES];
   const int64_t down = (out.rows + S::BM - 1) / S::BM, across = (out.cols + S::BN - 1) / S::BN, tiles = down * across;
-  const int64_t t = gemm_tile_number(blockIdx.x, tiles * splits);
-  if (t < 0) return;
   int64_t bi, bj;
   gemm_tile_place(t % tiles, down, across, bi, bj);
   const int64_t part = t / tiles, k0 = part * kpart, kend = k0 + kpart < k ? k0 + kpart : k;
@@ -215,6 +212,27 @@ __global__ __launch_bounds__(S::THREADS) void linear_tile_kernel(const Operand<T
     __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
     __builtin_amdgcn_wave_barrier();
   }
+}
+
+template <typename T, typename O, typename S, bool ROUTER, bool COUTER, bool DIRECT, bool SPLIT>
+__global__ __launch_bounds__(S::THREADS) void linear_tile_kernel(const Operand<T> r, const Operand<T> c, const int64_t k, const LinearOut<T, O> out,
+                                                                 const int64_t tiles, float* const parts, const int64_t kpart) {
+  __shared__ __attribute__((aligned(16))) char lds[LinearLds<S>::BYTES];
+  const int64_t t = gemm_tile_number(blockIdx.x, tiles);
+  if (t >= 0) linear_tile<T, O, S, ROUTER, COUTER, DIRECT, SPLIT>(t, lds, r, c, k, out, parts, kpart);
+}
+
+// Both products of a small layer's gradient in one launch, which fills the device where neither would: dx = dz W by the
+// first tiles, dW = dz^T x by the others.
+template <typename T, typename O, typename S, bool DIRECT>
+__global__ __launch_bounds__(S::THREADS) void linear_pair_kernel(const Operand<T> dzr, const Operand<T> w, const int64_t n, const LinearOut<T, T> dx,
+                                                                 const Operand<T> dzc, const Operand<T> x, const int64_t m, const LinearOut<T, O> dw,
+                                                                 const int64_t first, const int64_t tiles) {
+  __shared__ __attribute__((aligned(16))) char lds[LinearLds<S>::BYTES];
+  const int64_t t = gemm_tile_number(blockIdx.x, tiles);
+  if (t < 0) return;
+  if (t < first) linear_tile<T, T, S, false, true, DIRECT, false>(t, lds, dzr, w, n, dx, nullptr, n);
+  else linear_tile<T, O, S, true, true, DIRECT, false>(t - first, lds, dzc, x, m, dw, nullptr, m);
 }
 
 // The parts of the sum over k, added in their order, on their way out.
