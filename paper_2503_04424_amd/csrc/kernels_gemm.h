@@ -2,7 +2,7 @@
 // Gram matrix of a network's Jacobian.  R is the row operand (its index runs along the rows of D), C the column operand.
 //
 // Pieces.  Every operand is handled in pieces of 16 bytes along k: 8 elements in 16 bits, 4 in fp32, 2 in fp64.  A slab
-// is four or eight pieces of k.  Lane l of a wavefront supplies piece l / 16 of row l % 16 to a product, which takes
+// is eight pieces (128 bytes) of k.  Lane l of a wavefront supplies piece l / 16 of row l % 16 to a product, which takes
 // four pieces at once: one instruction of 16 x 16 x 32 in 16 bits, four of 16 x 16 x 4 in fp32, two
 // in fp64 (the e-th elements of the four pieces form the e-th of them; any assignment of k's is valid as long as R and C
 // use the same one).  Sums are fp32 for operands in 16 and 32 bits, fp64 for fp64.
@@ -16,6 +16,8 @@
 #include <type_traits>
 
 namespace mdet {
+
+constexpr int PIECES = 8;              // of a slab, along k
 
 template <typename T> struct Core;
 
@@ -78,11 +80,11 @@ struct Operand {
 // ---------------------------------------------------------------------------
 // The staged tile: BM x BN of D by WM x WN wavefronts, slabs of both operands in NB buffers in LDS.
 //
-// With k inner, lines of 128 bytes hold eight pieces, of one row or of two, line i's in the order piece ^ (i & 7): lanes
-// that read one piece of consecutive rows read from different places.  With k outer, the slab
-// lies as it does in memory, row k's elements side by side: in 16 bits the transposing read hands lane l the four k's of
-// column l % 16 out of four rows of 32 bytes, in fp32 the instructions take single elements.  There the blocks of 16
-// columns of row k stand in the order block ^ f(k), so that the rows read together lie in different banks.
+// With k inner, row i's eight pieces (a line of 128 bytes) stand in the order piece ^ (i & 7): lanes that read one piece of
+// consecutive rows read from different places.  With k outer, the slab lies as it does in memory, row k's elements side by
+// side: in 16 bits the transposing read hands lane l the four k's of column l % 16 out of four rows of 32 bytes, in fp32 the
+// instructions take single elements.  There the blocks of 16 columns of row k stand in the order block ^ f(k), so that the
+// rows read together lie in different banks.
 //
 // DIRECT: memory goes straight into LDS (every lane names the 16 bytes that land at its place), for operands whose rows
 // start on 16 bytes.  Otherwise pieces pass through registers, whole ones in one load of any alignment, those that hang
@@ -116,23 +118,23 @@ __device__ __forceinline__ void gemm_put_down() {
   asm volatile("" ::: "memory");
 }
 
-// P: pieces of k that a slab holds; NB: slabs in LDS.
-template <int BM_, int BN_, int WM_, int WN_, int P_, int NB_>
+// NB: slabs in LDS.
+template <int BM_, int BN_, int WM_, int WN_, int NB_>
 struct Tile {
-  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, P = P_, NB = NB_;
+  static constexpr int BM = BM_, BN = BN_, WM = WM_, WN = WN_, NB = NB_;
   static constexpr int WAVES = WM * WN, THREADS = 64 * WAVES;
   static constexpr int TM = BM / WM / 16, TN = BN / WN / 16;   // 16 x 16 parts of a wavefront, down and across
-  static constexpr int SLAB = 16 * P * (BM + BN);              // bytes of one slab of both operands
+  static constexpr int SLAB = 16 * PIECES * (BM + BN);         // bytes of one slab of both operands
 };
 
 // Staging of an operand: B rows of it from i0 on.
-template <typename T, int B, int WAVES, int P, bool OUTER, bool DIRECT, int HOLD>
+template <typename T, int B, int WAVES, bool OUTER, bool DIRECT, int HOLD>
 struct Stage {
   typedef typename Core<T>::piece_t piece_t;
-  static constexpr int VEC = Core<T>::VEC, BK = P * VEC;
-  static constexpr int NP = B * P / (64 * WAVES);              // pieces a lane brings of a slab
+  static constexpr int VEC = Core<T>::VEC, BK = PIECES * VEC;
+  static constexpr int NP = B * PIECES / (64 * WAVES);         // pieces a lane brings of a slab
   static constexpr int PR = B / VEC;                           // k outer: pieces of a row k
-  static_assert(NP * 64 * WAVES == B * P && (P == 4 || P == 8), "whole pieces");
+  static_assert(NP * 64 * WAVES == B * PIECES, "whole pieces");
 
   const T* p;
   int64_t stride, rows, i0;
@@ -152,10 +154,8 @@ struct Stage {
       const int at = id % PR;
       row = (((at / PB) ^ swizzle(k)) * PB + at % PB) * VEC;
     } else {
-      // eight pieces a line of 128 bytes, of one row or of two
-      const int line = id / 8, at = (id % 8) ^ (line & 7);
-      row = line * (8 / P) + at / P;
-      k = at % P * VEC;
+      row = id / PIECES;
+      k = ((id % PIECES) ^ (row & 7)) * VEC;
     }
   }
   static __device__ __forceinline__ int place(const int v) {
@@ -220,8 +220,7 @@ struct Stage {
   static __device__ __forceinline__ piece_t fragment(const char* const lds, const int t, const int h) {
     const int lane = threadIdx.x & 63, g = lane >> 4, j = lane & 15;
     if constexpr (!OUTER) {
-      const int line = (P == 8 ? 16 : 8) * t + (P == 8 ? j : j >> 1), at = P == 8 ? 4 * h + g : 4 * (j & 1) + g;
-      return *reinterpret_cast<const piece_t*>(lds + line * 128 + ((at ^ (line & 7)) << 4));
+      return *reinterpret_cast<const piece_t*>(lds + (16 * t + j) * 128 + (((4 * h + g) ^ (j & 7)) << 4));
     } else if constexpr (sizeof(T) == 2) {
       typedef short half_t __attribute__((ext_vector_type(4)));
       typedef __attribute__((address_space(3))) half_t* lds_half_ptr;
@@ -250,8 +249,8 @@ template <typename T, typename S, bool ROUTER, bool COUTER, bool DIRECT>
 struct TileStream {
   // slabs in registers: as many as small tiles, which wait for memory, have room for
   static constexpr int HOLD = DIRECT ? 1 : S::BM <= 32 ? 4 : S::BM <= 64 && sizeof(T) < 8 ? 3 : 1;
-  typedef Stage<T, S::BM, S::WAVES, S::P, ROUTER, DIRECT, HOLD> RS;
-  typedef Stage<T, S::BN, S::WAVES, S::P, COUTER, DIRECT, HOLD> CS;
+  typedef Stage<T, S::BM, S::WAVES, ROUTER, DIRECT, HOLD> RS;
+  typedef Stage<T, S::BN, S::WAVES, COUTER, DIRECT, HOLD> CS;
   typedef typename Core<T>::piece_t piece_t;
   static constexpr int BK = RS::BK, LOADS = RS::NP + CS::NP;   // loads of a wavefront for a slab
   RS rs;
@@ -296,10 +295,10 @@ struct TileStream {
       }
       if (ccomes) {
 #pragma unroll
-        for (int v = 0; v < CS::NP; ++v) cs.direct(cs.base(k), v, place + 16 * S::P * S::BM);
+        for (int v = 0; v < CS::NP; ++v) cs.direct(cs.base(k), v, place + 16 * PIECES * S::BM);
       } else {
         cs.load(k, kend);
-        cs.put(slab + 16 * S::P * S::BM, 0);
+        cs.put(slab + 16 * PIECES * S::BM, 0);
       }
       // run() counts loads straight to LDS: where some are missing, none is left to be counted
       if (!(rcomes && ccomes)) asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
@@ -317,7 +316,7 @@ struct TileStream {
     if (!DIRECT && held) {
       char* const slab = lds + (to == 0 ? S::NB - 1 : to - 1) * S::SLAB;
       rs.put(slab, 0);
-      cs.put(slab + 16 * S::P * S::BM, 0);
+      cs.put(slab + 16 * PIECES * S::BM, 0);
       held = false;
     }
   }
@@ -335,10 +334,10 @@ struct TileStream {
     const int wr = wave / S::WN * S::TM, wc = wave % S::WN * S::TN;    // first 16 x 16 part of this wavefront
     auto multiply = [&](const char* const slab, auto&& between) {
 #pragma unroll
-      for (int h = 0; h < S::P / 4; ++h) {
+      for (int h = 0; h < PIECES / 4; ++h) {
         piece_t cf[S::TN], rf[S::TM];
 #pragma unroll
-        for (int a = 0; a < S::TN; ++a) cf[a] = CS::fragment(slab + 16 * S::P * S::BM, wc + a, h);
+        for (int a = 0; a < S::TN; ++a) cf[a] = CS::fragment(slab + 16 * PIECES * S::BM, wc + a, h);
 #pragma unroll
         for (int b = 0; b < S::TM; ++b) rf[b] = RS::fragment(slab, wr + b, h);
 #pragma unroll
@@ -372,13 +371,13 @@ struct TileStream {
             // of rows in 16 bits (8192 x 16384 x 4096 1257 TFLOP/s, spread 1176), which wait longest; one behind each strip of
             // products otherwise (k outer 4096 x 4096 x 8192 1384, in front 1324; fp32 4096^3 142, 139).
             constexpr bool FIRST = sizeof(T) == 2 && !ROUTER && !COUTER;
-            constexpr int Q = S::TM * S::P / 4, EACH = (LOADS + Q - 1) / Q;
+            constexpr int Q = S::TM * PIECES / 4, EACH = (LOADS + Q - 1) / Q;
             auto pieces = [&](const int from, const int end) {
 #pragma unroll
               for (int v = from; v < end; ++v) {
                 if (v >= LOADS) break;
                 if (v < RS::NP) rs.direct(rfrom, v, place);
-                else cs.direct(cfrom, v - RS::NP, place + 16 * S::P * S::BM);
+                else cs.direct(cfrom, v - RS::NP, place + 16 * PIECES * S::BM);
               }
             };
             if constexpr (FIRST) pieces(0, LOADS);
@@ -411,7 +410,7 @@ struct TileStream {
               if (s + h + HOLD - 1 < steady) load((h + HOLD - 1) % HOLD);
               multiply(lds + at * S::SLAB, [](int) {});
               rs.put(lds + to * S::SLAB, h);
-              cs.put(lds + to * S::SLAB + 16 * S::P * S::BM, h);
+              cs.put(lds + to * S::SLAB + 16 * PIECES * S::BM, h);
               onward();
             }
           }

@@ -314,7 +314,7 @@ __global__ __launch_bounds__(64 * WAVES) void linear_rows_kernel(const Operand<T
 }
 
 // dz = dy act'(z) and the column sums of 16 EACH rows of it.  A workgroup takes 16 pieces of 16 bytes across; thread (t, c)
-// every sixteenth row of piece c, all of its loads at once.  Bytes bound it (4096 x 8192 bf16 with GELU: DZUS us).
+// every sixteenth row of piece c, all of its loads at once.  Bytes bound it (4096 x 8192 bf16 with GELU: 42 us, 4.8 TB/s).
 constexpr int DZ_PIECES = 16;
 
 template <typename T, int EACH>

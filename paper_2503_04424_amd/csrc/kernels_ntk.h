@@ -36,29 +36,25 @@ __global__ __launch_bounds__(256) void ntk_widen_kernel(const S* __restrict__ fr
   if (i < rows) to[i * ldto + k] = k < cols ? (double)from[i * ld + k] : 0.0;
 }
 
-// Blocks of the lower triangle: BM rows each, C = BM / BN blocks for every BM columns.  Bands of eight rows of blocks, each
+// Blocks of the lower triangle of `rows` rows of blocks, and where number t of them is: bands of eight rows of blocks, each
 // column by column and the triangle at its end row by row, so that neighbours read the same operands.
-template <int C>
-__host__ __device__ __forceinline__ int64_t ntk_blocks(const int64_t rows) {
-  return C * (rows * (rows + 1) / 2);
-}
-template <int C>
+__host__ __device__ __forceinline__ int64_t ntk_blocks(const int64_t rows) { return rows * (rows + 1) / 2; }
 __device__ __forceinline__ void ntk_block(const int64_t t, const int64_t rows, int64_t& bi, int64_t& bj) {
-  // C (32 r^2 + 4 r) blocks stand before band r
-  int64_t r = (int64_t)((sqrt(16.0 + (128.0 / C) * (double)t) - 4.0) * (1.0 / 64.0));
-  while (C * (32 * r * r + 4 * r) > t) --r;
-  while (C * (32 * (r + 1) * (r + 1) + 4 * (r + 1)) <= t) ++r;
-  const int64_t u = t - C * (32 * r * r + 4 * r);
+  // 32 r^2 + 4 r blocks stand before band r
+  int64_t r = (int64_t)((sqrt(16.0 + 128.0 * (double)t) - 4.0) * (1.0 / 64.0));
+  while (32 * r * r + 4 * r > t) --r;
+  while (32 * (r + 1) * (r + 1) + 4 * (r + 1) <= t) ++r;
+  const int64_t u = t - (32 * r * r + 4 * r);
   const int height = rows - 8 * r < 8 ? (int)(rows - 8 * r) : 8;
-  if (u < height * 8 * C * r) {
+  if (u < height * 8 * r) {
     bi = 8 * r + u % height;
     bj = u / height;
   } else {
-    const int v = (int)(u - height * 8 * C * r);
+    const int v = (int)(u - height * 8 * r);
     int i = 0;
-    while (C * ((i + 1) * (i + 2) / 2) <= v) ++i;
+    while ((i + 1) * (i + 2) / 2 <= v) ++i;
     bi = 8 * r + i;
-    bj = 8 * C * r + v - C * (i * (i + 1) / 2);
+    bj = 8 * r + v - i * (i + 1) / 2;
   }
 }
 
@@ -68,12 +64,11 @@ template <typename T, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS) void ntk_first_kernel(const NtkLayers<T> layers, const int64_t n, const typename Core<T>::acc1_t bias,
                                                                typename Core<T>::acc1_t* __restrict__ first) {
   __shared__ __attribute__((aligned(16))) char lds[S::NB * S::SLAB];
-  const int64_t rows = (n + S::BM - 1) / S::BM, blocks = ntk_blocks<S::BM / S::BN>(rows);
+  const int64_t rows = (n + S::BM - 1) / S::BM, blocks = ntk_blocks(rows);
   const int64_t t = gemm_tile_number(blockIdx.x, blocks * layers.count);
   if (t < 0) return;
   int64_t bi, bj;
-  ntk_block<S::BM / S::BN>(t % blocks, rows, bi, bj);
-  if (bj * S::BN >= n) return;                     // the last rows' block may reach less far than its columns
+  ntk_block(t % blocks, rows, bi, bj);
   const int l = (int)(t / blocks);
   const Operand<T> a{layers.a[l], layers.lda[l], n, (layers.near_a >> l & 1) != 0, (layers.straight_a >> l & 1) != 0};
   typename Core<T>::acc_t acc[S::TN][S::TM] = {};
@@ -104,7 +99,7 @@ __global__ __launch_bounds__(S::THREADS) void ntk_gram_kernel(const NtkLayers<T>
   const int64_t t = gemm_tile_number(blockIdx.x, EACH * count);
   if (t < 0) return;
   int64_t bi, bj;
-  ntk_block<S::BM / S::BN>(begin + t / EACH, rows, bi, bj);
+  ntk_block(begin + t / EACH, rows, bi, bj);
   if constexpr (PARTS) {
     bi = 2 * bi + (t >> 1 & 1);
     bj = 2 * bj + (t & 1);

@@ -42,11 +42,11 @@ bool fours(const LinearOut<T, O>& out) {
          four<T>(out.z, out.ldz, out.rows);
 }
 
-typedef Tile<256, 256, 2, 4, 8, 2> Big;
-typedef Tile<128, 128, 2, 2, 8, 2> Mid;
-typedef Tile<64, 64, 2, 2, 8, 2> Small;
-typedef Tile<64, 64, 2, 2, 8, 4> Ahead;
-typedef Tile<32, 32, 2, 2, 8, 4> Tiny;
+typedef Tile<256, 256, 2, 4, 2> Big;
+typedef Tile<128, 128, 2, 2, 2> Mid;
+typedef Tile<64, 64, 2, 2, 2> Small;
+typedef Tile<64, 64, 2, 2, 4> Ahead;
+typedef Tile<32, 32, 2, 2, 4> Tiny;
 
 // Few rows: W is read once.  Beyond 8192 rows of W a split sum over tiles is as fast for one row (16384 x 4096 bf16 22.3 us,
 // 23.7 this way) and faster for sixteen (23.4, 32.2), as it is for more rows at any size (17 rows of 4096 x 4096 11.5 us).

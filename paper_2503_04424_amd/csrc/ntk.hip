@@ -18,6 +18,7 @@ inline int64_t size_of(int32_t t) { return t == MDET_F64 ? 8 : t == MDET_F32 ? 4
 inline int launch_status() { return hipGetLastError() == hipSuccess ? MDET_OK : MDET_EHIP; }
 
 constexpr int64_t MOST = INT32_MAX;
+constexpr int64_t MOST_ELEMENTS = int64_t(1) << 38;      // of an operand: a terabyte or two; a launch over them fits 31 bits
 
 // Types, sizes and strides; pointers only where `pointers` is set.
 int check(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs, const mdet_ntk_layer* layers, int32_t count, bool pointers) {
@@ -25,9 +26,11 @@ int check(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs, const md
   if (dtype == MDET_F64 && out_dtype == MDET_F32) return MDET_EINVAL;      // arithmetic narrower than the operands
   if (n < 0 || outputs < 1 || count < 0 || (count > 0 && !layers)) return MDET_EINVAL;
   if (n > MOST || outputs > MOST || (n > 0 && outputs > MOST / n)) return MDET_EINVAL;
+  if (outputs > 1 && n > (int64_t(1) << 24)) return MDET_EINVAL;           // first factors of n x n
   for (int l = 0; l < count; ++l) {
     const mdet_ntk_layer& x = layers[l];
     if (x.p < 0 || x.q < 0 || x.p > MOST || x.q > MOST) return MDET_EINVAL;
+    if (n > 0 && (x.p > MOST_ELEMENTS / n || x.q > MOST_ELEMENTS / (n * outputs))) return MDET_EINVAL;
     if (!pointers || n == 0) continue;
     const int64_t s = size_of(dtype);
     if (x.p > 0 && (!x.a || (uintptr_t)x.a % s || x.lda > MOST || x.lda < 0 || (n > 1 && x.lda < x.p))) return MDET_EINVAL;
@@ -54,9 +57,9 @@ struct Call {
   hipStream_t st;
 };
 
-typedef Tile<128, 128, 2, 4, 8, 2> Large;
-typedef Tile<64, 64, 2, 2, 8, 2> Small;
-typedef Tile<32, 32, 2, 2, 8, 4> Tiny;
+typedef Tile<128, 128, 2, 4, 2> Large;
+typedef Tile<64, 64, 2, 2, 2> Small;
+typedef Tile<32, 32, 2, 2, 4> Tiny;
 
 constexpr int64_t COMPUTE_UNITS = 256;
 
@@ -94,10 +97,9 @@ int gram_tiles(NtkLayers<T>& list, const Call& c, int accumulate, void* first, R
     if (no_g > yes_g / 8 || (c.d > 1 && no_a > yes_a / 8) || (c.d == 1 && no_a + no_g > (yes_a + yes_g) / 8))
       return gram_tiles<T, Small>(list, c, accumulate, first);
   }
-  constexpr int C = S::BM / S::BN;
-  const int64_t blocks = ntk_blocks<C>(ceil_div(c.n * c.d, S::BM));
+  const int64_t blocks = ntk_blocks(ceil_div(c.n * c.d, S::BM));
   // What is left over behind whole rounds of large blocks would hold up a few compute units for as long as a round takes (fp64
-  // n = 8192, 2080 blocks: 3.08 ms): it goes out in quarters (REST ms).
+  // n = 8192, 2080 blocks: 3.08 ms): it goes out in quarters (2.88 ms).
   if constexpr (S::BM == 128) {
     const int64_t rest = blocks % COMPUTE_UNITS;
     if (range.count < 0 && rest > 0 && rest <= COMPUTE_UNITS / 2) {
@@ -107,7 +109,7 @@ int gram_tiles(NtkLayers<T>& list, const Call& c, int accumulate, void* first, R
   }
   if (range.count < 0) range.count = blocks;
   const int64_t all = ceil_div(range.count * (PARTS ? 4 : 1), 8) * 8;
-  const int64_t firsts = c.d > 1 ? ceil_div(ntk_blocks<C>(ceil_div(c.n, S::BM)) * list.count, 8) * 8 : 0;
+  const int64_t firsts = c.d > 1 ? ceil_div(ntk_blocks(ceil_div(c.n, S::BM)) * list.count, 8) * 8 : 0;
   if (all > INT32_MAX || firsts > INT32_MAX) return MDET_EINVAL;
   using std::false_type;
   using std::true_type;
