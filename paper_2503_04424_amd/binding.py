@@ -6,6 +6,7 @@ fallback of any kind.
 """
 from __future__ import annotations
 
+import array
 import ctypes as C
 import functools
 import itertools
@@ -596,7 +597,7 @@ def mdet_flodance_eval(coef, q, n_values, out=None, stream=None):
 
 
 _TYPE_CODES = {}
-_IS_CUDA = operator.attrgetter("is_cuda")
+_IS_CUDA, _DTYPE = operator.attrgetter("is_cuda"), operator.attrgetter("dtype")
 
 
 def _type_code(dtype) -> int:
@@ -754,7 +755,7 @@ def _adamw_pointers(tensors, name, dtype, sizes):
     """Addresses of contiguous CUDA tensors of one type and these sizes."""
     from torch import Tensor
     if list(map(Tensor.numel, tensors)) != sizes or not all(map(Tensor.is_contiguous, tensors)) or \
-            not all(map(_IS_CUDA, tensors)) or any(t.dtype != dtype for t in tensors):
+            not all(map(_IS_CUDA, tensors)) or set(map(_DTYPE, tensors)) != {dtype}:
         raise ValueError(f"{name}: contiguous CUDA tensors of {dtype} with {sizes} elements expected, not "
                          f"{[(tuple(t.shape), t.dtype) for t in tensors]}")
     return map(Tensor.data_ptr, tensors)
@@ -794,8 +795,8 @@ def mdet_adamw_step(params, grads, exp_avg, exp_avg_sq, *, lr, step, beta1=0.9, 
         none if wide else _adamw_pointers(scales, "scales", torch.float32, [(n + 255) // 256 * 2 for n in sizes]),
         none if copies is None else _adamw_pointers(copies, "copies", copies[0].dtype if copies else None, sizes),
         sizes)
-    table = (C.c_uint64 * (7 * count))(*itertools.chain.from_iterable(zip(*fields)))
-    _check_status(load().mdet_adamw_step(C.byref(a), C.cast(table, C.c_void_p), count, _operator_stream(stream, params[0])))
+    table = array.array("Q", itertools.chain.from_iterable(zip(*fields)))
+    _check_status(load().mdet_adamw_step(C.byref(a), table.buffer_info()[0], count, _operator_stream(stream, params[0])))
 
 
 def _ntk_layers(inputs, signals, outputs):

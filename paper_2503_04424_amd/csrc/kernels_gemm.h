@@ -29,6 +29,11 @@ template <> struct Core<__bf16> {
   static __device__ __forceinline__ void mma(const piece_t& c, const piece_t& r, acc_t& acc) {
     acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(c, r, acc, 0, 0, 0);
   }
+  // Two products into two accumulators, in turn: neither waits for the one before it.
+  static __device__ __forceinline__ void mma_two(const piece_t (&c)[2], const piece_t (&r)[2], acc_t& acc, acc_t& other) {
+    mma(c[0], r[0], acc);
+    mma(c[1], r[1], other);
+  }
   static __device__ __forceinline__ int col(int lane, int e) { return 4 * (lane >> 4) + e; }
 };
 
@@ -39,6 +44,10 @@ template <> struct Core<_Float16> {
   static constexpr int VEC = 8;
   static __device__ __forceinline__ void mma(const piece_t& c, const piece_t& r, acc_t& acc) {
     acc = __builtin_amdgcn_mfma_f32_16x16x32_f16(c, r, acc, 0, 0, 0);
+  }
+  static __device__ __forceinline__ void mma_two(const piece_t (&c)[2], const piece_t (&r)[2], acc_t& acc, acc_t& other) {
+    mma(c[0], r[0], acc);
+    mma(c[1], r[1], other);
   }
   static __device__ __forceinline__ int col(int lane, int e) { return 4 * (lane >> 4) + e; }
 };
@@ -52,6 +61,13 @@ template <> struct Core<float> {
 #pragma unroll
     for (int e = 0; e < 4; ++e) acc = __builtin_amdgcn_mfma_f32_16x16x4f32(c[e], r[e], acc, 0, 0, 0);
   }
+  static __device__ __forceinline__ void mma_two(const piece_t (&c)[2], const piece_t (&r)[2], acc_t& acc, acc_t& other) {
+#pragma unroll
+    for (int e = 0; e < 4; ++e) {
+      acc = __builtin_amdgcn_mfma_f32_16x16x4f32(c[0][e], r[0][e], acc, 0, 0, 0);
+      other = __builtin_amdgcn_mfma_f32_16x16x4f32(c[1][e], r[1][e], other, 0, 0, 0);
+    }
+  }
   static __device__ __forceinline__ int col(int lane, int e) { return 4 * (lane >> 4) + e; }
 };
 
@@ -63,6 +79,13 @@ template <> struct Core<double> {
   static __device__ __forceinline__ void mma(const piece_t& c, const piece_t& r, acc_t& acc) {
 #pragma unroll
     for (int e = 0; e < 2; ++e) acc = __builtin_amdgcn_mfma_f64_16x16x4f64(c[e], r[e], acc, 0, 0, 0);
+  }
+  static __device__ __forceinline__ void mma_two(const piece_t (&c)[2], const piece_t (&r)[2], acc_t& acc, acc_t& other) {
+#pragma unroll
+    for (int e = 0; e < 2; ++e) {
+      acc = __builtin_amdgcn_mfma_f64_16x16x4f64(c[0][e], r[0][e], acc, 0, 0, 0);
+      other = __builtin_amdgcn_mfma_f64_16x16x4f64(c[1][e], r[1][e], other, 0, 0, 0);
+    }
   }
   static __device__ __forceinline__ int col(int lane, int e) { return 4 * e + (lane >> 4); }
 };
@@ -332,7 +355,23 @@ struct TileStream {
   __device__ __forceinline__ void run(typename Core<T>::acc_t (&acc)[S::TN][S::TM], const int count, F&& next) {
     const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
     const int wr = wave / S::WN * S::TM, wc = wave % S::WN * S::TN;    // first 16 x 16 part of this wavefront
+    // A wavefront with a single part would wait for each product and each fragment: its two half slabs go into accumulators
+    // of their own, in turn, all fragments fetched in front.
+    constexpr bool ONE = S::TM * S::TN == 1;
+    typename Core<T>::acc_t other = {};
     auto multiply = [&](const char* const slab, auto&& between) {
+      if constexpr (ONE) {
+        piece_t cf[2], rf[2];
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          cf[h] = CS::fragment(slab + 16 * PIECES * S::BM, wc, h);
+          rf[h] = RS::fragment(slab, wr, h);
+        }
+#pragma unroll
+        for (int h = 0; h < 2; ++h) between(h);
+        Core<T>::mma_two(cf, rf, acc[0][0], other);
+        return;
+      }
 #pragma unroll
       for (int h = 0; h < PIECES / 4; ++h) {
         piece_t cf[S::TN], rf[S::TM];
@@ -427,6 +466,7 @@ struct TileStream {
       put();
       at = at + 1 == S::NB ? 0 : at + 1;
     }
+    if constexpr (ONE) acc[0][0] += other;
   }
 };
 
