@@ -118,12 +118,13 @@ typedef __attribute__((address_space(3))) char* gemm_lds_ptr;
 
 // 16 bytes a lane from base + off (base the same in all lanes) to LDS, lane by lane from byte `at` on.  Written out because
 // the compiler, told of the load, waits for it in front of the next read of anything in LDS; the caller waits for it by
-// itself (s_waitcnt vmcnt).
+// itself (s_waitcnt vmcnt).  The base may have come out of vector registers a moment ago: a memory instruction has to keep
+// five wait states behind a vector instruction that wrote its scalar registers, which the compiler does not see to in here.
 __device__ __forceinline__ void gemm_to_lds(const char* base, const unsigned off, const unsigned at) {
   const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)base);
   const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)((uintptr_t)base >> 32));
   const unsigned long long from = ((unsigned long long)hi << 32) | lo;
-  asm volatile("s_nop 0\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(at), "v"(off), "s"(from));
+  asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(at), "v"(off), "s"(from));
 }
 
 // All of a wavefront's loads but the last `LATER` and all of its LDS accesses are done, and behind the barrier those of all.

@@ -108,14 +108,23 @@ __global__ __launch_bounds__(S::THREADS) void ntk_gram_kernel(const NtkLayers<T>
   const int64_t row0 = bi * S::BM, col0 = bj * S::BN;
   if (row0 >= N || col0 >= N) return;              // a block may reach over the matrix's edge
   acc_t total[S::TN][S::TM] = {};
-  // the samples of this lane's rows and columns; where nothing is stored, any pair will do
-  int sample_row[S::TM], sample_col[S::TN][4];
-  if constexpr (FIRST)
+  // The first factors of a block's samples go through LDS: every one serves d^2 elements.  A large block's are those of three
+  // outputs or more, so that two workgroups' LDS fits a compute unit.
+  constexpr int SAMPLES = !FIRST ? 1 : S::BM == 128 ? 44 : S::BM / 2 + 1, EACH_THREAD = (SAMPLES * SAMPLES + S::THREADS - 1) / S::THREADS;
+  __shared__ typename Core<T>::acc1_t patch[SAMPLES * SAMPLES];
+  int patch_row[S::TM], patch_col[S::TN][4], down = 0, across = 0;
+  int64_t sample0 = 0;                             // of the patch's first element in `first`
+  if constexpr (FIRST) {
+    auto of = [&](const int64_t i) { return (int)((uint32_t)(i < N ? i : N - 1) / (uint32_t)d); };
+    const int i0 = of(row0), j0 = of(col0);
+    down = of(row0 + S::BM - 1) - i0 + 1;
+    across = of(col0 + S::BN - 1) - j0 + 1;
+    sample0 = i0 * n + j0;
     tile_each<T, S>([&](int a, int b, int e, int i, int j) {
-      const uint32_t I = (uint32_t)(row0 + i), J = (uint32_t)(col0 + j);
-      if (a == 0 && e == 0) sample_row[b] = row0 + i < N ? (int)(I / (uint32_t)d) : (int)n - 1;
-      if (b == 0) sample_col[a][e] = col0 + j < N ? (int)(J / (uint32_t)d) : 0;
+      if (a == 0 && e == 0) patch_row[b] = (of(row0 + i) - i0) * across;
+      if (b == 0) patch_col[a][e] = of(col0 + j) - j0;
     });
+  }
   auto of_a = [&](const int l) { return Operand<T>{layers.a[l], layers.lda[l], N, (layers.near_a >> l & 1) != 0, (layers.straight_a >> l & 1) != 0}; };
   auto of_g = [&](const int l) { return Operand<T>{layers.g[l], layers.ldg[l], N, (layers.near_g >> l & 1) != 0, (layers.straight_g >> l & 1) != 0}; };
   TileStream<T, S, false, false, DIRECT> stream(lds);
@@ -133,15 +142,34 @@ __global__ __launch_bounds__(S::THREADS) void ntk_gram_kernel(const NtkLayers<T>
   stream.begin(next);
   for (int l = 0; l < layers.count; ++l) {
     acc_t second[S::TN][S::TM] = {};
+    // brought beside the products where there are registers for it
+    constexpr bool EARLY = FIRST && sizeof(T) < 8;
+    typename Core<T>::acc1_t part[EACH_THREAD];
+    auto bring_part = [&] {
+#pragma unroll
+      for (int v = 0; v < EACH_THREAD; ++v) {
+        const int at = v * S::THREADS + (int)threadIdx.x;
+        // above the diagonal there are none; nothing is stored there
+        part[v] = at < down * across ? first[(l * n + at / across) * n + sample0 + at % across] : 0;
+      }
+    };
+    if constexpr (EARLY) bring_part();
     stream.run(second, stream.slabs(0, layers.q[l]), next);
     if constexpr (FIRST) {
-      const typename Core<T>::acc1_t* const from = first + l * n * n;
+      if constexpr (!EARLY) bring_part();
+      __syncthreads();                             // the layer before has been read
+#pragma unroll
+      for (int v = 0; v < EACH_THREAD; ++v) {
+        const int at = v * S::THREADS + (int)threadIdx.x;
+        if (at < down * across) patch[at] = part[v];
+      }
+      __syncthreads();
 #pragma unroll
       for (int b = 0; b < S::TM; ++b)
 #pragma unroll
         for (int a = 0; a < S::TN; ++a)
 #pragma unroll
-          for (int e = 0; e < 4; ++e) total[a][b][e] += from[(int64_t)sample_row[b] * n + sample_col[a][e]] * second[a][b][e];
+          for (int e = 0; e < 4; ++e) total[a][b][e] += patch[patch_row[b] + patch_col[a][e]] * second[a][b][e];
     } else {
       acc_t one[S::TN][S::TM] = {};
       stream.run(one, stream.slabs(0, layers.p[l]), next);
@@ -151,13 +179,32 @@ __global__ __launch_bounds__(S::THREADS) void ntk_gram_kernel(const NtkLayers<T>
         for (int b = 0; b < S::TM; ++b) total[a][b] += (one[a][b] + bias) * second[a][b];
     }
   }
-  tile_each<T, S>([&](int a, int b, int e, int i, int j) {
-    const int64_t I = row0 + i, J = col0 + j;
-    if (I >= N || J > I) return;
-    auto v = total[a][b][e] * scale;
-    if (accumulate) v += K[I * ldk + J];
-    K[I * ldk + J] = v;
-  });
+  // four neighbours of a row in one store where a lane has them
+  typedef typename Core<T>::acc1_t four_t __attribute__((ext_vector_type(4)));
+  const bool vec = sizeof(typename Core<T>::acc1_t) == 4 && (uintptr_t)K % 16 == 0 && ldk % 4 == 0;
+#pragma unroll
+  for (int b = 0; b < S::TM; ++b)
+#pragma unroll
+    for (int a = 0; a < S::TN; ++a) {
+      const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), lane = threadIdx.x & 63;
+      const int64_t I = row0 + (wave / S::WN * S::TM + b) * 16 + (lane & 15), J = col0 + (wave % S::WN * S::TN + a) * 16;
+      if (I >= N) continue;
+      if (vec && J + Core<T>::col(lane, 3) <= I) {
+        four_t* const to = reinterpret_cast<four_t*>(K + I * ldk + J + Core<T>::col(lane, 0));
+        four_t v = total[a][b] * scale;
+        if (accumulate) v += *to;
+        *to = v;
+      } else {
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int64_t j = J + Core<T>::col(lane, e);
+          if (j > I) continue;
+          auto v = total[a][b][e] * scale;
+          if (accumulate) v += K[I * ldk + j];
+          K[I * ldk + j] = v;
+        }
+      }
+    }
 }
 
 }  // namespace mdet

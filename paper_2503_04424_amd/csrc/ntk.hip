@@ -150,7 +150,7 @@ int gram(const mdet_ntk_layer* layers, int32_t count, const Call& c, void* first
     // compute units without one: n = 512 in fp32 21 us with the 32 x 32 tile, 35 with 64 x 64, in fp64 29 and 63.
     const int64_t order = c.n * c.d;
     int status;
-    if (order >= 8000 && (sizeof(T) == 8 || (sizeof(T) == 2 && c.d > 1))) {
+    if (order >= 8000 && c.d != 2 && (sizeof(T) == 8 || (sizeof(T) == 2 && c.d > 1))) {
       if constexpr (sizeof(T) != 4) status = gram_tiles<T, Large>(list, c, accumulate, first);
     } else if (sizeof(T) != 2 && order < 1500) {
       if constexpr (sizeof(T) != 2) status = gram_tiles<T, Tiny>(list, c, accumulate, first);
