@@ -116,14 +116,19 @@ struct Operand {
 // ---------------------------------------------------------------------------
 typedef __attribute__((address_space(3))) char* gemm_lds_ptr;
 
+// A value that is the same in all lanes, in scalar registers whatever the compiler had in mind for it.
+template <typename V>
+__device__ __forceinline__ V gemm_scalar(const V v) {
+  const uint64_t x = (uint64_t)v;
+  return (V)(((uint64_t)(unsigned)__builtin_amdgcn_readfirstlane((int)(x >> 32)) << 32) | (unsigned)__builtin_amdgcn_readfirstlane((int)x));
+}
+
 // 16 bytes a lane from base + off (base the same in all lanes) to LDS, lane by lane from byte `at` on.  Written out because
 // the compiler, told of the load, waits for it in front of the next read of anything in LDS; the caller waits for it by
 // itself (s_waitcnt vmcnt).  The base may have come out of vector registers a moment ago: a memory instruction has to keep
 // five wait states behind a vector instruction that wrote its scalar registers, which the compiler does not see to in here.
 __device__ __forceinline__ void gemm_to_lds(const char* base, const unsigned off, const unsigned at) {
-  const unsigned lo = __builtin_amdgcn_readfirstlane((unsigned)(uintptr_t)base);
-  const unsigned hi = __builtin_amdgcn_readfirstlane((unsigned)((uintptr_t)base >> 32));
-  const unsigned long long from = ((unsigned long long)hi << 32) | lo;
+  const uint64_t from = gemm_scalar((uint64_t)base);
   asm volatile("s_nop 4\n\tglobal_load_lds_dwordx4 %1, %2" ::"{m0}"(at), "v"(off), "s"(from));
 }
 
@@ -397,7 +402,11 @@ struct TileStream {
       if (ahead == (DIRECT ? S::NB - 1 : 1) && steady > 0) {
         left -= steady;
         const char *rfrom = rs.base(k), *cfrom = cs.base(k);
-        const int64_t rstep = rs.base(k + BK) - rfrom, cstep = cs.base(k + BK) - cfrom;
+        int64_t rstep = rs.base(k + BK) - rfrom, cstep = cs.base(k + BK) - cfrom;
+        if constexpr (DIRECT) {
+          rfrom = gemm_scalar(rfrom), cfrom = gemm_scalar(cfrom);
+          rstep = gemm_scalar(rstep), cstep = gemm_scalar(cstep);
+        }
         k += (int64_t)steady * BK;
         auto onward = [&] {
           to = to + 1 == S::NB ? 0 : to + 1;
