@@ -379,18 +379,25 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dy
   }
 }
 
-// db = sum of the strips' sums, four threads a column, in one order.
+// db = sum of the strips' sums, sixteen threads a column, in one order.
+constexpr int DB_COLS = 16;
+
 template <typename O>
 __global__ __launch_bounds__(256) void linear_db_kernel(const float* __restrict__ sums, const int64_t strips, const int64_t cols, O* __restrict__ db) {
-  __shared__ float part[4][64];
-  const int64_t col = (int64_t)blockIdx.x * 64 + (threadIdx.x & 63);
-  const int t = threadIdx.x >> 6;
+  __shared__ float part[16][DB_COLS];
+  const int t = threadIdx.x / DB_COLS, c = threadIdx.x % DB_COLS;
+  const int64_t col = (int64_t)blockIdx.x * DB_COLS + c;
   float sum = 0.0f;
   if (col < cols)
-    for (int64_t s = t; s < strips; s += 4) sum += sums[s * cols + col];
-  part[t][threadIdx.x & 63] = sum;
+    for (int64_t s = t; s < strips; s += 16) sum += sums[s * cols + col];
+  part[t][c] = sum;
   __syncthreads();
-  if (t == 0 && col < cols) db[col] = (O)((part[0][threadIdx.x] + part[1][threadIdx.x]) + (part[2][threadIdx.x] + part[3][threadIdx.x]));
+  if (t == 0 && col < cols) {
+    float v = part[0][c];
+#pragma unroll
+    for (int r = 1; r < 16; ++r) v += part[r][c];
+    db[col] = (O)v;
+  }
 }
 
 }  // namespace mdet

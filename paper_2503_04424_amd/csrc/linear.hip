@@ -214,7 +214,7 @@ int backward(const Grad& g) {
     else go(std::integral_constant<int, 4>{});
   }
   if (g.db && g.n > 0)
-    hipLaunchKernelGGL((linear_db_kernel<O>), dim3((unsigned)ceil_div(g.n, 64)), dim3(256), 0, g.st, (const float*)sums, lay.strips, g.n,
+    hipLaunchKernelGGL((linear_db_kernel<O>), dim3((unsigned)ceil_div(g.n, DB_COLS)), dim3(256), 0, g.st, (const float*)sums, lay.strips, g.n,
                        (O*)g.db);
   const bool want_dx = g.dx && g.m > 0 && g.k > 0, want_dw = g.dw && g.n > 0 && g.k > 0;
   if (!want_dx && !want_dw && !(g.db && g.n > 0) && !(dz && g.m > 0 && g.n > 0)) return MDET_OK;

@@ -146,7 +146,8 @@ int gram(const mdet_ntk_layer* layers, int32_t count, const Call& c, void* first
     }
     // Several workgroups a compute unit, and so the 64 x 64 tile, are better than one large one (fp32 n = 8192, three layers:
     // 1.48 ms, 1.65 with 128 x 128; fp64 n = 4096 54 and 47 TFLOP/s) except at the largest orders in fp64 (n = 8192 62.0 TFLOP/s,
-    // 59.6 with the small tile) and in 16 bits with several outputs (order 10000 433 us, 461).  A few small blocks would leave most
+    // 59.6 with the small tile, both before its last blocks went out in quarters) and in 16 bits with several outputs (order 10000
+    // 433 us, 461, both before the first factors went through LDS).  A few small blocks would leave most
     // compute units without one: n = 512 in fp32 21 us with the 32 x 32 tile, 35 with 64 x 64, in fp64 29 and 63.
     const int64_t order = c.n * c.d;
     int status;
