@@ -15,7 +15,8 @@
 // and the caller's seed.  A root that is not zero has a code of at least 1: a code of 0 would divide its m by eps.
 // This step's own update uses m and v before they are rounded.
 //
-// What bounds it: bytes.  28 a element with states, parameters and gradients in 32 bits.
+// What bounds it: bytes.  28 a element with states, parameters and gradients in 32 bits (67 million elements: 360 us,
+// 5.2 TB/s); with states in 8 bits, 16 and the two scales of a block (225 us, 4.9 TB/s), where the arithmetic is close behind.
 #pragma once
 #include <hip/hip_runtime.h>
 #include <stdint.h>

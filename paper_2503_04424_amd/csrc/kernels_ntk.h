@@ -87,6 +87,8 @@ __global__ __launch_bounds__(S::THREADS) void ntk_first_kernel(const NtkLayers<T
 // Blocks `begin` .. `begin` + `count` - 1 of K.  With PARTS the launch's workgroups take the four quarters (64 x 64) of blocks of
 // twice the tile's size.  FIRST: the first factors stand in `first`; otherwise (one output) both products are formed here, one
 // after the other, and multiplied in registers.  The sum over layers stays in registers, K is written once.
+// The matrix cores bound large orders of one output (n = 8192, three layers: fp64 2.87 ms, 66 TFLOP/s; fp32 1.47 ms, 129),
+// the chain of short products small ones (n = 512: 18 us) and those of several outputs (1000 x 10 bf16, four layers: 376 us).
 template <typename T, typename S, bool DIRECT, bool FIRST, bool PARTS>
 __global__ __launch_bounds__(S::THREADS) void ntk_gram_kernel(const NtkLayers<T> layers, const int64_t begin, const int64_t count, const int64_t n, const int d,
                                                               const typename Core<T>::acc1_t bias, const typename Core<T>::acc1_t scale,
