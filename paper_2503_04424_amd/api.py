@@ -13,6 +13,7 @@ Where the paper's call and this one differ:
     block only; the determinant does not depend on it).
   * ``scratch_dir`` and ``parallel_io`` belong to the file entry point and are not taken here.
 """
+import math
 import re
 
 from . import binding as B
@@ -149,11 +150,11 @@ def _linear_function():
     class LinearFunction(torch.autograd.Function):
         @staticmethod
         def forward(ctx, x, w, bias, residual, activation):
-            rows = x.reshape(-1, x.shape[-1])
+            rows = _as_rows(x)
             keep = activation != "none" and any(ctx.needs_input_grad[:3])
             z = rows.new_empty((rows.shape[0], w.shape[0])) if keep else None
-            r = None if residual is None else residual.reshape(-1, residual.shape[-1])
-            y = B.mdet_linear_forward(_rows(rows), _rows(w), bias, None if r is None else _rows(r), activation, preact=z)
+            y = B.mdet_linear_forward(_rows(rows), _rows(w), None if bias is None else bias.contiguous(),
+                                      None if residual is None else _rows(_as_rows(residual)), activation, preact=z)
             ctx.save_for_backward(rows, w, z)
             ctx.activation, ctx.shape = activation, x.shape
             return y.view(*x.shape[:-1], w.shape[0])
@@ -165,16 +166,25 @@ def _linear_function():
             need_x, need_w, need_b, need_r, _ = ctx.needs_input_grad
             dx = dw = db = None
             if need_x or need_w or need_b:
-                dx, dw, db = B.mdet_linear_backward(_rows(dy.reshape(-1, dy.shape[-1])), _rows(x), _rows(w), z, ctx.activation,
+                dx, dw, db = B.mdet_linear_backward(_rows(_as_rows(dy)), _rows(x), _rows(w), z, ctx.activation,
                                                     dx=need_x, dw=need_w, db=need_b)
             return None if dx is None else dx.view(ctx.shape), dw, db, dy if need_r else None, None
 
     return LinearFunction
 
 
+def _as_rows(t):
+    """The tensor as a matrix whose rows are its last axis (also where that or any other axis is empty)."""
+    return t.reshape(math.prod(t.shape[:-1]), t.shape[-1])
+
+
 def _rows(t):
-    """Rows of consecutive elements: the tensor itself where it has them (views and slices do), or a copy."""
-    return t if t.stride(-1) == 1 or t.shape[-1] <= 1 else t.contiguous()
+    """Rows of consecutive elements that do not overlap: the matrix itself where it has them (views and slices do), or a
+    copy.  Autograd hands over gradients that are one row, or one element, repeated (distances of zero)."""
+    if (t.shape[1] <= 1 or t.stride(1) == 1) and (t.shape[0] <= 1 or t.stride(0) >= t.shape[1]):
+        return t
+    # an empty one as well, which contiguous() would leave as it is
+    return t.new_empty(t.shape).copy_(t)
 
 
 _linear = None
@@ -184,6 +194,8 @@ def linear(x, w, bias=None, residual=None, activation="none"):
     """``act(x w^T + bias) + residual`` with its gradient (autograd): x (..., k), w (n, k), residual (..., n).
     activation: 'none', 'relu', 'gelu', 'gelu_tanh' or 'silu'.  One launch or two for the whole layer."""
     global _linear
+    if x.dim() < 1 or w.dim() != 2:
+        raise ValueError("x with rows of inputs as its last axis and a matrix w expected")
     if residual is not None and tuple(residual.shape) != (*x.shape[:-1], w.shape[0]):
         raise ValueError(f"residual: shape {(*x.shape[:-1], w.shape[0])} expected, not {tuple(residual.shape)}")
     if _linear is None:
