@@ -153,8 +153,7 @@ def _linear_function():
             rows = _as_rows(x)
             keep = activation != "none" and any(ctx.needs_input_grad[:3])
             z = rows.new_empty((rows.shape[0], w.shape[0])) if keep else None
-            y = B.mdet_linear_forward(_rows(rows), _rows(w), None if bias is None else bias.contiguous(),
-                                      None if residual is None else _rows(_as_rows(residual)), activation, preact=z)
+            y = _layer(rows, w, bias, residual, activation, z)
             ctx.save_for_backward(rows, w, z)
             ctx.activation, ctx.shape = activation, x.shape
             return y.view(*x.shape[:-1], w.shape[0])
@@ -171,6 +170,12 @@ def _linear_function():
             return None if dx is None else dx.view(ctx.shape), dw, db, dy if need_r else None, None
 
     return LinearFunction
+
+
+def _layer(rows, w, bias, residual, activation, z=None):
+    """The layer on a matrix x; z: where what stands in front of the activation is kept."""
+    return B.mdet_linear_forward(_rows(rows), _rows(w), None if bias is None else bias.contiguous(),
+                                 None if residual is None else _rows(_as_rows(residual)), activation, preact=z)
 
 
 def _as_rows(t):
@@ -198,6 +203,10 @@ def linear(x, w, bias=None, residual=None, activation="none"):
         raise ValueError("x with rows of inputs as its last axis and a matrix w expected")
     if residual is not None and tuple(residual.shape) != (*x.shape[:-1], w.shape[0]):
         raise ValueError(f"residual: shape {(*x.shape[:-1], w.shape[0])} expected, not {tuple(residual.shape)}")
+    import torch
+    if not torch.is_grad_enabled():
+        # ctx.needs_input_grad is true for parameters here as well: nothing is kept for a gradient that cannot be asked for
+        return _layer(_as_rows(x), w, bias, residual, activation).view(*x.shape[:-1], w.shape[0])
     if _linear is None:
         _linear = _linear_function()
     return _linear.apply(x, w, bias, residual, activation)

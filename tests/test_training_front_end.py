@@ -88,3 +88,15 @@ def test_shapes_are_refused(calls):
             M.linear(x, w)
     with pytest.raises(ValueError):
         M.linear(normal(4, 7), normal(6, 7), residual=normal(6))
+
+
+def test_nothing_is_kept_where_no_gradient_can_be_asked_for(calls):
+    x, w, b = normal(4, 7), normal(6, 7, seed=1).requires_grad_(), normal(6, seed=2).requires_grad_()
+    y = M.linear(x, w, b, activation="silu")
+    assert calls["forward"][-1]["preact"] is not None and y.requires_grad
+    for off in (torch.no_grad, torch.inference_mode):
+        with off():
+            z = M.linear(x, w, b, activation="silu")
+        assert calls["forward"][-1]["preact"] is None and not z.requires_grad and torch.equal(y.detach(), z)
+    M.linear(x, w.detach(), b.detach(), normal(4, 6).requires_grad_(), activation="silu")       # the residual's gradient is dy
+    assert calls["forward"][-1]["preact"] is None
