@@ -672,6 +672,8 @@ def _new(stream, make):
 def _operator_workspace(workspace, need, like, stream):
     """(address, bytes, tensor): the caller's, or a new one of the bytes that are needed."""
     if workspace is not None:
+        if not workspace.is_cuda or not workspace.is_contiguous():
+            raise ValueError("workspace: a contiguous CUDA tensor expected")
         return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
     if need == 0:
         return None, 0, None
