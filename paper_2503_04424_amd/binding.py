@@ -13,6 +13,7 @@ import itertools
 import math
 import operator
 import os
+import sys
 from dataclasses import dataclass
 from typing import Callable, Optional
 
@@ -597,7 +598,7 @@ def mdet_flodance_eval(coef, q, n_values, out=None, stream=None):
 
 
 _TYPE_CODES = {}
-_IS_CUDA, _DTYPE = operator.attrgetter("is_cuda"), operator.attrgetter("dtype")
+_GPU, _DTYPE = operator.methodcaller("get_device"), operator.attrgetter("dtype")
 
 
 def _type_code(dtype) -> int:
@@ -622,27 +623,35 @@ def _operand_type(t):
     return t
 
 
-def _matrix(t, name, rows, cols, dtype):
-    """(address, leading dimension) of a row-major CUDA matrix of this shape and type."""
-    if t.shape != (rows, cols) or t.dtype != dtype or not t.is_cuda:
-        raise ValueError(f"{name}: a CUDA tensor of {rows} x {cols} {dtype} expected, not {tuple(t.shape)} {t.dtype}")
+def _gpu(t, name):
+    """Number of the GPU that a tensor is on."""
+    gpu = t.get_device()
+    if gpu < 0:
+        raise ValueError(f"{name}: a CUDA tensor expected")
+    return gpu
+
+
+def _matrix(t, name, rows, cols, dtype, gpu):
+    """(address, leading dimension) of a row-major matrix of this shape and type on this GPU."""
+    if t.shape != (rows, cols) or t.dtype != dtype or t.get_device() != gpu:
+        raise ValueError(f"{name}: a tensor of {rows} x {cols} {dtype} on cuda:{gpu} expected, not {tuple(t.shape)} {t.dtype} on {t.device}")
     ld, inner = t.stride()
     if inner != 1 and cols > 1:
         raise ValueError(f"{name}: rows of consecutive elements expected")
     return t.data_ptr(), (ld if rows > 1 else max(ld, cols))
 
 
-def _vector(t, name, n, dtype):
-    if t.shape != (n,) or t.dtype != dtype or not t.is_cuda or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous CUDA tensor of {n} {dtype} expected, not {tuple(t.shape)} {t.dtype}")
+def _vector(t, name, n, dtype, gpu):
+    if t.shape != (n,) or t.dtype != dtype or t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor of {n} {dtype} on cuda:{gpu} expected, not {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr()
 
 
 _raw_stream = None
 
 
-def _operator_stream(stream, like):
-    """Handle of the caller's stream, or of the current one on the tensor's device."""
+def _operator_stream(stream, gpu):
+    """Handle of the caller's stream, or of the current one on this GPU."""
     if stream is not None:
         return _stream_handle(stream)
     global _raw_stream
@@ -650,7 +659,18 @@ def _operator_stream(stream, like):
         import torch
         # the handle alone where torch offers it: a tenth of the time of making a Stream object
         _raw_stream = getattr(torch._C, "_cuda_getCurrentRawStream", None) or (lambda d: torch.cuda.current_stream(d).cuda_stream)
-    return _raw_stream(like.device.index)
+    return _raw_stream(gpu)
+
+
+def _queue(gpu, entry, *args):
+    """An entry point that queues work, with the GPU of its tensors as the current one: a kernel goes to the current one, and
+    the default stream has the same handle on all."""
+    cuda = sys.modules["torch"].cuda           # the tensors are torch's: it is there, and an import statement would cost more
+    if gpu == cuda.current_device():
+        _check_status(entry(*args))
+    else:
+        with cuda.device(gpu):
+            _check_status(entry(*args))
 
 
 def _check_status(st):
@@ -669,16 +689,16 @@ def _new(stream, make):
         return make()
 
 
-def _operator_workspace(workspace, need, like, stream):
+def _operator_workspace(workspace, need, gpu, stream):
     """(address, bytes, tensor): the caller's, or a new one of the bytes that are needed."""
     if workspace is not None:
-        if not workspace.is_cuda or not workspace.is_contiguous():
-            raise ValueError("workspace: a contiguous CUDA tensor expected")
+        if workspace.get_device() != gpu or not workspace.is_contiguous():
+            raise ValueError(f"workspace: a contiguous tensor on cuda:{gpu} expected")
         return workspace.data_ptr(), workspace.numel() * workspace.element_size(), workspace
     if need == 0:
         return None, 0, None
     import torch
-    ws = _new(stream, lambda: torch.empty(need, dtype=torch.uint8, device=like.device))
+    ws = _new(stream, lambda: torch.empty(need, dtype=torch.uint8, device=torch.device("cuda", gpu)))
     return ws.data_ptr(), need, ws
 
 
@@ -701,18 +721,19 @@ def mdet_linear_forward(x, w, bias=None, residual=None, activation="none", out=N
     m, k = x.shape
     n = w.shape[0]
     act = _activation(activation)
-    xp, ldx = _matrix(x, "x", m, k, t)
-    wp, ldw = _matrix(w, "w", n, k, t)
-    bp = None if bias is None else _vector(bias, "bias", n, t)
-    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", m, n, t)
+    gpu = _gpu(x, "x")
+    xp, ldx = _matrix(x, "x", m, k, t, gpu)
+    wp, ldw = _matrix(w, "w", n, k, t, gpu)
+    bp = None if bias is None else _vector(bias, "bias", n, t, gpu)
+    rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", m, n, t, gpu)
     if out is None:
         out = _new(stream, lambda: x.new_empty((m, n)))
-    yp, ldy = _matrix(out, "out", m, n, t)
-    zp, ldz = (None, 0) if preact is None else _matrix(preact, "preact", m, n, t)
+    yp, ldy = _matrix(out, "out", m, n, t, gpu)
+    zp, ldz = (None, 0) if preact is None else _matrix(preact, "preact", m, n, t, gpu)
     need = 0 if workspace is not None else mdet_linear_workspace_query(t, m, n, k)
-    wsp, wsb, _ws = _operator_workspace(workspace, need, x, stream)
-    _check_status(load().mdet_linear_forward(_type_code(t), act, m, n, k, xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, zp, ldz,
-                                             wsp, wsb, _operator_stream(stream, x)))
+    wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
+    _queue(gpu, load().mdet_linear_forward, _type_code(t), act, m, n, k, xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, zp, ldz,
+           wsp, wsb, _operator_stream(stream, gpu))
     return out
 
 
@@ -730,36 +751,37 @@ def mdet_linear_backward(dy, x, w, preact=None, activation="none", dx=True, dw=T
     n = w.shape[0]
     act = _activation(activation)
     gt = t if grad_dtype is None else grad_dtype
-    dyp, lddy = _matrix(dy, "dy", m, n, t)
-    xp, ldx = _matrix(x, "x", m, k, t)
-    wp, ldw = _matrix(w, "w", n, k, t)
+    gpu = _gpu(x, "x")
+    dyp, lddy = _matrix(dy, "dy", m, n, t, gpu)
+    xp, ldx = _matrix(x, "x", m, k, t, gpu)
+    wp, ldw = _matrix(w, "w", n, k, t, gpu)
     if act and preact is None:
         raise ValueError("the gradient through an activation needs preact")
-    zp, ldz = _matrix(preact, "preact", m, n, t) if act else (None, 0)
+    zp, ldz = _matrix(preact, "preact", m, n, t, gpu) if act else (None, 0)
 
     def result(what, shape, dtype):
         if what is True:
             return _new(stream, lambda: torch.empty(shape, dtype=dtype, device=x.device))
         return None if what is False else what
     dx, dw, db = result(dx, (m, k), t), result(dw, (n, k), gt), result(db, (n,), gt)
-    dxp, lddx = (None, 0) if dx is None else _matrix(dx, "dx", m, k, t)
-    dwp, lddw = (None, 0) if dw is None else _matrix(dw, "dw", n, k, gt)
-    dbp = None if db is None else _vector(db, "db", n, gt)
-    dzp, lddz = (None, 0) if dz is None else _matrix(dz, "dz", m, n, t)
+    dxp, lddx = (None, 0) if dx is None else _matrix(dx, "dx", m, k, t, gpu)
+    dwp, lddw = (None, 0) if dw is None else _matrix(dw, "dw", n, k, gt, gpu)
+    dbp = None if db is None else _vector(db, "db", n, gt, gpu)
+    dzp, lddz = (None, 0) if dz is None else _matrix(dz, "dz", m, n, t, gpu)
     need = 0 if workspace is not None else mdet_linear_workspace_query(t, m, n, k, backward=True)
-    wsp, wsb, _ws = _operator_workspace(workspace, need, x, stream)
-    _check_status(load().mdet_linear_backward(_type_code(t), _type_code(gt), act, m, n, k, dyp, lddy, zp, ldz, xp, ldx, wp, ldw,
-                                              dxp, lddx, dwp, lddw, dbp, dzp, lddz, wsp, wsb, _operator_stream(stream, x)))
+    wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
+    _queue(gpu, load().mdet_linear_backward, _type_code(t), _type_code(gt), act, m, n, k, dyp, lddy, zp, ldz, xp, ldx, wp, ldw,
+           dxp, lddx, dwp, lddw, dbp, dzp, lddz, wsp, wsb, _operator_stream(stream, gpu))
     return dx, dw, db
 
 
-def _adamw_pointers(tensors, name, dtype, sizes):
-    """Addresses of contiguous CUDA tensors of one type and these sizes."""
+def _adamw_pointers(tensors, name, dtype, sizes, gpu):
+    """Addresses of contiguous tensors of one type and these sizes on this GPU."""
     from torch import Tensor
     if list(map(Tensor.numel, tensors)) != sizes or not all(map(Tensor.is_contiguous, tensors)) or \
-            not all(map(_IS_CUDA, tensors)) or set(map(_DTYPE, tensors)) != {dtype}:
-        raise ValueError(f"{name}: contiguous CUDA tensors of {dtype} with {sizes} elements expected, not "
-                         f"{[(tuple(t.shape), t.dtype) for t in tensors]}")
+            set(map(_GPU, tensors)) != {gpu} or set(map(_DTYPE, tensors)) != {dtype}:
+        raise ValueError(f"{name}: contiguous tensors of {dtype} with {sizes} elements on cuda:{gpu} expected, not "
+                         f"{[(tuple(t.shape), t.dtype, str(t.device)) for t in tensors]}")
     return map(Tensor.data_ptr, tensors)
 
 
@@ -776,6 +798,7 @@ def mdet_adamw_step(params, grads, exp_avg, exp_avg_sq, *, lr, step, beta1=0.9, 
             raise ValueError("no params, but other tensors")
         return
     sizes = [t.numel() for t in params]
+    gpu = _gpu(params[0], "params")
     wide = scales is None
     a = _AdamwParams()
     a.struct_size = C.sizeof(_AdamwParams)
@@ -785,20 +808,20 @@ def mdet_adamw_step(params, grads, exp_avg, exp_avg_sq, *, lr, step, beta1=0.9, 
     a.seed, a.step = int(seed) & 0xFFFFFFFF, int(step)
     a.lr, a.beta1, a.beta2, a.eps, a.weight_decay = float(lr), float(beta1), float(beta2), float(eps), float(weight_decay)
     if grad_scale is not None:
-        if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or not grad_scale.is_cuda:
-            raise ValueError("grad_scale: a CUDA tensor of one float32 expected")
+        if grad_scale.dtype != torch.float32 or grad_scale.numel() != 1 or grad_scale.get_device() != gpu:
+            raise ValueError(f"grad_scale: a tensor of one float32 on cuda:{gpu} expected")
         a.grad_scale = grad_scale.data_ptr()
     none = [0] * count
     fields = (
-        _adamw_pointers(params, "params", params[0].dtype, sizes),
-        _adamw_pointers(grads, "grads", grads[0].dtype if grads else None, sizes),
-        _adamw_pointers(exp_avg, "exp_avg", torch.float32 if wide else torch.int8, sizes),
-        _adamw_pointers(exp_avg_sq, "exp_avg_sq", torch.float32 if wide else torch.uint8, sizes),
-        none if wide else _adamw_pointers(scales, "scales", torch.float32, [(n + 255) // 256 * 2 for n in sizes]),
-        none if copies is None else _adamw_pointers(copies, "copies", copies[0].dtype if copies else None, sizes),
+        _adamw_pointers(params, "params", params[0].dtype, sizes, gpu),
+        _adamw_pointers(grads, "grads", grads[0].dtype if grads else None, sizes, gpu),
+        _adamw_pointers(exp_avg, "exp_avg", torch.float32 if wide else torch.int8, sizes, gpu),
+        _adamw_pointers(exp_avg_sq, "exp_avg_sq", torch.float32 if wide else torch.uint8, sizes, gpu),
+        none if wide else _adamw_pointers(scales, "scales", torch.float32, [(n + 255) // 256 * 2 for n in sizes], gpu),
+        none if copies is None else _adamw_pointers(copies, "copies", copies[0].dtype if copies else None, sizes, gpu),
         sizes)
     table = array.array("Q", itertools.chain.from_iterable(zip(*fields)))
-    _check_status(load().mdet_adamw_step(C.byref(a), table.buffer_info()[0], count, _operator_stream(stream, params[0])))
+    _queue(gpu, load().mdet_adamw_step, C.byref(a), table.buffer_info()[0], count, _operator_stream(stream, gpu))
 
 
 def _ntk_layers(inputs, signals, outputs):
@@ -806,20 +829,20 @@ def _ntk_layers(inputs, signals, outputs):
         raise ValueError("inputs and signals: one of each for every layer expected")
     if not inputs:
         raise ValueError("at least one layer expected")
-    n, dtype = inputs[0].shape[0], inputs[0].dtype
+    n, dtype, gpu = inputs[0].shape[0], inputs[0].dtype, _gpu(inputs[0], "inputs")
     table = (_NtkLayer * len(inputs))()
     for layer, a, g in zip(table, inputs, signals):
         if a.dim() != 2 or g.dim() != 2:
             raise ValueError("inputs and signals: matrices expected")
         layer.p, layer.q = a.shape[1], g.shape[1]
-        layer.a, layer.lda = _matrix(a, "inputs", n, layer.p, dtype)
-        layer.g, layer.ldg = _matrix(g, "signals", n * outputs, layer.q, dtype)
-    return n, dtype, table
+        layer.a, layer.lda = _matrix(a, "inputs", n, layer.p, dtype, gpu)
+        layer.g, layer.ldg = _matrix(g, "signals", n * outputs, layer.q, dtype, gpu)
+    return n, dtype, gpu, table
 
 
 def mdet_ntk_workspace_query(inputs, signals, out_dtype, outputs=1) -> int:
     """Device bytes of workspace for ``mdet_ntk_gram`` on these layers."""
-    n, dtype, table = _ntk_layers(inputs, signals, int(outputs))
+    n, dtype, _, table = _ntk_layers(inputs, signals, int(outputs))
     b = C.c_uint64(0)
     _check_status(load().mdet_ntk_workspace_query(_type_code(dtype), _type_code(out_dtype), n, int(outputs),
                                                   C.cast(table, C.c_void_p), len(table), C.byref(b)))
@@ -836,7 +859,7 @@ def mdet_ntk_gram(inputs, signals, out=None, outputs=1, bias=1.0, scale=1.0, acc
     outputs = int(outputs)
     if outputs < 1:
         raise ValueError("outputs must be 1 or more")
-    n, dtype, table = _ntk_layers(inputs, signals, outputs)
+    n, dtype, gpu, table = _ntk_layers(inputs, signals, outputs)
     order = n * outputs
     if out is None:
         if accumulate:
@@ -845,15 +868,15 @@ def mdet_ntk_gram(inputs, signals, out=None, outputs=1, bias=1.0, scale=1.0, acc
         out = _new(stream, lambda: torch.zeros((order, order), dtype=wide, device=inputs[0].device))
     if out.dtype not in (torch.float32, torch.float64):
         raise ValueError("out: float32 or float64 expected")
-    kp, ldk = _matrix(out, "out", order, order, out.dtype)
+    kp, ldk = _matrix(out, "out", order, order, out.dtype, gpu)
     lib_, layers = load(), C.cast(table, C.c_void_p)
     need = C.c_uint64(0)
     codes = _type_code(dtype), _type_code(out.dtype)
     if workspace is None:
         _check_status(lib_.mdet_ntk_workspace_query(*codes, n, outputs, layers, len(table), C.byref(need)))
-    wsp, wsb, _ws = _operator_workspace(workspace, need.value, out, stream)
-    _check_status(lib_.mdet_ntk_gram(*codes, n, outputs, layers, len(table), float(bias), float(scale), int(bool(accumulate)),
-                                     kp, ldk, wsp, wsb, _operator_stream(stream, out)))
+    wsp, wsb, _ws = _operator_workspace(workspace, need.value, gpu, stream)
+    _queue(gpu, lib_.mdet_ntk_gram, *codes, n, outputs, layers, len(table), float(bias), float(scale), int(bool(accumulate)),
+           kp, ldk, wsp, wsb, _operator_stream(stream, gpu))
     return out
 
 

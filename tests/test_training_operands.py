@@ -27,13 +27,14 @@ def on(gpu, *shape, dtype=torch.float32):
 
 @pytest.fixture
 def library(monkeypatch):
-    """Names of the library's entry points that were called."""
+    """Names of the entry points that were called to queue work."""
     called = []
 
     class Library:
         def __getattr__(self, name):
             def entry(*args):
-                called.append(name)
+                if not name.endswith("_query"):
+                    called.append(name)
                 return M.Status.OK
             return entry
     monkeypatch.setattr(B, "load", lambda: Library())
@@ -70,3 +71,66 @@ def test_a_workspace_is_device_memory_of_its_own_size(library, name):
         with pytest.raises(ValueError, match="workspace"):
             CALLS[name](ws=bad)
     assert library == [name]
+
+
+def step(gpus=(0,) * 7, count=2):
+    kinds = [torch.float32, torch.float32, torch.int8, torch.uint8, None, torch.bfloat16]
+    lists = [[on(g, 300, dtype=t) for _ in range(count)] if t else [on(g, 2, 2) for _ in range(count)] for g, t in zip(gpus, kinds)]
+    p, g, m, v, sc, co = lists
+    M.mdet_adamw_step(p, g, m, v, lr=1e-3, step=1, scales=sc, copies=co, grad_scale=on(gpus[6], 1), stream=0)
+
+
+@pytest.mark.parametrize("name,count", [("mdet_linear_forward", 6), ("mdet_linear_backward", 8), ("mdet_ntk_gram", 5), ("mdet_adamw_step", 7)])
+def test_operands_are_on_one_gpu(library, name, count):
+    """A kernel runs on one: each operand by itself on another, or in host memory, is refused before anything is queued."""
+    call = {**CALLS, "mdet_adamw_step": step}[name]
+    call((0,) * count)
+    assert library == [name]
+    for i in range(count):
+        for other in (1, -1):
+            with pytest.raises(ValueError):
+                call(tuple(other if j == i else 0 for j in range(count)))
+    if name in CALLS:
+        with pytest.raises(ValueError):
+            call(ws=on(1, 4096, dtype=torch.uint8))
+    assert library == [name]
+
+
+def test_one_tensor_of_a_list_on_another_gpu_is_refused(library):
+    lists = [[on(0, 8), on(0, 8)] for _ in range(4)]
+    for tensors in lists:
+        tensors[1].gpu = 1
+        with pytest.raises(ValueError):
+            M.mdet_adamw_step(*lists, lr=1e-3, step=1, stream=0)
+        tensors[1].gpu = 0
+    assert not library
+
+
+@pytest.mark.parametrize("name,count", [("mdet_linear_forward", 6), ("mdet_linear_backward", 8), ("mdet_ntk_gram", 5), ("mdet_adamw_step", 7)])
+def test_the_operands_gpu_is_the_current_one_of_the_call(library, monkeypatch, name, count):
+    current, at = [0], []
+
+    class Guard:
+        def __init__(self, gpu):
+            self.gpu = gpu
+
+        def __enter__(self):
+            self.before, current[0] = current[0], self.gpu
+
+        def __exit__(self, *_):
+            current[0] = self.before
+    monkeypatch.setattr(torch.cuda, "current_device", lambda: current[0])
+    monkeypatch.setattr(torch.cuda, "device", Guard)
+    noted = B.load()
+
+    class Library:
+        def __getattr__(self, entry):
+            def run(*args):
+                at.append((entry, current[0]))
+                return getattr(noted, entry)(*args)
+            return run
+    monkeypatch.setattr(B, "load", lambda: Library())
+    call = {**CALLS, "mdet_adamw_step": step}[name]
+    for gpu in (0, 3):
+        call((gpu,) * count)
+    assert [g for entry, g in at if entry == name] == [0, 3] and current == [0]
