@@ -237,10 +237,11 @@ class AdamW:
             grads = [p.grad for p in self.params]
         if any(g is None for g in grads):
             raise ValueError("a gradient for every tensor expected")
-        self.steps += 1
-        B.mdet_adamw_step([p.detach() for p in self.params], grads, self.exp_avg, self.exp_avg_sq, lr=self.lr, step=self.steps,
+        step = self.steps + 1
+        B.mdet_adamw_step([p.detach() for p in self.params], grads, self.exp_avg, self.exp_avg_sq, lr=self.lr, step=step,
                           beta1=self.betas[0], beta2=self.betas[1], eps=self.eps, weight_decay=self.weight_decay,
-                          scales=self.scales, copies=self.copies, grad_scale=grad_scale, seed=self.seed + self.steps, stream=stream)
+                          scales=self.scales, copies=self.copies, grad_scale=grad_scale, seed=self.seed + step, stream=stream)
+        self.steps = step                  # a step that was refused does not count
 
     def state_dict(self):
         return {"steps": self.steps, "seed": self.seed, "state_bits": self.state_bits, "exp_avg": list(self.exp_avg),
