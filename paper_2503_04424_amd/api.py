@@ -248,9 +248,12 @@ class AdamW:
                 "exp_avg_sq": list(self.exp_avg_sq), "scales": None if self.scales is None else list(self.scales)}
 
     def load_state_dict(self, state):
-        if state["state_bits"] != self.state_bits or len(state["exp_avg"]) != len(self.params):
-            raise ValueError("a state of the same width and number of tensors expected")
+        """Takes over what ``state_dict`` gave, whole or not at all."""
+        names = ("exp_avg", "exp_avg_sq") + (("scales",) if self.state_bits == 8 else ())
+        mine = [t for name in names for t in getattr(self, name)]
+        other = [t for name in names for t in state[name] or ()]
+        if state["state_bits"] != self.state_bits or [t.shape for t in mine] != [t.shape for t in other]:
+            raise ValueError("a state of the same width for tensors of the same shapes expected")
+        for a, b in zip(mine, other):
+            a.copy_(b)
         self.steps, self.seed = int(state["steps"]), int(state["seed"])
-        for mine, other in ((self.exp_avg, state["exp_avg"]), (self.exp_avg_sq, state["exp_avg_sq"]), (self.scales or [], state["scales"] or [])):
-            for a, b in zip(mine, other):
-                a.copy_(b)

@@ -38,3 +38,27 @@ def test_a_step_that_is_refused_does_not_count(steps):
         opt.step([p[1], p[1]])
     opt.step([t.clone() for t in p])
     assert steps == [(1, 101), (2, 102)] and opt.steps == 2
+
+
+@pytest.mark.parametrize("bits", [32, 8])
+def test_a_state_of_other_shapes_is_refused_whole(steps, bits):
+    opt = M.AdamW(tensors((4, 3), (300,)), state_bits=bits, seed=5)
+    opt.step(tensors((4, 3), (300,)))
+    for t in opt.exp_avg + opt.exp_avg_sq + (opt.scales or []):
+        t.fill_(7)
+    same = M.AdamW(tensors((4, 3), (300,)), state_bits=bits)
+    same.load_state_dict(opt.state_dict())
+    assert same.steps == 1 and same.seed == 5
+    assert all(bool((t == 7).all()) for t in same.exp_avg + same.exp_avg_sq + (same.scales or []))
+    for shapes in (((4, 3), (1,)), ((4, 3), (300, 1)), ((3, 4), (300,)), ((4, 3),), ((4, 3), (300,), (2,)), ()):
+        other = M.AdamW(tensors(*shapes), state_bits=bits)
+        source = M.AdamW(tensors((4, 3), (300,)), state_bits=bits)
+        for into, state in ((other, opt.state_dict()), (source, other.state_dict())):
+            with pytest.raises(ValueError):
+                into.load_state_dict(state)
+            assert into.steps == 0 and not any(bool(t.any()) for t in into.exp_avg + into.exp_avg_sq + (into.scales or []))
+    with pytest.raises(ValueError):
+        M.AdamW(tensors((4, 3), (300,)), state_bits=40 - bits).load_state_dict(opt.state_dict())
+    state = {**opt.state_dict(), "exp_avg_sq": opt.exp_avg_sq[:1]}
+    with pytest.raises(ValueError):
+        same.load_state_dict(state)
