@@ -678,6 +678,12 @@ def _check_status(st):
         raise MemdetError(st)
 
 
+def _written(*tensors):
+    """The caller's tensors that a call has written through their addresses: autograd refuses a gradient that goes through a
+    value from before, as after any other operation in place."""
+    sys.modules["torch"].autograd.graph.increment_version(tensors)
+
+
 def _new(stream, make):
     """make() with the stream that the tensor will be used on as the current one: its memory goes back to that stream's
     order when the tensor is dropped, and a fill runs on it."""
@@ -726,6 +732,7 @@ def mdet_linear_forward(x, w, bias=None, residual=None, activation="none", out=N
     wp, ldw = _matrix(w, "w", n, k, t, gpu)
     bp = None if bias is None else _vector(bias, "bias", n, t, gpu)
     rp, ldr = (None, 0) if residual is None else _matrix(residual, "residual", m, n, t, gpu)
+    given = [v for v in (out, preact) if v is not None]
     if out is None:
         out = _new(stream, lambda: x.new_empty((m, n)))
     yp, ldy = _matrix(out, "out", m, n, t, gpu)
@@ -734,6 +741,8 @@ def mdet_linear_forward(x, w, bias=None, residual=None, activation="none", out=N
     wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
     _queue(gpu, load().mdet_linear_forward, _type_code(t), act, m, n, k, xp, ldx, wp, ldw, bp, rp, ldr, yp, ldy, zp, ldz,
            wsp, wsb, _operator_stream(stream, gpu))
+    if given:
+        _written(*given)
     return out
 
 
@@ -763,6 +772,7 @@ def mdet_linear_backward(dy, x, w, preact=None, activation="none", dx=True, dw=T
         if what is True:
             return _new(stream, lambda: torch.empty(shape, dtype=dtype, device=x.device))
         return None if what is False else what
+    given = [v for v in (dx, dw, db, dz) if v is not None and not isinstance(v, bool)]
     dx, dw, db = result(dx, (m, k), t), result(dw, (n, k), gt), result(db, (n,), gt)
     dxp, lddx = (None, 0) if dx is None else _matrix(dx, "dx", m, k, t, gpu)
     dwp, lddw = (None, 0) if dw is None else _matrix(dw, "dw", n, k, gt, gpu)
@@ -772,6 +782,8 @@ def mdet_linear_backward(dy, x, w, preact=None, activation="none", dx=True, dw=T
     wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
     _queue(gpu, load().mdet_linear_backward, _type_code(t), _type_code(gt), act, m, n, k, dyp, lddy, zp, ldz, xp, ldx, wp, ldw,
            dxp, lddx, dwp, lddw, dbp, dzp, lddz, wsp, wsb, _operator_stream(stream, gpu))
+    if given:
+        _written(*given)
     return dx, dw, db
 
 
@@ -822,6 +834,7 @@ def mdet_adamw_step(params, grads, exp_avg, exp_avg_sq, *, lr, step, beta1=0.9, 
         sizes)
     table = array.array("Q", itertools.chain.from_iterable(zip(*fields)))
     _queue(gpu, load().mdet_adamw_step, C.byref(a), table.buffer_info()[0], count, _operator_stream(stream, gpu))
+    _written(*params, *(copies or ()))
 
 
 def _ntk_layers(inputs, signals, outputs):
@@ -861,6 +874,7 @@ def mdet_ntk_gram(inputs, signals, out=None, outputs=1, bias=1.0, scale=1.0, acc
         raise ValueError("outputs must be 1 or more")
     n, dtype, gpu, table = _ntk_layers(inputs, signals, outputs)
     order = n * outputs
+    given = out
     if out is None:
         if accumulate:
             raise ValueError("accumulate needs out")
@@ -877,6 +891,8 @@ def mdet_ntk_gram(inputs, signals, out=None, outputs=1, bias=1.0, scale=1.0, acc
     wsp, wsb, _ws = _operator_workspace(workspace, need.value, gpu, stream)
     _queue(gpu, lib_.mdet_ntk_gram, *codes, n, outputs, layers, len(table), float(bias), float(scale), int(bool(accumulate)),
            kp, ldk, wsp, wsb, _operator_stream(stream, gpu))
+    if given is not None:
+        _written(out)
     return out
 
 

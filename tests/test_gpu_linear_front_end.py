@@ -63,3 +63,17 @@ def test_axes_that_are_empty(M):
         assert not grads[1].any()                # no rows, or no columns
         if shape[-1] == 0:
             assert torch.equal(grads[2], y.shape[:-1].numel() * (b > 0).float())
+
+
+def test_a_gradient_through_weights_from_before_a_step_is_refused(M):
+    """The step writes parameters and copies in place: autograd notices that a graph from before it has lost its values."""
+    w = normal(24, 40).requires_grad_()
+    opt = M.AdamW([w], copy_dtype=torch.bfloat16)
+    for p in (w, opt.copies[0].requires_grad_()):
+        x = normal(8, 40, seed=1).to(p.dtype).requires_grad_()
+        old = M.linear(x, p, activation="gelu")
+        opt.step([torch.ones_like(w)])
+        with pytest.raises(RuntimeError, match="modified by an inplace operation"):
+            old.sum().backward()
+        M.linear(x, p, activation="gelu").sum().backward()
+        assert x.grad is not None and p.grad is not None

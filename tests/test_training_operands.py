@@ -134,3 +134,29 @@ def test_the_operands_gpu_is_the_current_one_of_the_call(library, monkeypatch, n
     for gpu in (0, 3):
         call((gpu,) * count)
     assert [g for entry, g in at if entry == name] == [0, 3] and current == [0]
+
+
+def test_what_a_call_writes_counts_as_changed(library):
+    """Tensors of the caller's that are written through their addresses: their autograd version goes up; those read, not."""
+    x, w, b, r, y, z = on(0, 4, 16), on(0, 8, 16), on(0, 8), on(0, 4, 8), on(0, 4, 8), on(0, 4, 8)
+    dx, dw, db, dz = on(0, 4, 16), on(0, 8, 16), on(0, 8), on(0, 4, 8)
+    p, g, m, v, c = (on(0, 8, dtype=t) for t in (torch.float32, torch.float32, torch.float32, torch.float32, torch.bfloat16))
+    k = on(0, 4, 4)
+    every = dict(x=x, w=w, b=b, r=r, y=y, z=z, dx=dx, dw=dw, db=db, dz=dz, p=p, g=g, c=c, k=k)
+
+    def changed(call):
+        before = {name: t._version for name, t in every.items()}
+        call()
+        return {name for name, t in every.items() if t._version != before[name]}
+    assert changed(lambda: M.mdet_linear_forward(x, w, b, r, "gelu", out=y, preact=z, stream=0)) == {"y", "z"}
+    assert changed(lambda: M.mdet_linear_forward(x, w, b, r, out=r, stream=0)) == {"r"}
+    assert changed(lambda: M.mdet_linear_backward(y, x, w, z, "gelu", dx, dw, db, dz=dz, stream=0)) == {"dx", "dw", "db", "dz"}
+    assert changed(lambda: M.mdet_linear_backward(y, x, w, z, "gelu", False, dw, None, stream=0)) == {"dw"}
+    assert changed(lambda: M.mdet_adamw_step([p], [g], [m], [v], lr=1e-3, step=1, copies=[c], stream=0)) == {"p", "c"}
+    assert changed(lambda: M.mdet_adamw_step([p.detach()], [g], [m], [v], lr=1e-3, step=2, stream=0)) == {"p"}
+    assert changed(lambda: M.mdet_ntk_gram([x], [y], k, stream=0)) == {"k"}
+
+    def refused():
+        with pytest.raises(ValueError):
+            M.mdet_adamw_step([p], [g[:7]], [m], [v], lr=1e-3, step=3, stream=0)
+    assert changed(refused) == set()
