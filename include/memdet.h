@@ -590,7 +590,7 @@ int mdet_linear_backward(int32_t dtype, int32_t grad_dtype, int32_t activation, 
                          int64_t lddx, void* dw, int64_t lddw, void* db, void* dz, int64_t lddz,
                          void* workspace, uint64_t workspace_bytes, void* stream);
 
-/* One tensor of an optimiser step, n consecutive elements. */
+/* One tensor of an optimiser step, n consecutive elements.  No two tensors of a call overlap. */
 typedef struct mdet_adamw_tensor {
   void* p;          /* parameters, updated in place                                          */
   const void* g;    /* gradient                                                              */

@@ -223,6 +223,9 @@ class AdamW:
         self.params = list(params)
         if state_bits not in (32, 8):
             raise ValueError("state_bits must be 32 or 8")
+        spans = sorted((p.data_ptr(), p.data_ptr() + p.numel() * p.element_size()) for p in self.params if p.numel())
+        if any(b[0] < a[1] for a, b in zip(spans[:-1], spans[1:])):
+            raise ValueError("a tensor twice, or tensors that overlap: a step would update the same memory from several places at once")
         self.lr, self.betas, self.eps, self.weight_decay = lr, tuple(betas), eps, weight_decay
         self.state_bits, self.seed, self.steps = state_bits, int(seed), 0
         types = (torch.float32, torch.float32) if state_bits == 32 else (torch.int8, torch.uint8)

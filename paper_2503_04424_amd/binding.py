@@ -799,7 +799,7 @@ def _adamw_pointers(tensors, name, dtype, sizes, gpu):
 
 def mdet_adamw_step(params, grads, exp_avg, exp_avg_sq, *, lr, step, beta1=0.9, beta2=0.999, eps=1e-8, weight_decay=0.01,
                     scales=None, copies=None, grad_scale=None, seed=0, stream=None) -> None:
-    """One AdamW step over lists of tensors, in place (asynchronous).  States: float32, or int8 codes of the mean and
+    """One AdamW step over lists of tensors that do not overlap, in place (asynchronous).  States: float32, or int8 codes of the mean and
     uint8 codes of the root of the mean square with ``scales[i]``, float32 of ceil(n / 256) x 2.  ``copies``: 16-bit
     tensors that receive the updated parameters as well.  ``grad_scale``: a float32 CUDA tensor of one element, a
     factor on all gradients.  ``seed``: of the random rounding of 8-bit states, another one each step."""

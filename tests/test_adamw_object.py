@@ -62,3 +62,13 @@ def test_a_state_of_other_shapes_is_refused_whole(steps, bits):
     state = {**opt.state_dict(), "exp_avg_sq": opt.exp_avg_sq[:1]}
     with pytest.raises(ValueError):
         same.load_state_dict(state)
+
+
+def test_a_tensor_twice_is_refused():
+    """Its update would run in several workgroups at once."""
+    a, b = tensors((40, 30), (5,))
+    flat = torch.zeros(100)
+    for bad in ([a, b, a], [a, b, a.view(30, 40)], [flat[:60], flat[59:]], [flat, flat[99:]], [a, a.detach()]):
+        with pytest.raises(ValueError, match="twice"):
+            M.AdamW(bad)
+    M.AdamW([a, b, flat[:60], flat[60:], torch.zeros(0), torch.zeros(0), flat[:0]])
