@@ -216,7 +216,7 @@ class AdamW:
     """AdamW over a list of CUDA tensors, updated in place by ``step()`` (``mdet_adamw_step``; asynchronous).
 
     state_bits: 32, or 8 for a mean and a root mean square in 8 bits each with two scales per 256 elements.
-    copy_dtype: torch.bfloat16 or torch.float16 keeps a 16-bit copy of every tensor in ``copies``, written by the step."""
+    copy_dtype: torch.bfloat16 or torch.float16 keeps a 16-bit copy of every tensor in ``copies``, written by the step and by ``load_state_dict``."""
 
     def __init__(self, params, lr=1e-3, betas=(0.9, 0.999), eps=1e-8, weight_decay=0.01, state_bits=32, copy_dtype=None, seed=0):
         import torch
@@ -251,7 +251,7 @@ class AdamW:
                 "exp_avg_sq": list(self.exp_avg_sq), "scales": None if self.scales is None else list(self.scales)}
 
     def load_state_dict(self, state):
-        """Takes over what ``state_dict`` gave, whole or not at all."""
+        """Takes over what ``state_dict`` gave, whole or not at all, and the parameters' present values into the copies."""
         names = ("exp_avg", "exp_avg_sq") + (("scales",) if self.state_bits == 8 else ())
         mine = [t for name in names for t in getattr(self, name)]
         other = [t for name in names for t in state[name] or ()]
@@ -259,4 +259,6 @@ class AdamW:
             raise ValueError("a state of the same width for tensors of the same shapes expected")
         for a, b in zip(mine, other):
             a.copy_(b)
+        for c, p in zip(self.copies or (), self.params):
+            c.detach().copy_(p.detach())
         self.steps, self.seed = int(state["steps"]), int(state["seed"])

@@ -72,3 +72,16 @@ def test_a_tensor_twice_is_refused():
         with pytest.raises(ValueError, match="twice"):
             M.AdamW(bad)
     M.AdamW([a, b, flat[:60], flat[60:], torch.zeros(0), torch.zeros(0), flat[:0]])
+
+
+def test_copies_follow_parameters_that_were_brought_back_with_a_state(steps):
+    p = tensors((4, 3), (5,))
+    opt = M.AdamW(p, copy_dtype=torch.bfloat16)
+    for c in opt.copies:
+        c.requires_grad_()
+    saved = M.AdamW(p).state_dict()
+    for t in p:
+        t.mul_(2).add_(1)                       # a checkpoint's values
+    opt.load_state_dict(saved)
+    for t, c in zip(p, opt.copies):
+        assert torch.equal(c.detach(), t.to(torch.bfloat16)) and c.requires_grad
