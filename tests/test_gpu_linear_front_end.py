@@ -77,3 +77,14 @@ def test_a_gradient_through_weights_from_before_a_step_is_refused(M):
             old.sum().backward()
         M.linear(x, p, activation="gelu").sum().backward()
         assert x.grad is not None and p.grad is not None
+
+
+@pytest.mark.parametrize("dtype", [torch.float32, torch.bfloat16], ids=str)
+def test_empty_axes_beside_long_ones(M, dtype):
+    """An empty batch through a wide layer and back, a layer without inputs, one without outputs."""
+    for m, n, k in ((0, 640, 1024), (0, 9000, 520), (1000, 64, 0), (1000, 0, 64)):
+        x, w, b = (normal(*s).to(dtype).requires_grad_() for s in ((m, k), (n, k), (n,)))
+        y = M.linear(x, w, b, activation="gelu")
+        dx, dw, db = torch.autograd.grad(y.sum(), (x, w, b))
+        assert y.shape == (m, n) and dx.shape == x.shape and dw.shape == w.shape and not dx.any() and not dw.any()
+        assert bool(db.any()) == (m * n > 0)

@@ -139,3 +139,26 @@ def test_the_hash_is_even():
             for u, v in ((low, high), (low[:-1], low[1:]), (high[:-1], high[1:]), (low, other / 65536.0)):
                 assert abs(float(np.corrcoef(u, v)[0, 1])) < 0.006
             assert abs(float(low.mean()) - 0.5) < 0.002 and abs(float(low.var()) - 1 / 12) < 0.002
+
+
+@pytest.mark.parametrize("dtype", [F32, F16, BF16])
+def test_empty_axes_beside_long_ones(M, dtype):
+    """A result without elements is cut into no tiles, however long the sum is that it would have been: figures and calls come
+    back (in a process of their own: a division by zero would end it)."""
+    import subprocess
+    import sys
+    code = f"""
+import ctypes as C
+import paper_2503_04424_amd as M
+L, A = M.load(), {A}
+for m, n, k in ((0, 512, 512), (0, 9000, 4096), (1000, 64, 0), (1000, 0, 64), (0, 0, 100000), (100000, 0, 0), (0, 1000, 0), (17, 0, 100000)):
+    for back in (0, 1):
+        b = C.c_uint64(1)
+        assert L.mdet_linear_workspace_query({dtype}, back, m, n, k, C.byref(b)) == 0
+        assert b.value < (1 << 30)
+    if m == 0 or n == 0:
+        assert L.mdet_linear_forward({dtype}, 2, m, n, k, A, k, A, k, None, None, 0, A, n, None, 0, A, 1 << 30, None) == 0
+assert L.mdet_linear_backward({dtype}, {dtype}, 0, 0, 0, 100000, A, 0, None, 0, A, 100000, A, 100000, A, 100000, A, 100000, A, None, 0, A, 1 << 30, None) == 0
+"""
+    done = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
+    assert done.returncode == 0, (done.returncode, done.stderr[-500:])
