@@ -553,7 +553,8 @@ int mdet_flodance_eval(const double* coef, int32_t q, const double* n_values, in
  * `stream` (a hipStream_t or NULL), allocates nothing and returns MDET_EINVAL for inconsistent
  * arguments, MDET_ENOMEM_DEVICE for a workspace that is too small and MDET_EHIP if a launch failed.
  * A workspace starts on 256 bytes.  Sizes of zero are allowed: an empty sum is zero, a call
- * without results does nothing.
+ * without results does nothing.  A product's result has at most 2^26 - 1024 squares of 32 x 32 (or parts
+ * of them): 6.9e10 elements, or 2.1e9 rows of up to 32.
  * ---------------------------------------------------------------------- */
 
 typedef enum {

@@ -54,7 +54,7 @@ extern "C" int mdet_adamw_step(const mdet_adamw_params* a, const mdet_adamw_tens
     if ((uintptr_t)t.p % ps || (uintptr_t)t.g % gs) return MDET_EINVAL;
     if (a->state_bits == 32 && (((uintptr_t)t.m | (uintptr_t)t.v) % 4)) return MDET_EINVAL;
     if ((a->state_bits == 8 && (uintptr_t)t.scales % 4) || (a->copy_dtype != -1 && (uintptr_t)t.copy % 2)) return MDET_EINVAL;
-    if (t.n > (int64_t)INT32_MAX * ADAMW_STEP) return MDET_EINVAL;
+    if (t.n > ADAMW_CHUNKS * ADAMW_STEP) return MDET_EINVAL;
     total += t.n;
   }
   AdamwFactors f;
@@ -79,7 +79,7 @@ extern "C" int mdet_adamw_step(const mdet_adamw_params* a, const mdet_adamw_tens
   // Tensors without elements keep their number (the hash goes by it) and take no chunk.
   for (int64_t i = 0; i <= count; ++i) {
     const int64_t chunks = i < count ? (tensors[i].n + list.chunk - 1) / list.chunk : 0;
-    if (i == count || list.count == ADAMW_TENSORS || list.first[list.count] + chunks > INT32_MAX) {
+    if (i == count || list.count == ADAMW_TENSORS || list.first[list.count] + chunks > ADAMW_CHUNKS) {
       if (list.first[list.count] > 0) {
         if (a->dtype == MDET_F32) launch_grad<float>(*a, f, list, st);
         else if (a->dtype == MDET_BF16) launch_grad<__bf16>(*a, f, list, st);

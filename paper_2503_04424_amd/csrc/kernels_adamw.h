@@ -29,6 +29,7 @@ constexpr int ADAMW_BLOCK = 256;       // elements that share a scale: one wavef
 constexpr int ADAMW_THREADS = 256;
 constexpr int ADAMW_STEP = 1024;       // elements a workgroup takes at a time
 constexpr int ADAMW_TENSORS = 48;      // a launch's, so that they fit the kernel's arguments
+constexpr int64_t ADAMW_CHUNKS = (int64_t)UINT32_MAX / ADAMW_THREADS;   // a launch's, which holds fewer than 2^32 threads
 
 struct AdamwFactors {
   float b1, a1, b2, a2, keep, rate, root, eps;

@@ -503,6 +503,13 @@ Operand<T> gemm_operand(const void* p, const int64_t stride, const int64_t rows,
   return Operand<T>{(const T*)p, stride, rows, near, straight};
 }
 
+// A launch holds fewer than 2^32 threads: f(first, count) for runs of workgroups that stay below that.
+template <typename F>
+void gemm_launches(const int64_t blocks, const int threads, F&& f) {
+  const int64_t most = (int64_t)UINT32_MAX / threads;
+  for (int64_t first = 0; first < blocks; first += most) f(first, dim3((unsigned)(blocks - first < most ? blocks - first : most)));
+}
+
 // Tile number of workgroup `id` of a launch of 8 ceil(total / 8): workgroups go round the eight chiplets, each of which gets
 // a run of consecutive tiles, so that what one L2 holds is read by neighbours.  -1: none.
 __device__ __forceinline__ int64_t gemm_tile_number(const int64_t id, const int64_t total) {

@@ -322,13 +322,14 @@ constexpr int DZ_PIECES = 16;
 template <typename T, int EACH>
 __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dy, const int64_t lddy, const T* __restrict__ z,
                                                         const int64_t ldz, T* __restrict__ dz, const int64_t lddz,
-                                                        float* __restrict__ sums, const int64_t rows, const int64_t cols, const int act) {
+                                                        float* __restrict__ sums, const int64_t rows, const int64_t cols, const int act,
+                                                        const int64_t first) {
   typedef typename Core<T>::piece_t piece_t;
   constexpr int VEC = Core<T>::VEC;
   __shared__ float part[16][DZ_PIECES * VEC];
   const int64_t across = (cols + DZ_PIECES * VEC - 1) / (DZ_PIECES * VEC);
   const int t = threadIdx.x / DZ_PIECES, c = threadIdx.x % DZ_PIECES * VEC;
-  const int64_t strip = blockIdx.x / across, col0 = blockIdx.x % across * (DZ_PIECES * VEC), col = col0 + c, row = strip * (16 * EACH) + t;
+  const int64_t id = first + blockIdx.x, strip = id / across, col0 = id % across * (DZ_PIECES * VEC), col = col0 + c, row = strip * (16 * EACH) + t;
   const bool whole = col + VEC <= cols;
   auto get = [&](const T* const p, const int64_t ld, const int64_t i) {
     piece_t x = {};
@@ -385,10 +386,11 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dy
 constexpr int DB_COLS = 16;
 
 template <typename O>
-__global__ __launch_bounds__(256) void linear_db_kernel(const float* __restrict__ sums, const int64_t strips, const int64_t cols, O* __restrict__ db) {
+__global__ __launch_bounds__(256) void linear_db_kernel(const float* __restrict__ sums, const int64_t strips, const int64_t cols, O* __restrict__ db,
+                                                        const int64_t first) {
   __shared__ float part[16][DB_COLS];
   const int t = threadIdx.x / DB_COLS, c = threadIdx.x % DB_COLS;
-  const int64_t col = (int64_t)blockIdx.x * DB_COLS + c;
+  const int64_t col = (first + blockIdx.x) * DB_COLS + c;
   float sum = 0.0f;
   if (col < cols)
     for (int64_t s = t; s < strips; s += 16) sum += sums[s * cols + col];

@@ -30,8 +30,8 @@ static_assert(NTK_LAYERS <= 32, "a bit for each");
 // Element i of a matrix in type S, as a double; the conversions to fp64 are exact.
 template <typename S>
 __global__ __launch_bounds__(256) void ntk_widen_kernel(const S* __restrict__ from, const int64_t ld, double* __restrict__ to, const int64_t rows,
-                                                        const int64_t cols, const int64_t ldto) {
-  const int64_t id = (int64_t)blockIdx.x * 256 + threadIdx.x;
+                                                        const int64_t cols, const int64_t ldto, const int64_t first) {
+  const int64_t id = (first + blockIdx.x) * 256 + threadIdx.x;
   const int64_t i = id / ldto, k = id % ldto;
   if (i < rows) to[i * ldto + k] = k < cols ? (double)from[i * ld + k] : 0.0;
 }

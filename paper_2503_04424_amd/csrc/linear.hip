@@ -24,6 +24,11 @@ inline bool sizes_fit(int64_t m, int64_t n, int64_t k) {
   return (!n || m <= most / n) && (!k || m <= most / k) && (!k || n <= most / k);
 }
 
+// Whether a product of this many rows and columns goes out in one launch, which holds fewer than 2^32 threads.  A tile of 256 (128) rows and
+// columns has 512 (256) threads for at least eight (four) squares of 32, the grid is rounded up by seven tiles at most, and smaller
+// tiles are taken for a few hundred squares only.
+inline bool tiles_fit(int64_t rows, int64_t cols) { return ceil_div(rows, 32) * ceil_div(cols, 32) <= (int64_t(1) << 26) - 1024; }
+
 // A matrix of r rows and c columns in memory: null only where it has no elements, rows that do not overlap.
 inline bool matrix_ok(const void* p, int64_t r, int64_t c, int64_t ld, int64_t size) {
   if (r == 0 || c == 0) return true;
@@ -117,7 +122,6 @@ void tiles(Operand<T> r, Operand<T> c, int64_t k, const LinearOut<T, O>& out, co
 template <typename T, typename O, bool ROUTER, bool COUTER>
 int product(Operand<T> r, Operand<T> c, int64_t k, LinearOut<T, O> out, float* parts, hipStream_t st) {
   const Cut cut = cut_of(out.rows, out.cols, k, sizeof(T), !ROUTER && !COUTER);
-  if (ceil_div(out.rows, 32) * ceil_div(out.cols, 32) > INT32_MAX / 32) return MDET_EINVAL;
   out.vec = fours(out);
   if (cut.tile == 0) {
     if constexpr (!ROUTER && !COUTER) rows_product<T, O>(r, c, k, out, st);
@@ -205,17 +209,19 @@ int backward(const Grad& g) {
   float* const sums = g.db ? (float*)(g.workspace + lay.sums) : nullptr;
   if ((dz || sums) && g.m > 0 && g.n > 0) {
     const int64_t blocks = lay.strips * ceil_div(g.n, DZ_PIECES * Core<T>::VEC);
-    if (blocks > INT32_MAX) return MDET_EINVAL;
     auto go = [&](auto each) {
-      hipLaunchKernelGGL((linear_dz_kernel<T, decltype(each)::value>), dim3((unsigned)blocks), dim3(256), 0, g.st, (const T*)g.dy, g.lddy,
-                         (const T*)g.z, g.ldz, dz, lddz, sums, g.m, g.n, g.act);
+      gemm_launches(blocks, 256, [&](const int64_t first, const dim3 grid) {
+        hipLaunchKernelGGL((linear_dz_kernel<T, decltype(each)::value>), grid, dim3(256), 0, g.st, (const T*)g.dy, g.lddy, (const T*)g.z, g.ldz, dz,
+                           lddz, sums, g.m, g.n, g.act, first);
+      });
     };
     if (lay.each == 1) go(std::integral_constant<int, 1>{});
     else go(std::integral_constant<int, 4>{});
   }
-  if (g.db && g.n > 0)
-    hipLaunchKernelGGL((linear_db_kernel<O>), dim3((unsigned)ceil_div(g.n, DB_COLS)), dim3(256), 0, g.st, (const float*)sums, lay.strips, g.n,
-                       (O*)g.db);
+  if (g.db)
+    gemm_launches(ceil_div(g.n, DB_COLS), 256, [&](const int64_t first, const dim3 grid) {
+      hipLaunchKernelGGL((linear_db_kernel<O>), grid, dim3(256), 0, g.st, (const float*)sums, lay.strips, g.n, (O*)g.db, first);
+    });
   const bool want_dx = g.dx && g.m > 0 && g.k > 0, want_dw = g.dw && g.n > 0 && g.k > 0;
   if (!want_dx && !want_dw && !(g.db && g.n > 0) && !(dz && g.m > 0 && g.n > 0)) return MDET_OK;
   int status = launch_status();
@@ -247,7 +253,7 @@ int mdet_linear_workspace_query(int32_t dtype, int32_t backward, int64_t m, int6
 int mdet_linear_forward(int32_t dtype, int32_t activation, int64_t m, int64_t n, int64_t k, const void* x, int64_t ldx, const void* w,
                         int64_t ldw, const void* bias, const void* residual, int64_t ldr, void* y, int64_t ldy, void* z, int64_t ldz,
                         void* workspace, uint64_t workspace_bytes, void* stream) {
-  if (!is_type(dtype) || activation < MDET_ACT_NONE || activation > MDET_ACT_SILU || !sizes_fit(m, n, k)) return MDET_EINVAL;
+  if (!is_type(dtype) || activation < MDET_ACT_NONE || activation > MDET_ACT_SILU || !sizes_fit(m, n, k) || !tiles_fit(m, n)) return MDET_EINVAL;
   const int64_t s = size_of(dtype);
   if (!matrix_ok(x, m, k, ldx, s) || !matrix_ok(w, n, k, ldw, s) || !matrix_ok(y, m, n, ldy, s)) return MDET_EINVAL;
   if ((residual && !matrix_ok(residual, m, n, ldr, s)) || (z && !matrix_ok(z, m, n, ldz, s)) || (uintptr_t)bias % s) return MDET_EINVAL;
@@ -272,8 +278,8 @@ int mdet_linear_backward(int32_t dtype, int32_t grad_dtype, int32_t activation, 
   if (activation < MDET_ACT_NONE || activation > MDET_ACT_SILU || !sizes_fit(m, n, k)) return MDET_EINVAL;
   const int64_t s = size_of(dtype), gs = size_of(grad_dtype);
   if (!matrix_ok(dy, m, n, lddy, s) || (activation != MDET_ACT_NONE && !matrix_ok(z, m, n, ldz, s))) return MDET_EINVAL;
-  if (dx && (!matrix_ok(dx, m, k, lddx, s) || !matrix_ok(w, n, k, ldw, s))) return MDET_EINVAL;
-  if (dw && (!matrix_ok(dw, n, k, lddw, gs) || !matrix_ok(x, m, k, ldx, s))) return MDET_EINVAL;
+  if (dx && (!matrix_ok(dx, m, k, lddx, s) || !matrix_ok(w, n, k, ldw, s) || !tiles_fit(m, k))) return MDET_EINVAL;
+  if (dw && (!matrix_ok(dw, n, k, lddw, gs) || !matrix_ok(x, m, k, ldx, s) || !tiles_fit(n, k))) return MDET_EINVAL;
   if ((uintptr_t)db % gs || (dz && !matrix_ok(dz, m, n, lddz, s))) return MDET_EINVAL;
   uint64_t need = 0;
   mdet_linear_workspace_query(dtype, 1, m, n, k, &need);

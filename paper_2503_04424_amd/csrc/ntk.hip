@@ -44,8 +44,10 @@ inline uint64_t wide_bytes(int64_t rows, int64_t cols) { return up256((uint64_t)
 
 template <typename S>
 void widen(const void* from, int64_t ld, int64_t rows, int64_t cols, double* to, hipStream_t st) {
-  const int64_t ldto = ceil_div(cols, 2) * 2, blocks = ceil_div(rows * ldto, 256);
-  if (blocks > 0) hipLaunchKernelGGL(ntk_widen_kernel<S>, dim3((unsigned)blocks), dim3(256), 0, st, (const S*)from, ld, to, rows, cols, ldto);
+  const int64_t ldto = ceil_div(cols, 2) * 2;
+  gemm_launches(ceil_div(rows * ldto, 256), 256, [&](const int64_t first, const dim3 grid) {
+    hipLaunchKernelGGL(ntk_widen_kernel<S>, grid, dim3(256), 0, st, (const S*)from, ld, to, rows, cols, ldto, first);
+  });
 }
 
 struct Call {
@@ -110,7 +112,7 @@ int gram_tiles(NtkLayers<T>& list, const Call& c, int accumulate, void* first, R
   if (range.count < 0) range.count = blocks;
   const int64_t all = ceil_div(range.count * (PARTS ? 4 : 1), 8) * 8;
   const int64_t firsts = c.d > 1 ? ceil_div(ntk_blocks(ceil_div(c.n, S::BM)) * list.count, 8) * 8 : 0;
-  if (all > INT32_MAX || firsts > INT32_MAX) return MDET_EINVAL;
+  if (all > (int64_t)UINT32_MAX / S::THREADS || firsts > (int64_t)UINT32_MAX / S::THREADS) return MDET_EINVAL;    // threads of a launch
   using std::false_type;
   using std::true_type;
   auto gram = [&](auto direct, auto several) {

@@ -162,3 +162,14 @@ assert L.mdet_linear_backward({dtype}, {dtype}, 0, 0, 0, 100000, A, 0, None, 0, 
 """
     done = subprocess.run([sys.executable, "-c", code], cwd=os.path.dirname(os.path.dirname(os.path.abspath(__file__))), capture_output=True, text=True, timeout=300)
     assert done.returncode == 0, (done.returncode, done.stderr[-500:])
+
+
+def test_products_beyond_a_launch_are_refused(M):
+    """A launch holds fewer than 2^32 threads; such a product is refused before anything is queued.  (These rows are single
+    elements: 2147483616 of them would be 2^32 threads.)"""
+    tall = (1 << 31) - 32
+    for m, n in ((tall, 1), (1, tall), (tall, 32), (1 << 18, (1 << 18) + 1)):
+        assert forward(M, m=m, n=n, k=1, ldx=1, ldw=1, ldy=n) == EINVAL
+    call = dict(n=1, k=1, lddy=1, ldx=1, ldw=1, lddx=1, lddw=1, ws=A, wsb=1 << 62)
+    assert backward(M, m=tall, dw=None, **call) == EINVAL
+    assert backward(M, **{**call, "m": 1, "n": tall, "lddy": tall, "dx": None}) == EINVAL
