@@ -66,6 +66,7 @@ extern "C" int mdet_adamw_step(const mdet_adamw_params* a, const mdet_adamw_tens
   f.rate = (float)(a->lr / (1.0 - std::pow(a->beta1, (double)a->step)));
   f.root = (float)(1.0 / std::sqrt(1.0 - std::pow(a->beta2, (double)a->step)));
   f.eps = (float)a->eps;
+  if (!std::isfinite(f.keep) || !std::isfinite(f.rate) || !std::isfinite(f.eps)) return MDET_EINVAL;     // beyond fp32
   f.grad_scale = a->grad_scale;
   f.seed = a->seed;
   hipStream_t st = (hipStream_t)stream;

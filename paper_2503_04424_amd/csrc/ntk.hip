@@ -184,7 +184,9 @@ int mdet_ntk_gram(int32_t dtype, int32_t out_dtype, int64_t n, int64_t outputs, 
                   double scale, int32_t accumulate, void* K, int64_t ldk, void* workspace, uint64_t workspace_bytes, void* stream) {
   int status = check(dtype, out_dtype, n, outputs, layers, count, true);
   if (status != MDET_OK) return status;
-  if (!std::isfinite(bias) || !std::isfinite(scale)) return MDET_EINVAL;
+  // in the type of the arithmetic
+  auto finite = [&](double x) { return out_dtype == MDET_F32 ? std::isfinite((float)x) : std::isfinite(x); };
+  if (!finite(bias) || !finite(scale)) return MDET_EINVAL;
   const int64_t N = n * outputs;
   if (N == 0) return MDET_OK;
   if (!K || (uintptr_t)K % size_of(out_dtype) || (N > 1 && ldk < N) || ldk > MOST) return MDET_EINVAL;

@@ -173,3 +173,11 @@ def test_products_beyond_a_launch_are_refused(M):
     call = dict(n=1, k=1, lddy=1, ldx=1, ldw=1, lddx=1, lddw=1, ws=A, wsb=1 << 62)
     assert backward(M, m=tall, dw=None, **call) == EINVAL
     assert backward(M, **{**call, "m": 1, "n": tall, "lddy": tall, "dx": None}) == EINVAL
+
+
+def test_factors_beyond_the_arithmetics_type_are_refused(M):
+    """Finite in 64 bits, infinite in the 32 that they are used in: every result would be infinite or NaN."""
+    for bad in (dict(bias=1e39), dict(scale=-1e200), dict(scale=3.5e38)):
+        assert ntk(M, **bad) == EINVAL
+    for bad in (dict(lr=1e39), dict(lr=1e38, beta1=0.999), dict(lr=1e30, weight_decay=1e30), dict(eps=1e39)):
+        assert adamw(M, **bad) == EINVAL
