@@ -22,50 +22,83 @@ constexpr float ACT_TANH_A = 0.79788456080286536f, ACT_TANH_B = 0.044715f;
 __device__ __forceinline__ float act_clamp(float z, float least, float most) {
   return z < least ? least : z > most ? most : z;
 }
-__device__ __forceinline__ float logistic(float t) { return 1.0f / (1.0f + __expf(-t)); }
 
-// Phi(z) and e = exp(-z^2 / 2), |z| <= 20.  With x = |z| / sqrt(2) and t = 1 / (1 + p x), 1 - erf(x) is exp(-x^2) times a polynomial
-// of degree 5 in t to 1.5e-7 (Abramowitz and Stegun, 7.1.26): a third of erff's instructions, which as the tail of a
-// large product cost 10 % of its time, and no branch.  Half of that error is 2^-23.7 of a factor that goes up to 1.
-__device__ __forceinline__ float normal_cdf(const float z, float& e) {
-  const float x = fabsf(z) * ACT_R2, t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
-  e = __expf(-x * x);
-  const float q = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
-  return z < 0.0f ? q : 1.0f - q;
+// 1 / (1 + exp(-t)).  For operands in fp32 without an exponential that overflows: what is small has its digits down to the least number.
+template <typename T>
+__device__ __forceinline__ float logistic(const float t) {
+  if constexpr (sizeof(T) == 4) {
+    const float e = expf(-fabsf(t));
+    return (t < 0.0f ? e : 1.0f) * __builtin_amdgcn_rcpf(1.0f + e);
+  } else return 1.0f / (1.0f + __expf(-t));
 }
 
-template <int ACT>
+// Phi(z) and e = exp(-z^2 / 2), |z| <= 20.  1 - erf(x), x = |z| / sqrt(2), is exp(-x^2) times a polynomial in t = 1 / (1 + p x): a third of
+// erff's instructions, which as the tail of a large product cost 10 % of its time, and no branch.
+//
+// For operands in 16 bits degree 5 to 1.5e-7 in all (Abramowitz and Stegun, 7.1.26).  Half of that error is 2^-23.7 of a factor that
+// goes up to 1; of a small factor it is a larger part (5e-4 at z = -4, 2e-3 at -5), where rounding to 16 bits is one of up to
+// 4e-3 (bf16) or 5e-4.
+//
+// For fp32 degree 8 to 4.4e-8 of the factor itself, however small: the best polynomial in that sense for t exp(x^2) (1 - erf(x)) over
+// 0 <= x <= 14.2 (Remez exchange), p = 1/2.  erfcf in its place takes 89 us for 4096 x 8192 x 64 and 975 for 4096^3; this, 70 and 966.
+template <typename T>
+__device__ __forceinline__ float normal_cdf(const float z, float& e) {
+  const float x = fabsf(z) * ACT_R2;
+  if constexpr (sizeof(T) == 4) {
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.5f * x);
+    e = __expf(-0.5f * z * z);
+    float q = -0.059386346489f;
+    q = q * t + 0.286123484373f;
+    q = q * t - 0.490405529737f;
+    q = q * t + 0.281732559204f;
+    q = q * t - 0.029148206115f;
+    q = q * t + 0.203752472997f;
+    q = q * t + 0.242835104465f;
+    q = q * t + 0.282412111759f;
+    q = q * t + 0.282084345818f;
+    q *= 0.5f * e * t;
+    return z < 0.0f ? q : 1.0f - q;
+  } else {
+    const float t = __builtin_amdgcn_rcpf(1.0f + 0.3275911f * x);
+    e = __expf(-x * x);
+    const float q = 0.5f * e * t * (0.254829592f + t * (-0.284496736f + t * (1.421413741f + t * (-1.453152027f + t * 1.061405429f))));
+    return z < 0.0f ? q : 1.0f - q;
+  }
+}
+
+// T: type of the operands.
+template <typename T, int ACT>
 __device__ __forceinline__ float act_value(const float z) {
   if constexpr (ACT == MDET_ACT_RELU) return z < 0.0f ? 0.0f : z;
   else if constexpr (ACT == MDET_ACT_GELU) {
     const float c = z < -20.0f ? -20.0f : z;         // the factor is zero there already
     float e;
-    return c * normal_cdf(c > 20.0f ? 20.0f : c, e);
+    return c * normal_cdf<T>(c > 20.0f ? 20.0f : c, e);
   } else if constexpr (ACT == MDET_ACT_GELU_TANH) {
     const float c = z < -20.0f ? -20.0f : z;
     const float t = act_clamp(c, -20.0f, 20.0f);     // (1 + tanh(u)) / 2 = logistic(2 u)
-    return c * logistic(2.0f * ACT_TANH_A * (t + ACT_TANH_B * t * t * t));
+    return c * logistic<T>(2.0f * ACT_TANH_A * (t + ACT_TANH_B * t * t * t));
   } else if constexpr (ACT == MDET_ACT_SILU) {
     const float c = z < -80.0f ? -80.0f : z;
-    return c * logistic(c);
+    return c * logistic<T>(c);
   } else return z;
 }
 
-template <int ACT>
+template <typename T, int ACT>
 __device__ __forceinline__ float act_slope(const float z) {
   if constexpr (ACT == MDET_ACT_RELU) return z > 0.0f ? 1.0f : z <= 0.0f ? 0.0f : z;
   else if constexpr (ACT == MDET_ACT_GELU) {
     const float c = act_clamp(z, -20.0f, 20.0f);
     float e;
-    const float cdf = normal_cdf(c, e);
+    const float cdf = normal_cdf<T>(c, e);
     return cdf + c * e * ACT_R2PI;
   } else if constexpr (ACT == MDET_ACT_GELU_TANH) {
     const float c = act_clamp(z, -20.0f, 20.0f);
-    const float q = logistic(2.0f * ACT_TANH_A * (c + ACT_TANH_B * c * c * c));
+    const float q = logistic<T>(2.0f * ACT_TANH_A * (c + ACT_TANH_B * c * c * c));
     return q + 2.0f * c * q * (1.0f - q) * ACT_TANH_A * (1.0f + 3.0f * ACT_TANH_B * c * c);
   } else if constexpr (ACT == MDET_ACT_SILU) {
     const float c = act_clamp(z, -80.0f, 80.0f);
-    const float q = logistic(c);
+    const float q = logistic<T>(c);
     return q * (1.0f + c * (1.0f - q));
   } else return 1.0f;
 }
@@ -101,7 +134,7 @@ template <typename T, typename O, int ACT>
 __device__ __forceinline__ void linear_put(const LinearOut<T, O>& o, const int64_t i, const int64_t j, float v) {
   if (o.bias) v += (float)o.bias[j];
   if (o.z) o.z[i * o.ldz + j] = (T)v;
-  v = act_value<ACT>(v);
+  v = act_value<T, ACT>(v);
   if (o.residual) v += (float)o.residual[i * o.ldr + j];
   o.y[i * o.ldy + j] = (O)v;
 }
@@ -132,7 +165,7 @@ __device__ __forceinline__ void linear_put4(const LinearOut<T, O>& o, const int6
     *reinterpret_cast<t4*>(o.z + i * o.ldz + j) = z;
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) v[e] = act_value<ACT>(v[e]);
+  for (int e = 0; e < 4; ++e) v[e] = act_value<T, ACT>(v[e]);
   if (o.residual) {
     const t4 r = *reinterpret_cast<const t4*>(o.residual + i * o.ldr + j);
 #pragma unroll
@@ -356,7 +389,7 @@ __global__ __launch_bounds__(256) void linear_dz_kernel(const T* __restrict__ dy
 #pragma unroll
       for (int e = 0; e < VEC; ++e) {
         float v = (float)y[r][e];
-        if constexpr (ACT != MDET_ACT_NONE) v *= act_slope<ACT>((float)a[r][e]);
+        if constexpr (ACT != MDET_ACT_NONE) v *= act_slope<T, ACT>((float)a[r][e]);
         if (row + 16 * r < rows) sum[e] += v;
         d[e] = (T)v;
       }
