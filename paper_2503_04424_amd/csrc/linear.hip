@@ -5,13 +5,13 @@
 #include <type_traits>
 
 #include "kernels_linear.h"
+#include "linear_cut.h"
 
 namespace {
 
 using namespace mdet;
 
 inline uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
-inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 inline int64_t size_of(int32_t t) { return t == MDET_F32 ? 4 : 2; }
 inline bool is_type(int32_t t) { return t == MDET_F32 || t == MDET_F16 || t == MDET_BF16; }
 inline int launch_status() { return hipGetLastError() == hipSuccess ? MDET_OK : MDET_EHIP; }
@@ -53,10 +53,6 @@ typedef Tile<64, 64, 2, 2, 2> Small;
 typedef Tile<64, 64, 2, 2, 4> Ahead;
 typedef Tile<32, 32, 2, 2, 4> Tiny;
 
-// Few rows: W is read once.  Beyond 8192 rows of W a split sum over tiles is as fast for one row (16384 x 4096 bf16 22.3 us,
-// 23.7 this way) and faster for sixteen (23.4, 32.2), as it is for more rows at any size (17 rows of 4096 x 4096 11.5 us).
-inline bool few_rows(int64_t rows, int64_t cols) { return rows <= 16 && cols <= 8192; }
-
 template <typename T, typename O>
 void rows_product(const Operand<T>& r, const Operand<T>& c, int64_t k, const LinearOut<T, O>& out, hipStream_t st) {
   const dim3 grid((unsigned)ceil_div(out.cols, 16));
@@ -64,35 +60,6 @@ void rows_product(const Operand<T>& r, const Operand<T>& c, int64_t k, const Lin
   else hipLaunchKernelGGL((linear_rows_kernel<T, O, 4>), grid, dim3(256), 0, st, r, c, k, out);
 }
 
-// How a product is cut: tile shape and parts of the sum over k.
-struct Cut {
-  int tile;                            // rows and columns of a tile: 32, 64, 128 or 256; 0: few rows
-  int splits;
-  int64_t kpart;
-};
-Cut cut_of(int64_t rows, int64_t cols, int64_t k, int64_t size, bool inner) {
-  Cut c;
-  if (inner && few_rows(rows, cols)) return Cut{0, 1, k};
-  const int64_t bk = 128 / size;
-  auto tiles = [&](int64_t b) { return ceil_div(rows, b) * ceil_div(cols, b); };
-  // The largest tile with which the device is full.  In 16 bits larger tiles also need less of LDS and cache for a product
-  // (2500^3, 400 tiles of 128: 59 us, 80 with 64; 2048^3, 256 of them: 28 and 27, k outer 34 and 29); in fp32 the matrix
-  // cores are slow enough for the small tile, whose workgroups even out (2500^3 303 and 266 us, 4096^3 962 us with 128).
-  c.tile = size == 2 && tiles(256) >= 192 ? 256 : tiles(128) > (size == 2 ? 256 : 800) ? 128 : tiles(64) >= 256 ? 64 : 32;
-  c.splits = 1;
-  c.kpart = k;
-  const int64_t t = tiles(c.tile);
-  if (c.tile <= 64 && t > 0 && t < 256 && k >= 8 * bk) {
-    int64_t most = k / (4 * bk), want = ceil_div(512, t);
-    int64_t s = want < most ? want : most;
-    if (s > 16) s = 16;
-    if (s > 1) {
-      c.kpart = ceil_div(ceil_div(k, s), bk) * bk;
-      c.splits = (int)ceil_div(k, c.kpart);
-    }
-  }
-  return c;
-}
 uint64_t parts_bytes(const Cut& c, int64_t rows, int64_t cols) { return c.splits > 1 ? up256((uint64_t)c.splits * rows * cols * 4) : 0; }
 
 template <typename T, typename O, typename S, bool ROUTER, bool COUTER>
