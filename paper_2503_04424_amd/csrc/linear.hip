@@ -75,10 +75,11 @@ void tiles(Operand<T> r, Operand<T> c, int64_t k, const LinearOut<T, O>& out, co
   };
   using std::false_type;
   using std::true_type;
+  // sums are split for the smallest tile alone (cut_of): the others are taken where there are enough of them
   if (cut.splits > 1) {
-    if constexpr (S::BM <= 64) {
+    if constexpr (std::is_same<S, Tiny>::value) {
       if (direct) go(true_type{}, true_type{});
-      else if constexpr (!std::is_same<S, Ahead>::value) go(false_type{}, true_type{});
+      else go(false_type{}, true_type{});
       const int64_t groups = ceil_div(out.rows * ceil_div(out.cols, 4), 256);
       hipLaunchKernelGGL((linear_join_kernel<T, O>), dim3((unsigned)groups), dim3(256), 0, st, (const float*)parts, cut.splits, out);
     }
@@ -98,7 +99,7 @@ int product(Operand<T> r, Operand<T> c, int64_t k, LinearOut<T, O> out, float* p
   else if (cut.tile == 64) {
     // three slabs on their way in 16 bits, where they last shortest, as long as all of the workgroups have room for them
     // at once (512 x 4096 x 4096 33 us with one, 28.5 with three)
-    const int64_t n = ceil_div(out.rows, 64) * ceil_div(out.cols, 64) * cut.splits;
+    const int64_t n = ceil_div(out.rows, 64) * ceil_div(out.cols, 64);
     const bool straight = gemm_operand<T, ROUTER, 64>(r.p, r.stride, r.rows, k).straight && gemm_operand<T, COUTER, 64>(c.p, c.stride, c.rows, k).straight;
     if (sizeof(T) == 2 && n <= 512 && straight) {
       if constexpr (sizeof(T) == 2) tiles<T, O, Ahead, ROUTER, COUTER>(r, c, k, out, cut, parts, st);

@@ -28,7 +28,7 @@ inline Cut cut_of(int64_t rows, int64_t cols, int64_t k, int64_t size, bool inne
   c.splits = 1;
   c.kpart = k;
   const int64_t t = tiles(c.tile);
-  if (c.tile <= 64 && t > 0 && t < 256 && k >= 8 * bk) {
+  if (c.tile == 32 && t > 0 && t < 256 && k >= 8 * bk) {
     int64_t most = k / (4 * bk), want = ceil_div(512, t);
     int64_t s = want < most ? want : most;
     if (s > 16) s = 16;

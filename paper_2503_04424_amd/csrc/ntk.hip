@@ -93,9 +93,11 @@ int gram_tiles(NtkLayers<T>& list, const Call& c, int accumulate, void* first, R
     (a.straight ? yes_a : no_a) += list.p[l];
     (g.straight ? yes_g : no_g) += list.q[l];
   }
-  // in fp64 the large tile has no registers left for operands that pass through them
-  constexpr bool REGISTERS = !(std::is_same<T, double>::value && S::BM == 128);
-  if constexpr (!REGISTERS) {
+  // In fp64 the large tile has no registers left for operands that pass through them; quarters come behind large blocks that went
+  // straight.  In 16 bits large blocks, and so quarters, are for several outputs.
+  constexpr bool REGISTERS = !(std::is_same<T, double>::value && (S::BM == 128 || PARTS));
+  constexpr bool ONE = !(sizeof(T) == 2 && (S::BM == 128 || PARTS));
+  if constexpr (!REGISTERS && !PARTS) {
     if (no_g > yes_g / 8 || (c.d > 1 && no_a > yes_a / 8) || (c.d == 1 && no_a + no_g > (yes_a + yes_g) / 8))
       return gram_tiles<T, Small>(list, c, accumulate, first);
   }
@@ -130,8 +132,10 @@ int gram_tiles(NtkLayers<T>& list, const Call& c, int accumulate, void* first, R
     }
     if (no_g <= yes_g / 8) gram(true_type{}, true_type{});
     else if constexpr (REGISTERS) gram(false_type{}, true_type{});
-  } else if (no_a + no_g <= (yes_a + yes_g) / 8) gram(true_type{}, false_type{});
-  else if constexpr (REGISTERS) gram(false_type{}, false_type{});
+  } else if constexpr (ONE) {
+    if (no_a + no_g <= (yes_a + yes_g) / 8) gram(true_type{}, false_type{});
+    else if constexpr (REGISTERS) gram(false_type{}, false_type{});
+  }
   return launch_status();
 }
 
