@@ -6,9 +6,14 @@ namespace mdet {
 
 inline int64_t ceil_div(int64_t a, int64_t b) { return (a + b - 1) / b; }
 
-// Few rows: W is read once.  Beyond 8192 rows of W a split sum over tiles is as fast for one row (16384 x 4096 bf16 22.3 us,
-// 23.7 this way) and faster for sixteen (23.4, 32.2), as it is for more rows at any size (17 rows of 4096 x 4096 11.5 us).
-inline bool few_rows(int64_t rows, int64_t cols) { return rows <= 16 && cols <= 8192; }
+// Few rows of x: a kernel of their own reads W once, in place of tiles, which take the same time for 1 as for 32 rows.  Each with W out of
+// memory, for 1, 4 and 16 rows, in us (tiles): bf16 4096 x 4096 8.7, 9.1, 11.0 (11.8); 8192 x 4096 14.1, 14.7, 19.3 (18.2); 16384 x 4096
+// 24.7, 25.9, 36 (31); 9000 x 8192 34, 37.6, 51 (36.6); 40000 x 4096 55, 59, 84 (79).  fp32 8192 x 4096 26.7, 27.0, 37 (39); 16384 x 4096
+// 50, 50, 70 (123); 40000 x 1024 38, 41, 52 (52).  In 16 bits a 16-row product of a long W is bound by the rows' own loads.
+// The last condition keeps a launch below 2^32 threads.
+inline bool few_rows(int64_t rows, int64_t cols, int64_t size) {
+  return rows <= 16 && (size == 4 || rows <= 4 || cols <= 8192) && cols <= (int64_t(1) << 25);
+}
 
 // How a product is cut: tile shape and parts of the sum over k.
 struct Cut {
@@ -18,7 +23,7 @@ struct Cut {
 };
 inline Cut cut_of(int64_t rows, int64_t cols, int64_t k, int64_t size, bool inner) {
   Cut c;
-  if (inner && few_rows(rows, cols)) return Cut{0, 1, k};
+  if (inner && few_rows(rows, cols, size)) return Cut{0, 1, k};
   const int64_t bk = 128 / size;
   auto tiles = [&](int64_t b) { return ceil_div(rows, b) * ceil_div(cols, b); };
   // The largest tile with which the device is full.  In 16 bits larger tiles also need less of LDS and cache for a product

@@ -88,3 +88,14 @@ def test_same_bits_each_time(M, dtype, m, n, k):
         got = (M.mdet_linear_forward(x, w, bias, residual, "gelu"), *M.mdet_linear_backward(dy, x, w, z, "gelu"))
         first = first or got
         assert all(torch.equal(a, b) for a, b in zip(got, first))
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16, torch.float32], ids=str)
+@pytest.mark.parametrize("m,n,k", [(1, 9001, 1001), (4, 16384, 2048), (5, 9001, 520), (16, 10000, 2049), (2, 33000, 64), (17, 9001, 520)])
+def test_few_rows_of_a_long_layer(M, m, n, k, dtype):
+    """Up to four rows (16 in fp32) by the kernel that reads W once, the others by tiles."""
+    for pad, shift in PLACES:
+        x, w, bias, residual = operands(m, n, k, dtype, m + n, pad, shift)
+        y = M.mdet_linear_forward(x, w, bias, residual, "silu")
+        want, _, err, _ = forward64(x, w, bias, residual, "silu")
+        check(y, want, err, dtype, f"pad {pad} shift {shift}")

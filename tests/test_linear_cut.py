@@ -51,3 +51,14 @@ def test_parts_cover_the_sum(cut):
         assert tile in (0, 32, 64, 128, 256) and (tile or (inner and rows <= 16)) and (tile != 256 or itemsize == 2)
         assert 1 <= parts <= 16 and parts * each >= k and ((parts - 1) * each < k or parts == 1)
         assert parts == 1 or each % (128 // itemsize) == 0
+
+
+def test_single_tokens_read_w_once_however_long_it_is(cut):
+    """One to four rows at any number of columns, up to 16 in fp32 or of a shorter W: no tile."""
+    for size in (2, 4):
+        for cols in (1, 8192, 8193, 151936, 1 << 25):
+            got = [t for t, _, _ in cut([(m, cols, 4096, size, 1) for m in range(1, 18)])]
+            few = 16 if size == 4 or cols <= 8192 else 4
+            assert got[:few] == [0] * few and all(got[few:])
+        assert cut([(1, (1 << 25) + 1, 64, size, 1)])[0][0]          # beyond a launch of fewer than 2^32 threads
+        assert all(t for t, _, _ in cut([(m, 100, 4096, size, 0) for m in range(1, 17)]))
