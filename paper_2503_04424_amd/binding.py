@@ -662,11 +662,17 @@ def _operator_stream(stream, gpu):
     return _raw_stream(gpu)
 
 
+_one_gpu = None
+
+
 def _queue(gpu, entry, *args):
     """An entry point that queues work, with the GPU of its tensors as the current one: a kernel goes to the current one, and
     the default stream has the same handle on all."""
+    global _one_gpu
     cuda = sys.modules["torch"].cuda           # the tensors are torch's: it is there, and an import statement would cost more
-    if gpu == cuda.current_device():
+    if _one_gpu is None:
+        _one_gpu = cuda.device_count() == 1
+    if _one_gpu or gpu == cuda.current_device():
         _check_status(entry(*args))
     else:
         with cuda.device(gpu):
@@ -678,10 +684,18 @@ def _check_status(st):
         raise MemdetError(st)
 
 
+_raise_version = None
+
+
 def _written(*tensors):
     """The caller's tensors that a call has written through their addresses: autograd refuses a gradient that goes through a
     value from before, as after any other operation in place."""
-    sys.modules["torch"].autograd.graph.increment_version(tensors)
+    global _raise_version
+    if _raise_version is None:
+        import torch
+        # without the wrapper's checks where torch offers it: half of the time
+        _raise_version = getattr(torch._C, "_increment_version", None) or torch.autograd.graph.increment_version
+    _raise_version(tensors)
 
 
 def _new(stream, make):
