@@ -150,14 +150,16 @@ int gram(const mdet_ntk_layer* layers, int32_t count, const Call& c, void* first
       list.a[l] = (const T*)x.a, list.lda[l] = x.lda, list.p[l] = x.p;
       list.g[l] = (const T*)x.g, list.ldg[l] = x.ldg, list.q[l] = x.q;
     }
-    // Several workgroups a compute unit, and so the 64 x 64 tile, are better than one large one (fp32 n = 8192, three layers:
-    // 1.48 ms, 1.65 with 128 x 128; fp64 n = 4096 54 and 47 TFLOP/s) except at the largest orders in fp64 (n = 8192 62.0 TFLOP/s,
-    // 59.6 with the small tile, both before its last blocks went out in quarters) and in 16 bits with several outputs (order 10000
-    // 433 us, 461, both before the first factors went through LDS).  A few small blocks would leave most
-    // compute units without one: n = 512 in fp32 21 us with the 32 x 32 tile, 35 with 64 x 64, in fp64 29 and 63.
+    // Several workgroups a compute unit, and so the 64 x 64 tile, are better than one large one in fp32 (n = 8192, three layers:
+    // 1.48 ms, 1.65 with 128 x 128) and at small orders.  In us, 128 x 128 and 64 x 64, fp64 with three layers of 512 to 784:
+    // one output order 2048 346, 305; 3000 482, 507; 4096 826, 894; 6000 1595, 1771; 8192 2866, 3200; 12000 6016, 6774; three
+    // outputs 3000 294, 260; 4500 499, 494; 6000 830, 876; 9000 1730, 1863.  bf16, ten outputs of four layers: 4000 103, 80; 6000 156,
+    // 147; 7000 205, 194; 8000 240, 252; 10000 366, 384; 16000 869, 932; three outputs: 3000 63, 50; 4500 88, 92; 6000 140, 142;
+    // 9000 275, 303.  A few small blocks would leave most compute units without one: n = 512 in fp32 21 us with the 32 x 32 tile, 35
+    // with 64 x 64, in fp64 29 and 63.
     const int64_t order = c.n * c.d;
     int status;
-    if (order >= 8000 && c.d != 2 && (sizeof(T) == 8 || (sizeof(T) == 2 && c.d > 1))) {
+    if (order >= (sizeof(T) == 8 ? 4500 : 8000) && c.d != 2 && (sizeof(T) == 8 || (sizeof(T) == 2 && c.d > 1))) {
       if constexpr (sizeof(T) != 4) status = gram_tiles<T, Large>(list, c, accumulate, first);
     } else if (sizeof(T) != 2 && order < 1500) {
       if constexpr (sizeof(T) != 2) status = gram_tiles<T, Tiny>(list, c, accumulate, first);

@@ -16,6 +16,7 @@ CASES = [
     (F64, F64, 1601, 1), (F64, F64, 530, 3), (F64, F64, 4010, 2),                    # 64 x 64
     (F64, F64, 700, 1), (F64, F64, 120, 10),                                       # 32 x 32
     (F64, F64, 8010, 1), (F64, F64, 8200, 1), (F64, F64, 2690, 3),                   # 128 x 128, with quarters and without
+    (F64, F64, 4499, 1), (F64, F64, 4500, 1), (F64, F64, 1501, 3), (F64, F64, 470, 10),   # on both sides of the choice
     (F32, F64, 1601, 1), (F32, F64, 2690, 3), (BF16, F64, 530, 3),                   # widened
     (BF16, F32, 1601, 1), (F16, F32, 530, 3), (F16, F32, 4010, 2),                   # 64 x 64
     (BF16, F32, 811, 10), (F16, F32, 2690, 3), (BF16, F32, 1200, 7),                 # 128 x 128
