@@ -598,7 +598,7 @@ def mdet_flodance_eval(coef, q, n_values, out=None, stream=None):
 
 
 _TYPE_CODES = {}
-_GPU, _DTYPE = operator.methodcaller("get_device"), operator.attrgetter("dtype")
+_DTYPE = operator.attrgetter("dtype")
 
 
 def _type_code(dtype) -> int:
@@ -805,7 +805,7 @@ def _adamw_pointers(tensors, name, dtype, sizes, gpu):
     """Addresses of contiguous tensors of one type and these sizes on this GPU."""
     from torch import Tensor
     if list(map(Tensor.numel, tensors)) != sizes or not all(map(Tensor.is_contiguous, tensors)) or \
-            set(map(_GPU, tensors)) != {gpu} or set(map(_DTYPE, tensors)) != {dtype}:
+            set(map(Tensor.get_device, tensors)) != {gpu} or set(map(_DTYPE, tensors)) != {dtype}:
         raise ValueError(f"{name}: contiguous tensors of {dtype} with {sizes} elements on cuda:{gpu} expected, not "
                          f"{[(tuple(t.shape), t.dtype, str(t.device)) for t in tensors]}")
     return map(Tensor.data_ptr, tensors)
@@ -823,7 +823,7 @@ def mdet_adamw_step(params, grads, exp_avg, exp_avg_sq, *, lr, step, beta1=0.9, 
         if any(len(v) for v in (grads, exp_avg, exp_avg_sq)):
             raise ValueError("no params, but other tensors")
         return
-    sizes = [t.numel() for t in params]
+    sizes = list(map(torch.Tensor.numel, params))
     gpu = _gpu(params[0], "params")
     wide = scales is None
     a = _AdamwParams()
@@ -848,7 +848,7 @@ def mdet_adamw_step(params, grads, exp_avg, exp_avg_sq, *, lr, step, beta1=0.9, 
         sizes)
     table = array.array("Q", itertools.chain.from_iterable(zip(*fields)))
     _queue(gpu, load().mdet_adamw_step, C.byref(a), table.buffer_info()[0], count, _operator_stream(stream, gpu))
-    _written(*params, *(copies or ()))
+    _written(*params) if copies is None else _written(*params, *copies)
 
 
 def _ntk_layers(inputs, signals, outputs):

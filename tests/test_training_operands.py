@@ -15,8 +15,11 @@ class OnGpu(torch.Tensor):
     is_cuda = property(lambda self: self.gpu >= 0)
     device = property(lambda self: torch.device("cuda", self.gpu) if self.gpu >= 0 else torch.device("cpu"))
 
-    def get_device(self):
-        return self.gpu
+    @classmethod
+    def __torch_function__(cls, func, types, args=(), kwargs=None):
+        if func is torch.Tensor.get_device:
+            return args[0].gpu
+        return super().__torch_function__(func, types, args, kwargs or {})
 
 
 def on(gpu, *shape, dtype=torch.float32):
