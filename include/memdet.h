@@ -548,8 +548,9 @@ int mdet_flodance_eval(const double* coef, int32_t q, const double* n_values, in
  * The matrices whose log-determinants this library takes are Gram matrices J J^T of a network's
  * Jacobian (the NTK, Sec. 2.1).  These operators are the step in front: dense layers and their
  * gradients, an optimiser step, and the Gram matrix itself, on the GPU.  All pointers are DEVICE
- * pointers unless said otherwise; matrices are row-major with any leading dimension and only need
- * the alignment of their elements; the caller owns every buffer.  Each call only queues kernels on
+ * pointers unless said otherwise, on the device that is current; matrices are row-major, with a leading
+ * dimension of their row's length or more, and only need the alignment of their elements; the caller owns
+ * every buffer, and outputs overlap no other operand unless said otherwise.  Each call only queues kernels on
  * `stream` (a hipStream_t or NULL), allocates nothing and returns MDET_EINVAL for inconsistent
  * arguments, MDET_ENOMEM_DEVICE for a workspace that is too small and MDET_EHIP if a launch failed.
  * A workspace starts on 256 bytes.  Sizes of zero are allowed: an empty sum is zero, a call
@@ -620,14 +621,17 @@ typedef struct mdet_adamw_params {
 /* m <- beta1 m + (1 - beta1) g, v <- beta2 v + (1 - beta2) g^2,
  * p <- p (1 - lr weight_decay) - lr mhat / (sqrt(vhat) + eps) with mhat = m / (1 - beta1^step) and
  * vhat = v / (1 - beta2^step), on `count` tensors (a HOST array), in fp32.  8-bit states are rounded up
- * or down at random, with a mean that is what is rounded; a gradient that is not finite makes the
- * 256 elements of its scale NaN at the next step.  Up to 48 tensors share a launch. */
+ * or down at random: the means of m and of the root of v are what is rounded (a root below one code is
+ * held at one; v, the square, comes out larger by the rounding's variance, which raises roots of 2 % of
+ * their block's largest by 6 %).  A gradient that is not finite makes the 256 elements of its scale NaN at
+ * the next step.  Up to 48 tensors share a launch. */
 int mdet_adamw_step(const mdet_adamw_params* params, const mdet_adamw_tensor* tensors, int64_t count,
                     void* stream);
 
-/* What a dense layer z = W a + b of a network with `outputs` outputs contributes to the Jacobian on
- * n samples: its inputs a (n x p, leading dimension lda) and the derivatives g of the network's
- * outputs by z (n * outputs x q, leading dimension ldg; row i * outputs + r: output r at sample i). */
+/* What a dense layer z = W a + b of a network with `outputs` outputs, applied once a sample, contributes
+ * to the Jacobian on n samples (weights shared over positions would need sums over pairs of them): its
+ * inputs a (n x p, leading dimension lda) and the derivatives g of the network's outputs by z
+ * (n * outputs x q, leading dimension ldg; row i * outputs + r: output r at sample i). */
 typedef struct mdet_ntk_layer {
   const void* a;
   int64_t lda, p;

@@ -197,7 +197,8 @@ _linear = None
 
 def linear(x, w, bias=None, residual=None, activation="none"):
     """``act(x w^T + bias) + residual`` with its gradient (autograd): x (..., k), w (n, k), residual (..., n).
-    activation: 'none', 'relu', 'gelu', 'gelu_tanh' or 'silu'.  One launch or two for the whole layer."""
+    activation: 'none', 'relu', 'gelu', 'gelu_tanh' or 'silu'.  One launch or two for the layer, up to six for its gradient;
+    operands and gradients that are views of any kind, repeated rows among them, are laid out first where they have to be."""
     global _linear
     if x.dim() < 1 or w.dim() != 2:
         raise ValueError("x with rows of inputs as its last axis and a matrix w expected")

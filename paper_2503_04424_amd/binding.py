@@ -733,7 +733,7 @@ def mdet_linear_workspace_query(dtype, m, n, k, backward=False) -> int:
 def mdet_linear_forward(x, w, bias=None, residual=None, activation="none", out=None, preact=None, workspace=None,
                         stream=None):
     """``act(x w^T + bias) + residual`` on the GPU (asynchronous): x (m, k), w (n, k), bias (n,), residual (m, n), all
-    of one type (float32, float16 or bfloat16), rows of consecutive elements at any distance.  ``preact`` (m, n)
+    of one type (float32, float16 or bfloat16), rows of consecutive elements that do not overlap.  ``preact`` (m, n)
     receives x w^T + bias for the gradient; ``out`` may be ``residual``.  Returns out."""
     if x.dim() != 2 or w.dim() != 2:
         raise ValueError("x and w: matrices expected")

@@ -15,6 +15,11 @@
 // and the caller's seed.  A root that is not zero has a code of at least 1: a code of 0 would divide its m by eps.
 // This step's own update uses m and v before they are rounded.
 //
+// The mean of what is stored is the root that was rounded (from one code on).  The recurrence squares it, and the mean of the square is
+// larger by the rounding's variance, so roots far below their block's largest settle too high and their steps are shorter by as much:
+// with b2 = 0.999, normal gradients and 6000 steps (simulated) by 1 % at 10 % of the block's largest, 3 % at 5 %, 6 % at 2 %,
+// 12 % at 1 % and 30 % at half a per cent.
+//
 // What bounds it: bytes.  28 a element with states, parameters and gradients in 32 bits (67 million elements: 360 us,
 // 5.2 TB/s); with states in 8 bits, 16 and the two scales of a block (225 us, 4.9 TB/s), where the arithmetic is close behind.
 #pragma once
