@@ -31,7 +31,7 @@ def build(verbose: bool = False, extra=()) -> str:
         objects = [os.path.join(tmp, os.path.basename(s) + ".o") for s in SOURCES]
         with ThreadPoolExecutor(max_workers=4) as pool:
             list(pool.map(run, [[HIPCC] + compile_flags + ["-c", "-o", o, s] for s, o in zip(SOURCES, objects)]))
-        run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC", "-o", LIB] + objects)
+        run([HIPCC, "--offload-arch=gfx950", "-shared", "-fPIC"] + list(extra) + ["-o", LIB] + objects)
     return LIB
 
 
