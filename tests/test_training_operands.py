@@ -43,6 +43,7 @@ def library(monkeypatch):
     monkeypatch.setattr(B, "load", lambda: Library())
     monkeypatch.setattr(B, "mdet_linear_workspace_query", lambda *a, **k: 0)
     monkeypatch.setattr(torch.cuda, "current_device", lambda: 0)
+    monkeypatch.setattr(B, "_one_gpu", False)           # several, wherever this runs
     return called
 
 
