@@ -654,6 +654,69 @@ int mdet_ntk_workspace_query(int32_t dtype, int32_t out_dtype, int64_t n, int64_
                              const mdet_ntk_layer* layers, int32_t count, uint64_t* bytes);
 
 /* ------------------------------------------------------------------------
+ * Networks over tokens: both ends and what stands between the layers
+ *
+ * A network over tokens begins with a table's rows and ends in a loss over the whole vocabulary (whose matrix may be the same
+ * table); layer norms stand between its linear layers.  Terms as above.  Ids and targets are consecutive int32_t or int64_t
+ * (index_bits 32 or 64).  Every sum has one order: the same bits each time.
+ * ---------------------------------------------------------------------- */
+
+/* Device bytes of workspace for the gradient of a table (pure host code): n ids, vocab x width. */
+int mdet_embedding_workspace_query(int64_t n, int64_t vocab, int64_t width, uint64_t* bytes);
+
+/* y_i = scale table[ids_i]: table is vocab x width, y n x width, both of dtype (MDET_F32, MDET_F16 or MDET_BF16).  An id outside of
+ * the table gives a row of zeros.  n is below 2^31 - 1024, vocab below 2^31. */
+int mdet_embedding_forward(int32_t dtype, int32_t index_bits, int64_t n, int64_t vocab, int64_t width, const void* ids,
+                           const void* table, int64_t ldt, double scale, void* y, int64_t ldy, void* stream);
+
+/* Gradient of the same: dtable_v = scale (sum over i with ids_i = v of dy_i), zero where an id does not occur; or, with
+ * accumulate != 0, that added to what dtable holds (rows that do not occur are not touched).  dy is of dtype, dtable of grad_dtype:
+ * dtype or MDET_F32.  Sums are fp32, rounded once. */
+int mdet_embedding_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, int64_t n, int64_t vocab, int64_t width,
+                            const void* ids, const void* dy, int64_t lddy, double scale, int32_t accumulate, void* dtable,
+                            int64_t ldt, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Device bytes of workspace for the gradient of a layer norm over m rows of n elements (pure host code). */
+int mdet_layernorm_workspace_query(int32_t dtype, int64_t m, int64_t n, uint64_t* bytes);
+
+/* y = (x - mean) rstd weight + bias for each row, with its mean and rstd = 1 / sqrt(var + eps), var the mean of (x - mean)^2.  x, y
+ * (m x n), weight and bias (n elements; NULL for ones and zeros) are of dtype (MDET_F32, MDET_F16 or MDET_BF16); mean and rstd (m floats
+ * each, for the gradient) may be NULL.  eps >= 0.  n is at most 2^32.  A row without elements has the mean 0. */
+int mdet_layernorm_forward(int32_t dtype, int64_t m, int64_t n, const void* x, int64_t ldx, const void* weight, const void* bias,
+                           double eps, void* y, int64_t ldy, float* mean, float* rstd, void* stream);
+
+/* Gradient of the same, from its x, mean and rstd: with h = (x - mean) rstd and u = dy weight, dx = rstd (u - avg(u) - h avg(u h)),
+ * dw = column sums of dy h, db those of dy; any of dx, dw, db may be NULL (not wanted).  dw and db are of grad_dtype: dtype or
+ * MDET_F32.  The workspace is for dw and db alone. */
+int mdet_layernorm_backward(int32_t dtype, int32_t grad_dtype, int64_t m, int64_t n, const void* dy, int64_t lddy, const void* x,
+                            int64_t ldx, const float* mean, const float* rstd, const void* weight, void* dx, int64_t lddx, void* dw,
+                            void* db, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Device bytes of workspace for the cross entropy of m rows of k elements over a vocabulary of n (pure host code): the forward call,
+ * or with backward != 0 the gradient (up to 2^29 elements of e, or m x 4096 if that is more, at a time). */
+int mdet_xent_workspace_query(int32_t dtype, int32_t backward, int64_t m, int64_t n, int64_t k, uint64_t* bytes);
+/* Device bytes of `kept` (m x n elements of dtype and a little more). */
+int mdet_xent_kept_query(int32_t dtype, int64_t m, int64_t n, int64_t k, uint64_t* bytes);
+
+/* loss_i = lse_i - z_i,t_i with z = x w^T + bias and lse_i = log(sum over j of exp(z_ij)), in fp32, without z in memory: x is
+ * m x k, w n x k, bias n elements (or NULL), all of dtype (MDET_F32, MDET_F16 or MDET_BF16); loss and lse m floats, either may be
+ * NULL.  A row whose target is `ignore`, or outside of the vocabulary, does not count: its loss is 0.  Where `kept` is not NULL it
+ * receives what spares the gradient the product z, starts on 256 bytes, and no workspace is needed. */
+int mdet_xent_forward(int32_t dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const void* x, int64_t ldx, const void* w,
+                      int64_t ldw, const void* bias, const void* target, int64_t ignore, float* loss, float* lse, void* kept,
+                      uint64_t kept_bytes, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* Gradient of sum over i of dloss_i loss_i, from the forward call's lse, and what it kept (NULL: z is formed once more): with
+ * e_ij = dloss_i (exp(z_ij - lse_i) - [j = t_i]),  dx = e w,  dw = e^T x,  db = column sums of e; any of dx, dw, db may be NULL (not
+ * wanted).  dw and db are of grad_dtype: dtype or MDET_F32.  e is rounded to dtype in front of the two products (in MDET_F16 scaled by a
+ * power of two, so that small probabilities are not lost); db sums the unrounded one.  Nothing of a row that does not count comes through,
+ * whatever its x and dloss hold, not even NaN. */
+int mdet_xent_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const float* dloss,
+                       const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* target, int64_t ignore,
+                       const float* lse, const void* kept, uint64_t kept_bytes, void* dx, int64_t lddx, void* dw, int64_t lddw,
+                       void* db, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* ------------------------------------------------------------------------
  * Measuring sticks for the benchmark (asynchronous, enqueue only; DEVICE pointers).
  * ---------------------------------------------------------------------- */
 

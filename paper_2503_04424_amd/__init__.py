@@ -15,7 +15,10 @@ from .binding import (  # noqa: F401
     mdet_sequence_workspace_query, mdet_principal_logdets, mdet_flodance_fit, mdet_flodance_eval,
     ACTIVATIONS, mdet_linear_workspace_query, mdet_linear_forward, mdet_linear_backward, mdet_adamw_step,
     mdet_ntk_gram, mdet_ntk_workspace_query,
+    mdet_embedding_workspace_query, mdet_embedding_forward, mdet_embedding_backward,
+    mdet_layernorm_workspace_query, mdet_layernorm_forward, mdet_layernorm_backward,
+    mdet_xent_workspace_query, mdet_xent_kept_query, mdet_xent_forward, mdet_xent_backward,
     mdet_step_copy, mdet_step_mfma_peak, mdet_logdet_device_noalloc,
     pack_lower_block_columns, pack_general_block_columns,
 )
-from .api import memdet, parse_bytes, FitLogdet, linear, AdamW  # noqa: E402,F401
+from .api import memdet, parse_bytes, FitLogdet, linear, AdamW, embedding, layer_norm, linear_cross_entropy  # noqa: E402,F401

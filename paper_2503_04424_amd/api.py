@@ -213,6 +213,132 @@ def linear(x, w, bias=None, residual=None, activation="none"):
     return _linear.apply(x, w, bias, residual, activation)
 
 
+def _embedding_function():
+    """The autograd node of ``embedding``."""
+    import torch
+
+    class EmbeddingFunction(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, table, ids, scale):
+            flat = ids.reshape(-1).contiguous()
+            ctx.save_for_backward(flat)
+            ctx.vocab, ctx.scale = table.shape[0], scale
+            return B.mdet_embedding_forward(flat, _rows(table), scale).view(*ids.shape, table.shape[1])
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dy):
+            ids, = ctx.saved_tensors
+            return B.mdet_embedding_backward(_rows(_as_rows(dy)), ids, ctx.vocab, ctx.scale), None, None
+
+    return EmbeddingFunction
+
+
+def _layer_norm_function():
+    """The autograd node of ``layer_norm``."""
+    import torch
+
+    class LayerNormFunction(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, weight, bias, eps):
+            rows = _rows(_as_rows(x))
+            weight = None if weight is None else weight.contiguous()
+            y, mean, rstd = B.mdet_layernorm_forward(rows, weight, None if bias is None else bias.contiguous(), eps)
+            ctx.save_for_backward(rows, weight, mean, rstd)
+            ctx.shape = x.shape
+            return y.view(x.shape)
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dy):
+            x, weight, mean, rstd = ctx.saved_tensors
+            need_x, need_w, need_b, _ = ctx.needs_input_grad
+            dx, dw, db = B.mdet_layernorm_backward(_rows(_as_rows(dy)), x, mean, rstd, weight, dx=need_x, dw=need_w, db=need_b)
+            return None if dx is None else dx.view(ctx.shape), dw, db, None
+
+    return LayerNormFunction
+
+
+def _cross_entropy_function():
+    """The autograd node of ``linear_cross_entropy``: the rows' losses."""
+    import torch
+
+    class CrossEntropyFunction(torch.autograd.Function):
+        @staticmethod
+        def forward(ctx, x, w, bias, target, ignore, keep):
+            rows, mat = _rows(_as_rows(x)), _rows(w)
+            bias = None if bias is None else bias.contiguous()
+            loss, lse, kept = B.mdet_xent_forward(rows, mat, target, bias, ignore, keep=keep)
+            ctx.save_for_backward(rows, mat, bias, target, lse, kept)
+            ctx.shape, ctx.ignore = x.shape, ignore
+            return loss
+
+        @staticmethod
+        @torch.autograd.function.once_differentiable
+        def backward(ctx, dloss):
+            x, w, bias, target, lse, kept = ctx.saved_tensors
+            need_x, need_w, need_b = ctx.needs_input_grad[:3]
+            dx, dw, db = B.mdet_xent_backward(dloss.contiguous(), x, w, target, lse, bias, ctx.ignore, kept, dx=need_x, dw=need_w, db=need_b)
+            return None if dx is None else dx.view(ctx.shape), dw, db, None, None, None
+
+    return CrossEntropyFunction
+
+
+_functions = {}
+
+
+def _function(make):
+    """The node that make() makes, made once."""
+    if make not in _functions:
+        _functions[make] = make()
+    return _functions[make]
+
+
+def embedding(ids, table, scale=1.0):
+    """``scale * table[ids]`` with its gradient by the table (autograd): ids (...) int32 or int64, table (vocab, width).  An id outside of the
+    table gives a row of zeros, and has no part in the gradient."""
+    if table.dim() != 2:
+        raise ValueError("table: a matrix expected")
+    import torch
+    if not torch.is_grad_enabled():
+        return B.mdet_embedding_forward(ids.reshape(-1).contiguous(), _rows(table), scale).view(*ids.shape, table.shape[1])
+    return _function(_embedding_function).apply(table, ids, scale)
+
+
+def layer_norm(x, weight=None, bias=None, eps=1e-5):
+    """Layer norm over the last axis of x (..., n) with its gradient (autograd); weight and bias (n,)."""
+    if x.dim() < 1:
+        raise ValueError("x with rows as its last axis expected")
+    import torch
+    if not torch.is_grad_enabled():
+        return B.mdet_layernorm_forward(_rows(_as_rows(x)), None if weight is None else weight.contiguous(),
+                                        None if bias is None else bias.contiguous(), eps, mean=False, rstd=False)[0].view(x.shape)
+    return _function(_layer_norm_function).apply(x, weight, bias, eps)
+
+
+def linear_cross_entropy(x, w, target, bias=None, ignore_index=-100, reduction="mean", keep=False):
+    """Softmax cross entropy of ``x w^T + bias`` with its gradient (autograd), without that matrix in memory: x (..., k), w (n, k), target
+    (...) int32 or int64.  Targets that are ``ignore_index``, or outside of the vocabulary, do not count.  reduction: 'mean' over those that
+    count (NaN if none does), 'sum', or 'none' (the losses, in float32, in target's shape).  ``keep`` spends x's rows times n elements between
+    the two passes on sparing the gradient one of its three products."""
+    if x.dim() < 1 or w.dim() != 2 or target.shape != x.shape[:-1]:
+        raise ValueError(f"x with rows as its last axis, a matrix w and a target for each row expected, not {tuple(x.shape)}, {tuple(w.shape)} and "
+                         f"{tuple(target.shape)}")
+    if reduction not in ("mean", "sum", "none"):
+        raise ValueError("reduction must be 'mean', 'sum' or 'none'")
+    import torch
+    flat = target.reshape(-1).contiguous()
+    if not torch.is_grad_enabled():
+        loss = B.mdet_xent_forward(_rows(_as_rows(x)), _rows(w), flat, None if bias is None else bias.contiguous(), ignore_index, lse=False)[0]
+    else:
+        loss = _function(_cross_entropy_function).apply(x, w, bias, flat, ignore_index, keep)
+    if reduction == "none":
+        return loss.view(target.shape)
+    if reduction == "sum":
+        return loss.sum()
+    return loss.sum() / ((flat >= 0) & (flat < w.shape[0]) & (flat != ignore_index)).sum()
+
+
 class AdamW:
     """AdamW over a list of CUDA tensors, updated in place by ``step()`` (``mdet_adamw_step``; asynchronous).
 

@@ -107,6 +107,9 @@ EXPORTS = [
     "mdet_logdet_device_noalloc",
     "mdet_linear_workspace_query", "mdet_linear_forward", "mdet_linear_backward",
     "mdet_adamw_step", "mdet_ntk_gram", "mdet_ntk_workspace_query",
+    "mdet_embedding_workspace_query", "mdet_embedding_forward", "mdet_embedding_backward",
+    "mdet_layernorm_workspace_query", "mdet_layernorm_forward", "mdet_layernorm_backward",
+    "mdet_xent_workspace_query", "mdet_xent_kept_query", "mdet_xent_forward", "mdet_xent_backward",
 ]
 
 _lib = None
@@ -157,6 +160,18 @@ def load():
     L.mdet_adamw_step.argtypes = [C.POINTER(_AdamwParams), vp, i64, vp]
     L.mdet_ntk_gram.argtypes = [i32, i32, i64, i64, vp, i32, C.c_double, C.c_double, i32, vp, i64, vp, u64, vp]
     L.mdet_ntk_workspace_query.argtypes = [i32, i32, i64, i64, vp, i32, C.POINTER(u64)]
+    f64 = C.c_double
+    L.mdet_embedding_workspace_query.argtypes = [i64, i64, i64, C.POINTER(u64)]
+    L.mdet_embedding_forward.argtypes = [i32, i32, i64, i64, i64, vp, vp, i64, f64, vp, i64, vp]
+    L.mdet_embedding_backward.argtypes = [i32, i32, i32, i64, i64, i64, vp, vp, i64, f64, i32, vp, i64, vp, u64, vp]
+    L.mdet_layernorm_workspace_query.argtypes = [i32, i64, i64, C.POINTER(u64)]
+    L.mdet_layernorm_forward.argtypes = [i32, i64, i64, vp, i64, vp, vp, f64, vp, i64, vp, vp, vp]
+    L.mdet_layernorm_backward.argtypes = [i32, i32, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, u64, vp]
+    L.mdet_xent_workspace_query.argtypes = [i32, i32, i64, i64, i64, C.POINTER(u64)]
+    L.mdet_xent_kept_query.argtypes = [i32, i64, i64, i64, C.POINTER(u64)]
+    L.mdet_xent_forward.argtypes = [i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, u64, vp, u64, vp]
+    L.mdet_xent_backward.argtypes = [i32, i32, i32, i64, i64, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, u64, vp, i64, vp, i64,
+                                     vp, vp, u64, vp]
     L.mdet_strerror.argtypes = [C.c_int]
     L.mdet_strerror.restype = C.c_char_p
     L.mdet_version.restype = C.c_char_p
@@ -908,6 +923,243 @@ def mdet_ntk_gram(inputs, signals, out=None, outputs=1, bias=1.0, scale=1.0, acc
     if given is not None:
         _written(out)
     return out
+
+
+_INDEX_BITS = {}
+
+
+def _indices(t, name, n, gpu):
+    """(address, bits) of n consecutive int32 or int64 on this GPU."""
+    if not _INDEX_BITS:
+        import torch
+        _INDEX_BITS.update({torch.int32: 32, torch.int64: 64})
+    bits = _INDEX_BITS.get(t.dtype)
+    if bits is None or t.shape != (n,) or t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor of {n} int32 or int64 on cuda:{gpu} expected, not {tuple(t.shape)} {t.dtype} on {t.device}")
+    return t.data_ptr(), bits
+
+
+def _given(*results):
+    """Those of the results that the caller brought along."""
+    return [v for v in results if v is not None and not isinstance(v, bool)]
+
+
+def _result_tensor(what, shape, like, dtype, stream):
+    """True: a new tensor; False or None: none; otherwise the tensor itself."""
+    if what is True:
+        return _new(stream, lambda: like.new_empty(shape, dtype=dtype))
+    return None if what is False else what
+
+
+@functools.lru_cache(maxsize=1024)
+def mdet_embedding_workspace_query(n, vocab, width) -> int:
+    """Device bytes of workspace for ``mdet_embedding_backward``."""
+    b = C.c_uint64(0)
+    _check_status(load().mdet_embedding_workspace_query(int(n), int(vocab), int(width), C.byref(b)))
+    return b.value
+
+
+def mdet_embedding_forward(ids, table, scale=1.0, out=None, stream=None):
+    """``scale * table[ids]`` on the GPU (asynchronous): ids (n,) int32 or int64, table (vocab, width) float32, float16 or
+    bfloat16, out (n, width) of the same type.  An id outside of the table gives a row of zeros.  Returns out."""
+    if ids.dim() != 1 or table.dim() != 2:
+        raise ValueError("ids: a vector, and table: a matrix expected")
+    t = _operand_type(table.dtype)
+    n, (vocab, width) = ids.shape[0], table.shape
+    gpu = _gpu(table, "table")
+    tp, ldt = _matrix(table, "table", vocab, width, t, gpu)
+    ip, bits = _indices(ids, "ids", n, gpu)
+    given = out
+    if out is None:
+        out = _new(stream, lambda: table.new_empty((n, width)))
+    yp, ldy = _matrix(out, "out", n, width, t, gpu)
+    _queue(gpu, load().mdet_embedding_forward, _type_code(t), bits, n, vocab, width, ip, tp, ldt, scale, yp, ldy, _operator_stream(stream, gpu))
+    if given is not None:
+        _written(out)
+    return out
+
+
+def mdet_embedding_backward(dy, ids, vocab, scale=1.0, dtable=None, accumulate=False, grad_dtype=None, workspace=None, stream=None):
+    """Gradient of ``mdet_embedding_forward`` by its table (asynchronous): row v is ``scale`` times the sum of the rows of dy
+    (n, width) whose id is v, zeros where there is none; with ``accumulate`` it is added to what ``dtable`` (vocab, width) holds.
+    dtable is of ``grad_dtype``: dy's type or float32 (a new one of dy's without it).  Returns dtable."""
+    if ids.dim() != 1 or dy.dim() != 2:
+        raise ValueError("ids: a vector, and dy: a matrix expected")
+    t = _operand_type(dy.dtype)
+    n, width = dy.shape
+    vocab = int(vocab)
+    gt = grad_dtype if grad_dtype is not None else t if dtable is None else dtable.dtype
+    gpu = _gpu(dy, "dy")
+    dyp, lddy = _matrix(dy, "dy", n, width, t, gpu)
+    ip, bits = _indices(ids, "ids", n, gpu)
+    given = dtable
+    if dtable is None:
+        if accumulate:
+            raise ValueError("accumulate needs dtable")
+        if vocab < 0:
+            raise ValueError("vocab must be 0 or more")
+        dtable = _new(stream, lambda: dy.new_empty((vocab, width), dtype=gt))
+    gp, ldt = _matrix(dtable, "dtable", vocab, width, gt, gpu)
+    need = 0 if workspace is not None else mdet_embedding_workspace_query(n, vocab, width)
+    wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
+    _queue(gpu, load().mdet_embedding_backward, _type_code(t), _type_code(gt), bits, n, vocab, width, ip, dyp, lddy, scale, int(bool(accumulate)),
+           gp, ldt, wsp, wsb, _operator_stream(stream, gpu))
+    if given is not None:
+        _written(dtable)
+    return dtable
+
+
+@functools.lru_cache(maxsize=1024)
+def mdet_layernorm_workspace_query(dtype, m, n) -> int:
+    """Device bytes of workspace for ``mdet_layernorm_backward``."""
+    b = C.c_uint64(0)
+    _check_status(load().mdet_layernorm_workspace_query(_type_code(dtype), int(m), int(n), C.byref(b)))
+    return b.value
+
+
+def mdet_layernorm_forward(x, weight=None, bias=None, eps=1e-5, out=None, mean=True, rstd=True, stream=None):
+    """``(x - mean) * rstd * weight + bias`` over the rows of x (m, n) on the GPU (asynchronous), rstd = 1 / sqrt(var + eps);
+    weight and bias (n,), all of one type (float32, float16 or bfloat16).  mean, rstd: True for a new float32 tensor (m,), False or None
+    where they are not kept for the gradient, or the tensor to write.  Returns out, mean, rstd."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x: a matrix expected")
+    t = _operand_type(x.dtype)
+    m, n = x.shape
+    gpu = _gpu(x, "x")
+    xp, ldx = _matrix(x, "x", m, n, t, gpu)
+    wp = None if weight is None else _vector(weight, "weight", n, t, gpu)
+    bp = None if bias is None else _vector(bias, "bias", n, t, gpu)
+    given = _given(out, mean, rstd)
+    if out is None:
+        out = _new(stream, lambda: x.new_empty((m, n)))
+    yp, ldy = _matrix(out, "out", m, n, t, gpu)
+    if mean is True and rstd is True:           # one allocation for both
+        mean, rstd = _new(stream, lambda: x.new_empty((2, m), dtype=torch.float32)).unbind()
+    mean, rstd = (_result_tensor(v, (m,), x, torch.float32, stream) for v in (mean, rstd))
+    mp = None if mean is None else _vector(mean, "mean", m, torch.float32, gpu)
+    rp = None if rstd is None else _vector(rstd, "rstd", m, torch.float32, gpu)
+    _queue(gpu, load().mdet_layernorm_forward, _type_code(t), m, n, xp, ldx, wp, bp, eps, yp, ldy, mp, rp, _operator_stream(stream, gpu))
+    if given:
+        _written(*given)
+    return out, mean, rstd
+
+
+def mdet_layernorm_backward(dy, x, mean, rstd, weight=None, dx=True, dw=True, db=True, grad_dtype=None, workspace=None, stream=None):
+    """Gradient of ``mdet_layernorm_forward`` (asynchronous): (dx, dw, db) from dy (m, n), its x, mean, rstd and weight.  dx, dw, db:
+    True for a new tensor, False or None for a gradient that is not wanted (None is returned), or the tensor to write; dw and db are of
+    ``grad_dtype``: x's type or float32."""
+    import torch
+    if x.dim() != 2:
+        raise ValueError("x: a matrix expected")
+    t = _operand_type(x.dtype)
+    m, n = x.shape
+    gt = t if grad_dtype is None else grad_dtype
+    gpu = _gpu(x, "x")
+    dyp, lddy = _matrix(dy, "dy", m, n, t, gpu)
+    xp, ldx = _matrix(x, "x", m, n, t, gpu)
+    mp, rp = _vector(mean, "mean", m, torch.float32, gpu), _vector(rstd, "rstd", m, torch.float32, gpu)
+    wp = None if weight is None else _vector(weight, "weight", n, t, gpu)
+    given = _given(dx, dw, db)
+    dx, dw, db = (_result_tensor(v, s, x, d, stream) for v, s, d in ((dx, (m, n), t), (dw, (n,), gt), (db, (n,), gt)))
+    dxp, lddx = (None, 0) if dx is None else _matrix(dx, "dx", m, n, t, gpu)
+    dwp = None if dw is None else _vector(dw, "dw", n, gt, gpu)
+    dbp = None if db is None else _vector(db, "db", n, gt, gpu)
+    need = 0 if workspace is not None or (dw is None and db is None) else mdet_layernorm_workspace_query(t, m, n)
+    wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
+    _queue(gpu, load().mdet_layernorm_backward, _type_code(t), _type_code(gt), m, n, dyp, lddy, xp, ldx, mp, rp, wp, dxp, lddx, dwp, dbp, wsp, wsb,
+           _operator_stream(stream, gpu))
+    if given:
+        _written(*given)
+    return dx, dw, db
+
+
+@functools.lru_cache(maxsize=1024)
+def mdet_xent_workspace_query(dtype, m, n, k, backward=False) -> int:
+    """Device bytes of workspace for ``mdet_xent_forward`` or, with ``backward``, the gradient."""
+    b = C.c_uint64(0)
+    _check_status(load().mdet_xent_workspace_query(_type_code(dtype), int(backward), int(m), int(n), int(k), C.byref(b)))
+    return b.value
+
+
+@functools.lru_cache(maxsize=1024)
+def mdet_xent_kept_query(dtype, m, n, k) -> int:
+    """Device bytes of what ``mdet_xent_forward`` keeps where it is told to."""
+    b = C.c_uint64(0)
+    _check_status(load().mdet_xent_kept_query(_type_code(dtype), int(m), int(n), int(k), C.byref(b)))
+    return b.value
+
+
+def _xent_operands(x, w, target, bias):
+    if x.dim() != 2 or w.dim() != 2 or target.dim() != 1:
+        raise ValueError("x and w: matrices, and target: a vector expected")
+    t = _operand_type(x.dtype)
+    m, k = x.shape
+    n = w.shape[0]
+    gpu = _gpu(x, "x")
+    xp, ldx = _matrix(x, "x", m, k, t, gpu)
+    wp, ldw = _matrix(w, "w", n, k, t, gpu)
+    bp = None if bias is None else _vector(bias, "bias", n, t, gpu)
+    tp, bits = _indices(target, "target", m, gpu)
+    return t, gpu, (m, n, k), (xp, ldx, wp, ldw, bp, tp), bits
+
+
+def mdet_xent_forward(x, w, target, bias=None, ignore=-100, loss=True, lse=True, keep=False, workspace=None, stream=None):
+    """Softmax cross entropy of the rows of ``x w^T + bias`` on the GPU (asynchronous), without that matrix in memory: x (m, k), w (n, k),
+    bias (n,) of one type (float32, float16 or bfloat16), target (m,) int32 or int64.  Rows whose target is ``ignore``, or outside of the
+    vocabulary, have the loss 0.  loss, lse (the log of the sum of the exponentials): True for a new float32 tensor (m,), False or None for
+    none, or the tensor to write.  keep: True, or a contiguous tensor of ``mdet_xent_kept_query`` bytes, for what spares the gradient a
+    product.  Returns loss, lse and what was kept (or None)."""
+    import torch
+    t, gpu, (m, n, k), (xp, ldx, wp, ldw, bp, tp), bits = _xent_operands(x, w, target, bias)
+    given = _given(loss, lse, keep)
+    loss, lse = (_result_tensor(v, (m,), x, torch.float32, stream) for v in (loss, lse))
+    lp = None if loss is None else _vector(loss, "loss", m, torch.float32, gpu)
+    sp = None if lse is None else _vector(lse, "lse", m, torch.float32, gpu)
+    kept = None if keep is None or keep is False else keep
+    kp, kb = None, 0
+    if kept is not None:
+        if kept is True:
+            kept = _new(stream, lambda: x.new_empty(mdet_xent_kept_query(t, m, n, k), dtype=torch.uint8))
+        kp, kb = _bytes(kept, "keep", gpu)
+    need = 0 if workspace is not None or kept is not None else mdet_xent_workspace_query(t, m, n, k)
+    wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
+    _queue(gpu, load().mdet_xent_forward, _type_code(t), bits, m, n, k, xp, ldx, wp, ldw, bp, tp, ignore, lp, sp, kp, kb, wsp, wsb,
+           _operator_stream(stream, gpu))
+    if given:
+        _written(*given)
+    return loss, lse, kept
+
+
+def _bytes(t, name, gpu):
+    """(address, bytes) of a contiguous tensor of any type on this GPU."""
+    if t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor on cuda:{gpu} expected")
+    return t.data_ptr(), t.numel() * t.element_size()
+
+
+def mdet_xent_backward(dloss, x, w, target, lse, bias=None, ignore=-100, kept=None, dx=True, dw=True, db=None, grad_dtype=None,
+                       workspace=None, stream=None):
+    """Gradient of the sum of ``dloss * loss`` of ``mdet_xent_forward`` (asynchronous): (dx, dw, db) from dloss (m,) float32, its operands,
+    its lse, and what it kept.  dx, dw, db: True for a new tensor, False or None for a gradient that is not wanted (None is returned; db
+    without a bias as a rule), or the tensor to write; dw and db are of ``grad_dtype``: x's type or float32."""
+    import torch
+    t, gpu, (m, n, k), (xp, ldx, wp, ldw, bp, tp), bits = _xent_operands(x, w, target, bias)
+    gt = t if grad_dtype is None else grad_dtype
+    gp, sp = _vector(dloss, "dloss", m, torch.float32, gpu), _vector(lse, "lse", m, torch.float32, gpu)
+    kp, kb = (None, 0) if kept is None else _bytes(kept, "kept", gpu)
+    given = _given(dx, dw, db)
+    dx, dw, db = (_result_tensor(v, s, x, d, stream) for v, s, d in ((dx, (m, k), t), (dw, (n, k), gt), (db, (n,), gt)))
+    dxp, lddx = (None, 0) if dx is None else _matrix(dx, "dx", m, k, t, gpu)
+    dwp, lddw = (None, 0) if dw is None else _matrix(dw, "dw", n, k, gt, gpu)
+    dbp = None if db is None else _vector(db, "db", n, gt, gpu)
+    need = 0 if workspace is not None else mdet_xent_workspace_query(t, m, n, k, backward=True)
+    wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
+    _queue(gpu, load().mdet_xent_backward, _type_code(t), _type_code(gt), bits, m, n, k, gp, xp, ldx, wp, ldw, bp, tp, ignore, sp, kp, kb,
+           dxp, lddx, dwp, lddw, dbp, wsp, wsb, _operator_stream(stream, gpu))
+    if given:
+        _written(*given)
+    return dx, dw, db
 
 
 def mdet_step_copy(dst, src, stream=None) -> None:

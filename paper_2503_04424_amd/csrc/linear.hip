@@ -6,34 +6,16 @@
 
 #include "kernels_linear.h"
 #include "linear_cut.h"
+#include "operands.h"
 
 namespace {
 
 using namespace mdet;
 
-inline uint64_t up256(uint64_t x) { return (x + 255) / 256 * 256; }
-inline int64_t size_of(int32_t t) { return t == MDET_F32 ? 4 : 2; }
-inline bool is_type(int32_t t) { return t == MDET_F32 || t == MDET_F16 || t == MDET_BF16; }
-inline int launch_status() { return hipGetLastError() == hipSuccess ? MDET_OK : MDET_EHIP; }
-
-// Sizes whose products and byte counts stay within 64 bits.
-constexpr int64_t MOST = int64_t(1) << 40;
-inline bool sizes_fit(int64_t m, int64_t n, int64_t k) {
-  if (m < 0 || n < 0 || k < 0 || m > MOST || n > MOST || k > MOST) return false;
-  const int64_t most = int64_t(1) << 52;
-  return (!n || m <= most / n) && (!k || m <= most / k) && (!k || n <= most / k);
-}
-
 // Whether a product of this many rows and columns goes out in one launch, which holds fewer than 2^32 threads.  A tile of 256 (128) rows and
 // columns has 512 (256) threads for at least eight (four) squares of 32, the grid is rounded up by seven tiles at most, and smaller
 // tiles are taken for a few hundred squares only.
 inline bool tiles_fit(int64_t rows, int64_t cols) { return ceil_div(rows, 32) * ceil_div(cols, 32) <= (int64_t(1) << 26) - 1024; }
-
-// A matrix of r rows and c columns in memory: null only where it has no elements, rows that do not overlap.
-inline bool matrix_ok(const void* p, int64_t r, int64_t c, int64_t ld, int64_t size) {
-  if (r == 0 || c == 0) return true;
-  return p && (uintptr_t)p % size == 0 && (r == 1 || ld >= c) && ld >= 0 && ld <= MOST;
-}
 
 // Whether four elements at a time can be moved at this place.
 template <typename T>

@@ -1,0 +1,266 @@
+// C ABI of the softmax cross entropy of a linear layer and its gradient: argument checks, workspace layout and kernel launches.  A
+// call only queues work on the caller's stream; nothing is allocated and nothing is waited for.
+#include <hip/hip_runtime.h>
+
+#include <type_traits>
+
+#include "kernels_xent.h"
+#include "linear_cut.h"
+#include "operands.h"
+#include "xent_cut.h"
+
+namespace {
+
+using namespace mdet;
+
+typedef Tile<256, 256, 2, 4, 2> Big;
+typedef Tile<128, 128, 2, 2, 2> Mid;
+typedef Tile<64, 64, 2, 2, 2> Small;
+typedef Tile<32, 32, 2, 2, 4> Tiny;
+
+// f(shape) with the tile shape that a cut names.
+template <typename T, typename F>
+void with_tile(int tile, F&& f) {
+  if (tile == 256) {
+    if constexpr (sizeof(T) == 2) f(Big{});
+  } else if (tile == 128) f(Mid{});
+  else if (tile == 64) f(Small{});
+  else f(Tiny{});
+}
+
+// The places of what the forward pass leaves: in the caller's `kept`, or without the exponentials in the workspace.
+template <typename T>
+XentForward<T> forward_places(char* at, const XentLayout& l, bool keep) {
+  XentForward<T> o{};
+  o.exps = keep ? (T*)at : nullptr;
+  o.ldexps = l.ldexps;
+  char* const rest = keep ? at + l.exps_bytes : at;
+  o.strips = (XentStrip*)rest;
+  o.across = l.across;
+  o.picked = (float*)(rest + l.strips_bytes);
+  return o;
+}
+
+template <typename T>
+int forward(Operand<T> x, Operand<T> w, int64_t k, XentForward<T> o, const XentLayout& l, float* loss, float* lse, hipStream_t st) {
+  if (o.cols > 0) {
+    if (l.cut.tile == 0) {
+      const dim3 grid((unsigned)ceil_div(o.cols, 16));
+      if (k * (int64_t)sizeof(T) >= 4096) hipLaunchKernelGGL((xent_forward_rows_kernel<T, 16>), grid, dim3(1024), 0, st, x, w, k, o);
+      else hipLaunchKernelGGL((xent_forward_rows_kernel<T, 4>), grid, dim3(256), 0, st, x, w, k, o);
+    } else
+      with_tile<T>(l.cut.tile, [&](auto shape) {
+        typedef decltype(shape) S;
+        x = gemm_operand<T, false, S::BM>(x.p, x.stride, x.rows, k);
+        w = gemm_operand<T, false, S::BN>(w.p, w.stride, w.rows, k);
+        const int64_t tiles = ceil_div(o.rows, S::BM) * ceil_div(o.cols, S::BN);
+        const dim3 grid((unsigned)(ceil_div(tiles, 8) * 8)), block(S::THREADS);
+        if (x.straight && w.straight) hipLaunchKernelGGL((xent_forward_kernel<T, S, true>), grid, block, 0, st, x, w, k, o, tiles);
+        else hipLaunchKernelGGL((xent_forward_kernel<T, S, false>), grid, block, 0, st, x, w, k, o, tiles);
+      });
+  }
+  // a row's strips by a wavefront, or by sixteen where they are many
+  if (l.across > 1024)
+    gemm_launches(o.rows, 1024, [&](const int64_t first, const dim3 grid) {
+      hipLaunchKernelGGL((xent_join_kernel<1024>), grid, dim3(1024), 0, st, (const XentStrip*)o.strips, l.across, (const float*)o.picked, o.t, o.rows,
+                         loss, lse, first);
+    });
+  else
+    gemm_launches(ceil_div(o.rows, 4), 256, [&](const int64_t first, const dim3 grid) {
+      hipLaunchKernelGGL((xent_join_kernel<64>), grid, dim3(256), 0, st, (const XentStrip*)o.strips, l.across, (const float*)o.picked, o.t, o.rows,
+                         loss, lse, first);
+    });
+  return launch_status();
+}
+
+template <typename O>
+bool fours(const XentOut<O>& o) {
+  return (uintptr_t)o.y % (4 * sizeof(O)) == 0 && (o.rows == 1 || o.ldy % 4 == 0) && (!o.total || o.cols % 4 == 0);
+}
+
+template <typename T, typename O, bool ROUTER>
+void product(Operand<T> r, Operand<T> c, int64_t k, XentOut<O> o, float* parts, hipStream_t st) {
+  const Cut cut = cut_of(o.rows, o.cols, k, sizeof(T), false);
+  o.vec = fours(o);
+  with_tile<T>(cut.tile, [&](auto shape) {
+    typedef decltype(shape) S;
+    r = gemm_operand<T, ROUTER, S::BM>(r.p, r.stride, r.rows, k);
+    c = gemm_operand<T, true, S::BN>(c.p, c.stride, c.rows, k);
+    const int64_t tiles = ceil_div(o.rows, S::BM) * ceil_div(o.cols, S::BN) * cut.splits;
+    const dim3 grid((unsigned)(ceil_div(tiles, 8) * 8)), block(S::THREADS);
+    auto go = [&](auto direct, auto split) {
+      hipLaunchKernelGGL((xent_product_kernel<T, O, S, ROUTER, decltype(direct)::value, decltype(split)::value>), grid, block, 0, st, r, c, k, o, tiles,
+                         parts, cut.kpart);
+    };
+    using std::false_type;
+    using std::true_type;
+    const bool direct = r.straight && c.straight;
+    if (cut.splits > 1) {              // the smallest tile alone
+      if constexpr (std::is_same<S, Tiny>::value) {
+        if (direct) go(true_type{}, true_type{});
+        else go(false_type{}, true_type{});
+        hipLaunchKernelGGL((xent_product_join_kernel<O>), dim3((unsigned)ceil_div(o.rows * ceil_div(o.cols, 4), 256)), dim3(256), 0, st,
+                           (const float*)parts, cut.splits, o);
+      }
+    } else if (direct) go(true_type{}, false_type{});
+    else go(false_type{}, false_type{});
+  });
+}
+
+struct Grad {
+  XentTargets t;
+  int64_t m, n, k;
+  const float *g, *lse;
+  const void *x, *w, *bias;
+  int64_t ldx, ldw;
+  char* kept;                          // null: nothing was kept
+  void *dx, *dw, *db;
+  int64_t lddx, lddw;
+  char* workspace;
+  hipStream_t st;
+};
+
+template <typename T, typename O>
+int backward(const Grad& a) {
+  const XentLayout f = xent_layout(a.m, a.n, a.k, sizeof(T));
+  const XentGradLayout l = xent_grad_layout(a.m, a.n, a.k, sizeof(T));
+  hipStream_t st = a.st;
+  T *const e = (T*)(a.workspace + l.e), *const rows = (T*)(a.workspace + l.rows);
+  float *const sums = (float*)(a.workspace + l.sums), *const total = (float*)(a.workspace + l.total), *const parts = (float*)(a.workspace + l.parts);
+  XentScale* scale = nullptr;
+  if constexpr (std::is_same<T, _Float16>::value) {
+    scale = (XentScale*)(a.workspace + l.scale);
+    hipLaunchKernelGGL(xent_scale_kernel, dim3(1), dim3(1024), 0, st, a.g, a.t, a.m, scale);
+  }
+  if (a.dw && a.k > 0)
+    gemm_launches(ceil_div(a.m * (l.ldrows / Core<T>::VEC), 256), 256, [&](const int64_t first, const dim3 grid) {
+      hipLaunchKernelGGL((xent_rows_kernel<T>), grid, dim3(256), 0, st, (const T*)a.x, a.ldx, a.t, a.m, a.k, rows, l.ldrows, first);
+    });
+  for (int64_t v = 0; v < a.n; v += l.piece) {
+    const int64_t n = a.n - v < l.piece ? a.n - v : l.piece;
+    const T* const w = (const T*)a.w + v * a.ldw;
+    const XentSlope<T> o{a.t, a.bias ? (const T*)a.bias + v : nullptr, a.lse, a.g, scale, e, l.lde, a.db ? sums : nullptr, a.m, n, v};
+    int64_t strips = 0;
+    if (a.kept) {
+      const XentForward<T> was = forward_places<T>(a.kept, f, true);
+      strips = ceil_div(a.m, 16 * XENT_EACH);
+      gemm_launches(strips * ceil_div(n, 16 * Core<T>::VEC), 256, [&](const int64_t first, const dim3 grid) {
+        hipLaunchKernelGGL((xent_slope_kept_kernel<T>), grid, dim3(256), 0, st, o, (const T*)was.exps, was.ldexps, (const XentStrip*)was.strips, was.across,
+                           f.strip, (const float*)was.picked, first);
+      });
+    } else
+      with_tile<T>(cut_of(a.m, n, a.k, sizeof(T), false).tile, [&](auto shape) {
+        typedef decltype(shape) S;
+        const Operand<T> x = gemm_operand<T, false, S::BM>(a.x, a.ldx, a.m, a.k), c = gemm_operand<T, false, S::BN>(w, a.ldw, n, a.k);
+        const int64_t tiles = ceil_div(a.m, S::BM) * ceil_div(n, S::BN);
+        const dim3 grid((unsigned)(ceil_div(tiles, 8) * 8)), block(S::THREADS);
+        strips = ceil_div(a.m, S::BM) * S::WM;
+        if (x.straight && c.straight) hipLaunchKernelGGL((xent_slope_kernel<T, S, true>), grid, block, 0, st, x, c, a.k, o, tiles);
+        else hipLaunchKernelGGL((xent_slope_kernel<T, S, false>), grid, block, 0, st, x, c, a.k, o, tiles);
+      });
+    if (a.db)
+      gemm_launches(ceil_div(n, 16), 256, [&](const int64_t first, const dim3 grid) {
+        hipLaunchKernelGGL((xent_columns_kernel<O>), grid, dim3(256), 0, st, (const float*)sums, strips, n, (O*)a.db + v, first);
+      });
+    if (a.dx && a.k > 0)
+      product<T, T, false>(Operand<T>{e, l.lde, a.m, false, false}, Operand<T>{w, a.ldw, a.k, false, false}, n,
+                           XentOut<T>{(T*)a.dx, a.lddx, scale, total, v == 0, v + n == a.n, a.m, a.k, false}, parts, st);
+    if (a.dw && a.k > 0)
+      product<T, O, true>(Operand<T>{e, l.lde, n, false, false}, Operand<T>{rows, l.ldrows, a.k, false, false}, a.m,
+                          XentOut<O>{(O*)a.dw + v * a.lddw, a.lddw, scale, nullptr, true, true, n, a.k, false}, parts, st);
+  }
+  return launch_status();
+}
+
+// A matrix without rows to sum over is zero.
+template <typename O>
+__global__ __launch_bounds__(256) void zero_kernel(O* to, const int64_t ld, const int64_t rows, const int64_t cols, const int64_t first) {
+  const int64_t id = (first + blockIdx.x) * 256 + threadIdx.x, i = id / cols;
+  if (i < rows) to[i * ld + (id - i * cols)] = (O)0.0f;
+}
+template <typename O>
+void zero(void* to, int64_t ld, int64_t rows, int64_t cols, hipStream_t st) {
+  if (!to || rows * cols == 0) return;
+  gemm_launches(ceil_div(rows * cols, 256), 256, [&](const int64_t first, const dim3 grid) {
+    hipLaunchKernelGGL((zero_kernel<O>), grid, dim3(256), 0, st, (O*)to, ld, rows, cols, first);
+  });
+}
+
+bool is_index(int32_t bits) { return bits == 32 || bits == 64; }
+
+// As tiles_fit of the linear layer.
+bool tiles_fit(int64_t rows, int64_t cols) { return ceil_div(rows, 32) * ceil_div(cols, 32) <= (int64_t(1) << 26) - 1024; }
+bool xent_fits(int64_t m, int64_t n, int64_t k) { return sizes_fit(m, n, k) && tiles_fit(m, n) && tiles_fit(m, k) && tiles_fit(n, k); }
+
+}  // namespace
+
+extern "C" {
+
+int mdet_xent_workspace_query(int32_t dtype, int32_t backward, int64_t m, int64_t n, int64_t k, uint64_t* bytes) {
+  if (!bytes || !is_type(dtype) || !xent_fits(m, n, k)) return MDET_EINVAL;
+  const XentLayout l = xent_layout(m, n, k, size_of(dtype));
+  *bytes = backward ? xent_grad_layout(m, n, k, size_of(dtype)).bytes : l.strips_bytes + l.picked_bytes;
+  return MDET_OK;
+}
+
+int mdet_xent_kept_query(int32_t dtype, int64_t m, int64_t n, int64_t k, uint64_t* bytes) {
+  if (!bytes || !is_type(dtype) || !xent_fits(m, n, k)) return MDET_EINVAL;
+  const XentLayout l = xent_layout(m, n, k, size_of(dtype));
+  *bytes = l.exps_bytes + l.strips_bytes + l.picked_bytes;
+  return MDET_OK;
+}
+
+int mdet_xent_forward(int32_t dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const void* x, int64_t ldx, const void* w, int64_t ldw,
+                      const void* bias, const void* target, int64_t ignore, float* loss, float* lse, void* kept, uint64_t kept_bytes,
+                      void* workspace, uint64_t workspace_bytes, void* stream) {
+  if (!is_type(dtype) || !is_index(index_bits) || !xent_fits(m, n, k)) return MDET_EINVAL;
+  const int64_t s = size_of(dtype);
+  if (!matrix_ok(x, m, k, ldx, s) || !matrix_ok(w, n, k, ldw, s) || (uintptr_t)bias % s || !vector_ok(target, m, index_bits / 8)) return MDET_EINVAL;
+  if ((uintptr_t)loss % 4 || (uintptr_t)lse % 4) return MDET_EINVAL;
+  const XentLayout l = xent_layout(m, n, k, s);
+  const uint64_t strips = l.strips_bytes + l.picked_bytes;
+  const int ok = kept ? workspace_ok(kept, kept_bytes, l.exps_bytes + strips) : workspace_ok(workspace, workspace_bytes, strips);
+  if (ok != MDET_OK) return ok;
+  if (m == 0 || (!loss && !lse && !kept)) return MDET_OK;
+  auto call = [&](auto zero) {
+    typedef decltype(zero) T;
+    XentForward<T> o = forward_places<T>((char*)(kept ? kept : workspace), l, kept != nullptr);
+    o.t = XentTargets{target, index_bits, ignore, n};
+    o.bias = (const T*)bias;
+    o.rows = m;
+    o.cols = n;
+    return forward<T>(Operand<T>{(const T*)x, ldx, m, false, false}, Operand<T>{(const T*)w, ldw, n, false, false}, k, o, l, loss, lse, (hipStream_t)stream);
+  };
+  return dtype == MDET_F32 ? call(0.0f) : dtype == MDET_BF16 ? call((__bf16)0.0f) : call((_Float16)0.0f);
+}
+
+int mdet_xent_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const float* dloss, const void* x,
+                       int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* target, int64_t ignore, const float* lse,
+                       const void* kept, uint64_t kept_bytes, void* dx, int64_t lddx, void* dw, int64_t lddw, void* db, void* workspace,
+                       uint64_t workspace_bytes, void* stream) {
+  if (!is_type(dtype) || (grad_dtype != dtype && grad_dtype != MDET_F32) || !is_index(index_bits) || !xent_fits(m, n, k)) return MDET_EINVAL;
+  const int64_t s = size_of(dtype), gs = size_of(grad_dtype);
+  if (!matrix_ok(x, m, k, ldx, s) || !matrix_ok(w, n, k, ldw, s) || (uintptr_t)bias % s || !vector_ok(target, m, index_bits / 8)) return MDET_EINVAL;
+  if (!vector_ok(dloss, m, 4) || !vector_ok(lse, m, 4)) return MDET_EINVAL;
+  if ((dx && !matrix_ok(dx, m, k, lddx, s)) || (dw && !matrix_ok(dw, n, k, lddw, gs)) || (uintptr_t)db % gs) return MDET_EINVAL;
+  const XentLayout f = xent_layout(m, n, k, s);
+  int ok = kept ? workspace_ok(kept, kept_bytes, f.exps_bytes + f.strips_bytes + f.picked_bytes) : MDET_OK;
+  if (ok == MDET_OK) ok = workspace_ok(workspace, workspace_bytes, xent_grad_layout(m, n, k, s).bytes);
+  if (ok != MDET_OK) return ok;
+  if (!dx && !dw && !db) return MDET_OK;
+  hipStream_t st = (hipStream_t)stream;
+  if (m == 0 || n == 0) {              // what is not empty is an empty sum
+    dtype == MDET_F32 ? zero<float>(dx, lddx, m, k, st) : zero<_Float16>(dx, lddx, m, k, st);
+    grad_dtype == MDET_F32 ? zero<float>(dw, lddw, n, k, st) : zero<_Float16>(dw, lddw, n, k, st);
+    grad_dtype == MDET_F32 ? zero<float>(db, n, 1, n, st) : zero<_Float16>(db, n, 1, n, st);
+    return launch_status();
+  }
+  const Grad a{XentTargets{target, index_bits, ignore, n}, m, n, k, dloss, lse, x, w, bias, ldx, ldw, (char*)kept, dx, dw, db, lddx, lddw, (char*)workspace, st};
+  auto call = [&](auto zero) {
+    typedef decltype(zero) T;
+    return grad_dtype == MDET_F32 ? backward<T, float>(a) : backward<T, T>(a);
+  };
+  return dtype == MDET_F32 ? call(0.0f) : dtype == MDET_BF16 ? call((__bf16)0.0f) : call((_Float16)0.0f);
+}
+
+}  // extern "C"

@@ -1,0 +1,68 @@
+// How the cross entropy is cut into strips and pieces of the vocabulary, and what its workspaces hold: host code by itself.
+#pragma once
+#include "linear_cut.h"
+
+namespace mdet {
+
+inline uint64_t xent_up256(uint64_t x) { return (x + 255) / 256 * 256; }
+
+// m rows, a vocabulary of n, rows of k elements of `size` bytes.
+struct XentLayout {
+  Cut cut;                             // of the forward pass; its sums are not split
+  int64_t strip, across;               // columns of a strip, strips of a row
+  int64_t ldexps;
+  uint64_t exps_bytes, strips_bytes, picked_bytes;
+};
+inline XentLayout xent_layout(int64_t m, int64_t n, int64_t k, int64_t size) {
+  XentLayout l;
+  l.cut = cut_of(m, n, k, size, true);
+  l.strip = l.cut.tile ? l.cut.tile : 16;
+  l.across = ceil_div(n, l.strip);
+  l.ldexps = ceil_div(n, 8) * 8;
+  l.exps_bytes = xent_up256((uint64_t)m * l.ldexps * size);
+  l.strips_bytes = xent_up256((uint64_t)m * l.across * 8);
+  l.picked_bytes = xent_up256((uint64_t)m * 4);
+  return l;
+}
+
+// Columns of the vocabulary that the gradient takes at once: e has 2^29 elements at most (1 GiB in 16 bits), so long as that leaves
+// pieces of 4096; dx adds the pieces up in fp32, which costs a piece of 4096 about 8 % of its products' time.
+inline int64_t xent_piece(int64_t m, int64_t n) {
+  int64_t most = m > 0 ? (int64_t(1) << 29) / m / 256 * 256 : n;
+  if (most < 4096) most = 4096;
+  const int64_t pieces = ceil_div(n, most);
+  return pieces <= 1 ? n : ceil_div(ceil_div(n, pieces), 256) * 256;
+}
+
+struct XentGradLayout {
+  int64_t piece, lde, ldrows;
+  uint64_t e, rows, scale, sums, total, parts, bytes;
+};
+inline XentGradLayout xent_grad_layout(int64_t m, int64_t n, int64_t k, int64_t size) {
+  XentGradLayout l;
+  l.piece = xent_piece(m, n);
+  l.lde = ceil_div(l.piece, 8) * 8;
+  l.ldrows = ceil_div(k, 8) * 8;
+  l.e = 0;
+  l.rows = xent_up256((uint64_t)m * l.lde * size);
+  l.scale = l.rows + xent_up256((uint64_t)m * l.ldrows * size);
+  l.sums = l.scale + 256;
+  // column sums of strips of 16 rows or more, of whole tiles
+  l.total = l.sums + xent_up256((uint64_t)(ceil_div(m, 256) * 16) * l.piece * 4);
+  l.parts = l.total + (l.piece < n ? xent_up256((uint64_t)m * k * 4) : 0);
+  uint64_t parts = 0;
+  auto room = [&](int64_t rows, int64_t cols, int64_t inner) {
+    const Cut c = cut_of(rows, cols, inner, size, false);
+    const uint64_t b = c.splits > 1 ? xent_up256((uint64_t)c.splits * rows * cols * 4) : 0;
+    if (b > parts) parts = b;
+  };
+  const int64_t last = n > 0 ? n - (n - 1) / l.piece * l.piece : 0;
+  room(m, k, l.piece);
+  room(m, k, last);
+  room(l.piece, k, m);
+  room(last, k, m);
+  l.bytes = l.parts + parts;
+  return l;
+}
+
+}  // namespace mdet
