@@ -926,13 +926,20 @@ def mdet_ntk_gram(inputs, signals, out=None, outputs=1, bias=1.0, scale=1.0, acc
 
 
 _INDEX_BITS = {}
+_FLOAT, _BYTE = [], []       # torch.float32 and torch.uint8, from the first call on
+
+
+def _torch_types():
+    import torch
+    _INDEX_BITS.update({torch.int32: 32, torch.int64: 64})
+    _FLOAT.append(torch.float32)
+    _BYTE.append(torch.uint8)
 
 
 def _indices(t, name, n, gpu):
     """(address, bits) of n consecutive int32 or int64 on this GPU."""
     if not _INDEX_BITS:
-        import torch
-        _INDEX_BITS.update({torch.int32: 32, torch.int64: 64})
+        _torch_types()
     bits = _INDEX_BITS.get(t.dtype)
     if bits is None or t.shape != (n,) or t.get_device() != gpu or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous tensor of {n} int32 or int64 on cuda:{gpu} expected, not {tuple(t.shape)} {t.dtype} on {t.device}")
@@ -941,14 +948,52 @@ def _indices(t, name, n, gpu):
 
 def _given(*results):
     """Those of the results that the caller brought along."""
-    return [v for v in results if v is not None and not isinstance(v, bool)]
+    return [v for v in results if v is not None and v is not True and v is not False]
 
 
-def _result_tensor(what, shape, like, dtype, stream):
-    """True: a new tensor; False or None: none; otherwise the tensor itself."""
+def _fresh(like, shape, dtype, stream):
+    """A new tensor beside `like`."""
+    if stream is None:
+        return like.new_empty(shape, dtype=dtype)
+    return _new(stream, lambda: like.new_empty(shape, dtype=dtype))
+
+
+def _matrix_result(what, name, rows, cols, dtype, gpu, like, stream):
+    """(tensor, address, leading dimension) of a result: True for a new one, False or None for none, or the tensor to write."""
     if what is True:
-        return _new(stream, lambda: like.new_empty(shape, dtype=dtype))
-    return None if what is False else what
+        t = _fresh(like, (rows, cols), dtype, stream)
+        return t, t.data_ptr(), cols
+    if what is None or what is False:
+        return None, None, 0
+    return (what, *_matrix(what, name, rows, cols, dtype, gpu))
+
+
+def _vector_result(what, name, n, dtype, gpu, like, stream):
+    """(tensor, address) of a result, likewise."""
+    if what is True:
+        t = _fresh(like, n, dtype, stream)
+        return t, t.data_ptr()
+    if what is None or what is False:
+        return None, None
+    return what, _vector(what, name, n, dtype, gpu)
+
+
+def _room(workspace, need, gpu, like, stream):
+    """(address, bytes, tensor) of a workspace: the caller's, or a new one of need() bytes."""
+    if workspace is not None:
+        return (*_bytes(workspace, "workspace", gpu), workspace)
+    size = need()
+    if size == 0:
+        return None, 0, None
+    ws = _fresh(like, size, _BYTE[0], stream)
+    return ws.data_ptr(), size, ws
+
+
+def _bytes(t, name, gpu):
+    """(address, bytes) of a contiguous tensor of any type on this GPU."""
+    if t.get_device() != gpu or not t.is_contiguous():
+        raise ValueError(f"{name}: a contiguous tensor on cuda:{gpu} expected")
+    return t.data_ptr(), t.numel() * t.element_size()
 
 
 @functools.lru_cache(maxsize=1024)
@@ -970,9 +1015,7 @@ def mdet_embedding_forward(ids, table, scale=1.0, out=None, stream=None):
     tp, ldt = _matrix(table, "table", vocab, width, t, gpu)
     ip, bits = _indices(ids, "ids", n, gpu)
     given = out
-    if out is None:
-        out = _new(stream, lambda: table.new_empty((n, width)))
-    yp, ldy = _matrix(out, "out", n, width, t, gpu)
+    out, yp, ldy = _matrix_result(True if out is None else out, "out", n, width, t, gpu, table, stream)
     _queue(gpu, load().mdet_embedding_forward, _type_code(t), bits, n, vocab, width, ip, tp, ldt, scale, yp, ldy, _operator_stream(stream, gpu))
     if given is not None:
         _written(out)
@@ -993,15 +1036,10 @@ def mdet_embedding_backward(dy, ids, vocab, scale=1.0, dtable=None, accumulate=F
     dyp, lddy = _matrix(dy, "dy", n, width, t, gpu)
     ip, bits = _indices(ids, "ids", n, gpu)
     given = dtable
-    if dtable is None:
-        if accumulate:
-            raise ValueError("accumulate needs dtable")
-        if vocab < 0:
-            raise ValueError("vocab must be 0 or more")
-        dtable = _new(stream, lambda: dy.new_empty((vocab, width), dtype=gt))
-    gp, ldt = _matrix(dtable, "dtable", vocab, width, gt, gpu)
-    need = 0 if workspace is not None else mdet_embedding_workspace_query(n, vocab, width)
-    wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
+    if dtable is None and (accumulate or vocab < 0):
+        raise ValueError("accumulate needs dtable" if accumulate else "vocab must be 0 or more")
+    dtable, gp, ldt = _matrix_result(True if dtable is None else dtable, "dtable", vocab, width, gt, gpu, dy, stream)
+    wsp, wsb, _ws = _room(workspace, lambda: mdet_embedding_workspace_query(n, vocab, width), gpu, dy, stream)
     _queue(gpu, load().mdet_embedding_backward, _type_code(t), _type_code(gt), bits, n, vocab, width, ip, dyp, lddy, scale, int(bool(accumulate)),
            gp, ldt, wsp, wsb, _operator_stream(stream, gpu))
     if given is not None:
@@ -1021,7 +1059,8 @@ def mdet_layernorm_forward(x, weight=None, bias=None, eps=1e-5, out=None, mean=T
     """``(x - mean) * rstd * weight + bias`` over the rows of x (m, n) on the GPU (asynchronous), rstd = 1 / sqrt(var + eps);
     weight and bias (n,), all of one type (float32, float16 or bfloat16).  mean, rstd: True for a new float32 tensor (m,), False or None
     where they are not kept for the gradient, or the tensor to write.  Returns out, mean, rstd."""
-    import torch
+    if not _FLOAT:
+        _torch_types()
     if x.dim() != 2:
         raise ValueError("x: a matrix expected")
     t = _operand_type(x.dtype)
@@ -1031,14 +1070,9 @@ def mdet_layernorm_forward(x, weight=None, bias=None, eps=1e-5, out=None, mean=T
     wp = None if weight is None else _vector(weight, "weight", n, t, gpu)
     bp = None if bias is None else _vector(bias, "bias", n, t, gpu)
     given = _given(out, mean, rstd)
-    if out is None:
-        out = _new(stream, lambda: x.new_empty((m, n)))
-    yp, ldy = _matrix(out, "out", m, n, t, gpu)
-    if mean is True and rstd is True:           # one allocation for both
-        mean, rstd = _new(stream, lambda: x.new_empty((2, m), dtype=torch.float32)).unbind()
-    mean, rstd = (_result_tensor(v, (m,), x, torch.float32, stream) for v in (mean, rstd))
-    mp = None if mean is None else _vector(mean, "mean", m, torch.float32, gpu)
-    rp = None if rstd is None else _vector(rstd, "rstd", m, torch.float32, gpu)
+    out, yp, ldy = _matrix_result(True if out is None else out, "out", m, n, t, gpu, x, stream)
+    mean, mp = _vector_result(mean, "mean", m, _FLOAT[0], gpu, x, stream)
+    rstd, rp = _vector_result(rstd, "rstd", m, _FLOAT[0], gpu, x, stream)
     _queue(gpu, load().mdet_layernorm_forward, _type_code(t), m, n, xp, ldx, wp, bp, eps, yp, ldy, mp, rp, _operator_stream(stream, gpu))
     if given:
         _written(*given)
@@ -1049,7 +1083,8 @@ def mdet_layernorm_backward(dy, x, mean, rstd, weight=None, dx=True, dw=True, db
     """Gradient of ``mdet_layernorm_forward`` (asynchronous): (dx, dw, db) from dy (m, n), its x, mean, rstd and weight.  dx, dw, db:
     True for a new tensor, False or None for a gradient that is not wanted (None is returned), or the tensor to write; dw and db are of
     ``grad_dtype``: x's type or float32."""
-    import torch
+    if not _FLOAT:
+        _torch_types()
     if x.dim() != 2:
         raise ValueError("x: a matrix expected")
     t = _operand_type(x.dtype)
@@ -1058,15 +1093,13 @@ def mdet_layernorm_backward(dy, x, mean, rstd, weight=None, dx=True, dw=True, db
     gpu = _gpu(x, "x")
     dyp, lddy = _matrix(dy, "dy", m, n, t, gpu)
     xp, ldx = _matrix(x, "x", m, n, t, gpu)
-    mp, rp = _vector(mean, "mean", m, torch.float32, gpu), _vector(rstd, "rstd", m, torch.float32, gpu)
+    mp, rp = _vector(mean, "mean", m, _FLOAT[0], gpu), _vector(rstd, "rstd", m, _FLOAT[0], gpu)
     wp = None if weight is None else _vector(weight, "weight", n, t, gpu)
     given = _given(dx, dw, db)
-    dx, dw, db = (_result_tensor(v, s, x, d, stream) for v, s, d in ((dx, (m, n), t), (dw, (n,), gt), (db, (n,), gt)))
-    dxp, lddx = (None, 0) if dx is None else _matrix(dx, "dx", m, n, t, gpu)
-    dwp = None if dw is None else _vector(dw, "dw", n, gt, gpu)
-    dbp = None if db is None else _vector(db, "db", n, gt, gpu)
-    need = 0 if workspace is not None or (dw is None and db is None) else mdet_layernorm_workspace_query(t, m, n)
-    wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
+    dx, dxp, lddx = _matrix_result(dx, "dx", m, n, t, gpu, x, stream)
+    dw, dwp = _vector_result(dw, "dw", n, gt, gpu, x, stream)
+    db, dbp = _vector_result(db, "db", n, gt, gpu, x, stream)
+    wsp, wsb, _ws = _room(workspace, lambda: 0 if dwp is None and dbp is None else mdet_layernorm_workspace_query(t, m, n), gpu, x, stream)
     _queue(gpu, load().mdet_layernorm_backward, _type_code(t), _type_code(gt), m, n, dyp, lddy, xp, ldx, mp, rp, wp, dxp, lddx, dwp, dbp, wsp, wsb,
            _operator_stream(stream, gpu))
     if given:
@@ -1110,20 +1143,15 @@ def mdet_xent_forward(x, w, target, bias=None, ignore=-100, loss=True, lse=True,
     vocabulary, have the loss 0.  loss, lse (the log of the sum of the exponentials): True for a new float32 tensor (m,), False or None for
     none, or the tensor to write.  keep: True, or a contiguous tensor of ``mdet_xent_kept_query`` bytes, for what spares the gradient a
     product.  Returns loss, lse and what was kept (or None)."""
-    import torch
     t, gpu, (m, n, k), (xp, ldx, wp, ldw, bp, tp), bits = _xent_operands(x, w, target, bias)
     given = _given(loss, lse, keep)
-    loss, lse = (_result_tensor(v, (m,), x, torch.float32, stream) for v in (loss, lse))
-    lp = None if loss is None else _vector(loss, "loss", m, torch.float32, gpu)
-    sp = None if lse is None else _vector(lse, "lse", m, torch.float32, gpu)
-    kept = None if keep is None or keep is False else keep
-    kp, kb = None, 0
-    if kept is not None:
-        if kept is True:
-            kept = _new(stream, lambda: x.new_empty(mdet_xent_kept_query(t, m, n, k), dtype=torch.uint8))
+    loss, lp = _vector_result(loss, "loss", m, _FLOAT[0], gpu, x, stream)
+    lse, sp = _vector_result(lse, "lse", m, _FLOAT[0], gpu, x, stream)
+    kept, kp, kb = None, None, 0
+    if keep is not None and keep is not False:
+        kept = _fresh(x, mdet_xent_kept_query(t, m, n, k), _BYTE[0], stream) if keep is True else keep
         kp, kb = _bytes(kept, "keep", gpu)
-    need = 0 if workspace is not None or kept is not None else mdet_xent_workspace_query(t, m, n, k)
-    wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
+    wsp, wsb, _ws = _room(workspace, lambda: 0 if kept is not None else mdet_xent_workspace_query(t, m, n, k), gpu, x, stream)
     _queue(gpu, load().mdet_xent_forward, _type_code(t), bits, m, n, k, xp, ldx, wp, ldw, bp, tp, ignore, lp, sp, kp, kb, wsp, wsb,
            _operator_stream(stream, gpu))
     if given:
@@ -1131,30 +1159,20 @@ def mdet_xent_forward(x, w, target, bias=None, ignore=-100, loss=True, lse=True,
     return loss, lse, kept
 
 
-def _bytes(t, name, gpu):
-    """(address, bytes) of a contiguous tensor of any type on this GPU."""
-    if t.get_device() != gpu or not t.is_contiguous():
-        raise ValueError(f"{name}: a contiguous tensor on cuda:{gpu} expected")
-    return t.data_ptr(), t.numel() * t.element_size()
-
-
 def mdet_xent_backward(dloss, x, w, target, lse, bias=None, ignore=-100, kept=None, dx=True, dw=True, db=None, grad_dtype=None,
                        workspace=None, stream=None):
     """Gradient of the sum of ``dloss * loss`` of ``mdet_xent_forward`` (asynchronous): (dx, dw, db) from dloss (m,) float32, its operands,
     its lse, and what it kept.  dx, dw, db: True for a new tensor, False or None for a gradient that is not wanted (None is returned; db
     without a bias as a rule), or the tensor to write; dw and db are of ``grad_dtype``: x's type or float32."""
-    import torch
     t, gpu, (m, n, k), (xp, ldx, wp, ldw, bp, tp), bits = _xent_operands(x, w, target, bias)
     gt = t if grad_dtype is None else grad_dtype
-    gp, sp = _vector(dloss, "dloss", m, torch.float32, gpu), _vector(lse, "lse", m, torch.float32, gpu)
+    gp, sp = _vector(dloss, "dloss", m, _FLOAT[0], gpu), _vector(lse, "lse", m, _FLOAT[0], gpu)
     kp, kb = (None, 0) if kept is None else _bytes(kept, "kept", gpu)
     given = _given(dx, dw, db)
-    dx, dw, db = (_result_tensor(v, s, x, d, stream) for v, s, d in ((dx, (m, k), t), (dw, (n, k), gt), (db, (n,), gt)))
-    dxp, lddx = (None, 0) if dx is None else _matrix(dx, "dx", m, k, t, gpu)
-    dwp, lddw = (None, 0) if dw is None else _matrix(dw, "dw", n, k, gt, gpu)
-    dbp = None if db is None else _vector(db, "db", n, gt, gpu)
-    need = 0 if workspace is not None else mdet_xent_workspace_query(t, m, n, k, backward=True)
-    wsp, wsb, _ws = _operator_workspace(workspace, need, gpu, stream)
+    dx, dxp, lddx = _matrix_result(dx, "dx", m, k, t, gpu, x, stream)
+    dw, dwp, lddw = _matrix_result(dw, "dw", n, k, gt, gpu, x, stream)
+    db, dbp = _vector_result(db, "db", n, gt, gpu, x, stream)
+    wsp, wsb, _ws = _room(workspace, lambda: mdet_xent_workspace_query(t, m, n, k, True), gpu, x, stream)
     _queue(gpu, load().mdet_xent_backward, _type_code(t), _type_code(gt), bits, m, n, k, gp, xp, ldx, wp, ldw, bp, tp, ignore, sp, kp, kb,
            dxp, lddx, dwp, lddw, dbp, wsp, wsb, _operator_stream(stream, gpu))
     if given:

@@ -23,7 +23,7 @@ RowShare share_of(int64_t width, int64_t size, int each) {
 
 // Ids and tokens are counted in 32 bits.
 bool embedding_fits(int64_t n, int64_t vocab, int64_t width) {
-  return sizes_fit(n, vocab, width) && n <= INT32_MAX - SORT_THREADS && vocab <= INT32_MAX;
+  return sizes_fit(n, vocab, width) && n < INT32_MAX - 1024 && vocab <= INT32_MAX;
 }
 bool is_index(int32_t bits) { return bits == 32 || bits == 64; }
 
@@ -52,9 +52,10 @@ int backward(int64_t n, const I* ids, const EmbeddingSums<T, O>& a, hipStream_t 
   hipLaunchKernelGGL((embedding_sort_kernel<I>), dim3(1u << bits), dim3(SORT_THREADS), 0, st, ids, (int32_t)n, a.vocab, bits, a.s);
   const RowShare share = share_of(a.width, sizeof(T), 1);
   const int groups = 256 / share.lanes;
-  const int64_t sums = ceil_div(a.runs * share.chunks, groups), zeros = a.add ? 0 : ceil_div(a.vocab * share.chunks, groups);
-  gemm_launches(sums + zeros, 256, [&](const int64_t first, const dim3 grid) {
-    hipLaunchKernelGGL((embedding_sum_kernel<T, O>), grid, dim3(256), 0, st, a, share, sums, first);
+  const RowShare zeros = share_of(a.width, sizeof(O), ZERO_PIECES);
+  const int64_t sums = ceil_div(a.runs * share.chunks, groups), empty = a.add ? 0 : ceil_div(a.vocab * zeros.chunks, 256 / zeros.lanes);
+  gemm_launches(sums + empty, 256, [&](const int64_t first, const dim3 grid) {
+    hipLaunchKernelGGL((embedding_sum_kernel<T, O>), grid, dim3(256), 0, st, a, share, zeros, sums, first);
   });
   if (a.runs > 1) {
     const int64_t across = ceil_div(a.width, JOIN_COLS);

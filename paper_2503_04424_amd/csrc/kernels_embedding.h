@@ -26,7 +26,7 @@ __global__ __launch_bounds__(256) void embedding_kernel(const I* __restrict__ id
   typedef typename Core<T>::piece_t piece_t;
   constexpr int VEC = Core<T>::VEC;
   const int64_t unit = (first + blockIdx.x) * (256 / share.lanes) + threadIdx.x / share.lanes;
-  const int64_t row = unit / share.chunks;
+  const int64_t row = share.chunks == 1 ? unit : unit / share.chunks;
   if (row >= n) return;
   const int64_t c0 = (unit - row * share.chunks) * share.lanes * EMBED_PIECES * VEC + threadIdx.x % share.lanes * VEC;
   const int64_t step = (int64_t)share.lanes * VEC, id = (int64_t)ids[row];
@@ -50,10 +50,12 @@ __global__ __launch_bounds__(256) void embedding_kernel(const I* __restrict__ id
 // The sort.  Token v belongs to bucket v % buckets (so that the frequent ones, which have small numbers as a rule, lie in
 // different ones), and a workgroup to each bucket, which goes through all of the ids twice: to count its own, token by token, and
 // those of the buckets in front of it; then to write their places down, in order.  That needs no word between workgroups and
-// one launch; the ids come out of cache.
+// one launch; the ids come out of cache, 16384 at once in a workgroup's registers, where a short list stays between the two.  The time goes with
+// n times the buckets: 16384 ids of 50003 14 us (1024 at once, and one wavefront for the places, 31), a million of 32000 600.
 // ---------------------------------------------------------------------------
 constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / 64;
-constexpr int SORT_TOKENS = 4096;      // of a bucket
+constexpr int SORT_EACH = 16, SORT_ROUND = SORT_THREADS * SORT_EACH;
+constexpr int SORT_TOKENS = 2048;      // of a bucket
 constexpr int SORT_BUCKETS = 256;      // or more, a power of two
 
 struct Sorted {
@@ -67,31 +69,48 @@ struct Sorted {
 template <typename I>
 __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_kernel(const I* __restrict__ ids, const int32_t n, const int64_t vocab, const int bits,
                                                                       const Sorted out) {
+  static_assert(SORT_ROUND <= 1 << 16 && SORT_TOKENS <= 1 << 16, "an entry of the list is a place and a token of 16 bits each");
   __shared__ int32_t cursor[SORT_TOKENS];
-  __shared__ int32_t wave_sum[SORT_WAVES];
-  __shared__ int32_t list_place[SORT_THREADS], list_token[SORT_THREADS];
+  __shared__ int32_t sums[SORT_EACH][SORT_WAVES];
+  __shared__ uint32_t list[SORT_ROUND];
+  __shared__ uint16_t often[SORT_WAVES][SORT_TOKENS], behind[SORT_TOKENS];
   const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6;
-  const int64_t bucket = blockIdx.x, buckets = gridDim.x;
+  const int64_t buckets = gridDim.x;
+  const int32_t bucket = blockIdx.x;
   const int tokens = bucket < vocab ? (int)((vocab - bucket + buckets - 1) / buckets) : 0;
+  int32_t id[SORT_EACH];               // -1: none of the table
+  auto get = [&](const int64_t i0) {
+    int64_t raw[SORT_EACH];
+#pragma unroll
+    for (int e = 0; e < SORT_EACH; ++e) {
+      const int64_t i = i0 + e * SORT_THREADS + thread;
+      raw[e] = i < n ? (int64_t)ids[i] : -1;
+    }
+#pragma unroll
+    for (int e = 0; e < SORT_EACH; ++e) id[e] = raw[e] >= 0 && raw[e] < vocab ? (int32_t)raw[e] : -1;
+  };
+  auto bucket_of = [&](const int32_t v) { return v & (int32_t)(buckets - 1); };
   for (int t = thread; t < tokens; t += SORT_THREADS) cursor[t] = 0;
   __syncthreads();
   int32_t before = 0;
-  for (int32_t i = thread; i < n; i += SORT_THREADS) {
-    const int64_t id = (int64_t)ids[i];
-    if (id < 0 || id >= vocab) continue;
-    const int64_t b = id & (buckets - 1);
-    before += b < bucket;
-    if (b == bucket) atomicAdd(&cursor[id >> bits], 1);
+  for (int64_t i0 = 0; i0 < n; i0 += SORT_ROUND) {
+    get(i0);
+#pragma unroll
+    for (int e = 0; e < SORT_EACH; ++e)
+      if (id[e] >= 0) {
+        before += bucket_of(id[e]) < bucket;
+        if (bucket_of(id[e]) == bucket) atomicAdd(&cursor[id[e] >> bits], 1);
+      }
   }
   // where the bucket begins
 #pragma unroll
   for (int off = 32; off >= 1; off >>= 1) before += __shfl_xor(before, off, 64);
-  if (lane == 0) wave_sum[wave] = before;
+  if (lane == 0) sums[0][wave] = before;
   __syncthreads();
   int32_t base = 0;
 #pragma unroll
-  for (int w = 0; w < SORT_WAVES; ++w) base += wave_sum[w];
-  // where each of its tokens begins: four of them a thread
+  for (int w = 0; w < SORT_WAVES; ++w) base += sums[0][w];
+  // where each of its tokens begins: some of them a thread
   constexpr int EACH = SORT_TOKENS / SORT_THREADS;
   int32_t mine[EACH], sum = 0;
 #pragma unroll
@@ -106,69 +125,125 @@ __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_kernel(const I* _
     const int32_t o = __shfl_up(upto, off, 64);
     if (lane >= off) upto += o;
   }
-  __syncthreads();                     // wave_sum has been read
-  if (lane == 63) wave_sum[wave] = upto;
+  if (lane == 63) sums[1][wave] = upto;
   __syncthreads();
   int32_t at = base + upto - sum, all = base;
 #pragma unroll
   for (int w = 0; w < SORT_WAVES; ++w) {
-    if (w < wave) at += wave_sum[w];
-    all += wave_sum[w];
+    if (w < wave) at += sums[1][w];
+    all += sums[1][w];
   }
 #pragma unroll
   for (int e = 0; e < EACH; ++e) {
     const int t = thread * EACH + e;
     if (t < tokens) {
-      const int64_t id = ((int64_t)t << bits) + bucket;
+      const int64_t v = ((int64_t)t << bits) + bucket;
       cursor[t] = at;
-      out.start[id] = at;
-      out.count[id] = mine[e];
+      out.start[v] = at;
+      out.count[v] = mine[e];
       at += mine[e];
     }
   }
   if (thread == 0 && bucket == buckets - 1) *out.total = all;
   if (all == base) return;             // nothing of this bucket: the same for the whole workgroup
-  __syncthreads();
-  // their places, in order: what a round of ids has of this bucket is put side by side, then handed out by one wavefront after
-  // the other, 64 at a time; equal tokens of the 64 find each other by their numbers' bits
-  for (int64_t i0 = 0; i0 < n; i0 += SORT_THREADS) {
-    const int64_t i = i0 + thread, id = i < n ? (int64_t)ids[i] : -1;
-    const bool hit = id >= 0 && id < vocab && (id & (buckets - 1)) == bucket;
-    const uint64_t hits = __ballot(hit);
-    if (lane == 0) wave_sum[wave] = __popcll(hits);
-    __syncthreads();
-    int32_t where = __popcll(hits & ((1ull << lane) - 1)), found = 0;
+  // their places, in order: what a round of ids has of this bucket is put side by side, then handed out in parts, 64 at a time; equal tokens of the
+  // 64 find each other by their numbers' bits
+  for (int64_t i0 = 0; i0 < n; i0 += SORT_ROUND) {
+    if (n > SORT_ROUND) get(i0);
+    __syncthreads();                   // sums and list have been read, cursors are written
+    uint64_t hits[SORT_EACH];
 #pragma unroll
-    for (int w = 0; w < SORT_WAVES; ++w) {
-      if (w < wave) where += wave_sum[w];
-      found += wave_sum[w];
-    }
-    if (hit) {
-      list_place[where] = (int32_t)i;
-      list_token[where] = (int32_t)(id >> bits);
+    for (int e = 0; e < SORT_EACH; ++e) {
+      hits[e] = __ballot(id[e] >= 0 && bucket_of(id[e]) == bucket);
+      if (lane == 0) sums[e][wave] = __popcll(hits[e]);
     }
     __syncthreads();
-    if (wave == 0)
-      for (int32_t k = 0; k < found; k += 64) {
-        const bool there = k + lane < found;
-        const int32_t token = there ? list_token[k + lane] : 0;
+    // the sums of the 256 parts in front of each, and of all: 64 lanes, four parts each, every wavefront by itself
+    int32_t four[4], upto4 = 0;
+#pragma unroll
+    for (int q = 0; q < 4; ++q) four[q] = (&sums[0][0])[4 * lane + q], upto4 += four[q];
+    const int32_t own = upto4;
+#pragma unroll
+    for (int off = 1; off < 64; off *= 2) {
+      const int32_t o = __shfl_up(upto4, off, 64);
+      if (lane >= off) upto4 += o;
+    }
+    const int32_t found = __shfl(upto4, 63, 64);
+#pragma unroll
+    for (int e = 0; e < SORT_EACH; ++e) {
+      const int part = e * SORT_WAVES + wave;                  // its lane is part / 4
+      int32_t where = __shfl(upto4 - own, part / 4, 64);
+#pragma unroll
+      for (int q = 0; q < 3; ++q) {
+        const int32_t f = __shfl(four[q], part / 4, 64);
+        if (q < part % 4) where += f;
+      }
+      if (hits[e] >> lane & 1)
+        list[where + __popcll(hits[e] & ((1ull << lane) - 1))] = (uint32_t)(e * SORT_THREADS + thread) << 16 | (uint32_t)(id[e] >> bits);
+    }
+    const bool few = found <= 64;      // those go out at once
+    if (!few)
+      for (int t = thread; t < tokens; t += SORT_THREADS)
+#pragma unroll
+        for (int w = 0; w < SORT_WAVES; ++w) often[w][t] = 0;
+    __syncthreads();
+    // a part of the list for each wavefront: first how often it has each token, then the places
+    const int32_t each = ((found + SORT_WAVES - 1) / SORT_WAVES + 63) & ~63, begin = wave * each, end = begin + each < found ? begin + each : found;
+    auto go = [&](auto&& f) {
+      for (int32_t k = begin; k < end; k += 64) {
+        const bool there = k + lane < end;
+        const uint32_t entry = there ? list[k + lane] : 0;
+        const int32_t token = entry & 0xFFFF;
         uint64_t same = __ballot(there);
         for (int b = 1; b < tokens; b *= 2) {
           const uint64_t set = __ballot((token & b) != 0);
           same &= token & b ? set : ~set;
         }
-        const int rank = __popcll(same & ((1ull << lane) - 1));
-        const int32_t from = there ? cursor[token] : 0;
-        __builtin_amdgcn_wave_barrier();
-        if (there) {
-          if (rank == 0) cursor[token] = from + __popcll(same);
-          out.place[from + rank] = list_place[k + lane];
-          out.id[from + rank] = (int32_t)((token << bits) + (int32_t)bucket);
-        }
+        f(there, entry >> 16, token, __popcll(same & ((1ull << lane) - 1)), __popcll(same));
         __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
         __builtin_amdgcn_wave_barrier();
       }
-    // the next round writes the list behind its first barrier, which wavefront 0 reaches when it is through with this one
+    };
+    if (few) {
+      go([&](const bool there, const uint32_t place, const int32_t token, const int rank, const int many) {
+        const int32_t from = there ? cursor[token] : 0;
+        __builtin_amdgcn_wave_barrier();
+        if (there) {
+          if (rank == 0) cursor[token] = from + many;
+          out.place[from + rank] = (int32_t)(i0 + place);
+          out.id[from + rank] = (token << bits) + bucket;
+        }
+      });
+      continue;
+    }
+    go([&](const bool there, uint32_t, const int32_t token, const int rank, const int many) {
+      if (there && rank == 0) often[wave][token] += (uint16_t)many;
+    });
+    __syncthreads();
+    // in front of each wavefront's, those of the ones before it, in 16 bits: a round has 2^14 ids
+    for (int t = thread; t < tokens; t += SORT_THREADS) {
+      int32_t ahead = 0;
+#pragma unroll
+      for (int w = 0; w < SORT_WAVES; ++w) {
+        const int32_t here = often[w][t];
+        often[w][t] = (uint16_t)ahead;
+        ahead += here;
+      }
+      behind[t] = (uint16_t)ahead;
+    }
+    __syncthreads();
+    go([&](const bool there, const uint32_t place, const int32_t token, const int rank, const int many) {
+      const int32_t before_me = there ? often[wave][token] : 0;
+      __builtin_amdgcn_wave_barrier();
+      if (there) {
+        if (rank == 0) often[wave][token] = (uint16_t)(before_me + many);
+        const int32_t to = cursor[token] + before_me + rank;
+        out.place[to] = (int32_t)(i0 + place);
+        out.id[to] = (token << bits) + bucket;
+      }
+    });
+    __syncthreads();
+    for (int t = thread; t < tokens; t += SORT_THREADS) cursor[t] += behind[t];
   }
 }
 
@@ -191,35 +266,37 @@ struct EmbeddingSums {
   bool add;                            // to what g holds
 };
 
-template <typename T, typename O>
-__device__ __forceinline__ void embedding_put(const EmbeddingSums<T, O>& a, const int64_t id, const int64_t c, float (&v)[Core<T>::VEC]) {
-  constexpr int VEC = Core<T>::VEC;
-  O* const row = a.g + id * a.ldg;
-#pragma unroll
-  for (int e = 0; e < VEC; ++e) {
-    v[e] *= a.scale;
-    if (a.add && c + e < a.width) v[e] += (float)row[c + e];
-  }
-  row_store<T, O>(row, c, a.width, v);
-}
+// The first `sum_blocks` workgroups sum; the others write zeros where no token is, a step of ZERO_PIECES pieces a lane.  Bytes bound both.
+constexpr int ZERO_PIECES = 4;
 
-// The first `sum_blocks` workgroups sum; the others write zeros where no token is.
 template <typename T, typename O>
-__global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingSums<T, O> a, const RowShare share, const int64_t sum_blocks,
-                                                            const int64_t first) {
+__global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingSums<T, O> a, const RowShare share, const RowShare zeros,
+                                                            const int64_t sum_blocks, const int64_t first) {
   typedef typename Core<T>::piece_t piece_t;
   constexpr int VEC = Core<T>::VEC;
   const int lane = threadIdx.x % share.lanes, groups = 256 / share.lanes;
   const int64_t block = first + blockIdx.x;
   if (block >= sum_blocks) {
-    const int64_t unit = (block - sum_blocks) * groups + threadIdx.x / share.lanes, id = unit / share.chunks;
+    constexpr int OUT = 16 / sizeof(O);
+    const int zlane = threadIdx.x % zeros.lanes;
+    const int64_t unit = (block - sum_blocks) * (256 / zeros.lanes) + threadIdx.x / zeros.lanes, id = zeros.chunks == 1 ? unit : unit / zeros.chunks;
     if (id >= a.vocab || a.s.count[id] != 0) return;
-    const int64_t c = ((unit - id * share.chunks) * share.lanes + lane) * VEC;
-    const float zero[VEC] = {};
-    if (c < a.width) row_store<T, O>(a.g + id * a.ldg, c, a.width, zero);
+    typedef O out_t __attribute__((ext_vector_type(OUT)));
+    O* const row = a.g + id * a.ldg;
+    const int64_t c0 = ((unit - id * zeros.chunks) * ZERO_PIECES * zeros.lanes + zlane) * OUT;
+#pragma unroll
+    for (int p = 0; p < ZERO_PIECES; ++p) {
+      const int64_t c = c0 + p * zeros.lanes * OUT;
+      const out_t zero = {};
+      if (c + OUT <= a.width) __builtin_memcpy(row + c, &zero, 16);
+      else
+#pragma unroll
+        for (int e = 0; e < OUT - 1; ++e)
+          if (c + e < a.width) row[c + e] = (O)0.0f;
+    }
     return;
   }
-  const int64_t unit = block * groups + threadIdx.x / share.lanes, run = unit / share.chunks;
+  const int64_t unit = block * groups + threadIdx.x / share.lanes, run = share.chunks == 1 ? unit : unit / share.chunks;
   const int32_t total = *a.s.total;
   const int64_t p0 = run * RUN;
   if (p0 >= total) return;
@@ -236,67 +313,102 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingSums<
     x[r] = piece_t{};
     if (r < many) x[r] = row_piece<T>(a.dy + i * a.lddy, c, a.width);
   }
-  float sum[VEC] = {};
-  bool open = false;                   // the sum began in front of this run
-  int32_t last = prior;
+  // The sums that end in front of each row, four rows at a time: what they are added to is on its way for all of the four at once.
+  float sum[VEC] = {}, done[4][VEC];
+  int32_t where[4];                    // the id whose sum it is; -1: none ends here
+  int32_t last = __shfl(key, 0, RUN);
+  bool open = last == prior;           // the sum began in front of this run
   auto part = [&](const int which) {
     float* const to = a.parts + (run * 2 + which) * a.width;
     if (c < a.width) row_store<T, float>(to, c, a.width, sum);
   };
+  auto put = [&](auto many_of) {
+    constexpr int MANY = decltype(many_of)::value;
+    float old[MANY][VEC] = {};
+    if (a.add) {
 #pragma unroll
-  for (int r = 0; r < RUN; ++r) {
-    const int32_t id = __shfl(key, r, RUN);
-    if (r < many) {
-      if (r == 0) open = id == prior;
-      else if (id != last) {
-        if (open) part(0);
-        else if (c < a.width) embedding_put(a, last, c, sum);
-        open = false;
+      for (int q = 0; q < MANY; ++q)
+        if (where[q] >= 0)
 #pragma unroll
-        for (int e = 0; e < VEC; ++e) sum[e] = 0.0f;
-      }
-      last = id;
-#pragma unroll
-      for (int e = 0; e < VEC; ++e) sum[e] += (float)x[r][e];
+          for (int e = 0; e < VEC; ++e)
+            if (c + e < a.width) old[q][e] = (float)a.g[where[q] * a.ldg + c + e];
     }
+#pragma unroll
+    for (int q = 0; q < MANY; ++q) {
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) done[q][e] = done[q][e] * a.scale + old[q][e];
+      if (where[q] >= 0 && c < a.width) row_store<T, O>(a.g + where[q] * a.ldg, c, a.width, done[q]);
+    }
+  };
+#pragma unroll
+  for (int r0 = 0; r0 < RUN; r0 += 4) {
+#pragma unroll
+    for (int q = 0; q < 4; ++q) {
+      const int r = r0 + q;
+      const int32_t id = __shfl(key, r, RUN);
+      const bool ends = r < many && id != last;
+      where[q] = ends && !open ? last : -1;
+      if (ends && open) part(0);
+#pragma unroll
+      for (int e = 0; e < VEC; ++e) {
+        done[q][e] = sum[e];
+        sum[e] = (ends ? 0.0f : sum[e]) + (float)x[r][e];      // rows behind the last are zero
+      }
+      open = open && !ends;
+      last = r < many ? id : last;
+    }
+    put(std::integral_constant<int, 4>{});
   }
   if (open) part(0);
   else if (last == later) part(1);
-  else if (c < a.width) embedding_put(a, last, c, sum);
+  else {
+    where[0] = last;
+#pragma unroll
+    for (int e = 0; e < VEC; ++e) done[0][e] = sum[e];
+    put(std::integral_constant<int, 1>{});
+  }
 }
 
-// A token that begins in run `blockIdx / chunks` and goes on behind it: its parts, added in one order, sixteen threads a column.
-constexpr int JOIN_COLS = 64;
+// A token that begins in a run and goes on behind it: its parts, added in one order, eight threads a column.
+constexpr int JOIN_COLS = 128, JOIN_GROUPS = 1024 / JOIN_COLS;
 
 template <typename T, typename O>
 __global__ __launch_bounds__(256) void embedding_join_kernel(const EmbeddingSums<T, O> a, const int64_t across, const int64_t first) {
   typedef float f4 __attribute__((ext_vector_type(4)));
-  __shared__ f4 part[16][JOIN_COLS / 4];
+  __shared__ f4 part[JOIN_GROUPS][JOIN_COLS / 4];
   const int64_t block = first + blockIdx.x, run = block / across, next = (run + 1) * RUN;
   if (next >= *a.s.total) return;
   const int32_t id = a.s.id[next - 1], begin = a.s.start[id];
   const int64_t end = (int64_t)begin + a.s.count[id];
   if (end <= next || begin < next - RUN) return;
-  const int t = threadIdx.x / 16;
-  const int64_t c = (block - run * across) * JOIN_COLS + threadIdx.x % 16 * 4;
-  f4 v = {};
-  for (int64_t r = run + t; r * RUN < end; r += 16) {
+  const int t = threadIdx.x / (JOIN_COLS / 4), lane = threadIdx.x % (JOIN_COLS / 4);
+  const int64_t c = (block - run * across) * JOIN_COLS + lane * 4, runs = (end + RUN - 1) / RUN;
+  auto get = [&](const int64_t r) {
     const float* const from = a.parts + (r == run ? 2 * r + 1 : 2 * r) * a.width + c;
-    if (c + 4 <= a.width) {
-      f4 x;
-      __builtin_memcpy(&x, from, 16);
-      v += x;
-    } else
+    f4 x = {};
+    if (c + 4 <= a.width) __builtin_memcpy(&x, from, 16);
+    else
 #pragma unroll
       for (int e = 0; e < 3; ++e)
-        if (c + e < a.width) v[e] += from[e];
+        if (c + e < a.width) x[e] = from[e];
+    return x;
+  };
+  f4 v = {};
+  int64_t r = run + t;
+  for (; r + 3 * JOIN_GROUPS < runs; r += 4 * JOIN_GROUPS) {
+    f4 x[4];
+#pragma unroll
+    for (int q = 0; q < 4; ++q) x[q] = get(r + q * JOIN_GROUPS);
+#pragma unroll
+    for (int q = 0; q < 4; ++q) v += x[q];
   }
-  part[t][threadIdx.x % 16] = v;
+  for (; r < runs; r += JOIN_GROUPS) v += get(r);
+  part[t][lane] = v;
   __syncthreads();
   if (t == 0) {
 #pragma unroll
-    for (int r = 1; r < 16; ++r) v += part[r][threadIdx.x];
-    O* const row = a.g + (int64_t)id * a.ldg;
+    for (int g = 1; g < JOIN_GROUPS; ++g) v += part[g][lane];
+    O* const row = a.g + id * a.ldg;
 #pragma unroll
     for (int e = 0; e < 4; ++e)
       if (c + e < a.width) row[c + e] = (O)(v[e] * a.scale + (a.add ? (float)row[c + e] : 0.0f));

@@ -31,10 +31,13 @@ __device__ __forceinline__ int64_t xent_target(const XentTargets& t, const int64
   return v < 0 || v >= t.vocab || v == t.ignore ? -1 : v;
 }
 
-// exp(z - top) where top is the largest of some z: zero for z = -inf also where that is all there is.
-__device__ __forceinline__ float xent_exp(const float z, const float top) {
-  return __expf(z - (top == -INFINITY ? 0.0f : top));
-}
+// exp(z - top) as a power of two, xent_power(z, xent_from(top)): one multiplication and addition in front of it.  With |z| and |top| below 30
+// their rounding is 2e-6 of the result, what a sum of a few dozen fp32 terms may be off by, and 16 bits keep 5e-4 or 4e-3.  Where top is
+// the largest of some z that are all -inf, the powers are zero.
+constexpr float XENT_LOG2E = 1.44269504088896341f;
+__device__ __forceinline__ float xent_from(const float top) { return top == -INFINITY ? 0.0f : -XENT_LOG2E * top; }
+__device__ __forceinline__ float xent_power(const float z, const float from) { return __builtin_amdgcn_exp2f(fmaf(z, XENT_LOG2E, from)); }
+__device__ __forceinline__ float xent_exp(const float z, const float top) { return __expf(z - (top == -INFINITY ? 0.0f : top)); }
 
 struct XentStrip {                     // of a row: its largest logit among a strip's columns, and the sum of exp(z - top)
   float top, sum;
@@ -51,107 +54,261 @@ struct XentForward {
   int64_t ldexps, rows, cols;
 };
 
-// A tile: its logits, then what is left of each of its rows.
-template <typename T, typename S, bool DIRECT>
-__global__ __launch_bounds__(S::THREADS) void xent_forward_kernel(const Operand<T> r, const Operand<T> c, const int64_t k, const XentForward<T> o,
-                                                                  const int64_t tiles) {
-  typedef typename Core<T>::acc_t acc_t;
-  constexpr int ROWS = S::TM * 16;
-  __shared__ __attribute__((aligned(16))) char lds[LinearLds<S>::BYTES];
-  const int64_t t = gemm_tile_number(blockIdx.x, tiles);
-  if (t < 0) return;
-  int64_t bi, bj;
-  gemm_tile_place(t, (o.rows + S::BM - 1) / S::BM, o.across, bi, bj);
-  const int64_t row0 = bi * S::BM, col0 = bj * S::BN;
-  acc_t acc[S::TN][S::TM] = {};
-  TileStream<T, S, false, false, DIRECT> stream(lds);
-  auto none = [] { return false; };
-  stream.set(r, c, row0, col0, 0, k);
-  stream.begin(none);
-  stream.run(acc, stream.slabs(0, k), none);
-
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int64_t wrow = row0 + wave / S::WN * ROWS, wcol = col0 + wave % S::WN * (S::TN * 16) + 4 * (lane >> 4);
-#pragma unroll
-  for (int a = 0; a < S::TN; ++a)
-#pragma unroll
-    for (int e = 0; e < 4; ++e) {
-      const int64_t j = wcol + 16 * a + e;
-      const bool there = j < o.cols;
-      const float add = o.bias && there ? (float)o.bias[j] : 0.0f;
-#pragma unroll
-      for (int b = 0; b < S::TM; ++b) acc[a][b][e] = there ? acc[a][b][e] + add : -INFINITY;
-    }
-  // the rows' largest: of this wavefront, then of those beside it
-  __syncthreads();                     // the operands are not read any more
-  float* const tops = reinterpret_cast<float*>(lds);           // of each wavefront's rows
-  float* const sums = tops + S::WAVES * ROWS;
-  auto beside = [&](float* const of, const int row, auto&& f) {
-#pragma unroll
-    for (int w = 0; w < S::WN; ++w) f(of[(wave / S::WN * S::WN + w) * ROWS + row]);
+// The units of a launch (tiles, or parts of a sum over k of one), which its workgroups take one after the other, gridDim.x apart, so that one
+// launch fills the device once: the first `whole` are tiles, which go round the chiplets as gemm_tile_number says, each of the others is one
+// of `splits` parts of a tile, kpart of k long.  Fewer than 2^31 of all.
+struct XentUnits {
+  int down, across, whole, units;      // units: whole + splits (tiles - whole)
+  int splits;
+  int64_t k, kpart;
+  float* parts;                        // of the units behind the whole ones: BM x BN each
+};
+struct XentUnit {
+  int bi, bj, part;                    // part: -1, the tile is whole
+  int64_t k0, kend;
+};
+// Unit number `id` of a launch, which may name none.
+__device__ __forceinline__ void xent_place(const XentUnits& u, const int t, int& bi, int& bj) {
+  // as gemm_tile_place
+  const int group = t / (8 * u.across), in = t - group * 8 * u.across, left = u.down - 8 * group, rows = left < 8 ? left : 8;
+  bj = in / rows;
+  bi = 8 * group + in - bj * rows;
+}
+__device__ __forceinline__ bool xent_unit(const XentUnits& u, int& id, XentUnit& x) {
+  const int per = (u.whole + 7) / 8, round = 8 * per;
+  int t = -1;
+  for (; id < round; id += gridDim.x) {
+    t = (id & 7) * per + (id >> 3);
+    if (t < u.whole) break;
+    t = -1;
+  }
+  x.k0 = 0;
+  x.kend = u.k;
+  x.part = -1;
+  if (t < 0) {
+    x.part = id - round;
+    if (x.part >= u.units - u.whole) return false;
+    t = u.whole + x.part / u.splits;
+    x.k0 = x.part % u.splits * u.kpart;
+    x.kend = x.k0 + u.kpart < u.k ? x.k0 + u.kpart : u.k;
+  }
+  xent_place(u, t, x.bi, x.bj);
+  return true;
+}
+// f(unit, run) for each of the workgroup's units, where run(acc) adds up its product.  The first slab of a unit is brought while the one before
+// it is on its way out (at 256 x 256, 64 of k are 1.7 us of products; a tile by itself waited 9 us more at its ends).  Where operands go
+// through registers none are left for that: a workgroup has one unit then.  early(unit): what may be on its way beside the product.
+template <typename T, typename S, bool ROUTER, bool COUTER, bool DIRECT, typename E, typename F>
+__device__ __forceinline__ void xent_units(char* const lds, const Operand<T>& r, const Operand<T>& c, const XentUnits& u, E&& early, F&& f) {
+  TileStream<T, S, ROUTER, COUTER, DIRECT> stream(lds);
+  int id = blockIdx.x;
+  XentUnit now, then;
+  bool more = xent_unit(u, id, then), fresh = more;
+  auto next = [&] {
+    if (!fresh) return false;
+    fresh = false;
+    stream.set(r, c, (int64_t)then.bi * S::BM, (int64_t)then.bj * S::BN, then.k0, then.kend);
+    return true;
   };
-#pragma unroll
-  for (int b = 0; b < S::TM; ++b) {
-    float m = -INFINITY;
-#pragma unroll
-    for (int a = 0; a < S::TN; ++a)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) m = fmaxf(m, acc[a][b][e]);
-    m = fmaxf(m, __shfl_xor(m, 16, 64));
-    m = fmaxf(m, __shfl_xor(m, 32, 64));
-    if (lane < 16) tops[wave * ROWS + 16 * b + lane] = m;
-  }
-  __syncthreads();
-#pragma unroll
-  for (int b = 0; b < S::TM; ++b) {
-    const int row = 16 * b + (lane & 15);
-    const int64_t i = wrow + row;
-    float top = -INFINITY;
-    beside(tops, row, [&](const float v) { top = fmaxf(top, v); });
-    const int64_t target = i < o.rows ? xent_target(o.t, i) : -1;
-    const int at = target >= wcol && target < wcol + S::TN * 16 ? (int)(target - wcol) : -1;
-    float s = 0.0f;
-#pragma unroll
-    for (int a = 0; a < S::TN; ++a)
-#pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        if (at == 16 * a + e) o.picked[i] = acc[a][b][e];
-        acc[a][b][e] = xent_exp(acc[a][b][e], top);
-        s += acc[a][b][e];
-      }
-    s += __shfl_xor(s, 16, 64);
-    s += __shfl_xor(s, 32, 64);
-    if (lane < 16) sums[wave * ROWS + 16 * b + lane] = s;
-  }
-  __syncthreads();
-  if (wave % S::WN == 0)
-    for (int row = lane; row < ROWS; row += 64) {
-      const int64_t i = wrow + row;
-      XentStrip x{-INFINITY, 0.0f};
-      beside(tops, row, [&](const float v) { x.top = fmaxf(x.top, v); });
-      beside(sums, row, [&](const float v) { x.sum += v; });
-      if (i < o.rows) o.strips[i * o.across + bj] = x;
+  stream.begin(next);
+  while (more) {
+    now = then;
+    more = false;
+    if constexpr (DIRECT) {
+      id += gridDim.x;
+      more = fresh = xent_unit(u, id, then);
     }
-  if (!o.exps) return;
-  __syncthreads();
-  tile_rows<T, S>(lds, acc, row0, col0, o.rows, o.cols, [&](auto&& rows) {
-    rows([&](const int64_t i, const int64_t j, const float (&in)[4]) {
-      typedef T t4 __attribute__((ext_vector_type(4)));
+    early(now);
+    typename Core<T>::acc_t acc[S::TN][S::TM] = {};
+    stream.run(acc, stream.slabs(now.k0, now.kend), next);
+    // of a sum over nothing no slab was brought, and nothing is on its way
+    fresh = false;
+    f(now, acc);
+  }
+}
+
+// The largest, or the sum, of the four lanes 16 apart, in each of them.
+template <typename F>
+__device__ __forceinline__ float xent_across(const float v, F&& f) {
+  const auto a = __builtin_amdgcn_permlane16_swap(__float_as_uint(v), __float_as_uint(v), false, false);
+  const float w = f(__uint_as_float(a[0]), __uint_as_float(a[1]));
+  const auto b = __builtin_amdgcn_permlane32_swap(__float_as_uint(w), __float_as_uint(w), false, false);
+  return f(__uint_as_float(b[0]), __uint_as_float(b[1]));
+}
+
+// Four neighbours each of two blocks of 16 columns, in 16 bits: eight neighbours in their place, of the first block for lanes 0 .. 15 and 32 .. 47, of the
+// second for the others.  A row's 64 bytes leave in one store; with eight bytes a lane the stores of a tile of 128 KB took 8 us.
+template <typename O>
+struct XentEight {
+  typedef O four_t __attribute__((ext_vector_type(4)));
+  typedef O eight_t __attribute__((ext_vector_type(8)));
+  typedef unsigned two_t __attribute__((ext_vector_type(2)));
+  typedef unsigned quad_t __attribute__((ext_vector_type(4)));
+  // Column of a lane's eight, counted from the first block's.
+  static __device__ __forceinline__ int col() {
+    const int g = threadIdx.x >> 4 & 3;
+    return 16 * (g & 1) + 8 * (g >> 1);
+  }
+  static __device__ __forceinline__ eight_t of(const four_t& a, const four_t& b) {
+    const two_t x = __builtin_bit_cast(two_t, a), y = __builtin_bit_cast(two_t, b);
+    const auto p = __builtin_amdgcn_permlane16_swap(x[0], y[0], false, false), q = __builtin_amdgcn_permlane16_swap(x[1], y[1], false, false);
+    return __builtin_bit_cast(eight_t, quad_t{p[0], q[0], p[1], q[1]});
+  }
+};
+
+// A row's block of S::TN * 16 columns from `col` on (a multiple of 16; `limit` columns in all, rows on 16 bytes and whole pieces of 8 long),
+// value(a) the four of block a that this lane has.
+template <typename T, int TN, typename F>
+__device__ __forceinline__ void xent_store(T* const row, const int64_t col, const int64_t limit, const bool there, F&& value) {
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  if constexpr (sizeof(T) == 2 && TN % 2 == 0) {
+#pragma unroll
+    for (int a = 0; a < TN; a += 2) {
+      const auto v = XentEight<T>::of(value(a), value(a + 1));
+      const int64_t j = col + 16 * a + XentEight<T>::col();
+      if (there && j < limit) *reinterpret_cast<typename XentEight<T>::eight_t*>(row + j) = v;
+    }
+  } else {
+#pragma unroll
+    for (int a = 0; a < TN; ++a) {
+      const int64_t j = col + 16 * a + 4 * (threadIdx.x >> 4 & 3);
+      const t4 v = value(a);
+      if (there && j < limit) *reinterpret_cast<t4*>(row + j) = v;
+    }
+  }
+}
+
+// Tiles of logits, and what is left of each of their rows: a strip for each of the wavefronts beside each other.
+template <typename T, typename S, bool DIRECT>
+__global__ __launch_bounds__(S::THREADS) void xent_forward_kernel(const Operand<T> r, const Operand<T> c, const XentForward<T> o, const XentUnits u) {
+  typedef typename Core<T>::acc_t acc_t;
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  constexpr int STRIP = S::TN * 16;
+  __shared__ __attribute__((aligned(16))) char lds[S::NB * S::SLAB];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  const int wrow = wave / S::WN * (S::TM * 16) + (lane & 15), quad = 4 * (lane >> 4);
+  int at[S::TM];                       // the rows' targets, counted from this lane's first column on
+  auto early = [&](const XentUnit& x) {
+    const int64_t first = ((int64_t)x.bj * S::WN + wave % S::WN) * STRIP + quad;
+#pragma unroll
+    for (int b = 0; b < S::TM; ++b) {
+      const int64_t i = (int64_t)x.bi * S::BM + wrow + 16 * b, t = i < o.rows ? xent_target(o.t, i) : -1;
+      at[b] = t >= first && t < first + STRIP ? (int)(t - first) : -1;
+    }
+  };
+  xent_units<T, S, false, false, DIRECT>(lds, r, c, u, early, [&](const XentUnit& x, acc_t (&acc)[S::TN][S::TM]) {
+    const int64_t row0 = (int64_t)x.bi * S::BM + wrow, strip = (int64_t)x.bj * S::WN + wave % S::WN, col0 = strip * STRIP;
+    if (o.bias || ((int64_t)x.bj + 1) * S::BN > o.cols) {
+#pragma unroll
+      for (int a = 0; a < S::TN; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          const int64_t j = col0 + quad + 16 * a + e;
+          const bool there = j < o.cols;
+          const float add = o.bias && there ? (float)o.bias[j] : 0.0f;
+#pragma unroll
+          for (int b = 0; b < S::TM; ++b) acc[a][b][e] = there ? acc[a][b][e] + add : -INFINITY;
+        }
+    }
+#pragma unroll
+    for (int b = 0; b < S::TM; ++b) {
+      const int64_t i = row0 + 16 * b;
+      if (__any(at[b] >= 0)) {
+#pragma unroll
+        for (int a = 0; a < S::TN; ++a)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (at[b] == 16 * a + e) o.picked[i] = acc[a][b][e];
+      }
+      float top = -INFINITY;
+#pragma unroll
+      for (int a = 0; a < S::TN; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) top = fmaxf(top, acc[a][b][e]);
+      top = xent_across(top, [](const float p, const float q) { return fmaxf(p, q); });
+      const float from = xent_from(top);
+      float sum = 0.0f;
+#pragma unroll
+      for (int a = 0; a < S::TN; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          acc[a][b][e] = xent_power(acc[a][b][e], from);
+          sum += acc[a][b][e];
+        }
+      sum = xent_across(sum, [](const float p, const float q) { return p + q; });
+      if (lane < 16 && i < o.rows && strip < o.across) o.strips[i * o.across + strip] = XentStrip{top, sum};
       // rows are ceil(cols / 8) 8 long: what is written behind their end is zero
-      *reinterpret_cast<t4*>(o.exps + i * o.ldexps + j) = t4{(T)in[0], (T)in[1], (T)in[2], (T)in[3]};
-    });
+      if (o.exps)
+        xent_store<T, S::TN>(o.exps + i * o.ldexps, col0, o.cols, i < o.rows, [&](const int a) {
+          return t4{(T)acc[a][b][0], (T)acc[a][b][1], (T)acc[a][b][2], (T)acc[a][b][3]};
+        });
+    }
   });
 }
 
-// Up to 16 rows: W is read once, 16 rows of it, a strip, by a workgroup.
-template <typename T, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void xent_forward_rows_kernel(const Operand<T> x, const Operand<T> w, const int64_t k, const XentForward<T> o) {
-  const int lane = threadIdx.x & 63, i = lane & 15;
-  const int64_t col0 = (int64_t)blockIdx.x * 16, c = col0 + 4 * (lane >> 4);
-  const typename Core<T>::acc_t sum = linear_rows_sum<T, WAVES>(x, w, k, col0);
-  if (threadIdx.x >= 64) return;
+// Up to 16 rows: W is read once, GROUPS times 16 rows of it by a workgroup whose wavefronts share k; a piece of x serves all of the groups.  A
+// strip is 16 columns, of a wavefront.  Bytes of W bound it: one row over 131072 words of 4096 in bf16 180 us (6 TB/s), 5 rows over 50003 of 1024 23.
+constexpr int XENT_WAVES = 4;
+
+template <typename T, int GROUPS>
+__global__ __launch_bounds__(64 * XENT_WAVES) void xent_forward_rows_kernel(const Operand<T> x, const Operand<T> w, const int64_t k, const XentForward<T> o) {
+  constexpr int WAVES = XENT_WAVES;
+  typedef typename Core<T>::piece_t piece_t;
+  typedef typename Core<T>::acc_t acc_t;
+  constexpr int VEC = Core<T>::VEC, STEP = 4 * VEC, UNROLL = GROUPS == 4 ? 4 : 8;
+  __shared__ acc_t part[WAVES][GROUPS][64];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), i = lane & 15, g = lane >> 4;
+  // rows behind the last are not stored
+  const T* wp[GROUPS];
+#pragma unroll
+  for (int q = 0; q < GROUPS; ++q) {
+    const int64_t j = ((int64_t)blockIdx.x * GROUPS + q) * 16 + i;
+    wp[q] = w.p + (j < w.rows ? j : w.rows - 1) * w.stride + g * VEC;
+  }
+  const T* const xp = x.p + (i < x.rows ? i : x.rows - 1) * x.stride + g * VEC;
+  acc_t acc[GROUPS] = {};
+  const int64_t steps = k / STEP, each = (steps + WAVES - 1) / WAVES;
+  int64_t s = wave * each;
+  const int64_t end = s + each < steps ? s + each : steps;
+  auto some = [&](auto count) {
+    constexpr int U = decltype(count)::value;
+    piece_t wf[U][GROUPS], xf[U];
+#pragma unroll
+    for (int u = 0; u < U; ++u) {
+#pragma unroll
+      for (int q = 0; q < GROUPS; ++q) __builtin_memcpy(&wf[u][q], wp[q] + (s + u) * STEP, 16);
+      __builtin_memcpy(&xf[u], xp + (s + u) * STEP, 16);
+    }
+#pragma unroll
+    for (int u = 0; u < U; ++u)
+#pragma unroll
+      for (int q = 0; q < GROUPS; ++q) Core<T>::mma(wf[u][q], xf[u], acc[q]);
+  };
+  for (; s + UNROLL <= end; s += UNROLL) some(std::integral_constant<int, UNROLL>{});
+  for (; s < end; ++s) some(std::integral_constant<int, 1>{});
+  if (wave == WAVES - 1 && steps * STEP < k) {                 // what is left over, element by element
+    const int64_t from = steps * STEP;
+    piece_t wf[GROUPS] = {}, xf = {};
+#pragma unroll
+    for (int e = 0; e < VEC; ++e)
+      if (from + g * VEC + e < k) {
+        xf[e] = xp[from + e];
+#pragma unroll
+        for (int q = 0; q < GROUPS; ++q) wf[q][e] = wp[q][from + e];
+      }
+#pragma unroll
+    for (int q = 0; q < GROUPS; ++q) Core<T>::mma(wf[q], xf, acc[q]);
+  }
+#pragma unroll
+  for (int q = 0; q < GROUPS; ++q) part[wave][q][lane] = acc[q];
+  __syncthreads();
+  if (wave >= GROUPS) return;
+  acc_t sum = part[0][wave][lane];
+#pragma unroll
+  for (int p = 1; p < WAVES; ++p) sum += part[p][wave][lane];
+  const int64_t strip = (int64_t)blockIdx.x * GROUPS + wave, c = strip * 16 + 4 * g;
   const int64_t target = i < o.rows ? xent_target(o.t, i) : -1;
-  float z[4], top = -INFINITY, s = 0.0f;
+  float z[4], top = -INFINITY, total = 0.0f;
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
     z[e] = c + e < o.cols ? sum[e] + (o.bias ? (float)o.bias[c + e] : 0.0f) : -INFINITY;
@@ -160,15 +317,16 @@ __global__ __launch_bounds__(64 * WAVES) void xent_forward_rows_kernel(const Ope
   }
   top = fmaxf(top, __shfl_xor(top, 16, 64));
   top = fmaxf(top, __shfl_xor(top, 32, 64));
+  const float from = xent_from(top);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    z[e] = xent_exp(z[e], top);
-    s += z[e];
+    z[e] = xent_power(z[e], from);
+    total += z[e];
   }
-  s += __shfl_xor(s, 16, 64);
-  s += __shfl_xor(s, 32, 64);
-  if (i >= o.rows) return;
-  if (lane < 16) o.strips[i * o.across + blockIdx.x] = XentStrip{top, s};
+  total += __shfl_xor(total, 16, 64);
+  total += __shfl_xor(total, 32, 64);
+  if (i >= o.rows || strip >= o.across) return;
+  if (lane < 16) o.strips[i * o.across + strip] = XentStrip{top, total};
   typedef T t4 __attribute__((ext_vector_type(4)));
   if (o.exps && c < o.cols) *reinterpret_cast<t4*>(o.exps + i * o.ldexps + c) = t4{(T)z[0], (T)z[1], (T)z[2], (T)z[3]};
 }
@@ -272,67 +430,84 @@ __device__ __forceinline__ XentRow xent_row(const XentSlope<T>& o, const int64_t
   return XentRow{o.lse[i], o.g[i], true, t - o.first - from};
 }
 
-// A tile of e.
+// Tiles of e.
 template <typename T, typename S, bool DIRECT>
-__global__ __launch_bounds__(S::THREADS) void xent_slope_kernel(const Operand<T> r, const Operand<T> c, const int64_t k, const XentSlope<T> o,
-                                                                const int64_t tiles) {
+__global__ __launch_bounds__(S::THREADS) void xent_slope_kernel(const Operand<T> r, const Operand<T> c, const XentSlope<T> o, const XentUnits u) {
   typedef typename Core<T>::acc_t acc_t;
-  constexpr int ROWS = S::TM * 16;
-  __shared__ __attribute__((aligned(16))) char lds[LinearLds<S>::BYTES];
-  const int64_t t = gemm_tile_number(blockIdx.x, tiles);
-  if (t < 0) return;
-  int64_t bi, bj;
-  gemm_tile_place(t, (o.rows + S::BM - 1) / S::BM, (o.cols + S::BN - 1) / S::BN, bi, bj);
-  const int64_t row0 = bi * S::BM, col0 = bj * S::BN;
-  acc_t acc[S::TN][S::TM] = {};
-  TileStream<T, S, false, false, DIRECT> stream(lds);
-  auto none = [] { return false; };
-  stream.set(r, c, row0, col0, 0, k);
-  stream.begin(none);
-  stream.run(acc, stream.slabs(0, k), none);
-
+  typedef T t4 __attribute__((ext_vector_type(4)));
+  constexpr int STRIP = S::TN * 16;
+  __shared__ __attribute__((aligned(16))) char lds[S::NB * S::SLAB];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  const int64_t wrow = row0 + wave / S::WN * ROWS, wcol = col0 + wave % S::WN * (S::TN * 16) + 4 * (lane >> 4);
-  const float up = o.scale ? o.scale->up : 1.0f;
-  float add[S::TN][4], sum[S::TN][4] = {};
+  const int wrow = wave / S::WN * (S::TM * 16) + (lane & 15), quad = 4 * (lane >> 4);
+  const float up = o.scale ? o.scale->up : 1.0f, down = o.scale ? o.scale->down : 1.0f;
+  float lse[S::TM], g[S::TM];
+  int at[S::TM];                       // -1: no target among this lane's columns; -2: the row does not count
+  auto early = [&](const XentUnit& x) {
+    const int64_t first = ((int64_t)x.bj * S::WN + wave % S::WN) * STRIP + quad;
 #pragma unroll
-  for (int a = 0; a < S::TN; ++a)
+    for (int b = 0; b < S::TM; ++b) {
+      const XentRow row = xent_row(o, (int64_t)x.bi * S::BM + wrow + 16 * b, first);
+      lse[b] = row.lse;
+      g[b] = row.g;
+      at[b] = !row.counts ? -2 : row.target >= 0 && row.target < STRIP ? (int)row.target : -1;
+    }
+  };
+  xent_units<T, S, false, false, DIRECT>(lds, r, c, u, early, [&](const XentUnit& x, acc_t (&acc)[S::TN][S::TM]) {
+    const int64_t row0 = (int64_t)x.bi * S::BM + wrow, col0 = ((int64_t)x.bj * S::WN + wave % S::WN) * STRIP;
+    if (o.bias) {
 #pragma unroll
-    for (int e = 0; e < 4; ++e) add[a][e] = o.bias && wcol + 16 * a + e < o.cols ? (float)o.bias[wcol + 16 * a + e] : 0.0f;
+      for (int a = 0; a < S::TN; ++a)
 #pragma unroll
-  for (int b = 0; b < S::TM; ++b) {
-    const XentRow row = xent_row(o, wrow + 16 * b + (lane & 15), wcol);
-    const int at = row.target >= 0 && row.target < S::TN * 16 ? (int)row.target : -1;
+        for (int e = 0; e < 4; ++e) {
+          const int64_t j = col0 + quad + 16 * a + e;
+          const float add = j < o.cols ? (float)o.bias[j] : 0.0f;
 #pragma unroll
-    for (int a = 0; a < S::TN; ++a)
+          for (int b = 0; b < S::TM; ++b) acc[a][b][e] += add;
+        }
+    }
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        const float p = __expf(acc[a][b][e] + add[a][e] - row.lse);
-        const float v = row.counts ? (at == 16 * a + e ? p - 1.0f : p) * row.g : 0.0f;
-        sum[a][e] += v;
-        acc[a][b][e] = v * up;
+    for (int b = 0; b < S::TM; ++b) {
+      const int64_t i = row0 + 16 * b;
+      const float from = -XENT_LOG2E * lse[b], weight = g[b] * up;
+#pragma unroll
+      for (int a = 0; a < S::TN; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) acc[a][b][e] = xent_power(acc[a][b][e], from);
+      if (__any(at[b] >= 0)) {
+#pragma unroll
+        for (int a = 0; a < S::TN; ++a)
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (at[b] == 16 * a + e) acc[a][b][e] -= 1.0f;
       }
-  }
-  if (o.sums) {
-    const int64_t part = bi * S::WM + wave / S::WN;
 #pragma unroll
-    for (int a = 0; a < S::TN; ++a)
+      for (int a = 0; a < S::TN; ++a) acc[a][b] *= weight;
+      if (__any(at[b] == -2)) {        // their logits may be anything
 #pragma unroll
-      for (int e = 0; e < 4; ++e) {
-        float s = sum[a][e];
+        for (int a = 0; a < S::TN; ++a)
 #pragma unroll
-        for (int off = 1; off < 16; off *= 2) s += __shfl_xor(s, off, 64);
-        const int64_t j = wcol + 16 * a + e;
-        if ((lane & 15) == 0 && j < o.cols) o.sums[part * o.cols + j] = s;
+          for (int e = 0; e < 4; ++e) acc[a][b][e] = at[b] == -2 ? 0.0f : acc[a][b][e];
       }
-  }
-  __syncthreads();                     // the operands are not read any more
-  tile_rows<T, S>(lds, acc, row0, col0, o.rows, o.cols, [&](auto&& rows) {
-    rows([&](const int64_t i, const int64_t j, const float (&in)[4]) {
-      typedef T t4 __attribute__((ext_vector_type(4)));
       // rows of e are whole pieces of 16 bytes long
-      *reinterpret_cast<t4*>(o.e + i * o.lde + j) = t4{(T)in[0], (T)in[1], (T)in[2], (T)in[3]};
-    });
+      xent_store<T, S::TN>(o.e + i * o.lde, col0, o.cols, i < o.rows, [&](const int a) {
+        return t4{(T)acc[a][b][0], (T)acc[a][b][1], (T)acc[a][b][2], (T)acc[a][b][3]};
+      });
+    }
+    if (o.sums) {
+      const int64_t part = (int64_t)x.bi * S::WM + wave / S::WN;
+#pragma unroll
+      for (int a = 0; a < S::TN; ++a)
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+          float s = 0.0f;
+#pragma unroll
+          for (int b = 0; b < S::TM; ++b) s += acc[a][b][e];
+#pragma unroll
+          for (int off = 1; off < 16; off *= 2) s += __shfl_xor(s, off, 64);
+          const int64_t j = col0 + quad + 16 * a + e;
+          if ((lane & 15) == 0 && j < o.cols) o.sums[part * o.cols + j] = s * down;
+        }
+    }
   });
 }
 
@@ -425,74 +600,96 @@ struct XentOut {
   float* total;                        // rows x cols
   bool begins, ends;                   // the first, the last piece
   int64_t rows, cols;
-  bool vec;                            // rows of y and total start where four elements can be moved at once
+  bool vec;                            // eight (fp32: four) elements of a row can be moved at once
 };
 
+// Four neighbours of a row from column j on: with what the pieces before came to.
 template <typename O>
-__device__ __forceinline__ void xent_put4(const XentOut<O>& o, const int64_t i, const int64_t j, const float (&in)[4]) {
+__device__ __forceinline__ void xent_sum(const XentOut<O>& o, const int64_t i, const int64_t j, const float down, float (&v)[4]) {
+  const float* const total = o.total + i * o.cols + j;
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    v[e] *= down;
+    if (!o.begins && i < o.rows && j + e < o.cols) v[e] += total[e];
+  }
+}
+template <typename O>
+__device__ __forceinline__ void xent_put(const XentOut<O>& o, const int64_t i, const int64_t j, const float (&v)[4]) {
   typedef O o4 __attribute__((ext_vector_type(4)));
-  typedef float f4 __attribute__((ext_vector_type(4)));
-  const float down = o.scale ? o.scale->down : 1.0f;
-  float* const total = o.total + i * o.cols + j;
-  O* const y = o.y + i * o.ldy + j;
-  if (o.vec && j + 4 <= o.cols) {
-    f4 v = f4{in[0], in[1], in[2], in[3]} * down;
-    if (!o.begins) v += *reinterpret_cast<const f4*>(total);
-    if (o.ends) *reinterpret_cast<o4*>(y) = o4{(O)v[0], (O)v[1], (O)v[2], (O)v[3]};
-    else *reinterpret_cast<f4*>(total) = v;
+  if (i >= o.rows) return;
+  if (o.ends && o.vec && j + 4 <= o.cols) {
+    *reinterpret_cast<o4*>(o.y + i * o.ldy + j) = o4{(O)v[0], (O)v[1], (O)v[2], (O)v[3]};
     return;
   }
 #pragma unroll
-  for (int e = 0; e < 4; ++e) {
-    if (j + e >= o.cols) break;
-    const float v = in[e] * down + (o.begins ? 0.0f : total[e]);
-    if (o.ends) y[e] = (O)v;
-    else total[e] = v;
-  }
+  for (int e = 0; e < 4; ++e)
+    if (j + e < o.cols) {
+      if (o.ends) o.y[i * o.ldy + j + e] = (O)v[e];
+      else o.total[i * o.cols + j + e] = v[e];
+    }
 }
 
-// dx = e W (C outer) and dW = e^T x (both outer).  SPLIT: part t / tiles of the sum over k.
-template <typename T, typename O, typename S, bool ROUTER, bool DIRECT, bool SPLIT>
-__global__ __launch_bounds__(S::THREADS) void xent_product_kernel(const Operand<T> r, const Operand<T> c, const int64_t k, const XentOut<O> o,
-                                                                  const int64_t tiles, float* const parts, const int64_t kpart) {
-  __shared__ __attribute__((aligned(16))) char lds[LinearLds<S>::BYTES];
-  const int64_t t = gemm_tile_number(blockIdx.x, tiles);
-  if (t < 0) return;
-  const int64_t down = (o.rows + S::BM - 1) / S::BM, across = (o.cols + S::BN - 1) / S::BN, one = down * across;
-  int64_t bi, bj;
-  gemm_tile_place(t % one, down, across, bi, bj);
-  const int64_t part = t / one, k0 = part * kpart, kend = k0 + kpart < k ? k0 + kpart : k;
-  const int64_t row0 = bi * S::BM, col0 = bj * S::BN;
-  typename Core<T>::acc_t acc[S::TN][S::TM] = {};
-  TileStream<T, S, ROUTER, true, DIRECT> stream(lds);
-  auto none = [] { return false; };
-  stream.set(r, c, row0, col0, k0, kend);
-  stream.begin(none);
-  stream.run(acc, stream.slabs(k0, kend), none);
-  __syncthreads();                     // the operands are not read any more
-  tile_rows<T, S>(lds, acc, row0, col0, o.rows, o.cols, [&](auto&& rows) {
-    rows([&](const int64_t i, const int64_t j, const float (&in)[4]) {
-      if constexpr (SPLIT) {
-        float* const to = parts + (part * o.rows + i) * o.cols + j;
+// dx = e W (C outer) and dW = e^T x (both outer).
+template <typename T, typename O, typename S, bool ROUTER, bool DIRECT>
+__global__ __launch_bounds__(S::THREADS) void xent_product_kernel(const Operand<T> r, const Operand<T> c, const XentOut<O> o, const XentUnits u) {
+  typedef typename Core<T>::acc_t acc_t;
+  typedef O o4 __attribute__((ext_vector_type(4)));
+  __shared__ __attribute__((aligned(16))) char lds[S::NB * S::SLAB];
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), quad = 4 * (lane >> 4);
+  const int wrow = wave / S::WN * (S::TM * 16) + (lane & 15), wcol = wave % S::WN * (S::TN * 16);
+  const float down = o.scale ? o.scale->down : 1.0f;
+  xent_units<T, S, ROUTER, true, DIRECT>(lds, r, c, u, [](const XentUnit&) {}, [&](const XentUnit& x, acc_t (&acc)[S::TN][S::TM]) {
+    if (x.part >= 0) {
+      float* const to = u.parts + (int64_t)x.part * (S::BM * S::BN) + wcol + quad;
 #pragma unroll
-        for (int e = 0; e < 4; ++e)
-          if (j + e < o.cols) to[e] = in[e];
-      } else xent_put4(o, i, j, in);
-    });
+      for (int b = 0; b < S::TM; ++b)
+#pragma unroll
+        for (int a = 0; a < S::TN; ++a) *reinterpret_cast<acc_t*>(to + (wrow + 16 * b) * S::BN + 16 * a) = acc[a][b];
+      return;
+    }
+    const int64_t row0 = (int64_t)x.bi * S::BM + wrow, col0 = (int64_t)x.bj * S::BN + wcol;
+#pragma unroll
+    for (int b = 0; b < S::TM; ++b) {
+      const int64_t i = row0 + 16 * b;
+#pragma unroll
+      for (int a = 0; a < S::TN; a += 2) {
+        float v[2][4];
+#pragma unroll
+        for (int h = 0; h < 2 && a + h < S::TN; ++h) {
+#pragma unroll
+          for (int e = 0; e < 4; ++e) v[h][e] = acc[a + h][b][e];
+          xent_sum(o, i, col0 + 16 * (a + h) + quad, down, v[h]);
+        }
+        if constexpr (sizeof(O) == 2 && S::TN % 2 == 0) {
+          const int64_t j = col0 + 16 * a;
+          if (o.ends && o.vec && j + 32 <= o.cols) {
+            const auto w = XentEight<O>::of(o4{(O)v[0][0], (O)v[0][1], (O)v[0][2], (O)v[0][3]}, o4{(O)v[1][0], (O)v[1][1], (O)v[1][2], (O)v[1][3]});
+            if (i < o.rows) *reinterpret_cast<typename XentEight<O>::eight_t*>(o.y + i * o.ldy + j + XentEight<O>::col()) = w;
+            continue;
+          }
+        }
+#pragma unroll
+        for (int h = 0; h < 2 && a + h < S::TN; ++h) xent_put(o, i, col0 + 16 * (a + h) + quad, v[h]);
+      }
+    }
   });
 }
 
-// The parts of the sum over k, added in their order.
-template <typename O>
-__global__ __launch_bounds__(256) void xent_product_join_kernel(const float* __restrict__ parts, const int splits, const XentOut<O> o) {
-  const int64_t across = (o.cols + 3) / 4, id = (int64_t)blockIdx.x * 256 + threadIdx.x, i = id / across, j = (id - i * across) * 4;
-  if (i >= o.rows) return;
-  float v[4] = {};
-  for (int s = 0; s < splits; ++s)
-#pragma unroll
-    for (int e = 0; e < 4; ++e)
-      if (j + e < o.cols) v[e] += parts[(s * o.rows + i) * o.cols + j + e];
-  xent_put4(o, i, j, v);
+// The parts of the tiles that were shared, added in their order: four neighbours of a row by a thread.
+template <typename O, int BM, int BN>
+__global__ __launch_bounds__(256) void xent_product_join_kernel(const XentOut<O> o, const XentUnits u) {
+  typedef float f4 __attribute__((ext_vector_type(4)));
+  constexpr int EACH = BM * BN / 1024;
+  const int tile = blockIdx.x / EACH, at = (int)(blockIdx.x % EACH * 256 + threadIdx.x) * 4;
+  int bi, bj;
+  xent_place(u, u.whole + tile, bi, bj);
+  const int64_t i = (int64_t)bi * BM + at / BN, j = (int64_t)bj * BN + at % BN;
+  if (i >= o.rows || j >= o.cols) return;
+  f4 sum = {};
+  for (int s = 0; s < u.splits; ++s) sum += *reinterpret_cast<const f4*>(u.parts + ((int64_t)tile * u.splits + s) * (BM * BN) + at);
+  float v[4] = {sum[0], sum[1], sum[2], sum[3]};
+  xent_sum(o, i, j, o.scale ? o.scale->down : 1.0f, v);
+  xent_put(o, i, j, v);
 }
 
 }  // namespace mdet

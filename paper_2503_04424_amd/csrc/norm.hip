@@ -13,44 +13,47 @@ namespace {
 
 using namespace mdet;
 
-// f(threads of a workgroup, lanes of a row, pieces of a lane): the fewest lanes that hold a row in registers; false: none do.  The
-// gradient, which also holds two sums for each column, has no room for more than two pieces in 1024 lanes.
-template <bool GRADIENT, typename F>
-bool norm_shape(int64_t cols, int64_t size, F&& f) {
+// f(threads of a workgroup, lanes of a row, pieces of a lane): lanes that hold a row in registers; false: none do.  The gradient, which also
+// holds two sums for each column, has fewer pieces a lane (rows of 4096 in bf16: two pieces in 256 lanes leave room for three wavefronts, one
+// in 512 for five), and in 1024 lanes no room for two pieces of 16-bit elements.
+template <bool GRADIENT, int SIZE, typename F>
+bool norm_shape(int64_t cols, F&& f) {
   using std::integral_constant;
-  const int64_t pieces = ceil_div(cols * size, 16);
+  const int64_t pieces = ceil_div(cols * SIZE, 16);
   typedef integral_constant<int, 1> one;
   typedef integral_constant<int, 2> two;
   typedef integral_constant<int, 4> four;
   typedef integral_constant<int, 256> small;
+  typedef integral_constant<int, 512> medium;
   typedef integral_constant<int, 1024> large;
   if (pieces <= 16) f(small{}, integral_constant<int, 16>{}, one{});
   else if (pieces <= 64) f(small{}, integral_constant<int, 64>{}, one{});
   else if (pieces <= 128) f(small{}, integral_constant<int, 64>{}, two{});
   else if (pieces <= 256) f(small{}, small{}, one{});
-  else if (pieces <= 512) f(small{}, small{}, two{});
-  else if (pieces <= 1024) f(small{}, small{}, four{});
-  else if (pieces <= 2048) f(large{}, large{}, two{});
-  else {
-    if constexpr (!GRADIENT)
-      if (pieces <= 4096) {
-        f(large{}, large{}, four{});
-        return true;
-      }
-    return false;
-  }
+  else if (pieces <= 512) {
+    if constexpr (GRADIENT) f(medium{}, medium{}, one{});
+    else f(small{}, small{}, two{});
+  } else if (pieces <= 1024) {
+    if constexpr (GRADIENT) f(large{}, large{}, one{});
+    else f(small{}, small{}, four{});
+  } else if (pieces <= 2048 && (!GRADIENT || SIZE == 4)) {
+    if constexpr (!GRADIENT || SIZE == 4) f(large{}, large{}, two{});
+  } else if (pieces <= 4096 && !GRADIENT) {
+    if constexpr (!GRADIENT) f(large{}, large{}, four{});
+  } else return false;
   return true;
 }
 
 // Strips of rows whose sums for dw and db stand in the workspace: as many as workgroups that fill the device.
 int64_t norm_strips(int64_t rows, int64_t cols, int64_t size) {
   int64_t strips = 0;
-  const bool held = norm_shape<true>(cols, size, [&](auto threads, auto lanes, auto) {
+  auto held_by = [&](auto threads, auto lanes, auto) {
     const int64_t groups = threads / lanes;
-    strips = threads == 1024 ? 256 : 1024;
-    if (strips > ceil_div(rows, groups)) strips = ceil_div(rows, groups);
-  });
-  if (!held) {
+    const int64_t turns = ceil_div(rows, groups), most = 262144 / threads;
+    // a few rows each before there are more than compute units: 777 x 1301 in fp32, a strip a row: 30 us, of which 17 for adding the strips up
+    strips = turns <= 256 ? turns : turns <= 1024 ? 256 : turns / 4 < most ? turns / 4 : most;
+  };
+  if (!(size == 4 ? norm_shape<true, 4>(cols, held_by) : norm_shape<true, 2>(cols, held_by))) {
     strips = 1024 / ceil_div(cols * size, 16 * NORM_THREADS);
     if (strips < 1) strips = 1;
     if (strips > rows) strips = rows;
@@ -60,7 +63,7 @@ int64_t norm_strips(int64_t rows, int64_t cols, int64_t size) {
 
 template <typename T>
 int forward(const NormForward<T>& a, hipStream_t st) {
-  const bool held = norm_shape<false>(a.cols, sizeof(T), [&](auto threads, auto lanes, auto pieces) {
+  const bool held = norm_shape<false, sizeof(T)>(a.cols, [&](auto threads, auto lanes, auto pieces) {
     constexpr int THREADS = decltype(threads)::value, LANES = decltype(lanes)::value;
     gemm_launches(ceil_div(a.rows, THREADS / LANES), THREADS, [&](const int64_t first, const dim3 grid) {
       hipLaunchKernelGGL((norm_forward_kernel<T, THREADS, LANES, decltype(pieces)::value>), grid, dim3(THREADS), 0, st, a, first);
@@ -77,7 +80,7 @@ template <typename T, typename O>
 int backward(const NormBackward<T>& a, O* dw, O* db, hipStream_t st) {
   const int64_t strips = norm_strips(a.rows, a.cols, sizeof(T));
   if (a.rows > 0 && (a.dx || a.sums)) {
-    const bool held = norm_shape<true>(a.cols, sizeof(T), [&](auto threads, auto lanes, auto pieces) {
+    const bool held = norm_shape<true, sizeof(T)>(a.cols, [&](auto threads, auto lanes, auto pieces) {
       constexpr int THREADS = decltype(threads)::value, LANES = decltype(lanes)::value;
       hipLaunchKernelGGL((norm_backward_kernel<T, THREADS, LANES, decltype(pieces)::value>), dim3((unsigned)strips), dim3(THREADS), 0, st, a);
     });
@@ -93,8 +96,8 @@ int backward(const NormBackward<T>& a, O* dw, O* db, hipStream_t st) {
     }
   }
   if (dw || db)                        // without rows as well: zeros
-    gemm_launches(ceil_div(a.cols, NORM_COLS), NORM_THREADS, [&](const int64_t first, const dim3 grid) {
-      hipLaunchKernelGGL((norm_join_kernel<O>), grid, dim3(NORM_THREADS), 0, st, (const float*)a.sums, strips, a.cols, dw, db, first);
+    gemm_launches(ceil_div(a.cols, NORM_COLS), NORM_COLS * NORM_JOIN, [&](const int64_t first, const dim3 grid) {
+      hipLaunchKernelGGL((norm_join_kernel<O>), grid, dim3(NORM_COLS * NORM_JOIN), 0, st, (const float*)a.sums, strips, a.cols, dw, db, first);
     });
   return launch_status();
 }

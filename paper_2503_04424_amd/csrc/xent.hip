@@ -28,6 +28,20 @@ void with_tile(int tile, F&& f) {
   else f(Tiny{});
 }
 
+template <typename S>
+XentUnits whole_units(int64_t rows, int64_t cols, int64_t k) {
+  const int64_t down = ceil_div(rows, S::BM), across = ceil_div(cols, S::BN);
+  return XentUnits{(int)down, (int)across, (int)(down * across), (int)(down * across), 1, k, k, nullptr};
+}
+
+// Workgroups for these units: a multiple of eight; for large tiles whose operands go straight to LDS, of which a compute unit holds one
+// and a workgroup can take several, no more than there are of those.
+template <typename S>
+dim3 units_grid(const XentUnits& u, bool direct) {
+  const int64_t all = ceil_div(ceil_div(u.whole, 8) * 8 + u.units - u.whole, 8) * 8;
+  return dim3((unsigned)(S::BM == 256 && direct && all > 256 ? 256 : all));
+}
+
 // The places of what the forward pass leaves: in the caller's `kept`, or without the exponentials in the workspace.
 template <typename T>
 XentForward<T> forward_places(char* at, const XentLayout& l, bool keep) {
@@ -45,18 +59,26 @@ template <typename T>
 int forward(Operand<T> x, Operand<T> w, int64_t k, XentForward<T> o, const XentLayout& l, float* loss, float* lse, hipStream_t st) {
   if (o.cols > 0) {
     if (l.cut.tile == 0) {
-      const dim3 grid((unsigned)ceil_div(o.cols, 16));
-      if (k * (int64_t)sizeof(T) >= 4096) hipLaunchKernelGGL((xent_forward_rows_kernel<T, 16>), grid, dim3(1024), 0, st, x, w, k, o);
-      else hipLaunchKernelGGL((xent_forward_rows_kernel<T, 4>), grid, dim3(256), 0, st, x, w, k, o);
+      // Few rows of x want more of W on its way, many share their own loads out over more of it, as long as that leaves enough workgroups.  us for
+      // one, two, four groups of W, rows of 4096 bf16: 4 rows over 131072 words 194, 198, 219, 8 rows 223, 212, 224, 16 rows 277, 243, 236; 16
+      // rows over 5000 words 23, 19, 31.  (Tiles of 256: 261 for 5 rows, 268 for 16.)
+      auto go = [&](auto groups) {
+        constexpr int G = decltype(groups)::value;
+        hipLaunchKernelGGL((xent_forward_rows_kernel<T, G>), dim3((unsigned)ceil_div(o.cols, 16 * G)), dim3(64 * XENT_WAVES), 0, st, x, w, k, o);
+      };
+      if (o.rows <= 4) go(std::integral_constant<int, 1>{});
+      else if (o.rows <= 8 || o.cols < 16384) go(std::integral_constant<int, 2>{});
+      else go(std::integral_constant<int, 4>{});
     } else
       with_tile<T>(l.cut.tile, [&](auto shape) {
         typedef decltype(shape) S;
         x = gemm_operand<T, false, S::BM>(x.p, x.stride, x.rows, k);
         w = gemm_operand<T, false, S::BN>(w.p, w.stride, w.rows, k);
-        const int64_t tiles = ceil_div(o.rows, S::BM) * ceil_div(o.cols, S::BN);
-        const dim3 grid((unsigned)(ceil_div(tiles, 8) * 8)), block(S::THREADS);
-        if (x.straight && w.straight) hipLaunchKernelGGL((xent_forward_kernel<T, S, true>), grid, block, 0, st, x, w, k, o, tiles);
-        else hipLaunchKernelGGL((xent_forward_kernel<T, S, false>), grid, block, 0, st, x, w, k, o, tiles);
+        const bool direct = x.straight && w.straight;
+        const XentUnits u = whole_units<S>(o.rows, o.cols, k);
+        const dim3 grid = units_grid<S>(u, direct), block(S::THREADS);
+        if (direct) hipLaunchKernelGGL((xent_forward_kernel<T, S, true>), grid, block, 0, st, x, w, o, u);
+        else hipLaunchKernelGGL((xent_forward_kernel<T, S, false>), grid, block, 0, st, x, w, o, u);
       });
   }
   // a row's strips by a wavefront, or by sixteen where they are many
@@ -74,36 +96,27 @@ int forward(Operand<T> x, Operand<T> w, int64_t k, XentForward<T> o, const XentL
 }
 
 template <typename O>
-bool fours(const XentOut<O>& o) {
-  return (uintptr_t)o.y % (4 * sizeof(O)) == 0 && (o.rows == 1 || o.ldy % 4 == 0) && (!o.total || o.cols % 4 == 0);
+bool whole_pieces(const XentOut<O>& o) {
+  return (uintptr_t)o.y % 16 == 0 && (o.rows == 1 || o.ldy * sizeof(O) % 16 == 0);
 }
 
 template <typename T, typename O, bool ROUTER>
 void product(Operand<T> r, Operand<T> c, int64_t k, XentOut<O> o, float* parts, hipStream_t st) {
-  const Cut cut = cut_of(o.rows, o.cols, k, sizeof(T), false);
-  o.vec = fours(o);
+  const XentCut cut = xent_cut(o.rows, o.cols, k, sizeof(T));
+  const XentUnits u{(int)cut.down, (int)cut.across, (int)cut.whole, (int)cut.units(), cut.splits, k, cut.kpart, parts};
+  o.vec = whole_pieces(o);
   with_tile<T>(cut.tile, [&](auto shape) {
     typedef decltype(shape) S;
     r = gemm_operand<T, ROUTER, S::BM>(r.p, r.stride, r.rows, k);
     c = gemm_operand<T, true, S::BN>(c.p, c.stride, c.rows, k);
-    const int64_t tiles = ceil_div(o.rows, S::BM) * ceil_div(o.cols, S::BN) * cut.splits;
-    const dim3 grid((unsigned)(ceil_div(tiles, 8) * 8)), block(S::THREADS);
-    auto go = [&](auto direct, auto split) {
-      hipLaunchKernelGGL((xent_product_kernel<T, O, S, ROUTER, decltype(direct)::value, decltype(split)::value>), grid, block, 0, st, r, c, k, o, tiles,
-                         parts, cut.kpart);
-    };
-    using std::false_type;
-    using std::true_type;
     const bool direct = r.straight && c.straight;
-    if (cut.splits > 1) {              // the smallest tile alone
-      if constexpr (std::is_same<S, Tiny>::value) {
-        if (direct) go(true_type{}, true_type{});
-        else go(false_type{}, true_type{});
-        hipLaunchKernelGGL((xent_product_join_kernel<O>), dim3((unsigned)ceil_div(o.rows * ceil_div(o.cols, 4), 256)), dim3(256), 0, st,
-                           (const float*)parts, cut.splits, o);
-      }
-    } else if (direct) go(true_type{}, false_type{});
-    else go(false_type{}, false_type{});
+    const dim3 grid = units_grid<S>(u, direct), block(S::THREADS);
+    if (direct) hipLaunchKernelGGL((xent_product_kernel<T, O, S, ROUTER, true>), grid, block, 0, st, r, c, o, u);
+    else hipLaunchKernelGGL((xent_product_kernel<T, O, S, ROUTER, false>), grid, block, 0, st, r, c, o, u);
+    if (u.units > u.whole) {
+      const int tiles = u.down * u.across - u.whole;
+      hipLaunchKernelGGL((xent_product_join_kernel<O, S::BM, S::BN>), dim3((unsigned)(tiles * (S::BM * S::BN / 1024))), dim3(256), 0, st, o, u);
+    }
   });
 }
 
@@ -152,11 +165,12 @@ int backward(const Grad& a) {
       with_tile<T>(cut_of(a.m, n, a.k, sizeof(T), false).tile, [&](auto shape) {
         typedef decltype(shape) S;
         const Operand<T> x = gemm_operand<T, false, S::BM>(a.x, a.ldx, a.m, a.k), c = gemm_operand<T, false, S::BN>(w, a.ldw, n, a.k);
-        const int64_t tiles = ceil_div(a.m, S::BM) * ceil_div(n, S::BN);
-        const dim3 grid((unsigned)(ceil_div(tiles, 8) * 8)), block(S::THREADS);
+        const bool direct = x.straight && c.straight;
+        const XentUnits u = whole_units<S>(a.m, n, a.k);
+        const dim3 grid = units_grid<S>(u, direct), block(S::THREADS);
         strips = ceil_div(a.m, S::BM) * S::WM;
-        if (x.straight && c.straight) hipLaunchKernelGGL((xent_slope_kernel<T, S, true>), grid, block, 0, st, x, c, a.k, o, tiles);
-        else hipLaunchKernelGGL((xent_slope_kernel<T, S, false>), grid, block, 0, st, x, c, a.k, o, tiles);
+        if (direct) hipLaunchKernelGGL((xent_slope_kernel<T, S, true>), grid, block, 0, st, x, c, o, u);
+        else hipLaunchKernelGGL((xent_slope_kernel<T, S, false>), grid, block, 0, st, x, c, o, u);
       });
     if (a.db)
       gemm_launches(ceil_div(n, 16), 256, [&](const int64_t first, const dim3 grid) {

@@ -15,8 +15,9 @@ struct XentLayout {
 };
 inline XentLayout xent_layout(int64_t m, int64_t n, int64_t k, int64_t size) {
   XentLayout l;
-  l.cut = cut_of(m, n, k, size, true);
-  l.strip = l.cut.tile ? l.cut.tile : 16;
+  l.cut = m <= 16 && n <= (int64_t(1) << 28) ? Cut{0, 1, k} : cut_of(m, n, k, size, false);
+  // a wavefront's columns of a tile
+  l.strip = l.cut.tile == 256 ? 64 : l.cut.tile == 128 ? 64 : l.cut.tile == 64 ? 32 : 16;
   l.across = ceil_div(n, l.strip);
   l.ldexps = ceil_div(n, 8) * 8;
   l.exps_bytes = xent_up256((uint64_t)m * l.ldexps * size);
@@ -32,6 +33,43 @@ inline int64_t xent_piece(int64_t m, int64_t n) {
   if (most < 4096) most = 4096;
   const int64_t pieces = ceil_div(n, most);
   return pieces <= 1 ? n : ceil_div(ceil_div(n, pieces), 256) * 256;
+}
+
+// How a product with e is shared out.
+struct XentCut {
+  int tile;                            // rows and columns of a tile
+  int64_t down, across, whole;         // tiles, and how many of them are one workgroup's
+  int splits;                          // workgroups of each of the others
+  int64_t kpart;
+  int64_t units() const { return whole + splits * (down * across - whole); }
+  uint64_t bytes() const { return splits > 1 ? xent_up256((uint64_t)(units() - whole) * tile * tile * 4) : 0; }
+};
+// Tiles of 256 in 16 bits also where they are few, if sums are long: the tiles behind the last whole round of 256 workgroups are shared by as
+// many workgroups each as fill another round, of at least eight slabs each.
+inline XentCut xent_cut(int64_t rows, int64_t cols, int64_t k, int64_t size) {
+  const Cut c = cut_of(rows, cols, k, size, false);
+  XentCut x;
+  const int64_t large = ceil_div(rows, 256) * ceil_div(cols, 256), rest = large % 256;
+  int64_t splits = rest ? 256 / rest : 1, most = k / 512;
+  if (splits > 16) splits = 16;
+  if (splits > most) splits = most;
+  // a unit of 64 of k is 1.7 us; the parts of a round are written and read in 35
+  const bool worth = size == 2 && splits > 1 && (double)k * 0.026 * (1.0 - 1.0 / (double)splits) > 35.0;
+  if (worth && (c.tile == 256 || rest * splits >= 160 || large > 256)) {
+    x.tile = 256;
+    x.whole = large - rest;
+    x.splits = (int)splits;
+    x.kpart = ceil_div(ceil_div(k, splits), 64) * 64;
+    x.splits = (int)ceil_div(k, x.kpart);
+  } else {
+    x.tile = c.tile;
+    x.splits = c.splits;
+    x.kpart = c.kpart;
+    x.whole = c.splits > 1 ? 0 : ceil_div(rows, c.tile) * ceil_div(cols, c.tile);
+  }
+  x.down = ceil_div(rows, x.tile);
+  x.across = ceil_div(cols, x.tile);
+  return x;
 }
 
 struct XentGradLayout {
@@ -52,8 +90,7 @@ inline XentGradLayout xent_grad_layout(int64_t m, int64_t n, int64_t k, int64_t 
   l.parts = l.total + (l.piece < n ? xent_up256((uint64_t)m * k * 4) : 0);
   uint64_t parts = 0;
   auto room = [&](int64_t rows, int64_t cols, int64_t inner) {
-    const Cut c = cut_of(rows, cols, inner, size, false);
-    const uint64_t b = c.splits > 1 ? xent_up256((uint64_t)c.splits * rows * cols * 4) : 0;
+    const uint64_t b = xent_cut(rows, cols, inner, size).bytes();
     if (b > parts) parts = b;
   };
   const int64_t last = n > 0 ? n - (n - 1) / l.piece * l.piece : 0;
