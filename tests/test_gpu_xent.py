@@ -333,7 +333,7 @@ def test_front_end(M, dtype):
                 total = (loss * weight).sum()
             else:
                 total = loss
-                assert abs(float(loss) - float((wl * g).sum())) <= float(((el + 64 * EPS32 * wl.abs()) * g).sum())
+                assert abs(float(loss.detach()) - float((wl * g).sum())) <= float(((el + 64 * EPS32 * wl.abs()) * g).sum())
             got = torch.autograd.grad(total, (x, w, bias))
             want = backward64(z, ez, x.detach(), w.detach(), t.view(-1), g.float(), lse, counts, dtype, keep)
             for v, (a, err), name in zip(got, want, ("dx", "dw", "db")):
