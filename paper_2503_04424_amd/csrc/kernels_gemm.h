@@ -478,6 +478,103 @@ struct TileStream {
     }
     if constexpr (ONE) acc[0][0] += other;
   }
+
+  // The same for a wavefront's part of 128 x 64 in 16 bits, with every fragment on its way while others are multiplied: a slab's products are 16
+  // steps (of 16 rows and half a slab each), a step's row fragment is fetched three steps ahead, the column fragments a few steps ahead of
+  // their half.  Behind step 13 everything of a slab is in registers: the next one has landed by then, its first fragments come in
+  // beside the last two steps, and its place in LDS is free for the one after it.  The same sums in the same order as run().
+  template <typename F>
+  __device__ __forceinline__ void run_rolling(typename Core<T>::acc_t (&acc)[S::TN][S::TM], const int count, F&& next) {
+    static_assert(DIRECT && sizeof(T) == 2 && S::NB == 2 && S::TM == 8 && S::TN == 4, "");
+    constexpr int STEPS = S::TM * PIECES / 4, AHEAD = 3, LAST = STEPS - 2;
+    const int wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+    const int wr = wave / S::WN * S::TM, wc = wave % S::WN * S::TN;
+    piece_t cf[2][S::TN], rf[4];
+    auto col = [&](const char* const slab, const int h, const int a) { cf[h][a] = CS::fragment(slab + 16 * PIECES * S::BM, wc + a, h); };
+    auto row = [&](const char* const slab, const int i) { rf[i % 4] = RS::fragment(slab, wr + i % S::TM, i / S::TM); };
+    auto products = [&](const int i) {
+#pragma unroll
+      for (int a = 0; a < S::TN; ++a) Core<T>::mma(cf[i / S::TM][a], rf[i % 4], acc[a][i % S::TM]);
+      __builtin_amdgcn_sched_barrier(0);
+    };
+    // Steps from 0 to `end` - 1 of a slab.
+    auto steps = [&](const char* const slab, auto end) {
+#pragma unroll
+      for (int i = 0; i < decltype(end)::value; ++i) {
+        if (i + AHEAD < STEPS) row(slab, i + AHEAD);
+        if (i >= AHEAD && i < AHEAD + S::TN) col(slab, 1, i - AHEAD);
+        products(i);
+      }
+    };
+    // What stands in front of step 0: without the third row, whose registers step 14 of the slab before still needs.
+    auto head = [&](const char* const slab) {
+#pragma unroll
+      for (int a = 0; a < S::TN; ++a) col(slab, 0, a);
+      row(slab, 0);
+      row(slab, 1);
+    };
+    using std::integral_constant;
+    typedef integral_constant<int, LAST> last;
+    typedef integral_constant<int, STEPS> all;
+    auto onward = [&] {
+      to = to + 1 == S::NB ? 0 : to + 1;
+      at = at + 1 == S::NB ? 0 : at + 1;
+    };
+    int left = count;
+    bool headed = false;               // the first fragments of the slab to be multiplied are on their way, and the next slab is
+    const int64_t end = kend - (rs.spare() > cs.spare() ? rs.spare() : cs.spare());
+    const int64_t whole = rquick && cquick && k < end ? (end - k) / BK : 0;
+    int steady = __builtin_amdgcn_readfirstlane(whole < left - ahead ? (int)whole : left - ahead);
+    if (ahead == S::NB - 1 && steady > 0) {
+      left -= steady - 1;
+      headed = true;
+      const char *rfrom = gemm_scalar(rs.base(k)), *cfrom = gemm_scalar(cs.base(k));
+      const int64_t rstep = gemm_scalar((int64_t)(rs.base(k + BK) - rs.base(k))), cstep = gemm_scalar((int64_t)(cs.base(k + BK) - cs.base(k)));
+      k += (int64_t)steady * BK;
+      auto load_rows = [&] {
+#pragma unroll
+        for (int v = 0; v < RS::NP; ++v) rs.direct(rfrom, v, lds0 + to * S::SLAB);
+        rfrom += rstep;
+      };
+      auto load_cols = [&] {
+#pragma unroll
+        for (int v = 0; v < CS::NP; ++v) cs.direct(cfrom, v, lds0 + to * S::SLAB + 16 * PIECES * S::BM);
+        cfrom += cstep;
+      };
+      gemm_landed<0>();
+      load_rows();
+      load_cols();
+      head(lds + at * S::SLAB);
+      row(lds + at * S::SLAB, 2);
+      for (; steady > 1; --steady) {
+        steps(lds + at * S::SLAB, last{});
+        gemm_landed<0>();              // the next slab, of all wavefronts; this one's fragments are in registers
+        onward();
+        head(lds + at * S::SLAB);
+        __builtin_amdgcn_sched_barrier(0);
+        products(LAST);
+        row(lds + at * S::SLAB, 2);
+        load_rows();
+        __builtin_amdgcn_sched_barrier(0);
+        products(LAST + 1);
+        load_cols();
+      }
+    }
+    for (; left > 0; --left) {
+      const char* const slab = lds + at * S::SLAB;
+      if (!headed) {
+        --ahead;
+        gemm_landed<0>();
+        bring(next);
+        head(slab);
+        row(slab, 2);
+      }
+      steps(slab, all{});
+      at = at + 1 == S::NB ? 0 : at + 1;
+      if (headed) to = to + 1 == S::NB ? 0 : to + 1;
+      headed = false;
+    }
+  }
 };
 
 // f(a, b, e, row, column of the tile) for each element e of acc[a][b] that this lane holds.

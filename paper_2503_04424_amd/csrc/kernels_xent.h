@@ -120,7 +120,8 @@ __device__ __forceinline__ void xent_units(char* const lds, const Operand<T>& r,
     }
     early(now);
     typename Core<T>::acc_t acc[S::TN][S::TM] = {};
-    stream.run(acc, stream.slabs(now.k0, now.kend), next);
+    if constexpr (DIRECT && S::BM == 256) stream.run_rolling(acc, stream.slabs(now.k0, now.kend), next);
+    else stream.run(acc, stream.slabs(now.k0, now.kend), next);
     // of a sum over nothing no slab was brought, and nothing is on its way
     fresh = false;
     f(now, acc);
