@@ -693,15 +693,16 @@ int mdet_layernorm_backward(int32_t dtype, int32_t grad_dtype, int64_t m, int64_
                             void* db, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* Device bytes of workspace for the cross entropy of m rows of k elements over a vocabulary of n (pure host code): the forward call,
- * or with backward != 0 the gradient (up to 2^29 elements of e, or m x 4096 if that is more, at a time). */
-int mdet_xent_workspace_query(int32_t dtype, int32_t backward, int64_t m, int64_t n, int64_t k, uint64_t* bytes);
-/* Device bytes of `kept` (m x n elements of dtype and a little more). */
+ * or with backward != 0 the gradient with dw and db of grad_dtype (up to 2^29 elements of e, or m x 4096 if that is more, at a time). */
+int mdet_xent_workspace_query(int32_t dtype, int32_t grad_dtype, int32_t backward, int64_t m, int64_t n, int64_t k,
+                              uint64_t* bytes);
+/* Device bytes of `kept`: m x n elements of two bytes for MDET_BF16, four otherwise, and a little more. */
 int mdet_xent_kept_query(int32_t dtype, int64_t m, int64_t n, int64_t k, uint64_t* bytes);
 
 /* loss_i = lse_i - z_i,t_i with z = x w^T + bias and lse_i = log(sum over j of exp(z_ij)), in fp32, without z in memory: x is
  * m x k, w n x k, bias n elements (or NULL), all of dtype (MDET_F32, MDET_F16 or MDET_BF16); loss and lse m floats, either may be
  * NULL.  A row whose target is `ignore`, or outside of the vocabulary, does not count: its loss is 0.  Where `kept` is not NULL it
- * receives what spares the gradient the product z, starts on 256 bytes, and no workspace is needed. */
+ * receives what spares the gradient the product z, and starts on 256 bytes; less workspace will do then, or none. */
 int mdet_xent_forward(int32_t dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const void* x, int64_t ldx, const void* w,
                       int64_t ldw, const void* bias, const void* target, int64_t ignore, float* loss, float* lse, void* kept,
                       uint64_t kept_bytes, void* workspace, uint64_t workspace_bytes, void* stream);
@@ -709,7 +710,8 @@ int mdet_xent_forward(int32_t dtype, int32_t index_bits, int64_t m, int64_t n, i
 /* Gradient of sum over i of dloss_i loss_i, from the forward call's lse, and what it kept (NULL: z is formed once more): with
  * e_ij = dloss_i (exp(z_ij - lse_i) - [j = t_i]),  dx = e w,  dw = e^T x,  db = column sums of e; any of dx, dw, db may be NULL (not
  * wanted).  dw and db are of grad_dtype: dtype or MDET_F32.  e is rounded to dtype in front of the two products (in MDET_F16 scaled by a
- * power of two, so that small probabilities are not lost); db sums the unrounded one.  Nothing of a row that does not count comes through,
+ * power of two, so that small probabilities are not lost); db sums the unrounded one.  With dw in MDET_F32 of operands in 16 bits e goes into dw
+ * unrounded, as the sum of two (MDET_F16) or three (MDET_BF16) numbers, which takes as many products, and `kept` is not used.  Nothing of a row that does not count comes through,
  * whatever its x and dloss hold, not even NaN. */
 int mdet_xent_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const float* dloss,
                        const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* target, int64_t ignore,

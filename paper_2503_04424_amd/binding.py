@@ -167,7 +167,7 @@ def load():
     L.mdet_layernorm_workspace_query.argtypes = [i32, i64, i64, C.POINTER(u64)]
     L.mdet_layernorm_forward.argtypes = [i32, i64, i64, vp, i64, vp, vp, f64, vp, i64, vp, vp, vp]
     L.mdet_layernorm_backward.argtypes = [i32, i32, i64, i64, vp, i64, vp, i64, vp, vp, vp, vp, i64, vp, vp, vp, u64, vp]
-    L.mdet_xent_workspace_query.argtypes = [i32, i32, i64, i64, i64, C.POINTER(u64)]
+    L.mdet_xent_workspace_query.argtypes = [i32, i32, i32, i64, i64, i64, C.POINTER(u64)]
     L.mdet_xent_kept_query.argtypes = [i32, i64, i64, i64, C.POINTER(u64)]
     L.mdet_xent_forward.argtypes = [i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, u64, vp, u64, vp]
     L.mdet_xent_backward.argtypes = [i32, i32, i32, i64, i64, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, u64, vp, i64, vp, i64,
@@ -1108,10 +1108,11 @@ def mdet_layernorm_backward(dy, x, mean, rstd, weight=None, dx=True, dw=True, db
 
 
 @functools.lru_cache(maxsize=1024)
-def mdet_xent_workspace_query(dtype, m, n, k, backward=False) -> int:
-    """Device bytes of workspace for ``mdet_xent_forward`` or, with ``backward``, the gradient."""
+def mdet_xent_workspace_query(dtype, m, n, k, backward=False, grad_dtype=None) -> int:
+    """Device bytes of workspace for ``mdet_xent_forward`` or, with ``backward``, the gradient with dw and db of ``grad_dtype``."""
     b = C.c_uint64(0)
-    _check_status(load().mdet_xent_workspace_query(_type_code(dtype), int(backward), int(m), int(n), int(k), C.byref(b)))
+    _check_status(load().mdet_xent_workspace_query(_type_code(dtype), _type_code(dtype if grad_dtype is None else grad_dtype), int(backward), int(m),
+                                                   int(n), int(k), C.byref(b)))
     return b.value
 
 
@@ -1151,7 +1152,7 @@ def mdet_xent_forward(x, w, target, bias=None, ignore=-100, loss=True, lse=True,
     if keep is not None and keep is not False:
         kept = _fresh(x, mdet_xent_kept_query(t, m, n, k), _BYTE[0], stream) if keep is True else keep
         kp, kb = _bytes(kept, "keep", gpu)
-    wsp, wsb, _ws = _room(workspace, lambda: 0 if kept is not None else mdet_xent_workspace_query(t, m, n, k), gpu, x, stream)
+    wsp, wsb, _ws = _room(workspace, lambda: mdet_xent_workspace_query(t, m, n, k), gpu, x, stream)
     _queue(gpu, load().mdet_xent_forward, _type_code(t), bits, m, n, k, xp, ldx, wp, ldw, bp, tp, ignore, lp, sp, kp, kb, wsp, wsb,
            _operator_stream(stream, gpu))
     if given:
@@ -1172,7 +1173,7 @@ def mdet_xent_backward(dloss, x, w, target, lse, bias=None, ignore=-100, kept=No
     dx, dxp, lddx = _matrix_result(dx, "dx", m, k, t, gpu, x, stream)
     dw, dwp, lddw = _matrix_result(dw, "dw", n, k, gt, gpu, x, stream)
     db, dbp = _vector_result(db, "db", n, gt, gpu, x, stream)
-    wsp, wsb, _ws = _room(workspace, lambda: mdet_xent_workspace_query(t, m, n, k, True), gpu, x, stream)
+    wsp, wsb, _ws = _room(workspace, lambda: mdet_xent_workspace_query(t, m, n, k, True, gt), gpu, x, stream)
     _queue(gpu, load().mdet_xent_backward, _type_code(t), _type_code(gt), bits, m, n, k, gp, xp, ldx, wp, ldw, bp, tp, ignore, sp, kp, kb,
            dxp, lddx, dwp, lddw, dbp, wsp, wsb, _operator_stream(stream, gpu))
     if given:

@@ -5,10 +5,12 @@
 //
 // Forward, each tile of z stays in the accumulators: what leaves it are each row's largest logit M and the sum of exp(z - M) over the
 // tile's columns (a strip), joined by a second launch, and the logit of the target.  Backward, z is formed once more in front
-// of e, a piece of the vocabulary at a time; or, where the forward pass kept them, exp(z - M) is read back in the operands' type (M is the
-// strip's: nothing overflows, and what is rounded keeps its relative precision), which spares that product.
+// of e, a piece of the vocabulary at a time; or, where the forward pass kept them, exp(z - M) is read back (M is the strip's: nothing
+// overflows, and what is rounded keeps its relative precision), which spares that product.
 //
-// Sums and everything behind them are fp32; e is rounded to the operands' type in front of its two products, db sums the unrounded one.
+// Sums and everything behind them are fp32; e is rounded to the operands' type in front of its two products, db sums the unrounded one.  Where dW
+// is wanted in 32 bits of operands in 16, that rounding would be all of its error: e goes in as two (fp16) or three (bf16) numbers that add up
+// to it, their rows one behind the other beside as many copies of x, a sum over two or three times the rows.
 // In fp16 e would vanish below 2^-24, where most probabilities of a large vocabulary lie: it is scaled by a power of two
 // that brings the largest |g| to 2^14 .. 2^15, and the products by its reciprocal.
 //
@@ -25,19 +27,37 @@ struct XentTargets {
   int bits;                            // 32 or 64
   int64_t ignore, vocab;
 };
-// The target of row i; -1 if it does not count.
-__device__ __forceinline__ int64_t xent_target(const XentTargets& t, const int64_t i) {
-  const int64_t v = t.bits == 32 ? (int64_t) static_cast<const int32_t*>(t.target)[i] : static_cast<const int64_t*>(t.target)[i];
+// The target of row i, in two steps, so that the loads of several rows can be on their way beside a product: what is in memory, then what it
+// says; -1 if the row does not count.
+__device__ __forceinline__ int64_t xent_raw(const XentTargets& t, const int64_t i) {
+  const int32_t* const p = static_cast<const int32_t*>(t.target) + (t.bits == 32 ? i : 2 * i);
+  const uint32_t low = (uint32_t)p[0], high = (uint32_t)p[t.bits == 32 ? 0 : 1];
+  return (int64_t)((uint64_t)high << 32 | low);
+}
+__device__ __forceinline__ int64_t xent_said(const XentTargets& t, const int64_t raw) {
+  const int64_t v = t.bits == 32 ? (int64_t)(int32_t)raw : raw;
   return v < 0 || v >= t.vocab || v == t.ignore ? -1 : v;
 }
 
+__device__ __forceinline__ int64_t xent_target(const XentTargets& t, const int64_t i) { return xent_said(t, xent_raw(t, i)); }
+
+// exp(z - top), from the difference: 2^-23 of its size is what the result is off by.  Zero for z = -inf also where top is.
+__device__ __forceinline__ float xent_exp(const float z, const float top) { return __expf(z - (top == -INFINITY ? 0.0f : top)); }
+
 // exp(z - top) as a power of two, xent_power(z, xent_from(top)): one multiplication and addition in front of it.  With |z| and |top| below 30
-// their rounding is 2e-6 of the result, what a sum of a few dozen fp32 terms may be off by, and 16 bits keep 5e-4 or 4e-3.  Where top is
-// the largest of some z that are all -inf, the powers are zero.
+// their rounding is 2e-6 of a term, and far less of the sum of many, which is all that leaves the forward pass in more than 16 bits (fp32:
+// from the difference).  Where top is the largest of some z that are all -inf, the powers are zero.
 constexpr float XENT_LOG2E = 1.44269504088896341f;
 __device__ __forceinline__ float xent_from(const float top) { return top == -INFINITY ? 0.0f : -XENT_LOG2E * top; }
-__device__ __forceinline__ float xent_power(const float z, const float from) { return __builtin_amdgcn_exp2f(fmaf(z, XENT_LOG2E, from)); }
-__device__ __forceinline__ float xent_exp(const float z, const float top) { return __expf(z - (top == -INFINITY ? 0.0f : top)); }
+template <typename T>
+__device__ __forceinline__ float xent_power(const float z, const float from, const float top) {
+  if constexpr (sizeof(T) == 4) return xent_exp(z, top);
+  else return __builtin_amdgcn_exp2f(fmaf(z, XENT_LOG2E, from));
+}
+
+// What is kept of exp(z - top): numbers up to 1, to 11 bits for operands in bf16 (fewer would add to what rounding e costs), to 24 otherwise.
+template <typename T> struct XentKept { typedef float type; };
+template <> struct XentKept<__bf16> { typedef _Float16 type; };
 
 struct XentStrip {                     // of a row: its largest logit among a strip's columns, and the sum of exp(z - top)
   float top, sum;
@@ -50,7 +70,7 @@ struct XentForward {
   XentStrip* strips;                   // rows x across
   int64_t across;
   float* picked;                       // of the rows that count: the target's logit
-  T* exps;                             // rows x ldexps, exp(z - top); null: not kept
+  typename XentKept<T>::type* exps;    // rows x ldexps, exp(z - top); null: not kept
   int64_t ldexps, rows, cols;
 };
 
@@ -120,7 +140,18 @@ __device__ __forceinline__ void xent_units(char* const lds, const Operand<T>& r,
     }
     early(now);
     typename Core<T>::acc_t acc[S::TN][S::TM] = {};
-    if constexpr (DIRECT && S::BM == 256) stream.run_rolling(acc, stream.slabs(now.k0, now.kend), next);
+    if constexpr (sizeof(T) == 4) {
+      // in 32 bits the sums' own rounding counts: 1024 terms at a time, which are then added up
+      for (int left = stream.slabs(now.k0, now.kend); left > 0; left -= 32) {
+        typename Core<T>::acc_t some[S::TN][S::TM] = {};
+        const int count = left < 32 ? left : 32;
+        stream.run(some, count, next);
+#pragma unroll
+        for (int a = 0; a < S::TN; ++a)
+#pragma unroll
+          for (int b = 0; b < S::TM; ++b) acc[a][b] += some[a][b];
+      }
+    } else if constexpr (DIRECT && S::BM == 256) stream.run_rolling(acc, stream.slabs(now.k0, now.kend), next);
     else stream.run(acc, stream.slabs(now.k0, now.kend), next);
     // of a sum over nothing no slab was brought, and nothing is on its way
     fresh = false;
@@ -183,22 +214,28 @@ __device__ __forceinline__ void xent_store(T* const row, const int64_t col, cons
 template <typename T, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS) void xent_forward_kernel(const Operand<T> r, const Operand<T> c, const XentForward<T> o, const XentUnits u) {
   typedef typename Core<T>::acc_t acc_t;
-  typedef T t4 __attribute__((ext_vector_type(4)));
+  typedef typename XentKept<T>::type K;
+  typedef K k4 __attribute__((ext_vector_type(4)));
   constexpr int STRIP = S::TN * 16;
   __shared__ __attribute__((aligned(16))) char lds[S::NB * S::SLAB];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
   const int wrow = wave / S::WN * (S::TM * 16) + (lane & 15), quad = 4 * (lane >> 4);
-  int at[S::TM];                       // the rows' targets, counted from this lane's first column on
+  int64_t raw[S::TM];                  // the rows' targets
   auto early = [&](const XentUnit& x) {
-    const int64_t first = ((int64_t)x.bj * S::WN + wave % S::WN) * STRIP + quad;
 #pragma unroll
     for (int b = 0; b < S::TM; ++b) {
-      const int64_t i = (int64_t)x.bi * S::BM + wrow + 16 * b, t = i < o.rows ? xent_target(o.t, i) : -1;
-      at[b] = t >= first && t < first + STRIP ? (int)(t - first) : -1;
+      const int64_t i = (int64_t)x.bi * S::BM + wrow + 16 * b;
+      raw[b] = xent_raw(o.t, i < o.rows ? i : o.rows - 1);
     }
   };
   xent_units<T, S, false, false, DIRECT>(lds, r, c, u, early, [&](const XentUnit& x, acc_t (&acc)[S::TN][S::TM]) {
     const int64_t row0 = (int64_t)x.bi * S::BM + wrow, strip = (int64_t)x.bj * S::WN + wave % S::WN, col0 = strip * STRIP;
+    int at[S::TM];                     // counted from this lane's first column on
+#pragma unroll
+    for (int b = 0; b < S::TM; ++b) {
+      const int64_t t = xent_said(o.t, raw[b]) - (col0 + quad);
+      at[b] = t >= 0 && t < STRIP && row0 + 16 * b < o.rows ? (int)t : -1;
+    }
     if (o.bias || ((int64_t)x.bj + 1) * S::BN > o.cols) {
 #pragma unroll
       for (int a = 0; a < S::TN; ++a)
@@ -233,15 +270,15 @@ __global__ __launch_bounds__(S::THREADS) void xent_forward_kernel(const Operand<
       for (int a = 0; a < S::TN; ++a)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          acc[a][b][e] = xent_power(acc[a][b][e], from);
+          acc[a][b][e] = xent_power<T>(acc[a][b][e], from, top);
           sum += acc[a][b][e];
         }
       sum = xent_across(sum, [](const float p, const float q) { return p + q; });
       if (lane < 16 && i < o.rows && strip < o.across) o.strips[i * o.across + strip] = XentStrip{top, sum};
       // rows are ceil(cols / 8) 8 long: what is written behind their end is zero
       if (o.exps)
-        xent_store<T, S::TN>(o.exps + i * o.ldexps, col0, o.cols, i < o.rows, [&](const int a) {
-          return t4{(T)acc[a][b][0], (T)acc[a][b][1], (T)acc[a][b][2], (T)acc[a][b][3]};
+        xent_store<K, S::TN>(o.exps + i * o.ldexps, col0, o.cols, i < o.rows, [&](const int a) {
+          return k4{(K)acc[a][b][0], (K)acc[a][b][1], (K)acc[a][b][2], (K)acc[a][b][3]};
         });
     }
   });
@@ -321,15 +358,16 @@ __global__ __launch_bounds__(64 * XENT_WAVES) void xent_forward_rows_kernel(cons
   const float from = xent_from(top);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    z[e] = xent_power(z[e], from);
+    z[e] = xent_power<T>(z[e], from, top);
     total += z[e];
   }
   total += __shfl_xor(total, 16, 64);
   total += __shfl_xor(total, 32, 64);
   if (i >= o.rows || strip >= o.across) return;
   if (lane < 16) o.strips[i * o.across + strip] = XentStrip{top, total};
-  typedef T t4 __attribute__((ext_vector_type(4)));
-  if (o.exps && c < o.cols) *reinterpret_cast<t4*>(o.exps + i * o.ldexps + c) = t4{(T)z[0], (T)z[1], (T)z[2], (T)z[3]};
+  typedef typename XentKept<T>::type K;
+  typedef K k4 __attribute__((ext_vector_type(4)));
+  if (o.exps && c < o.cols) *reinterpret_cast<k4*>(o.exps + i * o.ldexps + c) = k4{(K)z[0], (K)z[1], (K)z[2], (K)z[3]};
 }
 
 // lse and loss of a row from its strips, by LANES lanes.
@@ -392,7 +430,7 @@ __global__ __launch_bounds__(1024) void xent_scale_kernel(const float* __restric
   }
 }
 
-// x with zeros in the rows that do not count, rows on 16 bytes.
+// x with zeros in the rows that do not count (without targets: all do) and behind every row's end, rows on 16 bytes.
 template <typename T>
 __global__ __launch_bounds__(256) void xent_rows_kernel(const T* __restrict__ x, const int64_t ldx, const XentTargets t, const int64_t rows,
                                                         const int64_t k, T* __restrict__ to, const int64_t ldto, const int64_t first) {
@@ -400,7 +438,7 @@ __global__ __launch_bounds__(256) void xent_rows_kernel(const T* __restrict__ x,
   const int64_t across = ldto / Core<T>::VEC, id = (first + blockIdx.x) * 256 + threadIdx.x, i = id / across, c = (id - i * across) * Core<T>::VEC;
   if (i >= rows) return;
   piece_t v = {};
-  if (xent_target(t, i) >= 0) v = row_piece<T>(x + i * ldx, c, k);
+  if (!t.target || xent_target(t, i) >= 0) v = row_piece<T>(x + i * ldx, c, k);
   *reinterpret_cast<piece_t*>(to + i * ldto + c) = v;
 }
 
@@ -410,7 +448,7 @@ struct XentSlope {
   const T* bias;                       // null: none
   const float *lse, *g;
   const XentScale* scale;              // null: 1
-  T* e;                                // rows x lde, columns from `first` on
+  T* e;                                // rows x lde, columns from `first` on; then its other parts, likewise
   int64_t lde;
   float* sums;                         // parts x cols of db; null: not wanted
   int64_t rows, cols, first;           // of the piece
@@ -431,8 +469,8 @@ __device__ __forceinline__ XentRow xent_row(const XentSlope<T>& o, const int64_t
   return XentRow{o.lse[i], o.g[i], true, t - o.first - from};
 }
 
-// Tiles of e.
-template <typename T, typename S, bool DIRECT>
+// Tiles of e.  PARTS: numbers of type T that add up to an element of it.
+template <typename T, typename S, bool DIRECT, int PARTS>
 __global__ __launch_bounds__(S::THREADS) void xent_slope_kernel(const Operand<T> r, const Operand<T> c, const XentSlope<T> o, const XentUnits u) {
   typedef typename Core<T>::acc_t acc_t;
   typedef T t4 __attribute__((ext_vector_type(4)));
@@ -468,12 +506,11 @@ __global__ __launch_bounds__(S::THREADS) void xent_slope_kernel(const Operand<T>
     }
 #pragma unroll
     for (int b = 0; b < S::TM; ++b) {
-      const int64_t i = row0 + 16 * b;
-      const float from = -XENT_LOG2E * lse[b], weight = g[b] * up;
+      const float weight = g[b] * up;
 #pragma unroll
       for (int a = 0; a < S::TN; ++a)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[a][b][e] = xent_power(acc[a][b][e], from);
+        for (int e = 0; e < 4; ++e) acc[a][b][e] = __expf(acc[a][b][e] - lse[b]);
       if (__any(at[b] >= 0)) {
 #pragma unroll
         for (int a = 0; a < S::TN; ++a)
@@ -489,10 +526,6 @@ __global__ __launch_bounds__(S::THREADS) void xent_slope_kernel(const Operand<T>
 #pragma unroll
           for (int e = 0; e < 4; ++e) acc[a][b][e] = at[b] == -2 ? 0.0f : acc[a][b][e];
       }
-      // rows of e are whole pieces of 16 bytes long
-      xent_store<T, S::TN>(o.e + i * o.lde, col0, o.cols, i < o.rows, [&](const int a) {
-        return t4{(T)acc[a][b][0], (T)acc[a][b][1], (T)acc[a][b][2], (T)acc[a][b][3]};
-      });
     }
     if (o.sums) {
       const int64_t part = (int64_t)x.bi * S::WM + wave / S::WN;
@@ -509,6 +542,21 @@ __global__ __launch_bounds__(S::THREADS) void xent_slope_kernel(const Operand<T>
           if ((lane & 15) == 0 && j < o.cols) o.sums[part * o.cols + j] = s * down;
         }
     }
+#pragma unroll
+    for (int part = 0; part < PARTS; ++part) {
+#pragma unroll
+      for (int b = 0; b < S::TM; ++b) {
+        const int64_t i = row0 + 16 * b;
+        // rows of e are whole pieces of 16 bytes long
+        xent_store<T, S::TN>(o.e + (part * o.rows + i) * o.lde, col0, o.cols, i < o.rows, [&](const int a) {
+          const t4 v = t4{(T)acc[a][b][0], (T)acc[a][b][1], (T)acc[a][b][2], (T)acc[a][b][3]};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (PARTS > 1) acc[a][b][e] -= (float)v[e];                  // what is left for the next part
+          return v;
+        });
+      }
+    }
   });
 }
 
@@ -516,7 +564,8 @@ __global__ __launch_bounds__(S::THREADS) void xent_slope_kernel(const Operand<T>
 constexpr int XENT_EACH = 4;
 
 template <typename T>
-__global__ __launch_bounds__(256) void xent_slope_kept_kernel(const XentSlope<T> o, const T* __restrict__ exps, const int64_t ldexps,
+__global__ __launch_bounds__(256) void xent_slope_kept_kernel(const XentSlope<T> o, const typename XentKept<T>::type* __restrict__ exps,
+                                                              const int64_t ldexps,
                                                               const XentStrip* __restrict__ strips, const int64_t across, const int64_t strip,
                                                               const float* __restrict__ picked, const int64_t first) {
   typedef typename Core<T>::piece_t piece_t;
@@ -527,17 +576,18 @@ __global__ __launch_bounds__(256) void xent_slope_kept_kernel(const XentSlope<T>
   const int64_t col0 = (id - down * wide) * (16 * VEC), col = col0 + c, row = down * (16 * XENT_EACH) + t;
   const bool there = col < o.cols;
   const float up = o.scale ? o.scale->up : 1.0f;
-  piece_t x[XENT_EACH];
+  typedef typename XentKept<T>::type kept_t __attribute__((ext_vector_type(VEC)));
+  kept_t x[XENT_EACH];
   XentRow of[XENT_EACH];
   float top[XENT_EACH], hit[XENT_EACH];
 #pragma unroll
   for (int r = 0; r < XENT_EACH; ++r) {
     const int64_t i = row + 16 * r;
     of[r] = xent_row(o, i, col);
-    x[r] = piece_t{};
+    x[r] = kept_t{};
     top[r] = hit[r] = 0.0f;
     if (of[r].counts && there) {
-      x[r] = *reinterpret_cast<const piece_t*>(exps + i * ldexps + o.first + col);
+      x[r] = *reinterpret_cast<const kept_t*>(exps + i * ldexps + o.first + col);
       top[r] = strips[i * across + (o.first + col) / strip].top;
       hit[r] = picked[i];
     }

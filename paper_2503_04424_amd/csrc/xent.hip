@@ -46,7 +46,7 @@ dim3 units_grid(const XentUnits& u, bool direct) {
 template <typename T>
 XentForward<T> forward_places(char* at, const XentLayout& l, bool keep) {
   XentForward<T> o{};
-  o.exps = keep ? (T*)at : nullptr;
+  o.exps = keep ? (typename XentKept<T>::type*)at : nullptr;
   o.ldexps = l.ldexps;
   char* const rest = keep ? at + l.exps_bytes : at;
   o.strips = (XentStrip*)rest;
@@ -55,9 +55,26 @@ XentForward<T> forward_places(char* at, const XentLayout& l, bool keep) {
   return o;
 }
 
+// A copy of rows of k elements at a distance of `ld`.
 template <typename T>
-int forward(Operand<T> x, Operand<T> w, int64_t k, XentForward<T> o, const XentLayout& l, float* loss, float* lse, hipStream_t st) {
+void copy_rows(const T* from, int64_t ldfrom, const XentTargets& t, int64_t rows, int64_t k, T* to, int64_t ld, hipStream_t st) {
+  gemm_launches(ceil_div(rows * (ld / Core<T>::VEC), 256), 256, [&](const int64_t first, const dim3 grid) {
+    hipLaunchKernelGGL((xent_rows_kernel<T>), grid, dim3(256), 0, st, from, ldfrom, t, rows, k, to, ld, first);
+  });
+}
+
+template <typename T>
+int forward(Operand<T> x, Operand<T> w, int64_t k, XentForward<T> o, const XentLayout& l, char* copies, float* loss, float* lse,
+            hipStream_t st) {
   if (o.cols > 0) {
+    if (l.copies) {
+      const int64_t ld = xent_pad(k);
+      copy_rows<T>(x.p, x.stride, XentTargets{}, x.rows, k, (T*)copies, ld, st);
+      copy_rows<T>(w.p, w.stride, XentTargets{}, w.rows, k, (T*)(copies + l.x_bytes), ld, st);
+      x.p = (const T*)copies;
+      w.p = (const T*)(copies + l.x_bytes);
+      x.stride = w.stride = k = ld;
+    }
     if (l.cut.tile == 0) {
       // Few rows of x want more of W on its way, many share their own loads out over more of it, as long as that leaves enough workgroups.  us for
       // one, two, four groups of W, rows of 4096 bf16: 4 rows over 131072 words 194, 198, 219, 8 rows 223, 212, 224, 16 rows 277, 243, 236; 16
@@ -120,6 +137,11 @@ void product(Operand<T> r, Operand<T> c, int64_t k, XentOut<O> o, float* parts, 
   });
 }
 
+// Numbers of the operands' type that add up to an element of e: 8 bits each in bf16, 11 in fp16, of 24.
+int64_t parts_of(int32_t dtype, int32_t grad_dtype) { return dtype == MDET_F32 || grad_dtype != MDET_F32 ? 1 : dtype == MDET_BF16 ? 3 : 2; }
+
+int64_t kept_size(int32_t dtype) { return dtype == MDET_BF16 ? 2 : 4; }
+
 struct Grad {
   XentTargets t;
   int64_t m, n, k;
@@ -135,8 +157,11 @@ struct Grad {
 
 template <typename T, typename O>
 int backward(const Grad& a) {
-  const XentLayout f = xent_layout(a.m, a.n, a.k, sizeof(T));
-  const XentGradLayout l = xent_grad_layout(a.m, a.n, a.k, sizeof(T));
+  const XentLayout f = xent_layout(a.m, a.n, a.k, sizeof(T), sizeof(typename XentKept<T>::type));
+  constexpr int parts_of_e = sizeof(T) == sizeof(O) ? 1 : std::is_same<T, _Float16>::value ? 2 : 3;
+  const XentGradLayout l = xent_grad_layout(a.m, a.n, a.k, sizeof(T), parts_of_e);
+  // what was kept may be rounded to 11 bits, which is not enough for more than one part
+  char* const kept = parts_of_e == 1 ? a.kept : nullptr;
   hipStream_t st = a.st;
   T *const e = (T*)(a.workspace + l.e), *const rows = (T*)(a.workspace + l.rows);
   float *const sums = (float*)(a.workspace + l.sums), *const total = (float*)(a.workspace + l.total), *const parts = (float*)(a.workspace + l.parts);
@@ -145,42 +170,49 @@ int backward(const Grad& a) {
     scale = (XentScale*)(a.workspace + l.scale);
     hipLaunchKernelGGL(xent_scale_kernel, dim3(1), dim3(1024), 0, st, a.g, a.t, a.m, scale);
   }
-  if (a.dw && a.k > 0)
-    gemm_launches(ceil_div(a.m * (l.ldrows / Core<T>::VEC), 256), 256, [&](const int64_t first, const dim3 grid) {
-      hipLaunchKernelGGL((xent_rows_kernel<T>), grid, dim3(256), 0, st, (const T*)a.x, a.ldx, a.t, a.m, a.k, rows, l.ldrows, first);
-    });
+  const bool own_rows = a.k > 0 && (a.dw || (l.copies && !kept));
+  for (int part = 0; own_rows && part < parts_of_e; ++part)
+    copy_rows<T>((const T*)a.x, a.ldx, a.t, a.m, a.k, rows + part * a.m * l.ldrows, l.ldrows, st);
   for (int64_t v = 0; v < a.n; v += l.piece) {
     const int64_t n = a.n - v < l.piece ? a.n - v : l.piece;
-    const T* const w = (const T*)a.w + v * a.ldw;
+    const T* w = (const T*)a.w + v * a.ldw;
+    int64_t ldw = a.ldw, k = a.k;      // of the sums for e, zeros behind a row's end among them
+    const bool own_w = l.copies && (a.dx || !kept);
+    if (own_w) {
+      copy_rows<T>(w, ldw, XentTargets{}, n, a.k, (T*)(a.workspace + l.w), l.ldrows, st);
+      w = (const T*)(a.workspace + l.w);
+      ldw = k = l.ldrows;
+    }
     const XentSlope<T> o{a.t, a.bias ? (const T*)a.bias + v : nullptr, a.lse, a.g, scale, e, l.lde, a.db ? sums : nullptr, a.m, n, v};
     int64_t strips = 0;
-    if (a.kept) {
-      const XentForward<T> was = forward_places<T>(a.kept, f, true);
+    if (kept) {
+      const XentForward<T> was = forward_places<T>(kept, f, true);
       strips = ceil_div(a.m, 16 * XENT_EACH);
       gemm_launches(strips * ceil_div(n, 16 * Core<T>::VEC), 256, [&](const int64_t first, const dim3 grid) {
-        hipLaunchKernelGGL((xent_slope_kept_kernel<T>), grid, dim3(256), 0, st, o, (const T*)was.exps, was.ldexps, (const XentStrip*)was.strips, was.across,
-                           f.strip, (const float*)was.picked, first);
+        hipLaunchKernelGGL((xent_slope_kept_kernel<T>), grid, dim3(256), 0, st, o, was.exps, was.ldexps, (const XentStrip*)was.strips, was.across, f.strip,
+                           (const float*)was.picked, first);
       });
     } else
       with_tile<T>(cut_of(a.m, n, a.k, sizeof(T), false).tile, [&](auto shape) {
         typedef decltype(shape) S;
-        const Operand<T> x = gemm_operand<T, false, S::BM>(a.x, a.ldx, a.m, a.k), c = gemm_operand<T, false, S::BN>(w, a.ldw, n, a.k);
+        const Operand<T> x = own_w ? gemm_operand<T, false, S::BM>(rows, l.ldrows, a.m, k) : gemm_operand<T, false, S::BM>(a.x, a.ldx, a.m, k);
+        const Operand<T> c = gemm_operand<T, false, S::BN>(w, ldw, n, k);
         const bool direct = x.straight && c.straight;
-        const XentUnits u = whole_units<S>(a.m, n, a.k);
+        const XentUnits u = whole_units<S>(a.m, n, k);
         const dim3 grid = units_grid<S>(u, direct), block(S::THREADS);
         strips = ceil_div(a.m, S::BM) * S::WM;
-        if (direct) hipLaunchKernelGGL((xent_slope_kernel<T, S, true>), grid, block, 0, st, x, c, o, u);
-        else hipLaunchKernelGGL((xent_slope_kernel<T, S, false>), grid, block, 0, st, x, c, o, u);
+        if (direct) hipLaunchKernelGGL((xent_slope_kernel<T, S, true, parts_of_e>), grid, block, 0, st, x, c, o, u);
+        else hipLaunchKernelGGL((xent_slope_kernel<T, S, false, parts_of_e>), grid, block, 0, st, x, c, o, u);
       });
     if (a.db)
       gemm_launches(ceil_div(n, 16), 256, [&](const int64_t first, const dim3 grid) {
         hipLaunchKernelGGL((xent_columns_kernel<O>), grid, dim3(256), 0, st, (const float*)sums, strips, n, (O*)a.db + v, first);
       });
     if (a.dx && a.k > 0)
-      product<T, T, false>(Operand<T>{e, l.lde, a.m, false, false}, Operand<T>{w, a.ldw, a.k, false, false}, n,
+      product<T, T, false>(Operand<T>{e, l.lde, a.m, false, false}, Operand<T>{w, ldw, a.k, false, false}, n,
                            XentOut<T>{(T*)a.dx, a.lddx, scale, total, v == 0, v + n == a.n, a.m, a.k, false}, parts, st);
     if (a.dw && a.k > 0)
-      product<T, O, true>(Operand<T>{e, l.lde, n, false, false}, Operand<T>{rows, l.ldrows, a.k, false, false}, a.m,
+      product<T, O, true>(Operand<T>{e, l.lde, n, false, false}, Operand<T>{rows, l.ldrows, a.k, false, false}, parts_of_e * a.m,
                           XentOut<O>{(O*)a.dw + v * a.lddw, a.lddw, scale, nullptr, true, true, n, a.k, false}, parts, st);
   }
   return launch_status();
@@ -210,17 +242,17 @@ bool xent_fits(int64_t m, int64_t n, int64_t k) { return sizes_fit(m, n, k) && t
 
 extern "C" {
 
-int mdet_xent_workspace_query(int32_t dtype, int32_t backward, int64_t m, int64_t n, int64_t k, uint64_t* bytes) {
-  if (!bytes || !is_type(dtype) || !xent_fits(m, n, k)) return MDET_EINVAL;
-  const XentLayout l = xent_layout(m, n, k, size_of(dtype));
-  *bytes = backward ? xent_grad_layout(m, n, k, size_of(dtype)).bytes : l.strips_bytes + l.picked_bytes;
+int mdet_xent_workspace_query(int32_t dtype, int32_t grad_dtype, int32_t backward, int64_t m, int64_t n, int64_t k, uint64_t* bytes) {
+  if (!bytes || !is_type(dtype) || (grad_dtype != dtype && grad_dtype != MDET_F32) || !xent_fits(m, n, k)) return MDET_EINVAL;
+  const XentLayout l = xent_layout(m, n, k, size_of(dtype), kept_size(dtype));
+  *bytes = backward ? xent_grad_layout(m, n, k, size_of(dtype), parts_of(dtype, grad_dtype)).bytes : l.workspace(false);
   return MDET_OK;
 }
 
 int mdet_xent_kept_query(int32_t dtype, int64_t m, int64_t n, int64_t k, uint64_t* bytes) {
   if (!bytes || !is_type(dtype) || !xent_fits(m, n, k)) return MDET_EINVAL;
-  const XentLayout l = xent_layout(m, n, k, size_of(dtype));
-  *bytes = l.exps_bytes + l.strips_bytes + l.picked_bytes;
+  const XentLayout l = xent_layout(m, n, k, size_of(dtype), kept_size(dtype));
+  *bytes = l.kept();
   return MDET_OK;
 }
 
@@ -231,19 +263,20 @@ int mdet_xent_forward(int32_t dtype, int32_t index_bits, int64_t m, int64_t n, i
   const int64_t s = size_of(dtype);
   if (!matrix_ok(x, m, k, ldx, s) || !matrix_ok(w, n, k, ldw, s) || (uintptr_t)bias % s || !vector_ok(target, m, index_bits / 8)) return MDET_EINVAL;
   if ((uintptr_t)loss % 4 || (uintptr_t)lse % 4) return MDET_EINVAL;
-  const XentLayout l = xent_layout(m, n, k, s);
-  const uint64_t strips = l.strips_bytes + l.picked_bytes;
-  const int ok = kept ? workspace_ok(kept, kept_bytes, l.exps_bytes + strips) : workspace_ok(workspace, workspace_bytes, strips);
+  const XentLayout l = xent_layout(m, n, k, s, kept_size(dtype));
+  int ok = kept ? workspace_ok(kept, kept_bytes, l.kept()) : MDET_OK;
+  if (ok == MDET_OK) ok = workspace_ok(workspace, workspace_bytes, l.workspace(kept != nullptr));
   if (ok != MDET_OK) return ok;
   if (m == 0 || (!loss && !lse && !kept)) return MDET_OK;
   auto call = [&](auto zero) {
     typedef decltype(zero) T;
-    XentForward<T> o = forward_places<T>((char*)(kept ? kept : workspace), l, kept != nullptr);
+    XentForward<T> o = forward_places<T>(kept ? (char*)kept : (char*)workspace + l.x_bytes + l.w_bytes, l, kept != nullptr);
     o.t = XentTargets{target, index_bits, ignore, n};
     o.bias = (const T*)bias;
     o.rows = m;
     o.cols = n;
-    return forward<T>(Operand<T>{(const T*)x, ldx, m, false, false}, Operand<T>{(const T*)w, ldw, n, false, false}, k, o, l, loss, lse, (hipStream_t)stream);
+    return forward<T>(Operand<T>{(const T*)x, ldx, m, false, false}, Operand<T>{(const T*)w, ldw, n, false, false}, k, o, l, (char*)workspace, loss, lse,
+                      (hipStream_t)stream);
   };
   return dtype == MDET_F32 ? call(0.0f) : dtype == MDET_BF16 ? call((__bf16)0.0f) : call((_Float16)0.0f);
 }
@@ -257,9 +290,9 @@ int mdet_xent_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, in
   if (!matrix_ok(x, m, k, ldx, s) || !matrix_ok(w, n, k, ldw, s) || (uintptr_t)bias % s || !vector_ok(target, m, index_bits / 8)) return MDET_EINVAL;
   if (!vector_ok(dloss, m, 4) || !vector_ok(lse, m, 4)) return MDET_EINVAL;
   if ((dx && !matrix_ok(dx, m, k, lddx, s)) || (dw && !matrix_ok(dw, n, k, lddw, gs)) || (uintptr_t)db % gs) return MDET_EINVAL;
-  const XentLayout f = xent_layout(m, n, k, s);
-  int ok = kept ? workspace_ok(kept, kept_bytes, f.exps_bytes + f.strips_bytes + f.picked_bytes) : MDET_OK;
-  if (ok == MDET_OK) ok = workspace_ok(workspace, workspace_bytes, xent_grad_layout(m, n, k, s).bytes);
+  const XentLayout f = xent_layout(m, n, k, s, kept_size(dtype));
+  int ok = kept ? workspace_ok(kept, kept_bytes, f.kept()) : MDET_OK;
+  if (ok == MDET_OK) ok = workspace_ok(workspace, workspace_bytes, xent_grad_layout(m, n, k, s, parts_of(dtype, grad_dtype)).bytes);
   if (ok != MDET_OK) return ok;
   if (!dx && !dw && !db) return MDET_OK;
   hipStream_t st = (hipStream_t)stream;

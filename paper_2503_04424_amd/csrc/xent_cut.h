@@ -4,25 +4,41 @@
 
 namespace mdet {
 
+constexpr int64_t XENT_COPY = 768, XENT_COPY_GRAD = 512;
+
 inline uint64_t xent_up256(uint64_t x) { return (x + 255) / 256 * 256; }
 
-// m rows, a vocabulary of n, rows of k elements of `size` bytes.
+// Rows of x and W in 16 bits that are no whole pieces of 16 bytes long go through registers, which halves the rate of a product of large tiles.
+// From these many rows of x on they are copied first, at that distance, with zeros behind them.  us without and with copies, 32003 words of
+// 1501 in fp16: forward 512 rows 76 and 85, 1024 rows 144 and 127, 4096 rows 523 and 380; gradient 256 rows 352 and 361, 512 rows 295 and 298
+// (131071 words: 1156 and 1103), 4096 rows 1636 and 1266.
+inline int64_t xent_pad(int64_t k) { return k >= 1024 ? ceil_div(k, 64) * 64 : ceil_div(k, 8) * 8; }
+inline bool xent_copies(int64_t m, int64_t k, int64_t size, bool backward) { return size == 2 && k % 8 != 0 && m >= (backward ? XENT_COPY_GRAD : XENT_COPY); }
+
+// m rows, a vocabulary of n, rows of k elements of `size` bytes; kept_size: bytes of an exponential that is kept.
 struct XentLayout {
   Cut cut;                             // of the forward pass; its sums are not split
   int64_t strip, across;               // columns of a strip, strips of a row
   int64_t ldexps;
   uint64_t exps_bytes, strips_bytes, picked_bytes;
+  bool copies;                         // of x and W, in the workspace
+  uint64_t x_bytes, w_bytes;
+  uint64_t kept() const { return exps_bytes + strips_bytes + picked_bytes; }
+  uint64_t workspace(bool keep) const { return x_bytes + w_bytes + (keep ? 0 : strips_bytes + picked_bytes); }
 };
-inline XentLayout xent_layout(int64_t m, int64_t n, int64_t k, int64_t size) {
+inline XentLayout xent_layout(int64_t m, int64_t n, int64_t k, int64_t size, int64_t kept_size) {
   XentLayout l;
   l.cut = m <= 16 && n <= (int64_t(1) << 28) ? Cut{0, 1, k} : cut_of(m, n, k, size, false);
   // a wavefront's columns of a tile
   l.strip = l.cut.tile == 256 ? 64 : l.cut.tile == 128 ? 64 : l.cut.tile == 64 ? 32 : 16;
   l.across = ceil_div(n, l.strip);
   l.ldexps = ceil_div(n, 8) * 8;
-  l.exps_bytes = xent_up256((uint64_t)m * l.ldexps * size);
+  l.exps_bytes = xent_up256((uint64_t)m * l.ldexps * kept_size);
   l.strips_bytes = xent_up256((uint64_t)m * l.across * 8);
   l.picked_bytes = xent_up256((uint64_t)m * 4);
+  l.copies = xent_copies(m, k, size, false);
+  l.x_bytes = l.copies ? xent_up256((uint64_t)m * xent_pad(k) * size) : 0;
+  l.w_bytes = l.copies ? xent_up256((uint64_t)n * xent_pad(k) * size) : 0;
   return l;
 }
 
@@ -74,20 +90,24 @@ inline XentCut xent_cut(int64_t rows, int64_t cols, int64_t k, int64_t size) {
 
 struct XentGradLayout {
   int64_t piece, lde, ldrows;
-  uint64_t e, rows, scale, sums, total, parts, bytes;
+  bool copies;                         // of a piece of W; x's is there anyway
+  uint64_t e, rows, scale, sums, total, w, parts, bytes;
 };
-inline XentGradLayout xent_grad_layout(int64_t m, int64_t n, int64_t k, int64_t size) {
+// parts_of_e: numbers of the operands' type that add up to an element of e.
+inline XentGradLayout xent_grad_layout(int64_t m, int64_t n, int64_t k, int64_t size, int64_t parts_of_e) {
   XentGradLayout l;
-  l.piece = xent_piece(m, n);
+  l.piece = xent_piece(parts_of_e * m, n);
   l.lde = ceil_div(l.piece, 8) * 8;
-  l.ldrows = ceil_div(k, 8) * 8;
+  l.ldrows = xent_pad(k);
+  l.copies = xent_copies(m, k, size, true);
   l.e = 0;
-  l.rows = xent_up256((uint64_t)m * l.lde * size);
-  l.scale = l.rows + xent_up256((uint64_t)m * l.ldrows * size);
+  l.rows = xent_up256((uint64_t)parts_of_e * m * l.lde * size);
+  l.scale = l.rows + xent_up256((uint64_t)parts_of_e * m * l.ldrows * size);
   l.sums = l.scale + 256;
   // column sums of strips of 16 rows or more, of whole tiles
   l.total = l.sums + xent_up256((uint64_t)(ceil_div(m, 256) * 16) * l.piece * 4);
-  l.parts = l.total + (l.piece < n ? xent_up256((uint64_t)m * k * 4) : 0);
+  l.w = l.total + (l.piece < n ? xent_up256((uint64_t)m * k * 4) : 0);
+  l.parts = l.w + (l.copies ? xent_up256((uint64_t)l.piece * l.ldrows * size) : 0);
   uint64_t parts = 0;
   auto room = [&](int64_t rows, int64_t cols, int64_t inner) {
     const uint64_t b = xent_cut(rows, cols, inner, size).bytes();
@@ -96,8 +116,8 @@ inline XentGradLayout xent_grad_layout(int64_t m, int64_t n, int64_t k, int64_t 
   const int64_t last = n > 0 ? n - (n - 1) / l.piece * l.piece : 0;
   room(m, k, l.piece);
   room(m, k, last);
-  room(l.piece, k, m);
-  room(last, k, m);
+  room(l.piece, k, parts_of_e * m);
+  room(last, k, parts_of_e * m);
   l.bytes = l.parts + parts;
   return l;
 }

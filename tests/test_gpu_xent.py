@@ -1,6 +1,6 @@
 """The softmax cross entropy of a linear layer and its gradient against 64-bit references, with bounds derived from the arithmetic: a
 logit is a sum of k + 1 terms in fp32; an exponential is good to a few roundings and those of its argument; e is rounded to the operands'
-type in front of its two products (what the forward pass kept was rounded to it once before)."""
+type in front of its two products (what the forward pass kept was rounded once before, to fp16's or fp32's bits)."""
 import pytest
 
 torch = pytest.importorskip("torch")
@@ -11,7 +11,8 @@ pytestmark = pytest.mark.gpu
 TYPES = [torch.float32, torch.float16, torch.bfloat16]
 # rows, vocabulary, k: few rows (by themselves), every tile shape, several slabs, strips that end inside a tile
 SIZES = [(1, 1, 1), (1, 50, 5), (3, 100, 64), (4, 9000, 520), (16, 64, 64), (16, 1003, 2100), (17, 130, 72), (40, 1000, 33), (65, 129, 130), (130, 300, 257),
-         (300, 5003, 96), (300, 12001, 200), (520, 25003, 72), (260, 50000, 136), (1030, 257, 64)]
+         (300, 5003, 96), (300, 12001, 200), (520, 25003, 72), (260, 50000, 136), (1030, 257, 64), (600, 3001, 1030), (530, 12001, 77),
+         (300, 2000, 1501)]
 
 
 @pytest.fixture(scope="module")
@@ -62,8 +63,10 @@ def forward64(z, ez, t, n):
     return (loss, (el + ez.gather(1, at)[:, 0] + 2 * EPS32 * (lse.abs() + z.gather(1, at)[:, 0].abs())) * counts), (lse, el), counts
 
 
-def backward64(z, ez, x, w, t, g, lse, counts, dtype, kept):
-    """dx, dw, db with bounds, for the kernel's own lse."""
+def backward64(z, ez, x, w, t, g, lse, counts, dtype, kept, wide=False):
+    """dx, dw, db with bounds, for the kernel's own lse.  wide: dw and db in 32 bits, of an e that is not rounded to fewer (two fp16 numbers
+    are off by two of their roundings one behind the other, 2^-22, three of bf16 hold all 24 bits), nor taken from what was kept."""
+    kept = kept and not (wide and dtype != torch.float32)
     m, n = z.shape
     arg = z - lse.double()[:, None]
     p = torch.exp(arg)
@@ -74,16 +77,17 @@ def backward64(z, ez, x, w, t, g, lse, counts, dtype, kept):
     e[rows, t[rows]] -= 1
     e *= weight
     exact = (p * rel + EPS32 * e.abs()) * weight.abs()                 # in front of the rounding
-    if kept:                                                           # rounded once before, but the target's own; least numbers count as those of 1
-        first = (UNIT[dtype] * p + LEAST[dtype]) * weight.abs()
+    if kept:                                                           # rounded once before (bf16: to fp16's bits, of a part of 1), but the target's own
+        first = (2.0 ** -11 * p + 2.0 ** -24 if dtype == torch.bfloat16 else 2.0 ** -23 * p) * weight.abs()
         first[rows, t[rows]] = 0
         exact = exact + first
     least = LEAST[dtype] * (1.0 if dtype != torch.float16 else 2.0 ** -13 * float(weight.abs().max()))
     err = exact + UNIT[dtype] * (e.abs() + exact) + least
+    errw = exact + 2.0 ** -22 * e.abs() + least if wide and dtype != torch.float32 else err
     x = torch.where(counts[:, None], x.double(), 0.0)
     xa, wa, ea = x.abs(), w.double().abs(), e.abs()
     et = e.t().contiguous()
-    return ((e @ w.double(), err @ wa + (n + 8) * EPS32 * (ea @ wa)), (et @ x, err.t().contiguous() @ xa + (m + 8) * EPS32 * (et.abs() @ xa)),
+    return ((e @ w.double(), err @ wa + (n + 8) * EPS32 * (ea @ wa)), (et @ x, errw.t().contiguous() @ xa + (3 * m + 8) * EPS32 * (et.abs() @ xa)),
             (e.sum(0), exact.sum(0) + (m + 8) * EPS32 * ea.sum(0)))
 
 
@@ -107,7 +111,7 @@ def test_sizes(M, m, n, k, dtype):
                 dx = torch.full((m, k + pad), float("nan"), dtype=dtype, device="cuda")
                 dw = torch.full((n, k + pad), float("nan"), dtype=gt, device="cuda")
                 got = M.mdet_xent_backward(g, x, w, t, lse, bias, kept=what, dx=dx[:, :k], dw=dw[:, :k], db=True, grad_dtype=gt)
-                want = backward64(z, ez, x, w, t.long(), g, lse, counts, dtype, what is not None)
+                want = backward64(z, ez, x, w, t.long(), g, lse, counts, dtype, what is not None, gt == torch.float32)
                 for v, (a, err), ty, name in zip(got, want, (dtype, gt, gt), ("dx", "dw", "db")):
                     assert v.dtype == ty
                     check(v, a, err, ty, f"{name} pad {pad} kept {what is not None} {gt}")
@@ -213,6 +217,8 @@ def test_small_probabilities_in_fp16(M):
     unseen[t] = False
     want = (e.t().contiguous() @ x.double())[unseen]
     assert float((dw[unseen].double() - want).norm() / want.norm()) < 2e-3
+    narrow = M.mdet_xent_backward(g * 4096, x, w, t, lse)[1].double()[unseen] / 4096         # 16-bit results, of a loss that is scaled
+    assert float((narrow - want).norm() / want.norm()) < 2e-3
 
 
 def test_parts(M):
@@ -274,17 +280,18 @@ def test_gradient_against_differences(M, keep):
 
 
 def test_the_workspaces_asked_for_are_enough(M):
-    for dtype in (torch.float16, torch.float32):
-        for m, n, k in ((1, 5, 3), (40, 1000, 33), (7, 300, 64), (64, 64, 8192), (600, 2000, 130)):
+    for dtype, gt in ((torch.float16, torch.float16), (torch.float32, torch.float32), (torch.bfloat16, torch.float32), (torch.float16, torch.float32)):
+        for m, n, k in ((1, 5, 3), (40, 1000, 33), (7, 300, 64), (64, 64, 8192), (600, 2000, 130), (800, 700, 1001)):
             x, w, bias, t, g = operands(m, n, k, dtype, 1)
-            sizes = M.mdet_xent_workspace_query(dtype, m, n, k), M.mdet_xent_kept_query(dtype, m, n, k), M.mdet_xent_workspace_query(dtype, m, n, k, True)
+            sizes = (M.mdet_xent_workspace_query(dtype, m, n, k), M.mdet_xent_kept_query(dtype, m, n, k),
+                     M.mdet_xent_workspace_query(dtype, m, n, k, True, gt))
             a, b, c = (torch.full((s + 4096,), 0xFF, dtype=torch.uint8, device="cuda") for s in sizes)
             loss, lse, _ = M.mdet_xent_forward(x, w, t, bias, workspace=a[:sizes[0]])
             again = M.mdet_xent_forward(x, w, t, bias, keep=b[:sizes[1]])
             assert torch.equal(again[0], loss) and torch.equal(again[1], lse)
             for kept in (None, b[:sizes[1]]):
-                got = M.mdet_xent_backward(g, x, w, t, lse, bias, kept=kept, db=True, workspace=c[:sizes[2]])
-                want = M.mdet_xent_backward(g, x, w, t, lse, bias, kept=kept, db=True)
+                got = M.mdet_xent_backward(g, x, w, t, lse, bias, kept=kept, db=True, grad_dtype=gt, workspace=c[:sizes[2]])
+                want = M.mdet_xent_backward(g, x, w, t, lse, bias, kept=kept, db=True, grad_dtype=gt)
                 assert all(torch.equal(p, q) for p, q in zip(got, want))
             assert all(bool((room[s:] == 0xFF).all()) for room, s in zip((a, b, c), sizes))
 

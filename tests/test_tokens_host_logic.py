@@ -123,7 +123,8 @@ def test_cross_entropy_workspace(M):
             assert all(v % 256 == 0 for v in (forward, kept, back))
             # of 16 words or more a strip: a float pair; each row: a float
             assert forward <= m * ((n + 15) // 16) * 8 + m * 4 + 512
-            assert m * n * size + forward <= kept <= m * (n + 7) * size + forward + 256
+            each = 2 if dtype == BF16 else 4
+            assert m * n * each + forward <= kept <= m * (n + 7) * each + forward + 256
             # never the whole of e: 2^29 elements, or a few thousand words, with their column sums; x; dx and parts in fp32
             piece = min(n, max((1 << 29) // m, 4096))
             assert back <= m * (piece + 264) * size * 1.2 + (m // 16 + 32) * (piece + 256) * 4 + m * (k + 8) * (size + 4) + 4 * 256 * 65536 * 2 + 4096
@@ -133,6 +134,13 @@ def test_cross_entropy_workspace(M):
     assert xent_grad(M, wsb=need - 1) == ENOMEM and xent_grad(M, kept=A, kb=8) == ENOMEM
     assert xent(M, m=0, x=None, t=None) == OK and xent(M, loss=None, lse=None) == OK
     assert xent_grad(M, dx=None, dw=None) == OK
+    # of 16-bit operands, 32 bits of dw take e in two or three parts
+    for dtype, parts in ((F16, 2), (BF16, 3)):
+        one, more = (M.mdet_xent_workspace_query(dtype, 1000, 5000, 64, True, g) for g in (dtype, F32))
+        assert more - one >= (parts - 1) * 1000 * 5000 * 2
+    assert M.mdet_xent_workspace_query(F32, 1000, 5000, 64, True, F32) == M.mdet_xent_workspace_query(F32, 1000, 5000, 64, True)
+    with pytest.raises(M.MemdetError):
+        M.mdet_xent_workspace_query(F16, 1, 1, 1, True, BF16)
     for bad in ((F64, 1, 1, 1), (F32, -1, 1, 1), (F32, 1 << 31, 64, 1)):
         for query in (M.mdet_xent_workspace_query, M.mdet_xent_kept_query):
             with pytest.raises(M.MemdetError):
