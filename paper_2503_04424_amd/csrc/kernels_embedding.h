@@ -74,6 +74,7 @@ __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_kernel(const I* _
   __shared__ int32_t sums[SORT_EACH][SORT_WAVES];
   __shared__ uint32_t list[SORT_ROUND];
   __shared__ uint16_t often[SORT_WAVES][SORT_TOKENS], behind[SORT_TOKENS];
+  __shared__ int32_t all_found;
   const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6;
   const int64_t buckets = gridDim.x;
   const int32_t bucket = blockIdx.x;
@@ -158,29 +159,31 @@ __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_kernel(const I* _
       if (lane == 0) sums[e][wave] = __popcll(hits[e]);
     }
     __syncthreads();
-    // the sums of the 256 parts in front of each, and of all: 64 lanes, four parts each, every wavefront by itself
-    int32_t four[4], upto4 = 0;
+    // the sums of the 256 parts in front of each: four parts a lane of the first wavefront
+    if (wave == 0) {
+      int32_t four[4], upto4 = 0;
 #pragma unroll
-    for (int q = 0; q < 4; ++q) four[q] = (&sums[0][0])[4 * lane + q], upto4 += four[q];
-    const int32_t own = upto4;
+      for (int q = 0; q < 4; ++q) four[q] = (&sums[0][0])[4 * lane + q], upto4 += four[q];
+      const int32_t own = upto4;
 #pragma unroll
-    for (int off = 1; off < 64; off *= 2) {
-      const int32_t o = __shfl_up(upto4, off, 64);
-      if (lane >= off) upto4 += o;
-    }
-    const int32_t found = __shfl(upto4, 63, 64);
-#pragma unroll
-    for (int e = 0; e < SORT_EACH; ++e) {
-      const int part = e * SORT_WAVES + wave;                  // its lane is part / 4
-      int32_t where = __shfl(upto4 - own, part / 4, 64);
-#pragma unroll
-      for (int q = 0; q < 3; ++q) {
-        const int32_t f = __shfl(four[q], part / 4, 64);
-        if (q < part % 4) where += f;
+      for (int off = 1; off < 64; off *= 2) {
+        const int32_t o = __shfl_up(upto4, off, 64);
+        if (lane >= off) upto4 += o;
       }
-      if (hits[e] >> lane & 1)
-        list[where + __popcll(hits[e] & ((1ull << lane) - 1))] = (uint32_t)(e * SORT_THREADS + thread) << 16 | (uint32_t)(id[e] >> bits);
+      int32_t first = upto4 - own;
+#pragma unroll
+      for (int q = 0; q < 4; ++q) {
+        (&sums[0][0])[4 * lane + q] = first;
+        first += four[q];
+      }
+      if (lane == 63) all_found = upto4;
     }
+    __syncthreads();
+    const int32_t found = all_found;
+#pragma unroll
+    for (int e = 0; e < SORT_EACH; ++e)
+      if (hits[e] >> lane & 1)
+        list[sums[e][wave] + __popcll(hits[e] & ((1ull << lane) - 1))] = (uint32_t)(e * SORT_THREADS + thread) << 16 | (uint32_t)(id[e] >> bits);
     const bool few = found <= 64;      // those go out at once
     if (!few)
       for (int t = thread; t < tokens; t += SORT_THREADS)
@@ -251,7 +254,6 @@ __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_kernel(const I* _
 // The sums.  A group of lanes takes RUN sorted tokens and a chunk of columns.  Tokens that begin and end among them are stored; the
 // sum of one that began before (the head) or goes on behind (the tail) goes to the workspace, for the join.
 // ---------------------------------------------------------------------------
-constexpr int RUN = 16;
 
 template <typename T, typename O>
 struct EmbeddingSums {
@@ -261,7 +263,7 @@ struct EmbeddingSums {
   O* g;
   int64_t ldg;
   float* parts;                        // runs x 2 (head, tail) x width
-  int64_t vocab, width, runs;
+  int64_t n, vocab, width, runs;
   float scale;
   bool add;                            // to what g holds
 };
@@ -269,7 +271,7 @@ struct EmbeddingSums {
 // The first `sum_blocks` workgroups sum; the others write zeros where no token is, a step of ZERO_PIECES pieces a lane.  Bytes bound both.
 constexpr int ZERO_PIECES = 4;
 
-template <typename T, typename O>
+template <typename T, typename O, int RUN>
 __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingSums<T, O> a, const RowShare share, const RowShare zeros,
                                                             const int64_t sum_blocks, const int64_t first) {
   typedef typename Core<T>::piece_t piece_t;
@@ -297,15 +299,17 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingSums<
     return;
   }
   const int64_t unit = block * groups + threadIdx.x / share.lanes, run = share.chunks == 1 ? unit : unit / share.chunks;
-  const int32_t total = *a.s.total;
   const int64_t p0 = run * RUN;
+  if (run >= a.runs) return;
+  // A lane's place and id of the run's, and the ids beside it: groups are whole rows of lanes.  Behind the last there is something in memory as
+  // well, which is not looked at.
+  const int64_t own = p0 + lane % RUN < a.n ? p0 + lane % RUN : a.n - 1, behind = p0 + RUN < a.n ? p0 + RUN : a.n - 1;
+  const int32_t place = a.s.place[own], key = a.s.id[own], front = a.s.id[p0 > 0 ? p0 - 1 : 0], back = a.s.id[behind];
+  const int32_t total = *a.s.total;
   if (p0 >= total) return;
+  const int32_t prior = p0 > 0 ? front : -1, later = p0 + RUN < total ? back : -1;
   const int64_t c = ((unit - run * share.chunks) * share.lanes + lane) * VEC;
   const int many = total - p0 < RUN ? (int)(total - p0) : RUN;
-  // a lane's place and id of the sixteen: groups are whole rows of sixteen lanes
-  const int mine = lane % RUN < many ? lane % RUN : many - 1;
-  const int32_t place = a.s.place[p0 + mine], key = a.s.id[p0 + mine];
-  const int32_t prior = p0 > 0 ? a.s.id[p0 - 1] : -1, later = p0 + many < total ? a.s.id[p0 + many] : -1;
   piece_t x[RUN];
 #pragma unroll
   for (int r = 0; r < RUN; ++r) {
@@ -372,7 +376,7 @@ __global__ __launch_bounds__(256) void embedding_sum_kernel(const EmbeddingSums<
 // A token that begins in a run and goes on behind it: its parts, added in one order, eight threads a column.
 constexpr int JOIN_COLS = 128, JOIN_GROUPS = 1024 / JOIN_COLS;
 
-template <typename T, typename O>
+template <typename T, typename O, int RUN>
 __global__ __launch_bounds__(256) void embedding_join_kernel(const EmbeddingSums<T, O> a, const int64_t across, const int64_t first) {
   typedef float f4 __attribute__((ext_vector_type(4)));
   __shared__ f4 part[JOIN_GROUPS][JOIN_COLS / 4];

@@ -101,7 +101,7 @@ def test_gradient(M, n, vocab, width, dtype):
             assert torch.isnan(after[count == 0]).all()
 
 
-@pytest.mark.parametrize("n", [15, 16, 17, 31, 32, 33, 48, 1000, 20000])
+@pytest.mark.parametrize("n", [7, 8, 9, 15, 16, 17, 31, 32, 33, 48, 1000, 20000])
 @pytest.mark.parametrize("kind", ["one token", "in order", "backwards", "two in turn", "none"])
 def test_orders(M, n, kind):
     """Runs of one token over many parts of the sum, each token once, tokens that end where a part ends."""
