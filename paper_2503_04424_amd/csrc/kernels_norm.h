@@ -176,7 +176,8 @@ struct NormBackward {
 
 // Rows strip, strip + strips, ... by a workgroup, each by LANES lanes; the sums over its rows stay in registers, and the next row is on its way
 // while one is summed up.  Bytes bound it: 16384 x 4096 bf16 94 us (4.3 TB/s; without the next row on its way and with two pieces in 256 lanes 98);
-// few rows, the barriers of one behind the other (777 x 1301 fp32 11 us).  Behind a row's end dy counts as zero, and with it everything that is summed.
+// few rows, the barriers of one behind the other (777 x 1301 fp32 11 us).  Behind a row's end dy counts
+// as zero, and with it everything that is summed: x as an element of the row, since from a zero there mean rstd could overflow.
 template <typename T, int THREADS, int LANES, int P>
 __global__ __launch_bounds__(THREADS) void norm_backward_kernel(const NormBackward<T> a) {
   typedef typename Core<T>::piece_t piece_t;
@@ -192,7 +193,7 @@ __global__ __launch_bounds__(THREADS) void norm_backward_kernel(const NormBackwa
 #pragma unroll
     for (int p = 0; p < P; ++p) {
       d1[p] = row_piece<T>(a.dy + row * a.lddy, (p * LANES + lane) * VEC, a.cols);
-      h1[p] = row_piece<T>(a.x + row * a.ldx, (p * LANES + lane) * VEC, a.cols);
+      h1[p] = row_piece_filled<T>(a.x + row * a.ldx, (p * LANES + lane) * VEC, a.cols);
     }
     mean1 = a.mean[row];
     rstd1 = a.rstd[row];
@@ -281,7 +282,7 @@ __global__ __launch_bounds__(1024) void norm_backward_long_kernel(const NormBack
   const float mean = a.mean[row], rstd = a.rstd[row];
   float sum[2] = {0.0f, 0.0f};
   for (int64_t c = (int64_t)threadIdx.x * VEC; c < a.cols; c += 1024 * VEC) {
-    const auto d = row_piece<T>(dy, c, a.cols), h = row_piece<T>(x, c, a.cols);
+    const auto d = row_piece<T>(dy, c, a.cols), h = row_piece_filled<T>(x, c, a.cols);
     typename Core<T>::piece_t w;
     if (a.w) w = row_piece<T>(a.w, c, a.cols);
     float s0 = 0.0f, s1 = 0.0f;

@@ -140,6 +140,19 @@ def test_rows_that_are_constant_or_not_finite(M):
         assert torch.equal(y[i:i + 1], M.mdet_layernorm_forward(x[i:i + 1], eps=1e-5)[0])
 
 
+@pytest.mark.parametrize("dtype,value", [(torch.float32, 1.5 * 2.0 ** 120), (torch.bfloat16, 1.5 * 2.0 ** 120), (torch.float32, -1.25 * 2.0 ** 120)], ids=str)
+@pytest.mark.parametrize("n", [1, 50, 100, 129])
+def test_gradient_of_a_large_constant_row(M, n, dtype, value):
+    """mean rstd is more than fp32 holds, and nothing of it is needed: the row is its mean."""
+    x = torch.full((3, n), value, dtype=dtype, device="cuda")
+    dy = strided(3, n, dtype, gen(n))
+    y, mean, rstd = M.mdet_layernorm_forward(x, eps=1e-6)
+    assert not y.any() and bool((mean == value).all()) and bool(torch.isinf(mean * rstd).all())
+    got = M.mdet_layernorm_backward(dy, x, mean, rstd)
+    for v, (want, err), name in zip(got, backward64(dy, x, mean, rstd, None), ("dx", "dw", "db")):
+        check(v, want, err, dtype, name)
+
+
 def test_sizes_of_zero(M):
     x = torch.randn(4, 8, device="cuda")
     y, mean, rstd = M.mdet_layernorm_forward(x[:, :0], eps=0.25)
