@@ -665,7 +665,7 @@ int mdet_ntk_workspace_query(int32_t dtype, int32_t out_dtype, int64_t n, int64_
 int mdet_embedding_workspace_query(int64_t n, int64_t vocab, int64_t width, uint64_t* bytes);
 
 /* y_i = scale table[ids_i]: table is vocab x width, y n x width, both of dtype (MDET_F32, MDET_F16 or MDET_BF16).  An id outside of
- * the table gives a row of zeros.  n is below 2^31 - 1024, vocab below 2^31. */
+ * the table gives a row of zeros.  n is below 2^31 - 1025, vocab below 2^31. */
 int mdet_embedding_forward(int32_t dtype, int32_t index_bits, int64_t n, int64_t vocab, int64_t width, const void* ids,
                            const void* table, int64_t ldt, double scale, void* y, int64_t ldy, void* stream);
 
@@ -706,6 +706,11 @@ int mdet_xent_kept_query(int32_t dtype, int64_t m, int64_t n, int64_t k, uint64_
 int mdet_xent_forward(int32_t dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const void* x, int64_t ldx, const void* w,
                       int64_t ldw, const void* bias, const void* target, int64_t ignore, float* loss, float* lse, void* kept,
                       uint64_t kept_bytes, void* workspace, uint64_t workspace_bytes, void* stream);
+
+/* out = the sum of the losses of the rows that count, or with mean != 0 that divided by their number (NaN if none does); weights (m floats, or
+ * NULL): what out's gradient by each of the losses is, the `dloss` below: 1, or 1 / their number, and 0 for a row that does not count. */
+int mdet_xent_reduce(int32_t index_bits, int64_t m, int64_t n, const float* loss, const void* target, int64_t ignore, int32_t mean,
+                     float* out, float* weights, void* stream);
 
 /* Gradient of sum over i of dloss_i loss_i, from the forward call's lse, and what it kept (NULL: z is formed once more): with
  * e_ij = dloss_i (exp(z_ij - lse_i) - [j = t_i]),  dx = e w,  dw = e^T x,  db = column sums of e; any of dx, dw, db may be NULL (not

@@ -17,7 +17,7 @@ from .binding import (  # noqa: F401
     mdet_ntk_gram, mdet_ntk_workspace_query,
     mdet_embedding_workspace_query, mdet_embedding_forward, mdet_embedding_backward,
     mdet_layernorm_workspace_query, mdet_layernorm_forward, mdet_layernorm_backward,
-    mdet_xent_workspace_query, mdet_xent_kept_query, mdet_xent_forward, mdet_xent_backward,
+    mdet_xent_workspace_query, mdet_xent_kept_query, mdet_xent_forward, mdet_xent_reduce, mdet_xent_backward,
     mdet_step_copy, mdet_step_mfma_peak, mdet_logdet_device_noalloc,
     pack_lower_block_columns, pack_general_block_columns,
 )

@@ -260,26 +260,30 @@ def _layer_norm_function():
 
 
 def _cross_entropy_function():
-    """The autograd node of ``linear_cross_entropy``: the rows' losses."""
+    """The autograd node of ``linear_cross_entropy``."""
     import torch
 
     class CrossEntropyFunction(torch.autograd.Function):
         @staticmethod
-        def forward(ctx, x, w, bias, target, ignore, keep):
+        def forward(ctx, x, w, bias, target, ignore, reduction, keep):
             rows, mat = _rows(_as_rows(x)), _rows(w)
             bias = None if bias is None else bias.contiguous()
             loss, lse, kept = B.mdet_xent_forward(rows, mat, target, bias, ignore, keep=keep)
-            ctx.save_for_backward(rows, mat, bias, target, lse, kept)
+            weights = None
+            if reduction != "none":
+                loss, weights = B.mdet_xent_reduce(loss, target, mat.shape[0], ignore, reduction == "mean")
+            ctx.save_for_backward(rows, mat, bias, target, lse, kept, weights)
             ctx.shape, ctx.ignore = x.shape, ignore
             return loss
 
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, dloss):
-            x, w, bias, target, lse, kept = ctx.saved_tensors
+            x, w, bias, target, lse, kept, weights = ctx.saved_tensors
+            dloss = dloss.contiguous() if weights is None else weights * dloss
             need_x, need_w, need_b = ctx.needs_input_grad[:3]
-            dx, dw, db = B.mdet_xent_backward(dloss.contiguous(), x, w, target, lse, bias, ctx.ignore, kept, dx=need_x, dw=need_w, db=need_b)
-            return None if dx is None else dx.view(ctx.shape), dw, db, None, None, None
+            dx, dw, db = B.mdet_xent_backward(dloss, x, w, target, lse, bias, ctx.ignore, kept, dx=need_x, dw=need_w, db=need_b)
+            return None if dx is None else dx.view(ctx.shape), dw, db, None, None, None, None
 
     return CrossEntropyFunction
 
@@ -328,15 +332,13 @@ def linear_cross_entropy(x, w, target, bias=None, ignore_index=-100, reduction="
         raise ValueError("reduction must be 'mean', 'sum' or 'none'")
     import torch
     flat = target.reshape(-1).contiguous()
-    if not torch.is_grad_enabled():
-        loss = B.mdet_xent_forward(_rows(_as_rows(x)), _rows(w), flat, None if bias is None else bias.contiguous(), ignore_index, lse=False)[0]
+    if torch.is_grad_enabled():
+        loss = _function(_cross_entropy_function).apply(x, w, bias, flat, ignore_index, reduction, keep)
     else:
-        loss = _function(_cross_entropy_function).apply(x, w, bias, flat, ignore_index, keep)
-    if reduction == "none":
-        return loss.view(target.shape)
-    if reduction == "sum":
-        return loss.sum()
-    return loss.sum() / ((flat >= 0) & (flat < w.shape[0]) & (flat != ignore_index)).sum()
+        loss = B.mdet_xent_forward(_rows(_as_rows(x)), _rows(w), flat, None if bias is None else bias.contiguous(), ignore_index, lse=False)[0]
+        if reduction != "none":
+            loss = B.mdet_xent_reduce(loss, flat, w.shape[0], ignore_index, reduction == "mean", weights=False)[0]
+    return loss.view(target.shape) if reduction == "none" else loss
 
 
 class AdamW:

@@ -109,7 +109,7 @@ EXPORTS = [
     "mdet_adamw_step", "mdet_ntk_gram", "mdet_ntk_workspace_query",
     "mdet_embedding_workspace_query", "mdet_embedding_forward", "mdet_embedding_backward",
     "mdet_layernorm_workspace_query", "mdet_layernorm_forward", "mdet_layernorm_backward",
-    "mdet_xent_workspace_query", "mdet_xent_kept_query", "mdet_xent_forward", "mdet_xent_backward",
+    "mdet_xent_workspace_query", "mdet_xent_kept_query", "mdet_xent_forward", "mdet_xent_reduce", "mdet_xent_backward",
 ]
 
 _lib = None
@@ -170,6 +170,7 @@ def load():
     L.mdet_xent_workspace_query.argtypes = [i32, i32, i32, i64, i64, i64, C.POINTER(u64)]
     L.mdet_xent_kept_query.argtypes = [i32, i64, i64, i64, C.POINTER(u64)]
     L.mdet_xent_forward.argtypes = [i32, i32, i64, i64, i64, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, u64, vp, u64, vp]
+    L.mdet_xent_reduce.argtypes = [i32, i64, i64, vp, vp, i64, i32, vp, vp, vp]
     L.mdet_xent_backward.argtypes = [i32, i32, i32, i64, i64, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, u64, vp, i64, vp, i64,
                                      vp, vp, u64, vp]
     L.mdet_strerror.argtypes = [C.c_int]
@@ -1158,6 +1159,33 @@ def mdet_xent_forward(x, w, target, bias=None, ignore=-100, loss=True, lse=True,
     if given:
         _written(*given)
     return loss, lse, kept
+
+
+def mdet_xent_reduce(loss, target, vocab, ignore=-100, mean=True, out=True, weights=True, stream=None):
+    """The mean over the rows that count of ``mdet_xent_forward``'s loss, or with ``mean`` false their sum (asynchronous): NaN for the mean of no
+    rows.  weights: the ``dloss`` that this makes of a gradient of 1, zero for rows that do not count.  out (one float32; a new one has no axes)
+    and weights (m,): True for a new tensor, False or None for no weights, or the tensor to write.  Returns out, weights."""
+    if not _FLOAT:
+        _torch_types()
+    if loss.dim() != 1:
+        raise ValueError("loss: a vector expected")
+    m, vocab = loss.shape[0], int(vocab)
+    gpu = _gpu(loss, "loss")
+    lp = _vector(loss, "loss", m, _FLOAT[0], gpu)
+    tp, bits = _indices(target, "target", m, gpu)
+    given = _given(out, weights)
+    if out is True:
+        out = _fresh(loss, (), _FLOAT[0], stream)
+        op = out.data_ptr()
+    elif out is None or out is False:
+        raise ValueError("out: True, or a tensor expected")
+    else:
+        op = _vector(out if out.dim() else out.view(1), "out", 1, _FLOAT[0], gpu)
+    weights, wp = _vector_result(weights, "weights", m, _FLOAT[0], gpu, loss, stream)
+    _queue(gpu, load().mdet_xent_reduce, bits, m, vocab, lp, tp, ignore, int(bool(mean)), op, wp, _operator_stream(stream, gpu))
+    if given:
+        _written(*given)
+    return out, weights
 
 
 def mdet_xent_backward(dloss, x, w, target, lse, bias=None, ignore=-100, kept=None, dx=True, dw=True, db=None, grad_dtype=None,

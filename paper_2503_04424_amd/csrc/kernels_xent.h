@@ -41,19 +41,11 @@ __device__ __forceinline__ int64_t xent_said(const XentTargets& t, const int64_t
 
 __device__ __forceinline__ int64_t xent_target(const XentTargets& t, const int64_t i) { return xent_said(t, xent_raw(t, i)); }
 
-// exp(z - top), from the difference: 2^-23 of its size is what the result is off by.  Zero for z = -inf also where top is.
-__device__ __forceinline__ float xent_exp(const float z, const float top) { return __expf(z - (top == -INFINITY ? 0.0f : top)); }
-
-// exp(z - top) as a power of two, xent_power(z, xent_from(top)): one multiplication and addition in front of it.  With |z| and |top| below 30
-// their rounding is 2e-6 of a term, and far less of the sum of many, which is all that leaves the forward pass in more than 16 bits (fp32:
-// from the difference).  Where top is the largest of some z that are all -inf, the powers are zero.
-constexpr float XENT_LOG2E = 1.44269504088896341f;
-__device__ __forceinline__ float xent_from(const float top) { return top == -INFINITY ? 0.0f : -XENT_LOG2E * top; }
-template <typename T>
-__device__ __forceinline__ float xent_power(const float z, const float from, const float top) {
-  if constexpr (sizeof(T) == 4) return xent_exp(z, top);
-  else return __builtin_amdgcn_exp2f(fmaf(z, XENT_LOG2E, from));
-}
+// exp(z - top) is __expf(z - xent_from(top)), from the difference: 2^-23 of its size is what the result is off by, however large both are (the
+// product of each with log2(e) apart, one multiplication and addition, would round to more than 2^128 from logits of 1e10 on).  Zero for
+// z = -inf, also where top is the largest of some z that are all -inf.
+__device__ __forceinline__ float xent_from(const float top) { return top == -INFINITY ? 0.0f : top; }
+__device__ __forceinline__ float xent_exp(const float z, const float top) { return __expf(z - xent_from(top)); }
 
 // What is kept of exp(z - top): numbers up to 1, to 11 bits for operands in bf16 (fewer would add to what rounding e costs), to 24 otherwise.
 template <typename T> struct XentKept { typedef float type; };
@@ -272,7 +264,7 @@ __global__ __launch_bounds__(S::THREADS) void xent_forward_kernel(const Operand<
       for (int a = 0; a < S::TN; ++a)
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-          acc[a][b][e] = xent_power<T>(acc[a][b][e], from, top);
+          acc[a][b][e] = __expf(acc[a][b][e] - from);
           sum += acc[a][b][e];
         }
       sum = xent_across(sum, [](const float p, const float q) { return p + q; });
@@ -360,7 +352,7 @@ __global__ __launch_bounds__(64 * XENT_WAVES) void xent_forward_rows_kernel(cons
   const float from = xent_from(top);
 #pragma unroll
   for (int e = 0; e < 4; ++e) {
-    z[e] = xent_power<T>(z[e], from, top);
+    z[e] = __expf(z[e] - from);
     total += z[e];
   }
   total += __shfl_xor(total, 16, 64);
@@ -402,6 +394,47 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_join_kernel(co
     if (lse) lse[row] = l;
     if (loss) loss[row] = xent_target(t, row) >= 0 ? l - picked[row] : 0.0f;
   }
+}
+
+// The sum or mean of the losses of the rows that count, and what each of them has of it.  One workgroup, whose loads bound it: 4096 rows 4 us, 8192
+// 6.5, a million 590, beside products of milliseconds.
+__global__ __launch_bounds__(1024) void xent_reduce_kernel(const float* __restrict__ loss, const XentTargets t, const int64_t rows, const bool mean,
+                                                           float* __restrict__ out, float* __restrict__ weights) {
+  constexpr int EACH = 4;
+  __shared__ float sums[16];
+  __shared__ int counts[16];
+  float sum = 0.0f;
+  int count = 0;
+  for (int64_t i0 = threadIdx.x; i0 < rows; i0 += 1024 * EACH) {
+    int64_t raw[EACH];
+    float v[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int64_t i = i0 + 1024 * e;
+      raw[e] = xent_raw(t, i < rows ? i : rows - 1);
+      v[e] = i < rows ? loss[i] : 0.0f;
+    }
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+      if (i0 + 1024 * e < rows && xent_said(t, raw[e]) >= 0) {
+        sum += v[e];
+        ++count;
+      }
+  }
+#pragma unroll
+  for (int off = 1; off < 64; off *= 2) {
+    sum += __shfl_xor(sum, off, 64);
+    count += __shfl_xor(count, off, 64);
+  }
+  if ((threadIdx.x & 63) == 0) sums[threadIdx.x >> 6] = sum, counts[threadIdx.x >> 6] = count;
+  __syncthreads();
+  sum = sums[0], count = counts[0];
+#pragma unroll
+  for (int w = 1; w < 16; ++w) sum += sums[w], count += counts[w];
+  if (threadIdx.x == 0) *out = mean ? sum / (float)count : sum;
+  if (!weights) return;
+  const float weight = mean ? 1.0f / (float)count : 1.0f;
+  for (int64_t i = threadIdx.x; i < rows; i += 1024) weights[i] = xent_target(t, i) >= 0 ? weight : 0.0f;
 }
 
 // ---------------------------------------------------------------------------
@@ -456,7 +489,8 @@ struct XentSlope {
   int64_t rows, cols, first;           // of the piece
 };
 
-// What a row needs for its e: its weight (zero if it does not count), its target, counted from column `from` on.
+// What a row needs for its e: its weight (zero if it does not count; NaN where lse is no number, as all of its e), its target, counted from column
+// `from` on.
 struct XentRow {
   float lse, g;
   bool counts;
@@ -468,7 +502,8 @@ __device__ __forceinline__ XentRow xent_row(const XentSlope<T>& o, const int64_t
   if (i >= o.rows) return r;
   const int64_t t = xent_target(o.t, i);
   if (t < 0) return r;
-  return XentRow{o.lse[i], o.g[i], true, t - o.first - from};
+  const float lse = o.lse[i];
+  return XentRow{lse, o.g[i] + (lse - lse), true, t - o.first - from};
 }
 
 // Tiles of e.  PARTS: numbers of type T that add up to an element of it.  As the forward pass's (4096 x 1024 over 50003 words bf16 440 to 490 us).
@@ -509,10 +544,11 @@ __global__ __launch_bounds__(S::THREADS) void xent_slope_kernel(const Operand<T>
 #pragma unroll
     for (int b = 0; b < S::TM; ++b) {
       const float weight = g[b] * up;
+      // no logit is above lse, but for sums in another order than the forward pass's, which at 1e10 may differ by a thousand
 #pragma unroll
       for (int a = 0; a < S::TN; ++a)
 #pragma unroll
-        for (int e = 0; e < 4; ++e) acc[a][b][e] = __expf(acc[a][b][e] - lse[b]);
+        for (int e = 0; e < 4; ++e) acc[a][b][e] = __expf(fminf(acc[a][b][e] - lse[b], 0.0f));
       if (__any(at[b] >= 0)) {
 #pragma unroll
         for (int a = 0; a < S::TN; ++a)
@@ -599,8 +635,8 @@ __global__ __launch_bounds__(256) void xent_slope_kept_kernel(const XentSlope<T>
 #pragma unroll
   for (int r = 0; r < XENT_EACH; ++r) {
     const int64_t i = row + 16 * r;
-    // the strip may hold nothing but -inf, beside a row's finite logits
-    const float share = top[r] == -INFINITY ? __expf(-of[r].lse) : __expf(top[r] - of[r].lse);
+    // of a strip of nothing but -inf, whose exponentials are zero, beside finite logits of any size
+    const float share = top[r] == -INFINITY ? 1.0f : __expf(top[r] - of[r].lse);
     piece_t d;
 #pragma unroll
     for (int e = 0; e < VEC; ++e) {

@@ -281,6 +281,15 @@ int mdet_xent_forward(int32_t dtype, int32_t index_bits, int64_t m, int64_t n, i
   return dtype == MDET_F32 ? call(0.0f) : dtype == MDET_BF16 ? call((__bf16)0.0f) : call((_Float16)0.0f);
 }
 
+int mdet_xent_reduce(int32_t index_bits, int64_t m, int64_t n, const float* loss, const void* target, int64_t ignore, int32_t mean, float* out,
+                     float* weights, void* stream) {
+  if (!is_index(index_bits) || !xent_fits(m, n, 1) || !vector_ok(loss, m, 4) || !vector_ok(target, m, index_bits / 8)) return MDET_EINVAL;
+  if (!vector_ok(out, 1, 4) || (uintptr_t)weights % 4) return MDET_EINVAL;
+  hipLaunchKernelGGL(xent_reduce_kernel, dim3(1), dim3(1024), 0, (hipStream_t)stream, loss, XentTargets{target, index_bits, ignore, n}, m, mean != 0, out,
+                     weights);
+  return launch_status();
+}
+
 int mdet_xent_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const float* dloss, const void* x,
                        int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* target, int64_t ignore, const float* lse,
                        const void* kept, uint64_t kept_bytes, void* dx, int64_t lddx, void* dw, int64_t lddw, void* db, void* workspace,

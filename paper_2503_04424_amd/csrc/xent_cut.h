@@ -28,7 +28,8 @@ struct XentLayout {
 };
 inline XentLayout xent_layout(int64_t m, int64_t n, int64_t k, int64_t size, int64_t kept_size) {
   XentLayout l;
-  l.cut = m <= 16 && n <= (int64_t(1) << 28) ? Cut{0, 1, k} : cut_of(m, n, k, size, false);
+  // a workgroup of 256 threads for 16 columns or more, fewer than 2^32 of all
+  l.cut = m <= 16 && n <= (int64_t(1) << 27) ? Cut{0, 1, k} : cut_of(m, n, k, size, false);
   // a wavefront's columns of a tile
   l.strip = l.cut.tile == 256 ? 64 : l.cut.tile == 128 ? 64 : l.cut.tile == 64 ? 32 : 16;
   l.across = ceil_div(n, l.strip);

@@ -33,6 +33,8 @@ static bool holds(int64_t m, int64_t n, int64_t k, int64_t size, int64_t parts) 
   HOLDS(f.across * f.strip >= n && (f.across - 1) * f.strip < n && f.ldexps >= n && f.ldexps % 8 == 0);
   // a wavefront's columns: four of them beside each other in the largest tile, two in the others, one strip of 16 a wavefront for few rows
   HOLDS(f.cut.tile == 256 ? f.strip == 64 : f.cut.tile ? f.strip * 2 == f.cut.tile : f.strip == 16 && m <= 16);
+  // a launch is of fewer than 2^32 threads: a workgroup of 256 for 16 columns or more
+  HOLDS(f.cut.tile != 0 || ceil_div(n, 16) * 256 < (int64_t(1) << 32));
   const XentGradLayout g = xent_grad_layout(m, n, k, size, parts);
   HOLDS(g.piece >= 1 && g.piece <= n && (g.piece == n || g.piece % 256 == 0) && g.lde >= g.piece && g.lde % 8 == 0 && g.ldrows >= k);
   HOLDS(g.piece == n || parts * m * g.piece <= (int64_t(1) << 29) || g.piece <= 4096);
@@ -53,7 +55,18 @@ static bool holds(int64_t m, int64_t n, int64_t k, int64_t size, int64_t parts) 
   return true;
 }
 
+// A vocabulary of 2^28 words, and a few more or less, for one row and for sixteen.
+static bool launches_hold() {
+  for (int64_t m = 1; m <= 16; m += 15)
+    for (int64_t n = (int64_t(1) << 27) - 1; n < (int64_t(1) << 28) + 64; n = n < (int64_t(1) << 27) + 2 || n >= (int64_t(1) << 28) - 64 ? n + 1 : (int64_t(1) << 28) - 64) {
+      const int64_t k = 1, size = 2;
+      HOLDS(xent_layout(m, n, k, size, size).cut.tile != 0 || ceil_div(n, 16) * 256 < (int64_t(1) << 32));
+    }
+  return true;
+}
+
 int main() {
+  if (!launches_hold()) return 1;
   const int64_t sizes[] = {1, 2, 15, 16, 17, 33, 64, 65, 100, 127, 129, 255, 256, 257, 300, 512, 777, 1000, 1024, 1500, 2048, 4096, 5003, 8192, 9000, 16384, 32000,
                            50003, 65536, 131072, 140000, 1000000};
   for (const int64_t m : sizes)

@@ -200,6 +200,79 @@ def test_masked_vocabulary(M):
     assert bool((lse == float("-inf")).all()) and torch.isnan(loss).all()
 
 
+@pytest.mark.parametrize("dtype,up", [(torch.float32, 60), (torch.float16, 15), (torch.bfloat16, 60)], ids=str)
+def test_logits_far_beyond_the_exponential(M, dtype, up):
+    """One word's logit is 2^(2 up), all the others' half of that or less: every number of the result is exact, in both directions."""
+    n, k, best = 700, 8, 333
+    for m in (3, 7, 14, 40, 300):
+        x, w = torch.zeros(m, k, dtype=dtype, device="cuda"), torch.zeros(n, k, dtype=dtype, device="cuda")
+        x[:, 2] = 2.0 ** up
+        w[:, 2] = 2.0 ** (up - 1) * (torch.arange(n, device="cuda") % 3 - 1)
+        w[best, 2] = 2.0 ** up
+        t = torch.arange(m, device="cuda") % n
+        t[0] = best
+        g = torch.full((m,), 2.0 ** -9, device="cuda")
+        z = x.double() @ w.double().t()
+        e = -torch.eye(n, dtype=torch.float64, device="cuda")[t]
+        e[:, best] += 1
+        e *= 2.0 ** -9
+        for keep in (False, True):
+            loss, lse, kept = M.mdet_xent_forward(x, w, t, keep=keep)
+            assert torch.equal(lse.double(), z[:, best]) and torch.equal(loss.double(), (z[:, best:best + 1] - z.gather(1, t[:, None]))[:, 0])
+            dx, dw, db = M.mdet_xent_backward(g, x, w, t, lse, kept=kept, db=True)
+            for got, want in zip((dx, dw, db), (e @ w.double(), e.t() @ x.double(), e.sum(0))):
+                assert torch.equal(got, want.to(dtype))
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("m", [8, 40, 300])
+def test_masked_words_beside_small_logits(M, m, dtype):
+    """Whole strips of -inf where all of the other logits lie so low that the exponential of -lse is infinite."""
+    n, k = 700, 48
+    x, w, bias, t, g = operands(m, n, k, dtype, 6)
+    bias -= 300
+    bias[128:512] = float("-inf")
+    t = torch.where((t >= 128) & (t < 512), 5, t)
+    live = torch.cat((torch.arange(128), torch.arange(512, n))).cuda()
+    place = torch.full((n,), -1, device="cuda")
+    place[live] = torch.arange(len(live), device="cuda")
+    u = torch.where((t >= 0) & (t < n), place[t.clamp(0, n - 1)], -1)    # the same rows over the words that are left
+    z, ez = logits64(x, w[live], bias[live])
+    (wl, el), (ws, es), counts = forward64(z, ez, u, len(live))
+    for keep in (False, True):
+        loss, lse, kept = M.mdet_xent_forward(x, w, t, bias, keep=keep)
+        check(lse, ws, es, torch.float32)
+        check(loss, wl, el, torch.float32)
+        dx, dw, db = M.mdet_xent_backward(g, x, w, t, lse, bias, kept=kept, db=True)
+        assert not dw[128:512].any() and not db[128:512].any()
+        want = backward64(z, ez, x, w[live], u, g, lse, counts, dtype, keep)
+        for v, (a, err), name in zip((dx, dw[live], db[live]), want, ("dx", "dw", "db")):
+            check(v, a, err, dtype, f"{name} kept {keep}")
+
+
+@pytest.mark.parametrize("m", [0, 1, 63, 1024, 4097, 20000])
+@pytest.mark.parametrize("index", [torch.int32, torch.int64])
+def test_reduction(M, m, index):
+    loss = torch.rand(m, generator=gen(m + 1), device="cuda") * 10
+    t = torch.randint(-2, 12, (m,), generator=gen(m), device="cuda", dtype=index)
+    counts = (t >= 0) & (t < 10) & (t != 7)
+    loss[~counts] = float("nan")                                         # is not looked at
+    number, total = int(counts.sum()), float(loss[counts].double().sum())
+    for mean in (True, False):
+        out, weights = M.mdet_xent_reduce(loss, t, 10, 7, mean=mean)
+        assert out.shape == () and weights.shape == (m,) and not weights[~counts].any()
+        if number == 0:
+            assert torch.isnan(out) if mean else not out.any()
+            continue
+        want, weight = (total / number, torch.tensor(1 / number, dtype=torch.float32)) if mean else (total, torch.tensor(1.0))
+        # a thread's m / 1024 terms and a tree of ten, all of one sign, and the quotient
+        assert abs(float(out) - want) <= (m / 1024 + 12) * EPS32 * want
+        assert bool((weights[counts] == weight.cuda()).all())
+        held = torch.empty(1, device="cuda")
+        again, none = M.mdet_xent_reduce(loss, t, 10, 7, mean=mean, out=held, weights=False)
+        assert again is held and none is None and torch.equal(held[0], out)
+
+
 def test_small_probabilities_in_fp16(M):
     """A probability of 1e-8 and a weight of 1 / 4096 are far below fp16's least number: the gradients of the many words nobody expects
     add up to as much as that of the one that came."""
@@ -347,3 +420,32 @@ def test_front_end(M, dtype):
                 check(v, a, err, dtype, f"{name} {reduction} {keep}")
     with torch.no_grad():
         assert torch.equal(M.linear_cross_entropy(x.view(5, 6, 40), w, t, bias), M.linear_cross_entropy(x.view(5, 6, 40), w, t, bias).detach())
+
+
+@pytest.mark.parametrize("reduction", ["mean", "sum", "none"])
+def test_front_end_in_a_graph(M, reduction):
+    """Both passes in a graph, replayed between eager ones: so many rows that a reduction over all of them takes more than one workgroup."""
+    m, n, k = 20000, 130, 16
+    x, w, bias, t, _ = operands(m, n, k, torch.bfloat16, 1)
+    held = [v.contiguous() for v in (x, w, bias)] + [t]
+
+    def step():
+        leaves = [v.detach().requires_grad_() for v in held[:3]]
+        loss = M.linear_cross_entropy(leaves[0], leaves[1], held[3], leaves[2], reduction=reduction)
+        return (loss.detach(), *torch.autograd.grad(loss, leaves, torch.ones_like(loss)))
+    side = torch.cuda.Stream()
+    side.wait_stream(torch.cuda.current_stream())
+    with torch.cuda.stream(side):
+        step()
+    torch.cuda.current_stream().wait_stream(side)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        got = step()
+    for turn in range(4):
+        new = operands(m, n, k, torch.bfloat16, 10 + turn)
+        for v, u in zip(held, new):
+            v.copy_(u)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(p, q) for p, q in zip(got, step()))
+        torch.cuda.synchronize()

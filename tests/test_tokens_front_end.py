@@ -58,8 +58,15 @@ def calls(monkeypatch):
         e[torch.nonzero(c)[:, 0], target[c].long()] -= 1
         e = e * torch.where(c, dloss, 0.0)[:, None]
         return e @ w if dx else None, e.t() @ x if dw else None, e.sum(0) if db else None
+
+    def reduce(loss, target, vocab, ignore=-100, mean=True, out=True, weights=True, stream=None):
+        fits(vectors=(loss, target))
+        c = counted(target, vocab, ignore)
+        weight = 1 / c.sum().double() if mean else torch.ones(())
+        total = loss[c].sum()
+        return total / c.sum() if mean else total, c * weight.to(loss.dtype) if weights else None
     for name, f in dict(mdet_embedding_forward=embed, mdet_embedding_backward=embed_grad, mdet_layernorm_forward=norm, mdet_layernorm_backward=norm_grad,
-                        mdet_xent_forward=xent, mdet_xent_backward=xent_grad).items():
+                        mdet_xent_forward=xent, mdet_xent_reduce=reduce, mdet_xent_backward=xent_grad).items():
         monkeypatch.setattr(M.binding, name, f)
     return seen
 

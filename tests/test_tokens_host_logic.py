@@ -99,6 +99,16 @@ def xent_grad(M, dtype=F32, gt=F32, bits=64, m=4, n=10, k=8, g=A, x=A, ldx=8, w=
     return M.lib().mdet_xent_backward(dtype, gt, bits, m, n, k, g, x, ldx, w, ldw, b, t, ignore, lse, kept, kb, dx, lddx, dw, lddw, db, ws, wsb, None)
 
 
+def reduce(M, bits=64, m=4, n=10, loss=A, t=A, mean=1, out=A, weights=A):
+    return M.lib().mdet_xent_reduce(bits, m, n, loss, t, -100, mean, out, weights, None)
+
+
+@pytest.mark.parametrize("bad", [dict(bits=8), dict(m=-1), dict(n=-1), dict(m=1 << 41), dict(loss=None), dict(loss=A + 2), dict(t=None), dict(t=A + 4),
+                                 dict(out=None), dict(out=A + 1), dict(weights=A + 2)])
+def test_reduction_refuses(M, bad):
+    assert reduce(M, **bad) == EINVAL
+
+
 SIZES = [dict(m=-1), dict(n=-1), dict(k=-1), dict(m=1 << 41), dict(m=(1 << 31) - 32, n=64), dict(n=(1 << 31) - 32, k=64, ldx=64, ldw=64)]
 
 

@@ -59,6 +59,11 @@ def xent(gpus=(0,) * 7, ws=None):
     return M.mdet_xent_forward(x, w, t, b, loss=loss, lse=lse, keep=kept, workspace=ws, stream=0)
 
 
+def reduce(gpus=(0,) * 4):
+    loss, t, out, weights = (on(g, *s, dtype=d) for g, s, d in zip(gpus, ((4,), (4,), (1,), (4,)), (F, I, F, F)))
+    return M.mdet_xent_reduce(loss, t, 10, out=out, weights=weights, stream=0)
+
+
 def xent_grad(gpus=(0,) * 10, ws=None):
     shapes = ((4,), (4, 8), (10, 8), (4,), (4,), (10,), (4096,), (4, 8), (10, 8), (10,))
     types = (F, F, F, I, F, F, torch.uint8, F, F, F)
@@ -67,7 +72,7 @@ def xent_grad(gpus=(0,) * 10, ws=None):
 
 
 CALLS = {"mdet_embedding_forward": (embed, 3), "mdet_embedding_backward": (embed_grad, 3), "mdet_layernorm_forward": (norm, 6),
-         "mdet_layernorm_backward": (norm_grad, 8), "mdet_xent_forward": (xent, 7), "mdet_xent_backward": (xent_grad, 10)}
+         "mdet_layernorm_backward": (norm_grad, 8), "mdet_xent_forward": (xent, 7), "mdet_xent_reduce": (reduce, 4), "mdet_xent_backward": (xent_grad, 10)}
 WITH_ROOM = [n for n in CALLS if n.endswith("_backward") or n == "mdet_xent_forward"]
 
 
@@ -145,6 +150,8 @@ def test_what_a_call_writes_counts_as_changed(library):
     assert changed(lambda: M.mdet_layernorm_forward(x, w, b, out=y, mean=False, rstd=None, stream=0)) == {"y"}
     assert changed(lambda: M.mdet_layernorm_backward(x, x, m, r, w, y, nw, nb, stream=0)) == {"y", "nw", "nb"}
     assert changed(lambda: M.mdet_xent_forward(x, table, t, bias, loss=m, lse=r, keep=kept, stream=0)) == {"m", "r", "kept"}
+    assert changed(lambda: M.mdet_xent_reduce(m, t, 10, out=r[:1], weights=r, stream=0)) == {"r"}
+    assert changed(lambda: M.mdet_xent_reduce(m, t, 10, weights=r, stream=0)) == {"r"}
     assert changed(lambda: M.mdet_xent_backward(m, x, table, t, r, bias, kept=kept, dx=y, dw=dw, db=db, stream=0)) == {"y", "dw", "db"}
     assert changed(lambda: M.mdet_xent_backward(m, x, table, t, r, bias, dx=False, dw=dw, stream=0)) == {"dw"}
 
@@ -170,7 +177,9 @@ def test_what_is_refused(library):
              lambda: M.mdet_xent_forward(x, table, t, loss=on(0, 5), stream=0), lambda: M.mdet_xent_forward(x, table, t, keep=torch.zeros(8), stream=0),
              lambda: M.mdet_xent_forward(x.double(), table.double(), t, stream=0), lambda: M.mdet_xent_backward(t, x, table, t, m, stream=0),
              lambda: M.mdet_xent_backward(m, x, table, t, on(0, 4, dtype=torch.bfloat16), stream=0), lambda: M.mdet_xent_backward(m, x, table, t, m, dx=on(0, 8, 4).t(), stream=0),
-             lambda: M.mdet_xent_backward(m, x, table, t, m, db=on(0, 10, dtype=torch.bfloat16), stream=0)]
+             lambda: M.mdet_xent_backward(m, x, table, t, m, db=on(0, 10, dtype=torch.bfloat16), stream=0), lambda: M.mdet_xent_reduce(x, t, 10, stream=0),
+             lambda: M.mdet_xent_reduce(m, m, 10, stream=0), lambda: M.mdet_xent_reduce(m, t[:3], 10, stream=0), lambda: M.mdet_xent_reduce(m, t, 10, out=None, stream=0),
+             lambda: M.mdet_xent_reduce(m, t, 10, out=on(0, 4), stream=0), lambda: M.mdet_xent_reduce(m, t, 10, weights=on(0, 5), stream=0)]
     for call in calls:
         with pytest.raises(ValueError):
             call()
