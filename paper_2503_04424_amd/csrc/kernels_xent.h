@@ -269,7 +269,7 @@ __global__ __launch_bounds__(S::THREADS) void xent_forward_kernel(const Operand<
         }
       sum = xent_across(sum, [](const float p, const float q) { return p + q; });
       if (lane < 16 && i < o.rows && strip < o.across) o.strips[i * o.across + strip] = XentStrip{top, sum};
-      // rows are ceil(cols / 8) 8 long: what is written behind their end is zero
+      // rows are ceil(cols / 8) 8 long or more: what is written behind their end is zero
       if (o.exps)
         xent_store<K, S::TN>(o.exps + i * o.ldexps, col0, o.cols, i < o.rows, [&](const int a) {
           return k4{(K)acc[a][b][0], (K)acc[a][b][1], (K)acc[a][b][2], (K)acc[a][b][3]};

@@ -8,11 +8,13 @@ constexpr int64_t XENT_COPY = 768, XENT_COPY_GRAD = 512;
 
 inline uint64_t xent_up256(uint64_t x) { return (x + 255) / 256 * 256; }
 
+// Elements from row to row of what the library lays out itself: whole pieces of 16 bytes, and lines of 128 where rows are long: a slab's 128 bytes
+// would lie in two of them (4096 rows of e over 50003 words: dx 408 us and 357, e from what was kept 203 and 164).
+inline int64_t xent_pad(int64_t k) { return k >= 1024 ? ceil_div(k, 64) * 64 : ceil_div(k, 8) * 8; }
 // Rows of x and W in 16 bits that are no whole pieces of 16 bytes long go through registers, which halves the rate of a product of large tiles.
-// From these many rows of x on they are copied first, at that distance, with zeros behind them.  us without and with copies, 32003 words of
+// From these many rows of x on they are copied first, with zeros behind them.  us without and with copies, 32003 words of
 // 1501 in fp16: forward 512 rows 76 and 85, 1024 rows 144 and 127, 4096 rows 523 and 380; gradient 256 rows 352 and 361, 512 rows 295 and 298
 // (131071 words: 1156 and 1103), 4096 rows 1636 and 1266.
-inline int64_t xent_pad(int64_t k) { return k >= 1024 ? ceil_div(k, 64) * 64 : ceil_div(k, 8) * 8; }
 inline bool xent_copies(int64_t m, int64_t k, int64_t size, bool backward) { return size == 2 && k % 8 != 0 && m >= (backward ? XENT_COPY_GRAD : XENT_COPY); }
 
 // m rows, a vocabulary of n, rows of k elements of `size` bytes; kept_size: bytes of an exponential that is kept.
@@ -33,7 +35,7 @@ inline XentLayout xent_layout(int64_t m, int64_t n, int64_t k, int64_t size, int
   // a wavefront's columns of a tile
   l.strip = l.cut.tile == 256 ? 64 : l.cut.tile == 128 ? 64 : l.cut.tile == 64 ? 32 : 16;
   l.across = ceil_div(n, l.strip);
-  l.ldexps = ceil_div(n, 8) * 8;
+  l.ldexps = xent_pad(n);
   l.exps_bytes = xent_up256((uint64_t)m * l.ldexps * kept_size);
   l.strips_bytes = xent_up256((uint64_t)m * l.across * 8);
   l.picked_bytes = xent_up256((uint64_t)m * 4);
@@ -98,7 +100,7 @@ struct XentGradLayout {
 inline XentGradLayout xent_grad_layout(int64_t m, int64_t n, int64_t k, int64_t size, int64_t parts_of_e) {
   XentGradLayout l;
   l.piece = xent_piece(parts_of_e * m, n);
-  l.lde = ceil_div(l.piece, 8) * 8;
+  l.lde = xent_pad(l.piece);
   l.ldrows = xent_pad(k);
   l.copies = xent_copies(m, k, size, true);
   l.e = 0;
