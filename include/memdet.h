@@ -714,8 +714,8 @@ int mdet_xent_reduce(int32_t index_bits, int64_t m, int64_t n, const float* loss
 
 /* Gradient of sum over i of dloss_i loss_i, from the forward call's lse, and what it kept (NULL: z is formed once more): with
  * e_ij = dloss_i (exp(z_ij - lse_i) - [j = t_i]),  dx = e w,  dw = e^T x,  db = column sums of e; any of dx, dw, db may be NULL (not
- * wanted).  dw and db are of grad_dtype: dtype or MDET_F32.  e is rounded to dtype in front of the two products (in MDET_F16 scaled by a
- * power of two, so that small probabilities are not lost); db sums the unrounded one.  With dw in MDET_F32 of operands in 16 bits e goes into dw
+ * wanted).  dw and db are of grad_dtype: dtype or MDET_F32.  e is rounded to dtype in front of the two products (in 16 bits divided by the
+ * largest |dloss|, in MDET_F16 by 2^-14 of it, so that small probabilities are not lost); db sums the unrounded one.  With dw in MDET_F32 of operands in 16 bits e goes into dw
  * unrounded, as the sum of two (MDET_F16) or three (MDET_BF16) numbers, which takes as many products, and `kept` is not used.  Nothing of a row that does not count comes through,
  * whatever its x and dloss hold, not even NaN. */
 int mdet_xent_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const float* dloss,

@@ -11,8 +11,10 @@
 // Sums and everything behind them are fp32; e is rounded to the operands' type in front of its two products, db sums the unrounded one.  Where dW
 // is wanted in 32 bits of operands in 16, that rounding would be all of its error: e goes in as two (fp16) or three (bf16) numbers that add up
 // to it, their rows one behind the other beside as many copies of x, a sum over two or three times the rows.
-// In fp16 e would vanish below 2^-24, where most probabilities of a large vocabulary lie: it is scaled by a power of two
-// that brings the largest |g| to 2^14 .. 2^15, and the products by its reciprocal.
+// In 16 bits e is divided by the largest |g|, and the products multiplied by it: of a mean, whose g are all alike, the same rounding of 1 / count
+// would be in every row otherwise (a row that is not sure of its target has e = -g there, which is nearly all of its dx; the error of dx and dW
+// for 2048 rows of 512 over 16384 words in bf16 0.0025 and 0.0020 of their norm, of which 0.0017 are the results' own rounding).  In fp16 by
+// 2^-14 of it: e would vanish below 2^-24, where most probabilities of a large vocabulary lie.
 //
 // Rows whose target lies outside of the vocabulary, or is `ignore`, do not count: loss 0, e exactly 0 whatever their logits are, and zeros
 // in the place of their x in dW, so that nothing of them comes through.
@@ -441,27 +443,43 @@ __global__ __launch_bounds__(1024) void xent_reduce_kernel(const float* __restri
 // The gradient.
 // ---------------------------------------------------------------------------
 
-// Powers of two: what e is scaled by, and its reciprocal.
+// What e is multiplied by, and the products with it.
 struct XentScale {
   float up, down;
 };
 
-// For operands in fp16: the largest |g| of a row that counts comes to 2^14 .. 2^15.
+// For operands in 16 bits: the largest |g| of a row that counts comes to 1, in fp16 to 2^14.
+template <typename T>
 __global__ __launch_bounds__(1024) void xent_scale_kernel(const float* __restrict__ g, const XentTargets t, const int64_t rows, XentScale* scale) {
+  constexpr int EACH = 4;
+  constexpr float TOP = std::is_same<T, _Float16>::value ? 16384.0f : 1.0f;
   __shared__ float part[16];
   float most = 0.0f;
-  for (int64_t i = threadIdx.x; i < rows; i += 1024)
-    if (xent_target(t, i) >= 0) most = fmaxf(most, fabsf(g[i]));
+  for (int64_t i0 = threadIdx.x; i0 < rows; i0 += 1024 * EACH) {
+    int64_t raw[EACH];
+    float v[EACH];
+#pragma unroll
+    for (int e = 0; e < EACH; ++e) {
+      const int64_t i = i0 + 1024 * e < rows ? i0 + 1024 * e : rows - 1;
+      raw[e] = xent_raw(t, i);
+      v[e] = g[i];
+    }
+#pragma unroll
+    for (int e = 0; e < EACH; ++e)
+      if (xent_said(t, raw[e]) >= 0) most = fmaxf(most, fabsf(v[e]));
+  }
 #pragma unroll
   for (int off = 1; off < 64; off *= 2) most = fmaxf(most, __shfl_xor(most, off, 64));
   if ((threadIdx.x & 63) == 0) part[threadIdx.x >> 6] = most;
   __syncthreads();
   if (threadIdx.x == 0) {
     for (int w = 1; w < 16; ++w) most = fmaxf(most, part[w]);
-    int up = 0;
-    if (most > 0.0f && most < INFINITY) up = 14 - ilogbf(most);
-    up = up > 120 ? 120 : up < -100 ? -100 : up;
-    *scale = XentScale{ldexpf(1.0f, up), ldexpf(1.0f, -up)};
+    *scale = XentScale{1.0f, 1.0f};
+    if (most > 0.0f && most < INFINITY) {
+      most = fmaxf(most, 0x1p-100f);
+      if (TOP == 1.0f) most = fminf(most, 0x1p126f);           // its reciprocal stays a normal number
+      *scale = XentScale{TOP / most, most / TOP};
+    }
   }
 }
 

@@ -166,9 +166,9 @@ int backward(const Grad& a) {
   T *const e = (T*)(a.workspace + l.e), *const rows = (T*)(a.workspace + l.rows);
   float *const sums = (float*)(a.workspace + l.sums), *const total = (float*)(a.workspace + l.total), *const parts = (float*)(a.workspace + l.parts);
   XentScale* scale = nullptr;
-  if constexpr (std::is_same<T, _Float16>::value) {
+  if constexpr (sizeof(T) == 2) {
     scale = (XentScale*)(a.workspace + l.scale);
-    hipLaunchKernelGGL(xent_scale_kernel, dim3(1), dim3(1024), 0, st, a.g, a.t, a.m, scale);
+    hipLaunchKernelGGL((xent_scale_kernel<T>), dim3(1), dim3(1024), 0, st, a.g, a.t, a.m, scale);
   }
   const bool own_rows = a.k > 0 && (a.dw || (l.copies && !kept));
   for (int part = 0; own_rows && part < parts_of_e; ++part)
