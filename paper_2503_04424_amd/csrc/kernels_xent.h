@@ -206,7 +206,7 @@ __device__ __forceinline__ void xent_store(T* const row, const int64_t col, cons
 
 // Tiles of logits, and what is left of each of their rows: a strip for each of the wavefronts beside each other, so that no wavefront waits
 // for another behind the product.  The matrix cores and the power they draw bound long rows (8192 x 4096 over 131072 words bf16 6.4 to 6.7 ms,
-// 1.32 to 1.37 PFLOP/s; the library's product alone 5.98), the ends of a tile short ones (4096 x 1024 over 50003: 430 to 460 us, 0.95).
+// 1.32 to 1.37 PFLOP/s; the library's product alone 5.98), the ends of a tile short ones (4096 x 1024 over 50003: 370 to 450 us, 0.93 to 1.13).
 template <typename T, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS) void xent_forward_kernel(const Operand<T> r, const Operand<T> c, const XentForward<T> o, const XentUnits u) {
   typedef typename Core<T>::acc_t acc_t;
@@ -524,7 +524,7 @@ __device__ __forceinline__ XentRow xent_row(const XentSlope<T>& o, const int64_t
   return XentRow{lse, o.g[i] + (lse - lse), true, t - o.first - from};
 }
 
-// Tiles of e.  PARTS: numbers of type T that add up to an element of it.  As the forward pass's (4096 x 1024 over 50003 words bf16 440 to 490 us).
+// Tiles of e.  PARTS: numbers of type T that add up to an element of it.  As the forward pass's, with the stores of e (4096 x 1024 over 50003 words bf16 450 to 515 us).
 template <typename T, typename S, bool DIRECT, int PARTS>
 __global__ __launch_bounds__(S::THREADS) void xent_slope_kernel(const Operand<T> r, const Operand<T> c, const XentSlope<T> o, const XentUnits u) {
   typedef typename Core<T>::acc_t acc_t;
@@ -617,7 +617,7 @@ __global__ __launch_bounds__(S::THREADS) void xent_slope_kernel(const Operand<T>
 }
 
 // e from what the forward pass kept: 16 XENT_EACH rows of 16 pieces by a workgroup, as in the gradient of the activation.  Bytes bound it: 8192 rows
-// over 65536 words 440 us (2.1 GB, 4.9 TB/s), where forming z again takes 3500.
+// over 65536 words 424 us (2.1 GB, 5.1 TB/s), where forming z again takes 3500.
 constexpr int XENT_EACH = 4;
 
 template <typename T>
@@ -738,7 +738,7 @@ __device__ __forceinline__ void xent_put(const XentOut<O>& o, const int64_t i, c
 }
 
 // dx = e W (C outer) and dW = e^T x (both outer).  The matrix cores bound them: 8192 x 65536 x 4096 bf16 3.36 ms (1.31 PFLOP/s, the library's 1.31)
-// and 3.53 (1.25, 1.14); 4096 x 50003 x 1024 420 us each: dx's 64 tiles by four workgroups each (976 as 64-row tiles, unsplit).
+// and 3.53 (1.25, 1.14); 4096 x 50003 x 1024 357 and 395 us: dx's 64 tiles by four workgroups each (976 as tiles of 64, unsplit).
 template <typename T, typename O, typename S, bool ROUTER, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS) void xent_product_kernel(const Operand<T> r, const Operand<T> c, const XentOut<O> o, const XentUnits u) {
   typedef typename Core<T>::acc_t acc_t;
