@@ -186,44 +186,11 @@ struct LinearLds {
   static constexpr int BYTES = S::WAVES * WAVE_BYTES > S::NB * S::SLAB ? S::WAVES * WAVE_BYTES : S::NB * S::SLAB;
 };
 
-// The sums of a tile at (row0, col0) on their way out of a matrix of `nrows` x `ncols`: out(rows) is called for some rows of each wavefront's
-// part at a time and has rows(f) call f(row, column, four neighbours from there on).
-template <typename T, typename S, typename F>
-__device__ __forceinline__ void tile_rows(char* const lds, const typename Core<T>::acc_t (&acc)[S::TN][S::TM], const int64_t row0, const int64_t col0,
-                                          const int64_t nrows, const int64_t ncols, F&& out) {
-  typedef LinearLds<S> L;
-  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
-  float* const mine = reinterpret_cast<float*>(lds + wave * L::WAVE_BYTES);
-  const int64_t wrow = row0 + wave / S::WN * S::TM * 16, wcol = col0 + wave % S::WN * S::TN * 16;
-  constexpr int LANES = L::COLS / 4, STEP = 64 / LANES;        // lanes of a row, rows of a step
-#pragma unroll
-  for (int b0 = 0; b0 < S::TM; b0 += L::ROWS / 16) {
-#pragma unroll
-    for (int b = 0; b < L::ROWS / 16; ++b)
-#pragma unroll
-      for (int a = 0; a < S::TN; ++a)
-        *reinterpret_cast<typename Core<T>::acc_t*>(mine + (16 * b + (lane & 15)) * L::PITCH + 16 * a + 4 * (lane >> 4)) = acc[a][b0 + b];
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-    out([&](auto&& f) {
-#pragma unroll 1
-      for (int s = 0; s < L::ROWS; s += STEP) {
-        const int row = s + lane / LANES, col = lane % LANES * 4;
-        const int64_t i = wrow + b0 * 16 + row, j = wcol + col;
-        const typename Core<T>::acc_t v = *reinterpret_cast<const typename Core<T>::acc_t*>(mine + row * L::PITCH + col);
-        const float in[4] = {v[0], v[1], v[2], v[3]};
-        if (i < nrows && j < ncols) f(i, j, in);
-      }
-    });
-    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
-    __builtin_amdgcn_wave_barrier();
-  }
-}
-
 // Tile number t of the layer.  SPLIT: part t / tiles of the sum over k, kept in fp32 for linear_join_kernel.
 template <typename T, typename O, typename S, bool ROUTER, bool COUTER, bool DIRECT, bool SPLIT>
 __device__ __forceinline__ void linear_tile(const int64_t t, char* const lds, const Operand<T>& r, const Operand<T>& c, const int64_t k,
                                             const LinearOut<T, O>& out, float* const parts, const int64_t kpart) {
+  typedef LinearLds<S> L;
   const int64_t down = (out.rows + S::BM - 1) / S::BM, across = (out.cols + S::BN - 1) / S::BN, tiles = down * across;
   int64_t bi, bj;
   gemm_tile_place(t % tiles, down, across, bi, bj);
@@ -236,8 +203,30 @@ __device__ __forceinline__ void linear_tile(const int64_t t, char* const lds, co
   stream.begin(none);
   stream.run(acc, stream.slabs(k0, kend), none);
 
+  const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6);
+  float* const mine = reinterpret_cast<float*>(lds + wave * L::WAVE_BYTES);
+  const int64_t wrow = row0 + wave / S::WN * S::TM * 16, wcol = col0 + wave % S::WN * S::TN * 16;
+  constexpr int LANES = L::COLS / 4, STEP = 64 / LANES;        // lanes of a row, rows of a step
   __syncthreads();                                             // the operands are not read any more
-  tile_rows<T, S>(lds, acc, row0, col0, out.rows, out.cols, [&](auto&& rows) {
+#pragma unroll
+  for (int b0 = 0; b0 < S::TM; b0 += L::ROWS / 16) {
+#pragma unroll
+    for (int b = 0; b < L::ROWS / 16; ++b)
+#pragma unroll
+      for (int a = 0; a < S::TN; ++a)
+        *reinterpret_cast<typename Core<T>::acc_t*>(mine + (16 * b + (lane & 15)) * L::PITCH + 16 * a + 4 * (lane >> 4)) = acc[a][b0 + b];
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+    auto rows = [&](auto&& f) {
+#pragma unroll 1
+      for (int s = 0; s < L::ROWS; s += STEP) {
+        const int row = s + lane / LANES, col = lane % LANES * 4;
+        const int64_t i = wrow + b0 * 16 + row, j = wcol + col;
+        const typename Core<T>::acc_t v = *reinterpret_cast<const typename Core<T>::acc_t*>(mine + row * L::PITCH + col);
+        const float in[4] = {v[0], v[1], v[2], v[3]};
+        if (i < out.rows && j < out.cols) f(i, j, in);
+      }
+    };
     if constexpr (SPLIT) {
       float* const to = parts + part * out.rows * out.cols;
       const bool vec = out.cols % 4 == 0;
@@ -253,7 +242,9 @@ __device__ __forceinline__ void linear_tile(const int64_t t, char* const lds, co
         rows([&](const int64_t i, const int64_t j, const float (&in)[4]) { linear_put4<T, O, decltype(act)::value>(out, i, j, in); });
       });
     }
-  });
+    __builtin_amdgcn_fence(__ATOMIC_ACQ_REL, "wavefront");
+    __builtin_amdgcn_wave_barrier();
+  }
 }
 
 // y, dx and dW.  The matrix cores bound it, in 16 bits together with the waits between slabs: 8192 x 16384 x 4096 bf16 1250
@@ -307,14 +298,14 @@ __global__ __launch_bounds__(256) void linear_join_kernel(const float* __restric
 // Up to 16 rows of x (single tokens): W is read once, 16 rows of it by a workgroup whose wavefronts share k, each piece
 // straight into the registers of its product.  Bytes of W bound it, and how many are on their way: sixteen wavefronts a
 // workgroup (4096 x 4096 bf16, one row: 8.7 us, 3.9 TB/s; with four 9.4, as split 32-row tiles and a join 11.4).
-// Its sum: a lane of wavefront 0 gets those of row lane % 16 and four columns from col0 + 4 (lane / 16) on; the other wavefronts nothing.
-template <typename T, int WAVES>
-__device__ __forceinline__ typename Core<T>::acc_t linear_rows_sum(const Operand<T>& x, const Operand<T>& w, const int64_t k, const int64_t col0) {
+template <typename T, typename O, int WAVES>
+__global__ __launch_bounds__(64 * WAVES) void linear_rows_kernel(const Operand<T> x, const Operand<T> w, const int64_t k, const LinearOut<T, O> out) {
   typedef typename Core<T>::piece_t piece_t;
   typedef typename Core<T>::acc_t acc_t;
   constexpr int VEC = Core<T>::VEC, STEP = 4 * VEC, UNROLL = 8;
   __shared__ acc_t sums[WAVES][64];
   const int lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane((int)threadIdx.x >> 6), j = lane & 15, g = lane >> 4;
+  const int64_t col0 = (int64_t)blockIdx.x * 16;
   // rows behind the last are not stored
   const T* const wp = w.p + (col0 + j < w.rows ? col0 + j : w.rows - 1) * w.stride + g * VEC;
   const T* const xp = x.p + (j < x.rows ? j : x.rows - 1) * x.stride + g * VEC;
@@ -347,21 +338,14 @@ __device__ __forceinline__ typename Core<T>::acc_t linear_rows_sum(const Operand
   }
   sums[wave][lane] = acc;
   __syncthreads();
-  acc_t v = sums[0][lane];
-  if (wave == 0)
+  if (wave == 0) {
+    acc_t v = sums[0][lane];
 #pragma unroll
     for (int p = 1; p < WAVES; ++p) v += sums[p][lane];
-  return v;
-}
-
-template <typename T, typename O, int WAVES>
-__global__ __launch_bounds__(64 * WAVES) void linear_rows_kernel(const Operand<T> x, const Operand<T> w, const int64_t k, const LinearOut<T, O> out) {
-  const int lane = threadIdx.x & 63, j = lane & 15, g = lane >> 4;
-  const int64_t col0 = (int64_t)blockIdx.x * 16, c = col0 + 4 * g;
-  const typename Core<T>::acc_t v = linear_rows_sum<T, WAVES>(x, w, k, col0);
-  const float in[4] = {v[0], v[1], v[2], v[3]};
-  if (threadIdx.x < 64 && j < out.rows && c < out.cols)
-    act_switch(out.act, [&](auto act) { linear_put4<T, O, decltype(act)::value>(out, j, c, in); });
+    const int64_t c = col0 + 4 * g;
+    const float in[4] = {v[0], v[1], v[2], v[3]};
+    if (j < out.rows && c < out.cols) act_switch(out.act, [&](auto act) { linear_put4<T, O, decltype(act)::value>(out, j, c, in); });
+  }
 }
 
 // dz = dy act'(z) and the column sums of 16 EACH rows of it.  A workgroup takes 16 pieces of 16 bytes across; thread (t, c)

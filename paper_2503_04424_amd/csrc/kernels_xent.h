@@ -19,7 +19,7 @@
 // Rows whose target lies outside of the vocabulary, or is `ignore`, do not count: loss 0, e exactly 0 whatever their logits are, and zeros
 // in the place of their x in dW, so that nothing of them comes through.
 #pragma once
-#include "kernels_linear.h"
+#include "kernels_gemm.h"
 #include "kernels_rows.h"
 
 namespace mdet {
