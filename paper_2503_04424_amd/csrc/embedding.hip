@@ -28,19 +28,23 @@ bool embedding_fits(int64_t n, int64_t vocab, int64_t width) {
 }
 bool is_index(int32_t bits) { return bits == 32 || bits == 64; }
 
+// Sorted tokens of a group of lanes: few while there are few groups, each of which waits for one load behind the other; more of them where the sums
+// that cross runs count.  us with 4, 8 and 16: 173 tokens, rows of 40 15.3, 17.1, 21; 4096, 512 22, 25, 33 (added); 4096, 2000 40, 39, 42; 8192,
+// 512 28.1, 27.5, 33; 65536, 128 75, 67, 66; 16384, 1024 of 50003 68, 59, 54; 65536, 1024 169, 137, 130.
+int run_of(int64_t n, int64_t width) {
+  const int64_t elements = n * width;
+  return elements >= (int64_t(1) << 23) ? 16 : n < 6144 && elements < (int64_t(1) << 22) ? 4 : 8;
+}
+
 // Workspace of the gradient: the sorted ids and their places, where each id begins and how often it is there, how many there are,
 // then the parts of the sums that cross runs.
-// Sorted tokens of a group of lanes: few while there are few groups, each of which waits for one load behind the other (4099 tokens, rows of 777
-// fp32: 25.1 us added with 8, 28.2 with 16), more of them where the sums that cross runs count (8192 tokens, rows of 4096 bf16: 146 and 135).
-int run_of(int64_t n) { return n < 8192 ? 8 : 16; }
-
 struct SortLayout {
   int64_t runs;
   uint64_t id, start, count, total, parts, bytes;
 };
 SortLayout sort_layout(int64_t n, int64_t vocab, int64_t width) {
   SortLayout l;
-  l.runs = ceil_div(n, run_of(n));
+  l.runs = ceil_div(n, run_of(n, width));
   l.id = up256((uint64_t)n * 4);
   l.start = l.id + up256((uint64_t)n * 4);
   l.count = l.start + up256((uint64_t)vocab * 4);
@@ -70,7 +74,9 @@ int backward(int64_t n, const I* ids, const EmbeddingSums<T, O>& a, hipStream_t 
       hipLaunchKernelGGL((embedding_join_kernel<T, O, RUN>), grid, dim3(256), 0, st, a, across, first);
     });
   };
-  if (run_of(n) == 8) go(std::integral_constant<int, 8>{});
+  const int run = run_of(n, a.width);
+  if (run == 4) go(std::integral_constant<int, 4>{});
+  else if (run == 8) go(std::integral_constant<int, 8>{});
   else go(std::integral_constant<int, 16>{});
   return launch_status();
 }

@@ -117,6 +117,22 @@ def test_orders(M, n, kind):
         assert torch.equal(M.mdet_embedding_backward(dy, ids.int(), vocab, grad_dtype=torch.float32), got)
 
 
+@pytest.mark.parametrize("n,width", [(6143, 72), (6144, 72), (8400, 1001), (1000, 8400), (20000, 420)])
+@pytest.mark.parametrize("kind", ["some often", "one token", "in order"])
+def test_orders_of_wide_rows(M, n, width, kind):
+    """Each length of a run: of four sorted tokens, of eight, and of sixteen where there are 2^23 elements or more."""
+    i = torch.arange(n, device="cuda")
+    ids = {"some often": tokens(n, n, n), "one token": torch.full_like(i, 7), "in order": i}[kind]
+    dy = strided(n, width, torch.bfloat16, gen(n), 1.0, 3, 1)
+    got = M.mdet_embedding_backward(dy, ids, n, 0.5, grad_dtype=torch.float32)
+    want, err, _ = grad64(dy, ids, n, 0.5)
+    check(got, want, err, torch.float32)
+    before = strided(n, width, torch.float32, gen(3))
+    want, err, _ = grad64(dy, ids, n, 0.5, before)
+    check(M.mdet_embedding_backward(dy, ids, n, 0.5, before, accumulate=True), want, err, torch.float32, "added")
+    assert torch.equal(M.mdet_embedding_backward(dy, ids.int(), n, 0.5, grad_dtype=torch.float32), got)
+
+
 def test_many_tokens_of_a_bucket(M):
     """A vocabulary whose buckets are as large as they get, and one that has more of them."""
     for vocab in (524287, 524288, 1048575, 1100000):
