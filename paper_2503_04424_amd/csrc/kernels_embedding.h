@@ -51,11 +51,10 @@ __global__ __launch_bounds__(256) void embedding_kernel(const I* __restrict__ id
 // The sort.  Token v belongs to bucket v % buckets (so that the frequent ones, which have small numbers as a rule, lie in
 // different ones), and a workgroup to each bucket, which goes through all of the ids twice: to count its own, token by token, and
 // those of the buckets in front of it; then to write their places down, in order.  That needs no word between workgroups and
-// one launch; the ids come out of cache, 16384 at once in a workgroup's registers, where a short list stays between the two.  The time goes with
+// one launch; the ids come out of cache, up to 16384 at once in a workgroup's registers (SLOTS a thread), where a short list stays between the two.  The time goes with
 // n times the buckets: 16384 ids of 50003 13 us (1024 at once, and one wavefront for the places, 31), a million of 32000 560 to 830.
 // ---------------------------------------------------------------------------
 constexpr int SORT_THREADS = 1024, SORT_WAVES = SORT_THREADS / 64;
-constexpr int SORT_EACH = 16, SORT_ROUND = SORT_THREADS * SORT_EACH;
 constexpr int SORT_TOKENS = 2048;      // of a bucket
 constexpr int SORT_BUCKETS = 256;      // or more, a power of two
 
@@ -67,38 +66,39 @@ struct Sorted {
   int32_t* total;                      // how many ids lie in the table
 };
 
-template <typename I>
+template <typename I, int SLOTS>
 __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_kernel(const I* __restrict__ ids, const int32_t n, const int64_t vocab, const int bits,
                                                                       const Sorted out) {
-  static_assert(SORT_ROUND <= 1 << 16 && SORT_TOKENS <= 1 << 16, "an entry of the list is a place and a token of 16 bits each");
+  constexpr int ROUND = SORT_THREADS * SLOTS, PER = SLOTS * SORT_WAVES / 64;
+  static_assert(PER >= 1 && ROUND <= 1 << 16 && SORT_TOKENS <= 1 << 16, "an entry of the list is a place and a token of 16 bits each");
   __shared__ int32_t cursor[SORT_TOKENS];
-  __shared__ int32_t sums[SORT_EACH][SORT_WAVES];
-  __shared__ uint32_t list[SORT_ROUND];
+  __shared__ int32_t sums[SLOTS][SORT_WAVES];
+  __shared__ uint32_t list[ROUND];
   __shared__ uint16_t often[SORT_WAVES][SORT_TOKENS], behind[SORT_TOKENS];
   __shared__ int32_t all_found;
   const int thread = threadIdx.x, lane = thread & 63, wave = thread >> 6;
   const int64_t buckets = gridDim.x;
   const int32_t bucket = blockIdx.x;
   const int tokens = bucket < vocab ? (int)((vocab - bucket + buckets - 1) / buckets) : 0;
-  int32_t id[SORT_EACH];               // -1: none of the table
+  int32_t id[SLOTS];               // -1: none of the table
   auto get = [&](const int64_t i0) {
-    int64_t raw[SORT_EACH];
+    int64_t raw[SLOTS];
 #pragma unroll
-    for (int e = 0; e < SORT_EACH; ++e) {
+    for (int e = 0; e < SLOTS; ++e) {
       const int64_t i = i0 + e * SORT_THREADS + thread;
       raw[e] = i < n ? (int64_t)ids[i] : -1;
     }
 #pragma unroll
-    for (int e = 0; e < SORT_EACH; ++e) id[e] = raw[e] >= 0 && raw[e] < vocab ? (int32_t)raw[e] : -1;
+    for (int e = 0; e < SLOTS; ++e) id[e] = raw[e] >= 0 && raw[e] < vocab ? (int32_t)raw[e] : -1;
   };
   auto bucket_of = [&](const int32_t v) { return v & (int32_t)(buckets - 1); };
   for (int t = thread; t < tokens; t += SORT_THREADS) cursor[t] = 0;
   __syncthreads();
   int32_t before = 0;
-  for (int64_t i0 = 0; i0 < n; i0 += SORT_ROUND) {
+  for (int64_t i0 = 0; i0 < n; i0 += ROUND) {
     get(i0);
 #pragma unroll
-    for (int e = 0; e < SORT_EACH; ++e)
+    for (int e = 0; e < SLOTS; ++e)
       if (id[e] >= 0) {
         before += bucket_of(id[e]) < bucket;
         if (bucket_of(id[e]) == bucket) atomicAdd(&cursor[id[e] >> bits], 1);
@@ -150,39 +150,39 @@ __global__ __launch_bounds__(SORT_THREADS) void embedding_sort_kernel(const I* _
   if (all == base) return;             // nothing of this bucket: the same for the whole workgroup
   // their places, in order: what a round of ids has of this bucket is put side by side, then handed out in parts, 64 at a time; equal tokens of the
   // 64 find each other by their numbers' bits
-  for (int64_t i0 = 0; i0 < n; i0 += SORT_ROUND) {
-    if (n > SORT_ROUND) get(i0);
+  for (int64_t i0 = 0; i0 < n; i0 += ROUND) {
+    if (n > ROUND) get(i0);
     __syncthreads();                   // sums and list have been read, cursors are written
-    uint64_t hits[SORT_EACH];
+    uint64_t hits[SLOTS];
 #pragma unroll
-    for (int e = 0; e < SORT_EACH; ++e) {
+    for (int e = 0; e < SLOTS; ++e) {
       hits[e] = __ballot(id[e] >= 0 && bucket_of(id[e]) == bucket);
       if (lane == 0) sums[e][wave] = __popcll(hits[e]);
     }
     __syncthreads();
-    // the sums of the 256 parts in front of each: four parts a lane of the first wavefront
+    // the sums of the parts (64 ids each) in front of each: PER parts a lane of the first wavefront
     if (wave == 0) {
-      int32_t four[4], upto4 = 0;
+      int32_t some[PER], ahead_of = 0;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) four[q] = (&sums[0][0])[4 * lane + q], upto4 += four[q];
-      const int32_t own = upto4;
+      for (int q = 0; q < PER; ++q) some[q] = (&sums[0][0])[PER * lane + q], ahead_of += some[q];
+      const int32_t own = ahead_of;
 #pragma unroll
       for (int off = 1; off < 64; off *= 2) {
-        const int32_t o = __shfl_up(upto4, off, 64);
-        if (lane >= off) upto4 += o;
+        const int32_t o = __shfl_up(ahead_of, off, 64);
+        if (lane >= off) ahead_of += o;
       }
-      int32_t first = upto4 - own;
+      int32_t first = ahead_of - own;
 #pragma unroll
-      for (int q = 0; q < 4; ++q) {
-        (&sums[0][0])[4 * lane + q] = first;
-        first += four[q];
+      for (int q = 0; q < PER; ++q) {
+        (&sums[0][0])[PER * lane + q] = first;
+        first += some[q];
       }
-      if (lane == 63) all_found = upto4;
+      if (lane == 63) all_found = ahead_of;
     }
     __syncthreads();
     const int32_t found = all_found;
 #pragma unroll
-    for (int e = 0; e < SORT_EACH; ++e)
+    for (int e = 0; e < SLOTS; ++e)
       if (hits[e] >> lane & 1)
         list[sums[e][wave] + __popcll(hits[e] & ((1ull << lane) - 1))] = (uint32_t)(e * SORT_THREADS + thread) << 16 | (uint32_t)(id[e] >> bits);
     const bool few = found <= 64;      // those go out at once
