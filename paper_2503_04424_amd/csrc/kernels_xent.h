@@ -392,9 +392,10 @@ __global__ __launch_bounds__(LANES < 256 ? 256 : LANES) void xent_join_kernel(co
     for (int w = 1; w < WAVES; ++w) add(part[w]);
   }
   if (threadIdx.x % LANES == 0) {
-    const float l = all.top + logf(all.sum);
-    if (lse) lse[row] = l;
-    if (loss) loss[row] = xent_target(t, row) >= 0 ? l - picked[row] : 0.0f;
+    // the loss from the difference of the logits: of a row that is sure of its target, lse's rounding would be more than is left of it
+    const float l = logf(all.sum);
+    if (lse) lse[row] = all.top + l;
+    if (loss) loss[row] = xent_target(t, row) >= 0 ? (all.top - picked[row]) + l : 0.0f;
   }
 }
 

@@ -225,6 +225,22 @@ def test_logits_far_beyond_the_exponential(M, dtype, up):
 
 
 @pytest.mark.parametrize("dtype", TYPES, ids=str)
+@pytest.mark.parametrize("m", [3, 8, 16, 40, 300])
+def test_loss_of_rows_that_are_sure(M, m, dtype):
+    """Logits of a thousand, exact, the target's 8 above all others: the loss keeps the digits that lse, a number of a thousand, has not."""
+    n, k = 700, 24
+    x, w = torch.zeros(m, k, dtype=dtype, device="cuda"), torch.zeros(n, k, dtype=dtype, device="cuda")
+    x[:, 1], w[:, 1], w[77, 1] = 32.0, 31.75, 32.0
+    t = torch.full((m,), 77, device="cuda")
+    loss, lse, _ = M.mdet_xent_forward(x, w, t)
+    want = torch.log1p((n - 1) * torch.exp(torch.tensor(-8.0, dtype=torch.float64)))
+    part = float((n - 1) * torch.exp(torch.tensor(-8.0)))
+    # sums of 700 numbers over strips and lanes, each below 64 roundings of a sum up to 1.3; an exponential of -8 to 12 EPS32; the logarithm's own
+    assert float((loss.double() - float(want)).abs().max()) <= 64 * 2.0 ** -24 * 1.3 + 12 * EPS32 * part + 2 * EPS32
+    assert float((lse.double() - 1024 - float(want)).abs().max()) <= 2.0 ** -13 + 1e-5
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
 @pytest.mark.parametrize("m", [8, 40, 300])
 def test_masked_words_beside_small_logits(M, m, dtype):
     """Whole strips of -inf where all of the other logits lie so low that the exponential of -lse is infinite."""
