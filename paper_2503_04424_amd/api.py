@@ -192,6 +192,18 @@ def _rows(t):
     return t.new_empty(t.shape).copy_(t)
 
 
+def _derivatives(*operands):
+    """Whether a derivative can be asked for: gradients are on, or an operand carries a tangent of forward mode, which ``no_grad`` does not take
+    away (the nodes have no forward mode: with them such a call raises)."""
+    import torch
+    if torch.is_grad_enabled():
+        return True
+    forward = torch.autograd.forward_ad
+    if getattr(forward, "_current_level", 0) < 0:                # outside of forward mode there are none: a tenth of the time of asking each operand
+        return False
+    return any(t is not None and forward.unpack_dual(t).tangent is not None for t in operands)
+
+
 _linear = None
 
 
@@ -204,8 +216,7 @@ def linear(x, w, bias=None, residual=None, activation="none"):
         raise ValueError("x with rows of inputs as its last axis and a matrix w expected")
     if residual is not None and tuple(residual.shape) != (*x.shape[:-1], w.shape[0]):
         raise ValueError(f"residual: shape {(*x.shape[:-1], w.shape[0])} expected, not {tuple(residual.shape)}")
-    import torch
-    if not torch.is_grad_enabled():
+    if not _derivatives(x, w, bias, residual):
         # ctx.needs_input_grad is true for parameters here as well: nothing is kept for a gradient that cannot be asked for
         return _layer(_as_rows(x), w, bias, residual, activation).view(*x.shape[:-1], w.shape[0])
     if _linear is None:
@@ -303,8 +314,7 @@ def embedding(ids, table, scale=1.0):
     table gives a row of zeros, and has no part in the gradient."""
     if table.dim() != 2:
         raise ValueError("table: a matrix expected")
-    import torch
-    if not torch.is_grad_enabled():
+    if not _derivatives(table):
         return B.mdet_embedding_forward(ids.reshape(-1).contiguous(), _rows(table), scale).view(*ids.shape, table.shape[1])
     return _function(_embedding_function).apply(table, ids, scale)
 
@@ -313,8 +323,7 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
     """Layer norm over the last axis of x (..., n) with its gradient (autograd); weight and bias (n,)."""
     if x.dim() < 1:
         raise ValueError("x with rows as its last axis expected")
-    import torch
-    if not torch.is_grad_enabled():
+    if not _derivatives(x, weight, bias):
         return B.mdet_layernorm_forward(_rows(_as_rows(x)), None if weight is None else weight.contiguous(),
                                         None if bias is None else bias.contiguous(), eps, mean=False, rstd=False)[0].view(x.shape)
     return _function(_layer_norm_function).apply(x, weight, bias, eps)
@@ -330,9 +339,8 @@ def linear_cross_entropy(x, w, target, bias=None, ignore_index=-100, reduction="
                          f"{tuple(target.shape)}")
     if reduction not in ("mean", "sum", "none"):
         raise ValueError("reduction must be 'mean', 'sum' or 'none'")
-    import torch
     flat = target.reshape(-1).contiguous()
-    if torch.is_grad_enabled():
+    if _derivatives(x, w, bias):
         loss = _function(_cross_entropy_function).apply(x, w, bias, flat, ignore_index, reduction, keep)
     else:
         loss = B.mdet_xent_forward(_rows(_as_rows(x)), _rows(w), flat, None if bias is None else bias.contiguous(), ignore_index, lse=False)[0]
