@@ -15,7 +15,7 @@ import operator
 import os
 import sys
 from dataclasses import dataclass
-from typing import Callable, Optional
+from typing import Callable, NamedTuple, Optional
 
 from . import build as _build
 
@@ -926,22 +926,28 @@ def mdet_ntk_gram(inputs, signals, out=None, outputs=1, bias=1.0, scale=1.0, acc
     return out
 
 
-_INDEX_BITS = {}
-_FLOAT, _BYTE = [], []       # torch.float32 and torch.uint8, from the first call on
+_types = None
+
+
+class _Types(NamedTuple):
+    float32: object
+    uint8: object
+    index_bits: dict
 
 
 def _torch_types():
-    import torch
-    _INDEX_BITS.update({torch.int32: 32, torch.int64: 64})
-    _FLOAT.append(torch.float32)
-    _BYTE.append(torch.uint8)
+    """torch's types that the operators name, from the first call on: in one assignment, so that another thread finds all of them or none."""
+    global _types
+    types = _types
+    if types is None:
+        import torch
+        types = _types = _Types(torch.float32, torch.uint8, {torch.int32: 32, torch.int64: 64})
+    return types
 
 
 def _indices(t, name, n, gpu):
     """(address, bits) of n consecutive int32 or int64 on this GPU."""
-    if not _INDEX_BITS:
-        _torch_types()
-    bits = _INDEX_BITS.get(t.dtype)
+    bits = _torch_types().index_bits.get(t.dtype)
     if bits is None or t.shape != (n,) or t.get_device() != gpu or not t.is_contiguous():
         raise ValueError(f"{name}: a contiguous tensor of {n} int32 or int64 on cuda:{gpu} expected, not {tuple(t.shape)} {t.dtype} on {t.device}")
     return t.data_ptr(), bits
@@ -986,7 +992,7 @@ def _room(workspace, need, gpu, like, stream):
     size = need()
     if size == 0:
         return None, 0, None
-    ws = _fresh(like, size, _BYTE[0], stream)
+    ws = _fresh(like, size, _torch_types().uint8, stream)
     return ws.data_ptr(), size, ws
 
 
@@ -1060,20 +1066,19 @@ def mdet_layernorm_forward(x, weight=None, bias=None, eps=1e-5, out=None, mean=T
     """``(x - mean) * rstd * weight + bias`` over the rows of x (m, n) on the GPU (asynchronous), rstd = 1 / sqrt(var + eps);
     weight and bias (n,), all of one type (float32, float16 or bfloat16).  mean, rstd: True for a new float32 tensor (m,), False or None
     where they are not kept for the gradient, or the tensor to write.  Returns out, mean, rstd."""
-    if not _FLOAT:
-        _torch_types()
     if x.dim() != 2:
         raise ValueError("x: a matrix expected")
     t = _operand_type(x.dtype)
     m, n = x.shape
     gpu = _gpu(x, "x")
+    f32 = _torch_types().float32
     xp, ldx = _matrix(x, "x", m, n, t, gpu)
     wp = None if weight is None else _vector(weight, "weight", n, t, gpu)
     bp = None if bias is None else _vector(bias, "bias", n, t, gpu)
     given = _given(out, mean, rstd)
     out, yp, ldy = _matrix_result(True if out is None else out, "out", m, n, t, gpu, x, stream)
-    mean, mp = _vector_result(mean, "mean", m, _FLOAT[0], gpu, x, stream)
-    rstd, rp = _vector_result(rstd, "rstd", m, _FLOAT[0], gpu, x, stream)
+    mean, mp = _vector_result(mean, "mean", m, f32, gpu, x, stream)
+    rstd, rp = _vector_result(rstd, "rstd", m, f32, gpu, x, stream)
     _queue(gpu, load().mdet_layernorm_forward, _type_code(t), m, n, xp, ldx, wp, bp, eps, yp, ldy, mp, rp, _operator_stream(stream, gpu))
     if given:
         _written(*given)
@@ -1084,17 +1089,16 @@ def mdet_layernorm_backward(dy, x, mean, rstd, weight=None, dx=True, dw=True, db
     """Gradient of ``mdet_layernorm_forward`` (asynchronous): (dx, dw, db) from dy (m, n), its x, mean, rstd and weight.  dx, dw, db:
     True for a new tensor, False or None for a gradient that is not wanted (None is returned), or the tensor to write; dw and db are of
     ``grad_dtype``: x's type or float32."""
-    if not _FLOAT:
-        _torch_types()
     if x.dim() != 2:
         raise ValueError("x: a matrix expected")
     t = _operand_type(x.dtype)
     m, n = x.shape
     gt = t if grad_dtype is None else grad_dtype
     gpu = _gpu(x, "x")
+    f32 = _torch_types().float32
     dyp, lddy = _matrix(dy, "dy", m, n, t, gpu)
     xp, ldx = _matrix(x, "x", m, n, t, gpu)
-    mp, rp = _vector(mean, "mean", m, _FLOAT[0], gpu), _vector(rstd, "rstd", m, _FLOAT[0], gpu)
+    mp, rp = _vector(mean, "mean", m, f32, gpu), _vector(rstd, "rstd", m, f32, gpu)
     wp = None if weight is None else _vector(weight, "weight", n, t, gpu)
     given = _given(dx, dw, db)
     dx, dxp, lddx = _matrix_result(dx, "dx", m, n, t, gpu, x, stream)
@@ -1146,12 +1150,13 @@ def mdet_xent_forward(x, w, target, bias=None, ignore=-100, loss=True, lse=True,
     none, or the tensor to write.  keep: True, or a contiguous tensor of ``mdet_xent_kept_query`` bytes, for what spares the gradient a
     product.  Returns loss, lse and what was kept (or None)."""
     t, gpu, (m, n, k), (xp, ldx, wp, ldw, bp, tp), bits = _xent_operands(x, w, target, bias)
+    f32 = _torch_types().float32
     given = _given(loss, lse, keep)
-    loss, lp = _vector_result(loss, "loss", m, _FLOAT[0], gpu, x, stream)
-    lse, sp = _vector_result(lse, "lse", m, _FLOAT[0], gpu, x, stream)
+    loss, lp = _vector_result(loss, "loss", m, f32, gpu, x, stream)
+    lse, sp = _vector_result(lse, "lse", m, f32, gpu, x, stream)
     kept, kp, kb = None, None, 0
     if keep is not None and keep is not False:
-        kept = _fresh(x, mdet_xent_kept_query(t, m, n, k), _BYTE[0], stream) if keep is True else keep
+        kept = _fresh(x, mdet_xent_kept_query(t, m, n, k), _torch_types().uint8, stream) if keep is True else keep
         kp, kb = _bytes(kept, "keep", gpu)
     wsp, wsb, _ws = _room(workspace, lambda: mdet_xent_workspace_query(t, m, n, k), gpu, x, stream)
     _queue(gpu, load().mdet_xent_forward, _type_code(t), bits, m, n, k, xp, ldx, wp, ldw, bp, tp, ignore, lp, sp, kp, kb, wsp, wsb,
@@ -1165,23 +1170,22 @@ def mdet_xent_reduce(loss, target, vocab, ignore=-100, mean=True, out=True, weig
     """The mean over the rows that count of ``mdet_xent_forward``'s loss, or with ``mean`` false their sum (asynchronous): NaN for the mean of no
     rows.  weights: the ``dloss`` that this makes of a gradient of 1, zero for rows that do not count.  out (one float32; a new one has no axes)
     and weights (m,): True for a new tensor, False or None for no weights, or the tensor to write.  Returns out, weights."""
-    if not _FLOAT:
-        _torch_types()
     if loss.dim() != 1:
         raise ValueError("loss: a vector expected")
     m, vocab = loss.shape[0], int(vocab)
     gpu = _gpu(loss, "loss")
-    lp = _vector(loss, "loss", m, _FLOAT[0], gpu)
+    f32 = _torch_types().float32
+    lp = _vector(loss, "loss", m, f32, gpu)
     tp, bits = _indices(target, "target", m, gpu)
     given = _given(out, weights)
     if out is True:
-        out = _fresh(loss, (), _FLOAT[0], stream)
+        out = _fresh(loss, (), f32, stream)
         op = out.data_ptr()
     elif out is None or out is False:
         raise ValueError("out: True, or a tensor expected")
     else:
-        op = _vector(out if out.dim() else out.view(1), "out", 1, _FLOAT[0], gpu)
-    weights, wp = _vector_result(weights, "weights", m, _FLOAT[0], gpu, loss, stream)
+        op = _vector(out if out.dim() else out.view(1), "out", 1, f32, gpu)
+    weights, wp = _vector_result(weights, "weights", m, f32, gpu, loss, stream)
     _queue(gpu, load().mdet_xent_reduce, bits, m, vocab, lp, tp, ignore, int(bool(mean)), op, wp, _operator_stream(stream, gpu))
     if given:
         _written(*given)
@@ -1194,8 +1198,9 @@ def mdet_xent_backward(dloss, x, w, target, lse, bias=None, ignore=-100, kept=No
     its lse, and what it kept.  dx, dw, db: True for a new tensor, False or None for a gradient that is not wanted (None is returned; db
     without a bias as a rule), or the tensor to write; dw and db are of ``grad_dtype``: x's type or float32."""
     t, gpu, (m, n, k), (xp, ldx, wp, ldw, bp, tp), bits = _xent_operands(x, w, target, bias)
+    f32 = _torch_types().float32
     gt = t if grad_dtype is None else grad_dtype
-    gp, sp = _vector(dloss, "dloss", m, _FLOAT[0], gpu), _vector(lse, "lse", m, _FLOAT[0], gpu)
+    gp, sp = _vector(dloss, "dloss", m, f32, gpu), _vector(lse, "lse", m, f32, gpu)
     kp, kb = (None, 0) if kept is None else _bytes(kept, "kept", gpu)
     given = _given(dx, dw, db)
     dx, dxp, lddx = _matrix_result(dx, "dx", m, k, t, gpu, x, stream)
