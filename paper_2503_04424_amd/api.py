@@ -279,7 +279,7 @@ def _cross_entropy_function():
         def forward(ctx, x, w, bias, target, ignore, reduction, keep):
             rows, mat = _rows(_as_rows(x)), _rows(w)
             bias = None if bias is None else bias.contiguous()
-            loss, lse, kept = B.mdet_xent_forward(rows, mat, target, bias, ignore, keep=keep)
+            loss, lse, kept = B.mdet_xent_forward(rows, mat, target, bias, ignore, keep=keep and any(ctx.needs_input_grad[:3]))
             weights = None
             if reduction != "none":
                 loss, weights = B.mdet_xent_reduce(loss, target, mat.shape[0], ignore, reduction == "mean")
