@@ -723,6 +723,14 @@ int mdet_xent_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, in
                        const float* lse, const void* kept, uint64_t kept_bytes, void* dx, int64_t lddx, void* dw, int64_t lddw,
                        void* db, void* workspace, uint64_t workspace_bytes, void* stream);
 
+/* The same from the forward call's loss as well (m floats).  With it, or with `kept`, which holds it too, the target's e is dloss_i (exp(-loss_i) - 1)
+ * to a few 2^-24 of dloss_i.  Without both it is formed from lse and is off by the rounding of that, up to 2^-24 |lse_i| of dloss_i: of a row that is sure
+ * of its target too much may be lost (all of it where that is more than 1 - p). */
+int mdet_xent_backward_with_loss(int32_t dtype, int32_t grad_dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const float* dloss,
+                                 const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* target,
+                                 int64_t ignore, const float* lse, const float* loss, const void* kept, uint64_t kept_bytes, void* dx,
+                                 int64_t lddx, void* dw, int64_t lddw, void* db, void* workspace, uint64_t workspace_bytes, void* stream);
+
 /* ------------------------------------------------------------------------
  * Measuring sticks for the benchmark (asynchronous, enqueue only; DEVICE pointers).
  * ---------------------------------------------------------------------- */

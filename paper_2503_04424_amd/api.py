@@ -280,20 +280,23 @@ def _cross_entropy_function():
             rows, mat = _rows(_as_rows(x)), _rows(w)
             bias = None if bias is None else bias.contiguous()
             loss, lse, kept = B.mdet_xent_forward(rows, mat, target, bias, ignore, keep=keep and any(ctx.needs_input_grad[:3]))
-            weights = None
+            rows_loss, weights = loss, None
             if reduction != "none":
                 loss, weights = B.mdet_xent_reduce(loss, target, mat.shape[0], ignore, reduction == "mean")
-            ctx.save_for_backward(rows, mat, bias, target, lse, kept, weights)
+            elif kept is None:
+                loss = loss.clone()              # the caller's own, to be changed in place as any other result
+            ctx.save_for_backward(rows, mat, bias, target, lse, rows_loss if kept is None else None, kept, weights)
             ctx.shape, ctx.ignore = x.shape, ignore
             return loss
 
         @staticmethod
         @torch.autograd.function.once_differentiable
         def backward(ctx, dloss):
-            x, w, bias, target, lse, kept, weights = ctx.saved_tensors
+            x, w, bias, target, lse, loss, kept, weights = ctx.saved_tensors
             dloss = dloss.contiguous() if weights is None else weights * dloss
             need_x, need_w, need_b = ctx.needs_input_grad[:3]
-            dx, dw, db = B.mdet_xent_backward(dloss, x, w, target, lse, bias, ctx.ignore, kept, dx=need_x, dw=need_w, db=need_b)
+            dx, dw, db = B.mdet_xent_backward(dloss, x, w, target, lse, bias, ctx.ignore, kept, dx=need_x, dw=need_w, db=need_b,
+                                              loss=loss)
             return None if dx is None else dx.view(ctx.shape), dw, db, None, None, None, None
 
     return CrossEntropyFunction

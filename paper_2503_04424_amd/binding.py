@@ -110,6 +110,7 @@ EXPORTS = [
     "mdet_embedding_workspace_query", "mdet_embedding_forward", "mdet_embedding_backward",
     "mdet_layernorm_workspace_query", "mdet_layernorm_forward", "mdet_layernorm_backward",
     "mdet_xent_workspace_query", "mdet_xent_kept_query", "mdet_xent_forward", "mdet_xent_reduce", "mdet_xent_backward",
+    "mdet_xent_backward_with_loss",
 ]
 
 _lib = None
@@ -173,6 +174,8 @@ def load():
     L.mdet_xent_reduce.argtypes = [i32, i64, i64, vp, vp, i64, i32, vp, vp, vp]
     L.mdet_xent_backward.argtypes = [i32, i32, i32, i64, i64, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, u64, vp, i64, vp, i64,
                                      vp, vp, u64, vp]
+    L.mdet_xent_backward_with_loss.argtypes = [i32, i32, i32, i64, i64, i64, vp, vp, i64, vp, i64, vp, vp, i64, vp, vp, vp, u64, vp, i64, vp, i64,
+                                               vp, vp, u64, vp]
     L.mdet_strerror.argtypes = [C.c_int]
     L.mdet_strerror.restype = C.c_char_p
     L.mdet_version.restype = C.c_char_p
@@ -1193,22 +1196,24 @@ def mdet_xent_reduce(loss, target, vocab, ignore=-100, mean=True, out=True, weig
 
 
 def mdet_xent_backward(dloss, x, w, target, lse, bias=None, ignore=-100, kept=None, dx=True, dw=True, db=None, grad_dtype=None,
-                       workspace=None, stream=None):
+                       workspace=None, stream=None, loss=None):
     """Gradient of the sum of ``dloss * loss`` of ``mdet_xent_forward`` (asynchronous): (dx, dw, db) from dloss (m,) float32, its operands,
-    its lse, and what it kept.  dx, dw, db: True for a new tensor, False or None for a gradient that is not wanted (None is returned; db
-    without a bias as a rule), or the tensor to write; dw and db are of ``grad_dtype``: x's type or float32."""
+    its lse and loss, and what it kept.  With neither loss nor kept, rows that are sure of their target lose what the rounding of lse, a number
+    of the logits' size, takes from ``exp(z - lse) - 1``.  dx, dw, db: True for a new tensor, False or None for a gradient that is not wanted
+    (None is returned; db without a bias as a rule), or the tensor to write; dw and db are of ``grad_dtype``: x's type or float32."""
     t, gpu, (m, n, k), (xp, ldx, wp, ldw, bp, tp), bits = _xent_operands(x, w, target, bias)
     f32 = _torch_types().float32
     gt = t if grad_dtype is None else grad_dtype
     gp, sp = _vector(dloss, "dloss", m, f32, gpu), _vector(lse, "lse", m, f32, gpu)
+    entry, more = (load().mdet_xent_backward, ()) if loss is None else (load().mdet_xent_backward_with_loss, (_vector(loss, "loss", m, f32, gpu),))
     kp, kb = (None, 0) if kept is None else _bytes(kept, "kept", gpu)
     given = _given(dx, dw, db)
     dx, dxp, lddx = _matrix_result(dx, "dx", m, k, t, gpu, x, stream)
     dw, dwp, lddw = _matrix_result(dw, "dw", n, k, gt, gpu, x, stream)
     db, dbp = _vector_result(db, "db", n, gt, gpu, x, stream)
     wsp, wsb, _ws = _room(workspace, lambda: mdet_xent_workspace_query(t, m, n, k, True, gt), gpu, x, stream)
-    _queue(gpu, load().mdet_xent_backward, _type_code(t), _type_code(gt), bits, m, n, k, gp, xp, ldx, wp, ldw, bp, tp, ignore, sp, kp, kb,
-           dxp, lddx, dwp, lddw, dbp, wsp, wsb, _operator_stream(stream, gpu))
+    _queue(gpu, entry, _type_code(t), _type_code(gt), bits, m, n, k, gp, xp, ldx, wp, ldw, bp, tp, ignore, sp, *more, kp, kb, dxp, lddx,
+           dwp, lddw, dbp, wsp, wsb, _operator_stream(stream, gpu))
     if given:
         _written(*given)
     return dx, dw, db

@@ -101,12 +101,12 @@ int forward(Operand<T> x, Operand<T> w, int64_t k, XentForward<T> o, const XentL
   // a row's strips by a wavefront, or by sixteen where they are many
   if (l.across > 1024)
     gemm_launches(o.rows, 1024, [&](const int64_t first, const dim3 grid) {
-      hipLaunchKernelGGL((xent_join_kernel<1024>), grid, dim3(1024), 0, st, (const XentStrip*)o.strips, l.across, (const float*)o.picked, o.t, o.rows,
+      hipLaunchKernelGGL((xent_join_kernel<1024>), grid, dim3(1024), 0, st, (const XentStrip*)o.strips, l.across, o.picked, o.t, o.rows,
                          loss, lse, first);
     });
   else
     gemm_launches(ceil_div(o.rows, 4), 256, [&](const int64_t first, const dim3 grid) {
-      hipLaunchKernelGGL((xent_join_kernel<64>), grid, dim3(256), 0, st, (const XentStrip*)o.strips, l.across, (const float*)o.picked, o.t, o.rows,
+      hipLaunchKernelGGL((xent_join_kernel<64>), grid, dim3(256), 0, st, (const XentStrip*)o.strips, l.across, o.picked, o.t, o.rows,
                          loss, lse, first);
     });
   return launch_status();
@@ -145,7 +145,7 @@ int64_t kept_size(int32_t dtype) { return dtype == MDET_BF16 ? 2 : 4; }
 struct Grad {
   XentTargets t;
   int64_t m, n, k;
-  const float *g, *lse;
+  const float *g, *lse, *loss;         // loss null: what lse says of it
   const void *x, *w, *bias;
   int64_t ldx, ldw;
   char* kept;                          // null: nothing was kept
@@ -162,6 +162,8 @@ int backward(const Grad& a) {
   const XentGradLayout l = xent_grad_layout(a.m, a.n, a.k, sizeof(T), parts_of_e);
   // what was kept may be rounded to 11 bits, which is not enough for more than one part
   char* const kept = parts_of_e == 1 ? a.kept : nullptr;
+  const XentForward<T> was = a.kept ? forward_places<T>(a.kept, f, true) : XentForward<T>{};
+  const float* const loss = a.kept ? was.picked : a.loss;
   hipStream_t st = a.st;
   T *const e = (T*)(a.workspace + l.e), *const rows = (T*)(a.workspace + l.rows);
   float *const sums = (float*)(a.workspace + l.sums), *const total = (float*)(a.workspace + l.total), *const parts = (float*)(a.workspace + l.parts);
@@ -183,14 +185,12 @@ int backward(const Grad& a) {
       w = (const T*)(a.workspace + l.w);
       ldw = k = l.ldrows;
     }
-    const XentSlope<T> o{a.t, a.bias ? (const T*)a.bias + v : nullptr, a.lse, a.g, scale, e, l.lde, a.db ? sums : nullptr, a.m, n, v};
+    const XentSlope<T> o{a.t, a.bias ? (const T*)a.bias + v : nullptr, a.lse, a.g, loss, scale, e, l.lde, a.db ? sums : nullptr, a.m, n, v};
     int64_t strips = 0;
     if (kept) {
-      const XentForward<T> was = forward_places<T>(kept, f, true);
       strips = ceil_div(a.m, 16 * XENT_EACH);
       gemm_launches(strips * ceil_div(n, 16 * Core<T>::VEC), 256, [&](const int64_t first, const dim3 grid) {
-        hipLaunchKernelGGL((xent_slope_kept_kernel<T>), grid, dim3(256), 0, st, o, was.exps, was.ldexps, (const XentStrip*)was.strips, was.across, f.strip,
-                           (const float*)was.picked, first);
+        hipLaunchKernelGGL((xent_slope_kept_kernel<T>), grid, dim3(256), 0, st, o, was.exps, was.ldexps, (const XentStrip*)was.strips, was.across, f.strip, first);
       });
     } else
       with_tile<T>(cut_of(a.m, n, a.k, sizeof(T), false).tile, [&](auto shape) {
@@ -290,14 +290,14 @@ int mdet_xent_reduce(int32_t index_bits, int64_t m, int64_t n, const float* loss
   return launch_status();
 }
 
-int mdet_xent_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const float* dloss, const void* x,
-                       int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* target, int64_t ignore, const float* lse,
-                       const void* kept, uint64_t kept_bytes, void* dx, int64_t lddx, void* dw, int64_t lddw, void* db, void* workspace,
-                       uint64_t workspace_bytes, void* stream) {
+int mdet_xent_backward_with_loss(int32_t dtype, int32_t grad_dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const float* dloss,
+                                 const void* x, int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* target, int64_t ignore,
+                                 const float* lse, const float* loss, const void* kept, uint64_t kept_bytes, void* dx, int64_t lddx, void* dw,
+                                 int64_t lddw, void* db, void* workspace, uint64_t workspace_bytes, void* stream) {
   if (!is_type(dtype) || (grad_dtype != dtype && grad_dtype != MDET_F32) || !is_index(index_bits) || !xent_fits(m, n, k)) return MDET_EINVAL;
   const int64_t s = size_of(dtype), gs = size_of(grad_dtype);
   if (!matrix_ok(x, m, k, ldx, s) || !matrix_ok(w, n, k, ldw, s) || (uintptr_t)bias % s || !vector_ok(target, m, index_bits / 8)) return MDET_EINVAL;
-  if (!vector_ok(dloss, m, 4) || !vector_ok(lse, m, 4)) return MDET_EINVAL;
+  if (!vector_ok(dloss, m, 4) || !vector_ok(lse, m, 4) || (uintptr_t)loss % 4) return MDET_EINVAL;
   if ((dx && !matrix_ok(dx, m, k, lddx, s)) || (dw && !matrix_ok(dw, n, k, lddw, gs)) || (uintptr_t)db % gs) return MDET_EINVAL;
   const XentLayout f = xent_layout(m, n, k, s, kept_size(dtype));
   int ok = kept ? workspace_ok(kept, kept_bytes, f.kept()) : MDET_OK;
@@ -311,12 +311,21 @@ int mdet_xent_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, in
     grad_dtype == MDET_F32 ? zero<float>(db, n, 1, n, st) : zero<_Float16>(db, n, 1, n, st);
     return launch_status();
   }
-  const Grad a{XentTargets{target, index_bits, ignore, n}, m, n, k, dloss, lse, x, w, bias, ldx, ldw, (char*)kept, dx, dw, db, lddx, lddw, (char*)workspace, st};
+  const Grad a{XentTargets{target, index_bits, ignore, n}, m, n, k, dloss, lse, loss, x, w, bias, ldx, ldw, (char*)kept, dx, dw, db, lddx, lddw, (char*)workspace,
+               st};
   auto call = [&](auto zero) {
     typedef decltype(zero) T;
     return grad_dtype == MDET_F32 ? backward<T, float>(a) : backward<T, T>(a);
   };
   return dtype == MDET_F32 ? call(0.0f) : dtype == MDET_BF16 ? call((__bf16)0.0f) : call((_Float16)0.0f);
+}
+
+int mdet_xent_backward(int32_t dtype, int32_t grad_dtype, int32_t index_bits, int64_t m, int64_t n, int64_t k, const float* dloss, const void* x,
+                       int64_t ldx, const void* w, int64_t ldw, const void* bias, const void* target, int64_t ignore, const float* lse,
+                       const void* kept, uint64_t kept_bytes, void* dx, int64_t lddx, void* dw, int64_t lddw, void* db, void* workspace,
+                       uint64_t workspace_bytes, void* stream) {
+  return mdet_xent_backward_with_loss(dtype, grad_dtype, index_bits, m, n, k, dloss, x, ldx, w, ldw, bias, target, ignore, lse, nullptr, kept, kept_bytes,
+                                      dx, lddx, dw, lddw, db, workspace, workspace_bytes, stream);
 }
 
 }  // extern "C"
