@@ -693,7 +693,8 @@ int mdet_layernorm_backward(int32_t dtype, int32_t grad_dtype, int64_t m, int64_
                             void* db, void* workspace, uint64_t workspace_bytes, void* stream);
 
 /* Device bytes of workspace for the cross entropy of m rows of k elements over a vocabulary of n (pure host code): the forward call,
- * or with backward != 0 the gradient with dw and db of grad_dtype (up to 2^29 elements of e, or m x 4096 if that is more, at a time). */
+ * or with backward != 0 the gradient with dw and db of grad_dtype (up to 2^29 elements of e, or m x 4096 if that is more, at a time;
+ * of operands in 16 bits with grad_dtype MDET_F32 in two or three numbers each, which count one by one). */
 int mdet_xent_workspace_query(int32_t dtype, int32_t grad_dtype, int32_t backward, int64_t m, int64_t n, int64_t k,
                               uint64_t* bytes);
 /* Device bytes of `kept`: m x n elements of two bytes for MDET_BF16, four otherwise, and a little more. */

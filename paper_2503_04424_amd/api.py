@@ -333,8 +333,8 @@ def layer_norm(x, weight=None, bias=None, eps=1e-5):
 
 
 def linear_cross_entropy(x, w, target, bias=None, ignore_index=-100, reduction="mean", keep=False):
-    """Softmax cross entropy of ``x w^T + bias`` with its gradient (autograd), without that matrix in memory: x (..., k), w (n, k), target
-    (...) int32 or int64.  Targets that are ``ignore_index``, or outside of the vocabulary, do not count.  reduction: 'mean' over those that
+    """Softmax cross entropy of ``x w^T + bias`` with its gradient (autograd), without that matrix in memory in the forward pass, and with one like it
+    in the gradient, a piece of up to 2^29 elements (or 4096 of each row, if that is more) at a time: x (..., k), w (n, k), target (...) int32 or int64.  Targets that are ``ignore_index``, or outside of the vocabulary, do not count.  reduction: 'mean' over those that
     count (NaN if none does), 'sum', or 'none' (the losses, in float32, in target's shape).  ``keep`` spends x's rows times n elements between
     the two passes on sparing the gradient one of its three products."""
     if x.dim() < 1 or w.dim() != 2 or target.shape != x.shape[:-1]:

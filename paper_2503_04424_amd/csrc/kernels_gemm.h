@@ -483,7 +483,7 @@ struct TileStream {
   // steps (of 16 rows and half a slab each), a step's row fragment is fetched three steps ahead, the column fragments a few steps ahead of
   // their half.  Behind step 13 everything of a slab is in registers: the next one has landed by then, its first fragments come in
   // beside the last two steps, and its place in LDS is free for the one after it.  The same sums in the same order as run().  (Cross entropy of 8192 x 4096 over 131072
-  // words in bf16: 6.45 ms, 6.72 with run(); matrix cores busy 67 and 60 % of the cycles.)
+  // words in bf16: 6.4 ms, 7.05 with run(); matrix cores busy 67 and 54 % of the cycles.)
   template <typename F>
   __device__ __forceinline__ void run_rolling(typename Core<T>::acc_t (&acc)[S::TN][S::TM], const int count, F&& next) {
     static_assert(DIRECT && sizeof(T) == 2 && S::NB == 2 && S::TM == 8 && S::TN == 4, "");

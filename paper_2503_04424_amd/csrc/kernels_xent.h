@@ -209,8 +209,8 @@ __device__ __forceinline__ void xent_store(T* const row, const int64_t col, cons
 }
 
 // Tiles of logits, and what is left of each of their rows: a strip for each of the wavefronts beside each other, so that no wavefront waits
-// for another behind the product.  The matrix cores and the power they draw bound long rows (8192 x 4096 over 131072 words bf16 6.4 to 6.7 ms,
-// 1.32 to 1.37 PFLOP/s; the library's product alone 5.98), the ends of a tile short ones (4096 x 1024 over 50003: 370 to 450 us, 0.93 to 1.13).
+// for another behind the product.  The matrix cores and the power they draw bound long rows (8192 x 4096 over 131072 words bf16 6.4 to 6.9 ms,
+// 1.28 to 1.38 PFLOP/s; the library's product alone 5.98), the ends of a tile short ones (4096 x 1024 over 50003: 370 to 450 us, 0.93 to 1.13).
 template <typename T, typename S, bool DIRECT>
 __global__ __launch_bounds__(S::THREADS) void xent_forward_kernel(const Operand<T> r, const Operand<T> c, const XentForward<T> o, const XentUnits u) {
   typedef typename Core<T>::acc_t acc_t;

@@ -15,6 +15,9 @@ inline int64_t xent_pad(int64_t k) { return k >= 1024 ? ceil_div(k, 64) * 64 : c
 // From these many rows of x on they are copied first, with zeros behind them.  us without and with copies, 32003 words of
 // 1501 in fp16: forward 512 rows 76 and 85, 1024 rows 144 and 127, 4096 rows 523 and 380; gradient 256 rows 352 and 361, 512 rows 295 and 298
 // (131071 words: 1156 and 1103), 4096 rows 1636 and 1266.
+// The rule knows the rows' length, which a workspace query is told, not their distance or address.  So rows that are whole pieces long and stand
+// off 16 bytes go through registers (4096 rows of 1024 over 50003 words in bf16, forward and gradient: 1027 apart 510 and 1498 us, 1024 apart 368 and
+// 1151), and rows that are not, at a distance that is, are copied all the same (1021 long and 1024 apart 404 and 1246; 1021 apart 407 and 1251).
 inline bool xent_copies(int64_t m, int64_t k, int64_t size, bool backward) { return size == 2 && k % 8 != 0 && m >= (backward ? XENT_COPY_GRAD : XENT_COPY); }
 
 // m rows, a vocabulary of n, rows of k elements of `size` bytes; kept_size: bytes of an exponential that is kept.
