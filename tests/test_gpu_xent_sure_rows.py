@@ -124,3 +124,16 @@ def test_more_than_one_piece_of_the_vocabulary(M):
         check(db[best], own.sum(), off.sum() + (m + 8) * EPS32 * own.abs().sum(), f32, f"db {keep}")
         size = own.abs() * x[:, 1].double()
         check(dw[best, 1], (own * x[:, 1].double()).sum(), (off * x[:, 1].double()).sum() + (m + 8) * EPS32 * size.sum(), f32, f"dw {keep}")
+
+
+@pytest.mark.parametrize("dtype", TYPES, ids=str)
+def test_what_is_kept_does_not_depend_on_the_results_asked_for(M, dtype):
+    """The losses are among what is kept, also where the caller wants none; where both are there the result is the same, bit by bit."""
+    x, w, t, g = operands(40, 701, dtype)
+    t[::5] = -100
+    loss, lse, kept = M.mdet_xent_forward(x, w, t, keep=True)
+    want = M.mdet_xent_backward(g, x, w, t, lse, kept=kept, db=True)
+    for without in (dict(loss=None), dict(lse=None), dict(loss=None, lse=None)):
+        other = M.mdet_xent_forward(x, w, t, keep=True, **without)[2]
+        for given in (None, loss):
+            assert all(torch.equal(a, b) for a, b in zip(want, M.mdet_xent_backward(g, x, w, t, lse, kept=other, db=True, loss=given)))
